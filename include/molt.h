@@ -413,6 +413,89 @@ molt_status molt_token_logprobs_fwd_noalloc(const uint16_t* hidden, const uint16
                                             float* logp_out, float* entropy_out, cudaStream_t stream);
 
 /*
+ * ---------------------------------------------------------------------------
+ * Around the LM head (no paper counterpart): what a training or serving program
+ * runs on the residual stream between token ids and the hidden states of the
+ * calls above.
+ * ---------------------------------------------------------------------------
+ */
+typedef enum { MOLT_BF16 = 0, MOLT_FP16 = 1, MOLT_FP32 = 2 } molt_dtype;
+
+/*
+ * Token embedding: out[t] = scale * E[tokens[t]].
+ *   E [V,H] of E_dtype, out [T,H] of out_dtype (E's type, or MOLT_FP32 for a
+ *   residual stream in 32 bits), tokens [T] int32.  Any H up to 65536; rows that
+ *   are whole 16-byte vectors on 16-byte boundaries are the fast ones.
+ *   A token outside [0, V) gives a row of zeros and sets MOLT_DEV_TOKEN_RANGE.
+ */
+molt_status molt_token_embedding(const void* E, int E_dtype, const int32_t* tokens, int64_t T, int64_t H, int64_t V,
+                                 float scale, void* out, int out_dtype, cudaStream_t stream);
+
+/*
+ * Its gradient: dE[v] (+)= scale * sum_{t: tokens[t] = v} dout[t].
+ *   dout [T,H] of dout_dtype, dE [V,H] of dE_dtype (dout's type or MOLT_FP32).
+ *   accumulate = 0 writes all of dE (rows of tokens that do not occur are 0),
+ *   1 adds to it and needs MOLT_FP32 (tied weights: the dW of a loss call; or the
+ *   microbatches of one window); then only the rows of tokens that occur are touched.
+ *   padding_idx: a token that takes no gradient, or negative for none.  Tokens
+ *   outside [0, V) take none and set MOLT_DEV_TOKEN_RANGE.
+ * Equal tokens are added in fp32 in a fixed order (token order within pieces of the
+ * sorted tokens, then the pieces), so the result is bitwise reproducible.
+ */
+size_t molt_token_embedding_bwd_workspace_bytes(int64_t T, int64_t H, int64_t V);
+molt_status molt_token_embedding_bwd(const void* dout, int dout_dtype, const int32_t* tokens, int64_t T, int64_t H,
+                                     int64_t V, float scale, int64_t padding_idx, void* dE, int dE_dtype, int accumulate,
+                                     void* workspace, size_t workspace_bytes, cudaStream_t stream);
+
+/*
+ * Residual norm: a block's output x enters the residual stream through a norm, a
+ * gate and a scaled residual, and the next block reads the stream through its norm:
+ *   u_t  = x_t rstd_post,t (weight_offset + w_post),  rstd_post = 1 / sqrt(mean x^2 + eps)
+ *   r'_t = res_scale r_t + g u_t
+ *   y_t  = r'_t rstd_pre,t (weight_offset + w_pre),   rstd_pre = 1 / sqrt(mean r'^2 + eps)
+ * Parts are left out with NULL: w_post (then u = x), residual (then r' = g u), w_pre
+ * and y (together), residual_out (the stream is not wanted, e.g. a plain RMS norm of
+ * x).  Sums are fp32 and y is formed from r' before it is rounded.
+ */
+#define MOLT_GATE_NONE 0      /* g = 1 */
+#define MOLT_GATE_CHANNEL 1   /* gate [H] of param_dtype */
+#define MOLT_GATE_TOKEN 2     /* gate [T] fp32 */
+#define MOLT_GATE_FULL 3      /* gate [T,H] of dtype */
+typedef struct {
+  int64_t T, H;               /* T >= 0, 1 <= H <= 65536 */
+  int64_t x_stride, residual_stride, dy_stride;   /* elements between rows of x, of the residual
+                                 stream read, and of dy; 0: H (all other rows lie side by side) */
+  int dtype;                  /* molt_dtype of x, y and their gradients, and of a full gate */
+  int residual_dtype;         /* of the residual stream and its gradient: dtype or MOLT_FP32 */
+  int param_dtype;            /* of w_post, w_pre and a channel gate: dtype or MOLT_FP32 */
+  int gate_kind;              /* MOLT_GATE_* */
+  float res_scale, eps, weight_offset;   /* weight_offset 1: weights are stored as w - 1 */
+} molt_norm_desc;
+
+/* rstd_post [T], rstd_pre [T] fp32: what the backward needs of the row sums, each
+ * NULL where it is not wanted (serving).  residual_out may be the residual itself. */
+molt_status molt_residual_norm_fwd(const molt_norm_desc* desc, const void* x, const void* residual, const void* w_post,
+                                   const void* gate, const void* w_pre, void* y, void* residual_out, float* rstd_post,
+                                   float* rstd_pre, cudaStream_t stream);
+
+/*
+ * Backward, from dy (NULL without w_pre) and dresidual, the gradient of r' from later
+ * blocks (NULL: none).  x, gate and weights as in the forward; residual is the r' that
+ * the forward wrote (with its stride in residual_stride), rstd_* its statistics.
+ *   dx [T,H] of dtype; dresidual_out [T,H] of residual_dtype (NULL: the forward had no
+ *   residual); dw_post, dw_pre [H] fp32; dgate: [H] fp32, [T] fp32 or [T,H] of dtype by
+ *   the gate's kind.  accumulate = 1 adds to dw_post, dw_pre and a channel gate's
+ *   gradient (microbatches), 0 overwrites them.
+ * Results are bitwise reproducible on one kind of device.
+ */
+size_t molt_residual_norm_bwd_workspace_bytes(const molt_norm_desc* desc);
+molt_status molt_residual_norm_bwd(const molt_norm_desc* desc, const void* dy, const void* dresidual, const void* x,
+                                   const void* residual, const float* rstd_post, const float* rstd_pre,
+                                   const void* w_post, const void* gate, const void* w_pre, void* dx,
+                                   void* dresidual_out, float* dw_post, void* dgate, float* dw_pre, int accumulate,
+                                   void* workspace, size_t workspace_bytes, cudaStream_t stream);
+
+/*
  * Per-kernel timing hook for benchmarks.  While set, every LM-head call made
  * from the calling thread records starts[k] / stops[k] (caller-created CUDA
  * events) on its stream around kernel group k:

@@ -21,7 +21,7 @@ __all__ = [
     "broadcast_advantages", "mask_count", "token_logprobs", "policy_loss_fwd_bwd", "device_status",
     "token_logprobs_workspace_bytes", "policy_loss_workspace_bytes", "header_functions", "backward_plan",
     "vp_partials", "vp_loss", "vp_backward", "vocab_shard_bounds", "gather_shard_partials", "sum_dhidden",
-    "policy_loss_vocab_parallel",
+    "policy_loss_vocab_parallel", "token_embedding", "token_embedding_bwd", "residual_norm_fwd", "residual_norm_bwd",
 ]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -30,7 +30,8 @@ _CSRC = os.path.join(_PKG, "csrc")
 _INCLUDE = os.path.join(_ROOT, "include")
 _BUILD = os.path.join(_ROOT, "_build")
 _LIB = os.path.join(_PKG, "libmolt.so")
-_SOURCES = ["rows.cu", "lmhead_fwd.cu", "lmhead_bwd.cu", "lmhead_bwd4.cu", "lmhead_bwd_chunk.cu", "api.cu", "noalloc.cu"]
+_SOURCES = ["rows.cu", "lmhead_fwd.cu", "lmhead_bwd.cu", "lmhead_bwd4.cu", "lmhead_bwd_chunk.cu", "api.cu", "noalloc.cu",
+            "embed.cu", "norm.cu", "norm_bf16.cu", "norm_fp16.cu", "norm_fp32.cu"]
 ARCH_FLAGS = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 STATUS = {
@@ -140,6 +141,12 @@ def load():
         "molt_vp_loss": (I32, [P, I32, P, P, P, I64, F, F, D, P, P, P, P, P, P, P, P, SZ, P]),
         "molt_vp_backward_workspace_bytes": (SZ, [I64, I64, I64]),
         "molt_vp_backward": (I32, [P, P, P, P, P, I64, I64, I64, I64, P, P, I32, P, SZ, P]),
+        "molt_token_embedding": (I32, [P, I32, P, I64, I64, I64, F, P, I32, P]),
+        "molt_token_embedding_bwd_workspace_bytes": (SZ, [I64, I64, I64]),
+        "molt_token_embedding_bwd": (I32, [P, I32, P, I64, I64, I64, F, I64, P, I32, I32, P, SZ, P]),
+        "molt_residual_norm_fwd": (I32, [P] * 11),
+        "molt_residual_norm_bwd_workspace_bytes": (SZ, [P]),
+        "molt_residual_norm_bwd": (I32, [P] * 15 + [I32, P, SZ, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -617,3 +624,6 @@ def policy_loss_vocab_parallel(hidden, weight_shard, v_begin, tokens, behavior_l
     out["dhidden"] = sum_dhidden(dh, group)
     out["dW"] = dW
     return out
+
+
+from .stream import residual_norm_bwd, residual_norm_fwd, token_embedding, token_embedding_bwd  # noqa: E402

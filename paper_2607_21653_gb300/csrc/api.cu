@@ -439,16 +439,6 @@ molt_status check_shape(int64_t T, int64_t H, int64_t V) {
   return MOLT_OK;
 }
 
-// Scratch memory of one call: the caller's buffer, or a stream-ordered allocation.
-struct Scratch {
-  void* ptr = nullptr;
-  bool owned = false;
-  cudaStream_t s = nullptr;
-  ~Scratch() {
-    if (owned && ptr) cudaFreeAsync(ptr, s);
-  }
-};
-
 // Vocab split of the raster backward (see the side lanes below): the first
 // Vq columns go to the cluster kernel, the rest to the single-CTA kernel on the
 // `spare` SMs.  Vq is the multiple of 512 that minimises the later of the two
@@ -475,25 +465,6 @@ int64_t choose_vocab_split(int64_t T, int64_t V, int clusters, int spare) {
     }
   }
   return best;
-}
-
-molt_status get_scratch(Scratch& sc, void* ws, size_t ws_bytes, size_t need, cudaStream_t s) {
-  sc.s = s;
-  if (ws) {
-    if (ws_bytes < need)
-      return fail(MOLT_ERR_WORKSPACE, "workspace of " + std::to_string(ws_bytes) + " bytes, need " +
-                                          std::to_string(need));
-    sc.ptr = ws;
-    return MOLT_OK;
-  }
-  cudaError_t e = cudaMallocAsync(&sc.ptr, need, s);
-  if (e != cudaSuccess) {
-    cudaGetLastError();
-    sc.ptr = nullptr;
-    return fail(MOLT_ERR_NO_MEMORY, std::string("cudaMallocAsync: ") + cudaGetErrorString(e));
-  }
-  sc.owned = true;
-  return MOLT_OK;
 }
 
 // Side lanes of the calls that take the cluster kernel.  Clusters of four leave the
@@ -913,6 +884,25 @@ molt_status policy_loss_impl(const uint16_t* hidden, const uint16_t* W, const in
 }  // namespace
 
 void set_last_error(const std::string& msg) { t_last_error = msg; }
+
+molt_status get_scratch(Scratch& sc, void* ws, size_t ws_bytes, size_t need, cudaStream_t s) {
+  sc.s = s;
+  if (ws) {
+    if (ws_bytes < need)
+      return fail(MOLT_ERR_WORKSPACE, "workspace of " + std::to_string(ws_bytes) + " bytes, need " +
+                                          std::to_string(need));
+    sc.ptr = ws;
+    return MOLT_OK;
+  }
+  cudaError_t e = cudaMallocAsync(&sc.ptr, need, s);
+  if (e != cudaSuccess) {
+    cudaGetLastError();
+    sc.ptr = nullptr;
+    return fail(MOLT_ERR_NO_MEMORY, std::string("cudaMallocAsync: ") + cudaGetErrorString(e));
+  }
+  sc.owned = true;
+  return MOLT_OK;
+}
 
 void timing_event(int k, bool stop, cudaStream_t s) {
   if (stop)

@@ -136,6 +136,18 @@ void set_last_error(const std::string& msg);
 // benchmark timing hook (molt_set_timing_events): record the calling thread's
 // start (stop = false) or stop event of kernel group k on stream s, if set
 void timing_event(int k, bool stop, cudaStream_t s);
+// Scratch memory of one call: the caller's buffer, or a stream-ordered allocation.
+struct Scratch {
+  void* ptr = nullptr;
+  bool owned = false;
+  cudaStream_t s = nullptr;
+  ~Scratch() {
+    if (owned && ptr) cudaFreeAsync(ptr, s);
+  }
+  // on a 256-byte boundary (sizes asked for hold 256 bytes for it)
+  void* aligned() const { return reinterpret_cast<void*>((reinterpret_cast<uintptr_t>(ptr) + 255) & ~uintptr_t(255)); }
+};
+molt_status get_scratch(Scratch& sc, void* ws, size_t ws_bytes, size_t need, cudaStream_t s);
 unsigned* device_status_word(molt_status* st);   // current device's status word
 int device_sm_count();                           // current device's SM count
 // vocab splits of the forward pass over Tcap packed rows

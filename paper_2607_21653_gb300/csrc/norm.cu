@@ -1,0 +1,260 @@
+// C ABI of the residual norm (include/molt.h): argument checks, the layout of a row
+// over threads, and the sum of the blocks' parts of the weights' gradients.
+#include <algorithm>
+#include <cstdint>
+#include <cuda_runtime.h>
+#include <initializer_list>
+
+#include "molt_internal.cuh"
+#include "norm_kernels.cuh"
+
+namespace molt {
+namespace {
+
+constexpr int kSumCols = 32, kSumWarps = 16;
+
+// out[c] (+)= sum over blocks of part[block][which][c], blocks in a fixed order: warp w
+// takes every 16th, then the warps' sums are added one after the other.
+__global__ void __launch_bounds__(kSumCols * kSumWarps) norm_part_sum_kernel(const float* __restrict__ part, int blocks, int H,
+                                                                             float* o0, float* o1, float* o2, int accumulate) {
+  __shared__ float sh[kSumWarps][kSumCols];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int which = blockIdx.y;
+  float* out = which == 0 ? o0 : which == 1 ? o1 : o2;
+  if (out == nullptr) return;
+  const int c = blockIdx.x * kSumCols + lane;
+  float s = 0.f;
+  if (c < H) {
+#pragma unroll 4
+    for (int b = warp; b < blocks; b += kSumWarps) s += part[(static_cast<int64_t>(b) * 3 + which) * H + c];
+  }
+  sh[warp][lane] = s;
+  __syncthreads();
+  if (warp != 0 || c >= H) return;
+  s = 0.f;
+#pragma unroll
+  for (int w = 0; w < kSumWarps; ++w) s += sh[w][lane];
+  out[c] = accumulate ? out[c] + s : s;
+}
+
+molt_status fail(molt_status s, const char* msg) {
+  set_last_error(msg);
+  return s;
+}
+molt_status cuda_fail(cudaError_t e, const char* what) {
+  set_last_error(std::string(what) + ": " + cudaGetErrorString(e));
+  return MOLT_ERR_CUDA;
+}
+
+bool known_type(int dt) { return dt == MOLT_BF16 || dt == MOLT_FP16 || dt == MOLT_FP32; }
+bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+molt_status check_desc(const molt_norm_desc* d) {
+  if (!d) return fail(MOLT_ERR_INVALID_ARG, "desc is NULL");
+  if (d->T < 0 || d->H < 1) return fail(MOLT_ERR_INVALID_ARG, "sizes must satisfy T >= 0, H >= 1");
+  if (d->T >= (int64_t(1) << 31) || d->H > 65536)
+    return fail(MOLT_ERR_UNSUPPORTED_SHAPE, "T must be below 2^31 and H at most 65536");
+  if (!known_type(d->dtype) || !known_type(d->residual_dtype) || !known_type(d->param_dtype))
+    return fail(MOLT_ERR_INVALID_ARG, "unknown element type");
+  if (d->residual_dtype != d->dtype && d->residual_dtype != MOLT_FP32)
+    return fail(MOLT_ERR_INVALID_ARG, "the residual stream is of x's type or fp32");
+  if (d->param_dtype != d->dtype && d->param_dtype != MOLT_FP32)
+    return fail(MOLT_ERR_INVALID_ARG, "the weights are of x's type or fp32");
+  if (d->gate_kind < MOLT_GATE_NONE || d->gate_kind > MOLT_GATE_FULL) return fail(MOLT_ERR_INVALID_ARG, "unknown gate kind");
+  if (!(d->eps >= 0.f && d->eps <= 1e30f)) return fail(MOLT_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  if (!(d->res_scale >= -1e30f && d->res_scale <= 1e30f) || !(d->weight_offset >= -1e30f && d->weight_offset <= 1e30f))
+    return fail(MOLT_ERR_INVALID_ARG, "res_scale and weight_offset must be finite");
+  for (const int64_t ld : {d->x_stride, d->residual_stride, d->dy_stride})
+    if (ld != 0 && ld < d->H) return fail(MOLT_ERR_INVALID_ARG, "a row stride is 0 (rows side by side) or at least H");
+  return MOLT_OK;
+}
+
+// every pointer that is given, aligned to its element
+struct Operand {
+  const void* p;
+  int dtype;
+};
+molt_status check_elements(std::initializer_list<Operand> ops) {
+  for (const Operand& o : ops)
+    if (o.p && !aligned(o.p, static_cast<size_t>(dtype_bytes(o.dtype))))
+      return fail(MOLT_ERR_INVALID_ARG, "a pointer is not aligned to its element type");
+  return MOLT_OK;
+}
+
+NormArgs base_args(const molt_norm_desc* d) {
+  NormArgs a{};
+  a.T = d->T;
+  a.H = static_cast<int>(d->H);
+  a.x_ld = d->x_stride ? d->x_stride : d->H;
+  a.r_ld = d->residual_stride ? d->residual_stride : d->H;
+  a.dy_ld = d->dy_stride ? d->dy_stride : d->H;
+  a.alpha = d->res_scale;
+  a.eps = d->eps;
+  a.offset = d->weight_offset;
+  a.gate_kind = d->gate_kind;
+  a.param_f32 = d->param_dtype == MOLT_FP32;
+  return a;
+}
+
+// Whether rows can be read 16 bytes at a time: the row length in whole vectors, and
+// every row and parameter on a 16-byte boundary.
+bool vectors(const molt_norm_desc* d, const NormArgs& a, std::initializer_list<const void*> ptrs) {
+  if (a.H % 8 != 0) return false;
+  const int b = dtype_bytes(d->dtype), rb = dtype_bytes(d->residual_dtype);
+  if (a.x_ld * b % 16 != 0 || a.r_ld * rb % 16 != 0 || a.dy_ld * b % 16 != 0) return false;
+  for (const void* p : ptrs)
+    if (!aligned(p, 16)) return false;
+  return true;
+}
+
+NormShape row_shape(int H, bool vec) {
+  NormShape s{};
+  s.vec = vec ? 8 : 1;
+  s.elems = H <= 8 * kNormMaxThreads ? 8 : H <= 16 * kNormMaxThreads ? 16 : H <= kNormMaxH ? 32 : 0;
+  s.threads = s.elems == 0 ? kNormMaxThreads : ((H + s.elems - 1) / s.elems + 31) / 32 * 32;
+  s.rows = s.threads == 32 ? 4 : 1;
+  return s;
+}
+
+constexpr int kMaxBlocksPerSM = 8;
+int64_t max_blocks(int n_sm) { return kMaxBlocksPerSM * static_cast<int64_t>(n_sm); }
+
+cudaError_t launch(const molt_norm_desc* d, const NormArgs& a, const NormShape& s, int grid, bool bwd, cudaStream_t stream) {
+  const bool r_f32 = d->residual_dtype == MOLT_FP32;
+  if (d->dtype == MOLT_FP32) return launch_norm_fp32(a, s, grid, bwd, stream);
+  return d->dtype == MOLT_FP16 ? launch_norm_fp16(a, s, grid, r_f32, bwd, stream)
+                               : launch_norm_bf16(a, s, grid, r_f32, bwd, stream);
+}
+
+}  // namespace
+}  // namespace molt
+
+using namespace molt;
+
+extern "C" {
+
+molt_status molt_residual_norm_fwd(const molt_norm_desc* desc, const void* x, const void* residual, const void* w_post,
+                                   const void* gate, const void* w_pre, void* y, void* residual_out, float* rstd_post,
+                                   float* rstd_pre, cudaStream_t stream) {
+  if (const molt_status st = check_desc(desc); st != MOLT_OK) return st;
+  if (desc->T == 0) return MOLT_OK;
+  if (!x || (desc->gate_kind != MOLT_GATE_NONE && !gate)) return fail(MOLT_ERR_INVALID_ARG, "null pointer");
+  if ((w_pre == nullptr) != (y == nullptr)) return fail(MOLT_ERR_INVALID_ARG, "w_pre and y come together");
+  if (!y && !residual_out) return fail(MOLT_ERR_INVALID_ARG, "neither y nor residual_out is wanted");
+  const int gate_type = desc->gate_kind == MOLT_GATE_TOKEN     ? MOLT_FP32
+                        : desc->gate_kind == MOLT_GATE_CHANNEL ? desc->param_dtype
+                                                               : desc->dtype;
+  if (const molt_status st = check_elements({{x, desc->dtype},
+                                             {residual, desc->residual_dtype},
+                                             {w_post, desc->param_dtype},
+                                             {gate, gate_type},
+                                             {w_pre, desc->param_dtype},
+                                             {y, desc->dtype},
+                                             {residual_out, desc->residual_dtype},
+                                             {rstd_post, MOLT_FP32},
+                                             {rstd_pre, MOLT_FP32}});
+      st != MOLT_OK)
+    return st;
+  NormArgs a = base_args(desc);
+  a.x = x;
+  a.r = residual;
+  a.w_post = w_post;
+  a.gate = gate;
+  a.w_pre = w_pre;
+  a.y = y;
+  a.r_out = residual_out;
+  a.rstd_post = rstd_post;
+  a.rstd_pre = rstd_pre;
+  const NormShape s = row_shape(a.H, vectors(desc, a, {x, residual, w_post, w_pre, y, residual_out,
+                                                       desc->gate_kind == MOLT_GATE_TOKEN ? nullptr : gate}));
+  const int grid = static_cast<int>((a.T + s.rows - 1) / s.rows);
+  if (const cudaError_t e = launch(desc, a, s, grid, false, stream); e != cudaSuccess) return cuda_fail(e, "residual norm");
+  note_launches(1);
+  return MOLT_OK;
+}
+
+size_t molt_residual_norm_bwd_workspace_bytes(const molt_norm_desc* desc) {
+  if (check_desc(desc) != MOLT_OK) return 0;
+  return static_cast<size_t>(std::min<int64_t>(desc->T, max_blocks(device_sm_count()))) * 3 * desc->H * sizeof(float) + 256;
+}
+
+molt_status molt_residual_norm_bwd(const molt_norm_desc* desc, const void* dy, const void* dresidual, const void* x,
+                                   const void* residual, const float* rstd_post, const float* rstd_pre, const void* w_post,
+                                   const void* gate, const void* w_pre, void* dx, void* dresidual_out, float* dw_post,
+                                   void* dgate, float* dw_pre, int accumulate, void* workspace, size_t workspace_bytes,
+                                   cudaStream_t stream) {
+  if (const molt_status st = check_desc(desc); st != MOLT_OK) return st;
+  const bool channel = desc->gate_kind == MOLT_GATE_CHANNEL;
+  if ((w_post && !dw_post) || (w_pre && !dw_pre) || (desc->gate_kind != MOLT_GATE_NONE && desc->T > 0 && !dgate) ||
+      (channel && !dgate))
+    return fail(MOLT_ERR_INVALID_ARG, "every weight and gate needs its gradient's buffer");
+  if (desc->T > 0) {
+    if (!x || !dx || (desc->gate_kind != MOLT_GATE_NONE && !gate)) return fail(MOLT_ERR_INVALID_ARG, "null pointer");
+    if (w_pre && (!dy || !residual || !rstd_pre))
+      return fail(MOLT_ERR_INVALID_ARG, "w_pre needs dy, the residual stream and rstd_pre");
+    if (!w_pre && !dresidual) return fail(MOLT_ERR_INVALID_ARG, "without w_pre the gradient comes from dresidual");
+    if (w_post && !rstd_post) return fail(MOLT_ERR_INVALID_ARG, "w_post needs rstd_post");
+  }
+  const int gate_type = desc->gate_kind == MOLT_GATE_TOKEN ? MOLT_FP32 : channel ? desc->param_dtype : desc->dtype;
+  const int dgate_type = desc->gate_kind == MOLT_GATE_FULL ? desc->dtype : MOLT_FP32;
+  if (const molt_status st = check_elements({{dy, desc->dtype},
+                                             {dresidual, desc->residual_dtype},
+                                             {x, desc->dtype},
+                                             {residual, desc->residual_dtype},
+                                             {rstd_post, MOLT_FP32},
+                                             {rstd_pre, MOLT_FP32},
+                                             {w_post, desc->param_dtype},
+                                             {gate, gate_type},
+                                             {w_pre, desc->param_dtype},
+                                             {dx, desc->dtype},
+                                             {dresidual_out, desc->residual_dtype},
+                                             {dw_post, MOLT_FP32},
+                                             {dgate, dgate_type},
+                                             {dw_pre, MOLT_FP32}});
+      st != MOLT_OK)
+    return st;
+  float* sums[3] = {w_post ? dw_post : nullptr, channel ? static_cast<float*>(dgate) : nullptr, w_pre ? dw_pre : nullptr};
+  if (desc->T == 0) {
+    for (float* o : sums)
+      if (o && !accumulate)
+        if (const cudaError_t e = cudaMemsetAsync(o, 0, static_cast<size_t>(desc->H) * sizeof(float), stream); e != cudaSuccess)
+          return cuda_fail(e, "memset");
+    return MOLT_OK;
+  }
+  Scratch sc;
+  if (const molt_status st = get_scratch(sc, workspace, workspace_bytes, molt_residual_norm_bwd_workspace_bytes(desc), stream);
+      st != MOLT_OK)
+    return st;
+  NormArgs a = base_args(desc);
+  a.dy = dy;
+  a.dr = dresidual;
+  a.x = x;
+  a.r = residual;
+  a.rstd_post = const_cast<float*>(rstd_post);
+  a.rstd_pre = const_cast<float*>(rstd_pre);
+  a.w_post = w_post;
+  a.gate = gate;
+  a.w_pre = w_pre;
+  a.dx = dx;
+  a.dr_out = dresidual_out;
+  a.dgate = dgate;
+  a.part = static_cast<float*>(sc.aligned());
+  const NormShape s =
+      row_shape(a.H, vectors(desc, a, {dy, dresidual, x, residual, w_post, w_pre, dx, dresidual_out,
+                                       desc->gate_kind == MOLT_GATE_TOKEN ? nullptr : gate,
+                                       desc->gate_kind == MOLT_GATE_FULL ? dgate : nullptr}));
+  const int per_sm = std::min(kMaxBlocksPerSM, std::max(1, 768 / (s.threads * s.rows)));
+  const int n_sm = device_sm_count();
+  const int grid = static_cast<int>(std::min<int64_t>((a.T + s.rows - 1) / s.rows, int64_t(n_sm) * per_sm));
+  if (const cudaError_t e = launch(desc, a, s, grid, true, stream); e != cudaSuccess)
+    return cuda_fail(e, "residual norm backward");
+  note_launches(1);
+  if (!sums[0] && !sums[1] && !sums[2]) return MOLT_OK;
+  norm_part_sum_kernel<<<dim3((a.H + kSumCols - 1) / kSumCols, 3), kSumCols * kSumWarps, 0, stream>>>(
+      a.part, grid, a.H, sums[0], sums[1], sums[2], accumulate ? 1 : 0);
+  if (const cudaError_t e = cudaGetLastError(); e != cudaSuccess) return cuda_fail(e, "residual norm weight gradients");
+  note_launches(1);
+  return MOLT_OK;
+}
+
+}  // extern "C"
