@@ -496,6 +496,52 @@ molt_status molt_residual_norm_bwd(const molt_norm_desc* desc, const void* dy, c
                                    void* workspace, size_t workspace_bytes, cudaStream_t stream);
 
 /*
+ * Softmax cross entropy over the LM head, forward and backward, without keeping the
+ * logits (they are formed in pieces of the vocabulary, again in the backward):
+ *   z_tv = sum_k hidden[t,k] W[v,k];  lse_t = log sum_v exp z_tv;  x_t = targets[t]
+ *   l_t  = lse_t - (1 - e) z_{t,x_t} - e mean_v z_tv + c lse_t^2
+ *   loss = sum_t w_t l_t / D    over the active rows, targets[t] != ignore_index
+ *   D    = denom if denom > 0, else the number of active rows
+ *   dL/dz_tv = (w_t / D) [ (1 + 2 c lse_t) softmax(z_t)_v - e / V - (1 - e) [v == x_t] ]
+ *   dhidden = dL/dz W [T,H] bf16 (ignored rows are exactly 0),  dW (+)= dL/dz^T hidden [V,H]
+ * with e = label_smoothing, c = z_loss, w = token_weight [T] fp32 (NULL: 1; D does not
+ * follow the weights, pass denom for a weighted mean).
+ * hidden [T,H] bf16, W [V,H] bf16, both 16-byte aligned; targets [T] int32.  Shapes as
+ * molt_token_logprobs_fwd.  A target outside [0, V) that is not ignore_index sets
+ * MOLT_DEV_TOKEN_RANGE; its row counts in D and has no loss and no gradient.  With
+ * denom <= 0 and no active row the loss and the gradients are 0 and
+ * MOLT_DEV_ZERO_DENOM is set.
+ * Outputs: loss_out (device fp32 scalar); optional (may be NULL) logp_out [T] =
+ * z_{t,x_t} - lse_t and lse_out [T], 0 on ignored rows, and stats_out (device
+ * molt_ce_stats).  dW_out of dW_dtype: MOLT_FP32, or MOLT_BF16 (summed in fp32 in the
+ * workspace and rounded once); accumulate_dW = 1 adds to an fp32 dW.
+ */
+typedef struct {
+  int64_t ignore_index;   /* rows with this target are left out; a value that no int32 has: none are */
+  float label_smoothing;  /* in [0, 1] */
+  float z_loss;           /* >= 0 */
+} molt_ce_options;        /* NULL: { -100, 0, 0 } */
+typedef struct {
+  double denom;           /* D actually used */
+  double loss;            /* sum w l / D */
+  double sum_nll;         /* sum of -logp over the active rows */
+  double sum_lse_sq;      /* sum of lse^2 */
+  int64_t n_active;
+} molt_ce_stats;
+size_t molt_cross_entropy_workspace_bytes(int64_t T, int64_t H, int64_t V, int with_backward, int dW_dtype);
+molt_status molt_cross_entropy_fwd(const uint16_t* hidden, const uint16_t* W, const int32_t* targets,
+                                   const float* token_weight, int64_t T, int64_t H, int64_t V, double denom,
+                                   const molt_ce_options* opts, float* loss_out, float* logp_out, float* lse_out,
+                                   molt_ce_stats* stats_out, void* workspace, size_t workspace_bytes,
+                                   cudaStream_t stream);
+molt_status molt_cross_entropy_fwd_bwd(const uint16_t* hidden, const uint16_t* W, const int32_t* targets,
+                                       const float* token_weight, int64_t T, int64_t H, int64_t V, double denom,
+                                       const molt_ce_options* opts, float* loss_out, uint16_t* dhidden_out,
+                                       void* dW_out, int dW_dtype, int accumulate_dW, float* logp_out,
+                                       float* lse_out, molt_ce_stats* stats_out, void* workspace,
+                                       size_t workspace_bytes, cudaStream_t stream);
+
+/*
  * Per-kernel timing hook for benchmarks.  While set, every LM-head call made
  * from the calling thread records starts[k] / stops[k] (caller-created CUDA
  * events) on its stream around kernel group k:

@@ -205,11 +205,8 @@ struct ChunkPlan {
 // 50257 (8 x 8 in eight): 0.52 ms at a lag of 3, 0.489 at 4, 0.493 at 5, 0.565 at 7; T =
 // 12000, H = 768, V = 40000 1.42 at 3, 1.55 at 4; T = 32768, H = 1024, V = 50000 7.05 at
 // 2, 6.88 at 3; a step too short costs up to half.
-ChunkPlan chunk_plan(int64_t T, int64_t H, int64_t V, bool det) {
+ChunkPlan chunk_shape(int64_t T, int64_t H, int64_t V, bool det) {
   ChunkPlan p;
-  if (T <= 0 || H < 256 || (H == 256 && T <= 768 && V > 4096 && V <= 20480) || (H > 256 && H < 512 && T < 512) ||
-      (det && H <= 512 && T > 128 && V >= 25600))
-    return p;
   p.n_t = (T + 255) / 256;
   p.n_v = (V + 255) / 256;
   p.n_h = (H + 255) / 256;
@@ -239,6 +236,12 @@ ChunkPlan chunk_plan(int64_t T, int64_t H, int64_t V, bool det) {
   p.n_buf = static_cast<int>(std::min<int64_t>(most_buf, std::max<int64_t>(2, 512 / (ct * cv))));
   return p;
 }
+ChunkPlan chunk_plan(int64_t T, int64_t H, int64_t V, bool det) {
+  if (T <= 0 || H < 256 || (H == 256 && T <= 768 && V > 4096 && V <= 20480) || (H > 256 && H < 512 && T < 512) ||
+      (det && H <= 512 && T > 128 && V >= 25600))
+    return ChunkPlan{};
+  return chunk_shape(T, H, V, det);
+}
 
 // turn counters of the deterministic schedule: an abort word (padded to 64
 // words), then [token quads, H jobs, 32] for dhidden and [vocab blocks, H jobs,
@@ -266,11 +269,11 @@ TurnLayout turn_layout(int64_t Tcap, int64_t H, int64_t V) {
 struct ChunkReserve {
   size_t g = 0, ctl = 0, turns = 0;   // bytes
 };
-ChunkReserve chunk_reserve(int64_t T, int64_t H, int64_t V, bool det) {
+ChunkReserve chunk_reserve(int64_t T, int64_t H, int64_t V, bool det, bool always = false) {
   ChunkReserve r;
   const int64_t n_t = (T + 255) / 256, n_v = (V + 255) / 256;
   const ChunkPlan plain = chunk_plan(T, H, V, false), p = chunk_plan(T, H, V, det);
-  if (plain.use || p.use) {
+  if (always || plain.use || p.use) {
     r.g = static_cast<size_t>(std::min<int64_t>(512, 16 * std::min<int64_t>(n_t, 16) * std::min<int64_t>(n_v, 16))) *
           (256 * 256 * 2);
     r.ctl = static_cast<size_t>(kChunkCtlHead + 4 * ((n_t + 3) / 4) * ((n_v + 3) / 4)) * 4;
@@ -391,6 +394,47 @@ Layout vp_backward_layout(int64_t T, int64_t H, int64_t V) {
   L.ctl = take(cr.ctl);
   L.row_map = L.pos = L.tok_p = L.b_p = L.adv_p = L.h_p = L.part = L.zx = L.lse = L.coef = L.red =
       L.lp_p = L.ent_p = L.ecoef = L.mu = L.gate_p = L.ecoef_l = L.mu_l = o;
+  L.turns = kNoRegion;
+  L.total = o + 256;
+  return L;
+}
+
+// Workspace of the cross entropy: the active rows packed, which are the backward's rows
+// too; `dW32`: an fp32 dW that is rounded at the end.
+Layout ce_layout(int64_t T, int64_t H, int64_t V, int n_sm, bool with_bwd, bool dW32, size_t* dW32_off) {
+  const int64_t Tcap = round_tiles(T);
+  Layout L{};
+  size_t o = 0;
+  auto take = [&o](size_t bytes) {
+    size_t r = o;
+    o += up256(bytes);
+    return r;
+  };
+  L.counts = take(64);
+  L.row_map = take(T * 4);
+  L.pos = take(T * 4);
+  L.tok_p = take(Tcap * 4);
+  L.b_p = take(Tcap * 4);
+  L.h_p = take(Tcap * H * 2);
+  L.part = take(static_cast<size_t>(part_rows(Tcap, V, n_sm)) * 16);
+  L.zx = take(Tcap * 4);
+  L.lse = take(Tcap * 4);
+  L.coef = take(Tcap * 4);
+  L.ecoef = take(Tcap * 4);
+  L.mu = take(Tcap * 4);
+  L.red = take(Tcap / kRedRows * kRedSlots * 8);
+  L.dh32 = with_bwd ? take(static_cast<size_t>(Tcap) * H * 4) : o;
+  const ChunkReserve cr = chunk_reserve(T, H, V, false, true);
+  L.g = with_bwd ? take(cr.g) : o;
+  L.ctl = with_bwd ? take(cr.ctl) : o;
+  *dW32_off = with_bwd && dW32 ? take(static_cast<size_t>(V) * H * 4) : o;
+  L.adv_p = L.tile_list = L.lp_p = L.ent_p = L.gate_p = L.live_of = o;
+  L.h_l = L.h_p;
+  L.tok_l = L.tok_p;
+  L.lse_l = L.lse;
+  L.coef_l = L.coef;
+  L.ecoef_l = L.ecoef;
+  L.mu_l = L.mu;
   L.turns = kNoRegion;
   L.total = o + 256;
   return L;
@@ -562,6 +606,29 @@ struct ZeroJoin {
     if (s_ != MOLT_OK) return s_;        \
   } while (0)
 
+// The forward kernel over the packed rows.
+molt_status run_forward_kernel(const DeviceInfo* di, int64_t Tcap, int64_t H, int64_t V, int S, const Workspace& w,
+                               const CUtensorMap& tm_h, const CUtensorMap& tm_w, bool ordered, bool sum_z, cudaStream_t s) {
+  FwdArgs fa{};
+  fa.tok_p = w.tok_p;
+  fa.counts = w.counts;
+  fa.rows_cap = static_cast<int>(Tcap);
+  fa.V = static_cast<int>(V);
+  fa.H = static_cast<int>(H);
+  fa.n_split = S;
+  fa.n_vtiles = static_cast<int>((V + kFwdBN - 1) / kFwdBN);
+  fa.ordered = ordered;
+  fa.sum_z = sum_z;
+  fa.next_unit = w.counts + 4;
+  fa.part = w.part;
+  fa.zx = w.zx;
+  fa.err = di->status;
+  ev_start(1, s);
+  MOLT_LAUNCH(launch_lmhead_fwd(tm_h, tm_w, fa, di->n_sm, s), "lmhead forward");
+  ev_stop(1, s);
+  return MOLT_OK;
+}
+
 // Shared front half of the LM-head calls: the active rows packed and the
 // forward kernel (tensor maps already encoded by the caller).
 // tok_shift is subtracted from the tokens (a vocabulary shard's first column);
@@ -576,23 +643,7 @@ molt_status run_forward(const DeviceInfo* di, const uint16_t* hidden, const int3
                           ctl_words, di->n_sm, s),
               "pack");
   ev_stop(0, s);
-  FwdArgs fa{};
-  fa.tok_p = w.tok_p;
-  fa.counts = w.counts;
-  fa.rows_cap = static_cast<int>(Tcap);
-  fa.V = static_cast<int>(V);
-  fa.H = static_cast<int>(H);
-  fa.n_split = S;
-  fa.n_vtiles = static_cast<int>((V + kFwdBN - 1) / kFwdBN);
-  fa.ordered = ordered;
-  fa.next_unit = w.counts + 4;
-  fa.part = w.part;
-  fa.zx = w.zx;
-  fa.err = di->status;
-  ev_start(1, s);
-  MOLT_LAUNCH(launch_lmhead_fwd(tm_h, tm_w, fa, di->n_sm, s), "lmhead forward");
-  ev_stop(1, s);
-  return MOLT_OK;
+  return run_forward_kernel(di, Tcap, H, V, S, w, tm_h, tm_w, ordered, false, s);
 }
 
 // Zero on stream s what the backward adds to: the deterministic schedule's turn
@@ -615,7 +666,7 @@ molt_status zero_backward_targets(const Workspace& w, int64_t T, int64_t H, int6
 
 // The backward over chunks: as run_backward.
 molt_status run_backward_chunk(const DeviceInfo* di, const ChunkPlan& cp, const uint16_t* W, int64_t T, int64_t H,
-                               int64_t V, const Workspace& w, bool det, int det_clusters, bool with_ecoef,
+                               int64_t V, const Workspace& w, bool det, int det_clusters, int form,
                                float* dW_out, int accumulate_dW, cudaStream_t stream) {
   const int64_t Tcap = round_tiles(T);
   const auto bf16 = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
@@ -635,7 +686,8 @@ molt_status run_backward_chunk(const DeviceInfo* di, const ChunkPlan& cp, const 
   a.tok_p = w.tok_l;
   a.lse = w.lse_l;
   a.coef = w.coef_l;
-  if (with_ecoef) {
+  a.form = form;
+  if (form != kGradPlain) {
     a.ecoef = w.ecoef_l;
     a.mu = w.mu_l;
   }
@@ -672,7 +724,8 @@ molt_status run_backward(const DeviceInfo* di, const uint16_t* W, int64_t T, int
                          bool zeroed, cudaStream_t stream) {
   if (!zeroed) MOLT_TRY(zero_backward_targets(w, T, H, V, det, dW_out, accumulate_dW, stream));
   if (const ChunkPlan cp = chunk_plan(T, H, V, det); cp.use)
-    return run_backward_chunk(di, cp, W, T, H, V, w, det, n_det, with_ecoef, dW_out, accumulate_dW, stream);
+    return run_backward_chunk(di, cp, W, T, H, V, w, det, n_det, with_ecoef ? kGradEntropy : kGradPlain, dW_out,
+                              accumulate_dW, stream);
   const int64_t Tcap = round_tiles(T);
   const bool pair_bwd = (H % 128) == 0;   // the cluster backward
   CUtensorMap tm_wz, tm_wn, tm_dh, tm_dw;
@@ -876,7 +929,81 @@ molt_status policy_loss_impl(const uint16_t* hidden, const uint16_t* W, const in
   if (cp.use && det && opts->det_clusters == 0) n_det = 0;
   MOLT_TRY(run_backward(di, W, T, H, V, w, det, n_det, with_ecoef, dW_out, accumulate_dW, zj.lane != nullptr, stream));
   ev_start(4, stream);
-  MOLT_LAUNCH(launch_cast_dh(w, static_cast<int>(T), static_cast<int>(H), dhidden_out, di->n_sm, stream), "cast dh");
+  MOLT_LAUNCH(launch_cast_dh(w, false, static_cast<int>(T), static_cast<int>(H), dhidden_out, di->n_sm, stream), "cast dh");
+  ev_stop(4, stream);
+  return MOLT_OK;
+}
+
+// Both cross-entropy entry points: pack, forward, merge with the loss, and with
+// `grad` the backward over chunks (for every size: its other kernels have no form for
+// the smoothed gradient) and the rounding of its sums.
+molt_status cross_entropy_impl(const uint16_t* hidden, const uint16_t* W, const int32_t* targets,
+                               const float* token_weight, int64_t T, int64_t H, int64_t V, double denom,
+                               const molt_ce_options* opts, float* loss_out, bool grad, uint16_t* dhidden_out,
+                               void* dW_out, int dW_dtype, int accumulate_dW, float* logp_out, float* lse_out,
+                               molt_ce_stats* stats_out, void* workspace, size_t workspace_bytes,
+                               cudaStream_t stream) {
+  MOLT_TRY(check_shape(T, H, V));
+  if (!loss_out || (T > 0 && (!hidden || !W || !targets)) || (grad && (!dW_out || (T > 0 && !dhidden_out))))
+    return fail(MOLT_ERR_INVALID_ARG, "null pointer");
+  if (!aligned16(hidden) || !aligned16(W) || !aligned16(dhidden_out) || !aligned16(dW_out))
+    return fail(MOLT_ERR_INVALID_ARG, "hidden, W, dhidden and dW must be 16-byte aligned");
+  if (denom != denom) return fail(MOLT_ERR_INVALID_ARG, "denom is NaN");
+  if (dW_dtype != MOLT_FP32 && dW_dtype != MOLT_BF16) return fail(MOLT_ERR_INVALID_ARG, "dW is fp32 or bf16");
+  if (accumulate_dW && dW_dtype != MOLT_FP32) return fail(MOLT_ERR_INVALID_ARG, "only an fp32 dW can be added to");
+  CeArgs a{targets, token_weight, -100, 0.f, 0.f, denom};
+  if (opts) {
+    a.ignore_index = opts->ignore_index;
+    a.smoothing = opts->label_smoothing;
+    a.z_loss = opts->z_loss;
+    if (!(a.smoothing >= 0.f && a.smoothing <= 1.f))
+      return fail(MOLT_ERR_INVALID_ARG, "label_smoothing must lie in [0, 1]");
+    if (!(a.z_loss >= 0.f && a.z_loss <= 1e30f)) return fail(MOLT_ERR_INVALID_ARG, "z_loss must be finite and >= 0");
+  }
+  const ChunkPlan cp = chunk_shape(T, H, V, false);
+  if (grad && T > 0 && !cp.use) return fail(MOLT_ERR_UNSUPPORTED_SHAPE, "T and V are too large together");
+  molt_status st;
+  const DeviceInfo* di = device_info(&st);
+  if (!di) return st;
+  if (T == 0) {
+    MOLT_CUDA(cudaMemsetAsync(loss_out, 0, sizeof(float), stream), "memset loss");
+    if (grad && !accumulate_dW)
+      MOLT_CUDA(cudaMemsetAsync(dW_out, 0, static_cast<size_t>(V) * H * (dW_dtype == MOLT_FP32 ? 4 : 2), stream),
+                "memset dW");
+    if (stats_out) MOLT_CUDA(cudaMemsetAsync(stats_out, 0, sizeof(molt_ce_stats), stream), "memset stats");
+    return MOLT_OK;
+  }
+  const int64_t Tcap = round_tiles(T);
+  const int S = forward_splits(Tcap, H, V, di->n_sm);
+  const bool round_dW = dW_dtype != MOLT_FP32;
+  size_t dW32_off;
+  const Layout L = ce_layout(T, H, V, di->n_sm, grad, round_dW, &dW32_off);
+  Scratch sc;
+  MOLT_TRY(get_scratch(sc, workspace, workspace_bytes, L.total, stream));
+  const Workspace w = carve(sc.ptr, L);
+  CUtensorMap tm_h, tm_w;
+  MOLT_TRY(make_tmap(&tm_h, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, w.h_p, Tcap, H, kBK, kTileM));
+  MOLT_TRY(make_tmap(&tm_w, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, W, V, H, kBK, 128));
+  ev_start(0, stream);
+  MOLT_LAUNCH(launch_ce_pack(a, static_cast<int>(T), static_cast<int>(H), hidden, w, logp_out, lse_out,
+                             grad ? cp.ctl_words() : 0, di->n_sm, stream),
+              "pack");
+  ev_stop(0, stream);
+  const bool smooth = a.smoothing != 0.f || a.z_loss != 0.f;
+  MOLT_TRY(run_forward_kernel(di, Tcap, H, V, S, w, tm_h, tm_w, false, smooth, stream));
+  ev_start(2, stream);
+  MOLT_LAUNCH(launch_ce_merge(a, smooth, static_cast<int>(Tcap), static_cast<int>(V), S, w, loss_out, logp_out, lse_out,
+                              stats_out, di->status, stream),
+              "merge");
+  ev_stop(2, stream);
+  if (!grad) return MOLT_OK;
+  float* dW = round_dW ? reinterpret_cast<float*>(static_cast<uint8_t*>(sc.aligned()) + dW32_off)
+                       : static_cast<float*>(dW_out);
+  MOLT_TRY(run_backward_chunk(di, cp, W, T, H, V, w, false, 0, smooth ? kGradSmooth : kGradPlain, dW, accumulate_dW, stream));
+  ev_start(4, stream);
+  MOLT_LAUNCH(launch_cast_dh(w, true, static_cast<int>(T), static_cast<int>(H), dhidden_out, di->n_sm, stream), "cast dh");
+  if (round_dW)
+    MOLT_LAUNCH(launch_cast_bf16(dW, V * H, static_cast<uint16_t*>(dW_out), di->n_sm, stream), "cast dW");
   ev_stop(4, stream);
   return MOLT_OK;
 }
@@ -1165,6 +1292,34 @@ molt_status molt_policy_loss_fwd_bwd_ex(const uint16_t* hidden, const uint16_t* 
                           token_loss_out, nullptr, stats_out, workspace, workspace_bytes, stream);
 }
 
+
+// ------------------------------------------------------------ cross entropy
+size_t molt_cross_entropy_workspace_bytes(int64_t T, int64_t H, int64_t V, int with_backward, int dW_dtype) {
+  if (check_shape(T, H, V) != MOLT_OK) return 0;
+  molt_status st;
+  const DeviceInfo* di = device_info(&st);
+  size_t dW32;
+  return ce_layout(T, H, V, di ? di->n_sm : 152, with_backward != 0, dW_dtype != MOLT_FP32, &dW32).total;
+}
+
+molt_status molt_cross_entropy_fwd(const uint16_t* hidden, const uint16_t* W, const int32_t* targets,
+                                   const float* token_weight, int64_t T, int64_t H, int64_t V, double denom,
+                                   const molt_ce_options* opts, float* loss_out, float* logp_out, float* lse_out,
+                                   molt_ce_stats* stats_out, void* workspace, size_t workspace_bytes,
+                                   cudaStream_t stream) {
+  return cross_entropy_impl(hidden, W, targets, token_weight, T, H, V, denom, opts, loss_out, false, nullptr, nullptr,
+                            MOLT_FP32, 0, logp_out, lse_out, stats_out, workspace, workspace_bytes, stream);
+}
+
+molt_status molt_cross_entropy_fwd_bwd(const uint16_t* hidden, const uint16_t* W, const int32_t* targets,
+                                       const float* token_weight, int64_t T, int64_t H, int64_t V, double denom,
+                                       const molt_ce_options* opts, float* loss_out, uint16_t* dhidden_out, void* dW_out,
+                                       int dW_dtype, int accumulate_dW, float* logp_out, float* lse_out,
+                                       molt_ce_stats* stats_out, void* workspace, size_t workspace_bytes,
+                                       cudaStream_t stream) {
+  return cross_entropy_impl(hidden, W, targets, token_weight, T, H, V, denom, opts, loss_out, true, dhidden_out, dW_out,
+                            dW_dtype, accumulate_dW, logp_out, lse_out, stats_out, workspace, workspace_bytes, stream);
+}
 
 // ------------------------------------------------ vocabulary-parallel calls
 size_t molt_vp_partials_workspace_bytes(int64_t T, int64_t H, int64_t V_shard) {

@@ -2,7 +2,8 @@
 // tokens x vocabulary plane.
 //
 //   g_tv = coef_t (softmax(z_t)_v - [v == x_t]),  coef_t = m_t c_t / D   (Eq. 2)
-//          (+ ecoef_t softmax(z_t)_v (z_tv - mu_t) with an entropy bonus)
+//          (+ ecoef_t softmax(z_t)_v (z_tv - mu_t) with an entropy bonus; label
+//          smoothing and a z term: see kGradSmooth)
 //   dH_t = sum_v g_tv W_v          dW_v = sum_t g_tv h_t
 //
 // A chunk is up to 4096 tokens x 4096 vocab columns.  Its g (bf16, at most
@@ -234,8 +235,8 @@ __device__ __forceinline__ void write_box32(uint32_t box, int lane, const float 
   }
 }
 
-// kEnt: with an entropy bonus; kDet: reproducible sums
-template <bool kEnt, bool kDet>
+// kForm: how z becomes g (kGrad*); kDet: reproducible sums
+template <int kForm, bool kDet>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     lmhead_bwd_chunk_kernel(const __grid_constant__ ChunkMaps m, const ChunkArgs a) {
   extern __shared__ uint8_t smem_raw[];
@@ -562,7 +563,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const bool in = row < n_rows;
         const float coef = in ? a.coef[row] : 0.f;
         float ecoef = 0.f, mu = 0.f;
-        if constexpr (kEnt) {
+        if constexpr (kForm != kGradPlain) {
           if (in) {
             ecoef = a.ecoef[row];
             mu = a.mu[row];
@@ -588,7 +589,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             const int nv = nvalid - c * 64 - u * 32;
             auto p_of = [&](int j) -> float {   // g without the target's term
               const float e = ex2_approx(fmaf(v[j], kLog2e, -lseL));
-              if constexpr (kEnt) return fmaf(ecoef, v[j] - mu, coef) * e;
+              if constexpr (kForm == kGradEntropy) return fmaf(ecoef, v[j] - mu, coef) * e;
+              if constexpr (kForm == kGradSmooth) return fmaf(ecoef, e, -mu);
               return coef * e;
             };
             // a target or an invalid column among the warp's 32 x 32 values is rare
@@ -727,9 +729,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 }  // namespace
 
 cudaError_t launch_lmhead_bwd_chunk(const ChunkMaps& m, const ChunkArgs& a, int n_ctas, cudaStream_t s) {
-  const bool ent = a.ecoef != nullptr;
-  auto* k = a.det_turns != nullptr ? (ent ? &lmhead_bwd_chunk_kernel<true, true> : &lmhead_bwd_chunk_kernel<false, true>)
-                                   : (ent ? &lmhead_bwd_chunk_kernel<true, false> : &lmhead_bwd_chunk_kernel<false, false>);
+  void (*k)(const ChunkMaps, const ChunkArgs) = nullptr;
+  if (a.det_turns != nullptr)
+    k = a.form == kGradEntropy ? &lmhead_bwd_chunk_kernel<kGradEntropy, true> : &lmhead_bwd_chunk_kernel<kGradPlain, true>;
+  else
+    k = a.form == kGradEntropy  ? &lmhead_bwd_chunk_kernel<kGradEntropy, false>
+        : a.form == kGradSmooth ? &lmhead_bwd_chunk_kernel<kGradSmooth, false>
+                                : &lmhead_bwd_chunk_kernel<kGradPlain, false>;
   const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
   if (e != cudaSuccess) return e;
   k<<<n_ctas / 2 * 2, kThreads, kSmemBytes, s>>>(m, a);

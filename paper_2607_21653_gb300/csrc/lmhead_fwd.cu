@@ -55,9 +55,13 @@ constexpr uint32_t kIdesc = idesc_bf16_f32(256, 256, false, false);
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
-template <bool kOrdered>
+// What a row's statistics are: (m, s, q); the same in the reproducible loss call's
+// order; or (m, s, sum of z), which label smoothing needs in the place of q.
+enum Mode : int { kStats = 0, kOrdered = 1, kSumZ = 2 };
+
+template <int kMode>
 __device__ __forceinline__ void split_range(int s, int S, int n_vt, int& vt0, int& vt1) {
-  if constexpr (kOrdered) {
+  if constexpr (kMode == kOrdered) {
     vt0 = static_cast<int>(static_cast<int64_t>(s) * n_vt / S);
     vt1 = static_cast<int>(static_cast<int64_t>(s + 1) * n_vt / S);
   } else {
@@ -67,26 +71,28 @@ __device__ __forceinline__ void split_range(int s, int S, int n_vt, int& vt0, in
   }
 }
 
-// Running statistics of one row.  q2 is in log2 units: q2 = sum e (z - m) log2(e).
+// Running statistics of one row.  q2 is in log2 units: q2 = sum e (z - m) log2(e)
+// (kSumZ: the plain sum of z, which no new maximum rescales).
 // s is summed with its rounding carried along in c (Kahan), so that log s hardly
 // depends on how the columns are split; in the ordered sums it is not (c stays 0).
 struct Stats {
   float m = -INFINITY, s = 0.f, c = 0.f, q2 = 0.f;
+  template <int kMode>
   __device__ __forceinline__ void raise(float cmax) {
     if (cmax > m) {
       if (m != -INFINITY) {
         const float d2 = (m - cmax) * kLog2e;
         const float sc = ex2_approx(d2);
-        q2 = sc * fmaf(d2, s, q2);
+        if constexpr (kMode != kSumZ) q2 = sc * fmaf(d2, s, q2);
         s *= sc;
         c *= sc;
       }
       m = cmax;
     }
   }
-  template <bool kOrdered>
+  template <int kMode>
   __device__ __forceinline__ void add(float ds, float dq) {
-    if constexpr (kOrdered) {
+    if constexpr (kMode == kOrdered) {
       s += ds;
     } else {
       const float y = ds - c, t = s + y;
@@ -98,52 +104,55 @@ struct Stats {
 };
 
 // fold 32 logits (all columns valid) into the row's statistics
-template <bool kOrdered>
+template <int kMode>
 __device__ __forceinline__ void fold_full(const float (&v)[32], Stats& r) {
   float cm[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
   for (int j = 4; j < 32; ++j) cm[j & 3] = fmaxf(cm[j & 3], v[j]);
-  r.raise(fmaxf(fmaxf(cm[0], cm[1]), fmaxf(cm[2], cm[3])));
+  r.raise<kMode>(fmaxf(fmaxf(cm[0], cm[1]), fmaxf(cm[2], cm[3])));
   const float mL = r.m * kLog2e;
-  constexpr int kSums = kOrdered ? 2 : 4;
+  constexpr int kSums = kMode == kOrdered ? 2 : 4;
   float s[4] = {0.f, 0.f, 0.f, 0.f}, q[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int j = 0; j < 32; ++j) {
     const float y = fmaf(v[j], kLog2e, -mL);
     const float e = ex2_approx(y);
     s[j % kSums] += e;
-    q[j % kSums] = fmaf(e, y, q[j % kSums]);
+    if constexpr (kMode == kSumZ)
+      q[j % kSums] += v[j];
+    else
+      q[j % kSums] = fmaf(e, y, q[j % kSums]);
   }
-  if constexpr (kOrdered)
-    r.add<true>(s[0] + s[1], q[0] + q[1]);
+  if constexpr (kMode == kOrdered)
+    r.add<kMode>(s[0] + s[1], q[0] + q[1]);
   else
-    r.add<false>((s[0] + s[1]) + (s[2] + s[3]), (q[0] + q[1]) + (q[2] + q[3]));
+    r.add<kMode>((s[0] + s[1]) + (s[2] + s[3]), (q[0] + q[1]) + (q[2] + q[3]));
 }
 
 // same for a chunk where only the first `nv` (1..31) columns are valid
-template <bool kOrdered>
+template <int kMode>
 __device__ __forceinline__ void fold_partial(const float (&v)[32], int nv, Stats& r) {
   float cmax = v[0];
 #pragma unroll
   for (int j = 1; j < 32; ++j)
     if (j < nv) cmax = fmaxf(cmax, v[j]);
-  r.raise(cmax);
+  r.raise<kMode>(cmax);
   const float mL = r.m * kLog2e;
-  float s = kOrdered ? r.s : 0.f, q = kOrdered ? r.q2 : 0.f;
+  float s = kMode == kOrdered ? r.s : 0.f, q = kMode == kOrdered ? r.q2 : 0.f;
 #pragma unroll
   for (int j = 0; j < 32; ++j) {
     if (j < nv) {
       const float y = fmaf(v[j], kLog2e, -mL);
       const float e = ex2_approx(y);
       s += e;
-      q = fmaf(e, y, q);
+      q = kMode == kSumZ ? q + v[j] : fmaf(e, y, q);
     }
   }
-  if constexpr (kOrdered) {
+  if constexpr (kMode == kOrdered) {
     r.s = s;
     r.q2 = q;
   } else {
-    r.add<false>(s, q);
+    r.add<kMode>(s, q);
   }
 }
 
@@ -156,14 +165,14 @@ __device__ __forceinline__ void unit_of(int u, int n_mt, int S, int& mt, int& s)
   mt = g * kGroup + (r - s * g_mt);
 }
 
-// kOrdered: the sums of the reproducible loss call.  Its results stay the same bits
+// Mode kOrdered: the sums of the reproducible loss call.  Its results stay the same bits
 // from one version of the library to the next, so a row's columns are summed one
 // after the other by one thread (the four warps of the lower column half take all
 // 256 columns, the others none), uncompensated, in the splits of ordered_splits
 // (api.cu) and merged in their order.  T = 16384, V = 65536: 0.49 against
 // 0.38 ms at H = 256, 0.73 and 0.62 at H = 512, 1.33 and 1.21 at H = 1024; at H = 4096
 // the products hide it (4.94 and 4.93).
-template <bool kOrdered>
+template <int kMode>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     lmhead_fwd_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__ CUtensorMap tm_w,
                       const FwdArgs a) {
@@ -194,7 +203,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(smem_u32(&accf_bar[b]), 1);
-      mbar_init(smem_u32(&acce_bar[b]), kOrdered ? kEpiWarps : 2 * kEpiWarps);
+      mbar_init(smem_u32(&acce_bar[b]), kMode == kOrdered ? kEpiWarps : 2 * kEpiWarps);
     }
     for (int s = 0; s < kSlots; ++s) {
       mbar_init(smem_u32(&ufull_bar[s]), 1);
@@ -249,7 +258,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       for (uint32_t ui = 0; u >= 0 && ok; ++ui) {
         int mt, s, vt0, vt1;
         unit_of(u, n_mt, S, mt, s);
-        split_range<kOrdered>(s, S, a.n_vtiles, vt0, vt1);
+        split_range<kMode>(s, S, a.n_vtiles, vt0, vt1);
         for (int vt = vt0; vt < vt1 && ok; ++vt) {
           const int y = (is_a ? mt : vt) * 256 + static_cast<int>(rank) * 128;
           for (int kb = 0; kb < kblocks; ++kb) {
@@ -282,7 +291,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       for (uint32_t ui = 0; u >= 0 && ok; ++ui) {
         int mt, s, vt0, vt1;
         unit_of(u, n_mt, S, mt, s);
-        split_range<kOrdered>(s, S, a.n_vtiles, vt0, vt1);
+        split_range<kMode>(s, S, a.n_vtiles, vt0, vt1);
         for (int vt = vt0; vt < vt1 && ok; ++vt) {
           const uint32_t buf = acc_it & 1u;
           if (!(ok = mbar_wait(smem_u32(&acce_bar[buf]), ((acc_it >> 1) & 1u) ^ 1u, abort_flag, a.err))) break;
@@ -343,7 +352,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     // epilogue: warp w may read TMEM lanes [32 (w % 4), 32 (w % 4) + 32)
     const int q = warp & 3;
     const int hf = (warp - 2) >> 2;
-    constexpr int kCols = kOrdered ? 256 : 128;   // columns of a tile that one warp reads
+    constexpr int kCols = kMode == kOrdered ? 256 : 128;   // columns of a tile that one warp reads
     const int r_in_tile = static_cast<int>(rank) * 128 + q * 32 + lane;
     const uint32_t acce_lead0 = mapa_shared(smem_u32(&acce_bar[0]), 0);
     uint32_t acc_it = 0;
@@ -353,10 +362,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       if (lane == 0) u = next_unit(ui);
       u = __shfl_sync(0xffffffffu, u, 0);
       if (u < 0) break;
-      if (kOrdered && hf == 1) continue;
+      if (kMode == kOrdered && hf == 1) continue;
       int mt, s, vt0, vt1;
       unit_of(u, n_mt, S, mt, s);
-      split_range<kOrdered>(s, S, a.n_vtiles, vt0, vt1);
+      split_range<kMode>(s, S, a.n_vtiles, vt0, vt1);
       const int row = mt * 256 + r_in_tile;
       const bool valid = row < n_rows;
       const int x = valid ? a.tok_p[row] : -1;
@@ -384,9 +393,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             found = true;
           }
           if (c0 + 32 <= ncols)
-            fold_full<kOrdered>(v, st);
+            fold_full<kMode>(v, st);
           else
-            fold_partial<kOrdered>(v, ncols - c0, st);
+            fold_partial<kMode>(v, ncols - c0, st);
         }
         // every lane's TMEM reads are complete: one arrival per warp hands it back
         tc_fence_before();
@@ -396,7 +405,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       }
       if (!ok) break;
       if (valid && found) a.zx[row] = zxv;
-      if constexpr (kOrdered) {
+      if constexpr (kMode == kOrdered) {
         if (valid) a.part[static_cast<int64_t>(s) * a.rows_cap + row] = make_float4(st.m, st.s, st.q2 * kLn2, 0.f);
         continue;
       }
@@ -420,12 +429,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             const float d = (mi - M) * kLog2e;
             const float f = ex2_approx(d);
             S2 = fmaf(f, si, S2);
-            Q2 = fmaf(f, fmaf(d, si, qi), Q2);
+            if constexpr (kMode == kSumZ)
+              Q2 += qi;
+            else
+              Q2 = fmaf(f, fmaf(d, si, qi), Q2);
           }
         };
         add(st.m, st.s, st.q2);
         add(mo, so, qo);
-        if (valid) a.part[static_cast<int64_t>(s) * a.rows_cap + row] = make_float4(M, S2, Q2 * kLn2, 0.f);
+        if (valid)
+          a.part[static_cast<int64_t>(s) * a.rows_cap + row] = make_float4(M, S2, kMode == kSumZ ? Q2 : Q2 * kLn2, 0.f);
       }
     }
   }
@@ -445,9 +458,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 cudaError_t launch_lmhead_fwd(const CUtensorMap& tm_h, const CUtensorMap& tm_w, const FwdArgs& a, int grid,
                               cudaStream_t s) {
   // the shared-memory attribute is per device: set it on each device once
-  static std::atomic<unsigned long long> attr_set[2] = {};
-  auto* const k = a.ordered ? &lmhead_fwd_kernel<true> : &lmhead_fwd_kernel<false>;
-  auto& set = attr_set[a.ordered ? 1 : 0];
+  static std::atomic<unsigned long long> attr_set[3] = {};
+  const int mode = a.ordered ? kOrdered : a.sum_z ? kSumZ : kStats;
+  auto* const k = mode == kOrdered ? &lmhead_fwd_kernel<kOrdered>
+                  : mode == kSumZ  ? &lmhead_fwd_kernel<kSumZ>
+                                   : &lmhead_fwd_kernel<kStats>;
+  auto& set = attr_set[mode];
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;

@@ -18,7 +18,8 @@ constexpr int kBK = 64;       // K elements per 128-byte swizzled row
 // Device pointers into one call's workspace (all regions 256-byte aligned).
 struct Workspace {
   int32_t* counts;      // [0] active rows n, [1] backward tiles, [2] rejected sequences,
-                        // [3] rows with a gradient (the backward's rows), [4] the forward's next unit
+                        // [3] rows with a gradient (the backward's rows), [4] the forward's next unit,
+                        // [5] cross entropy: merge blocks that are done
   int32_t* row_map;     // [T]    packed row -> original row
   int32_t* pos_of_row;  // [T]    original row -> packed row or -1
   int32_t* tok_p;       // [Tcap] packed tokens
@@ -63,6 +64,7 @@ struct FwdArgs {
   int V, H;
   int n_split;
   int n_vtiles;
+  bool sum_z;           // partials hold the sum of z in the place of sum e (z - max)
   bool ordered;         // the reproducible loss call's sums: columns in order, by ordered_splits
   int32_t* next_unit;   // zeroed
   float4* part;         // [n_split, rows_cap]
@@ -95,6 +97,10 @@ struct BwdArgs {
 // backward over chunks of the tokens x vocabulary plane (lmhead_bwd_chunk.cu)
 constexpr int kChunkCtlHead = 64;    // control words before the per-chunk counters:
                                      // [0] next tile, [1] set once any wait gives up
+// g of one logit z of a row, p = e^(z - lse):
+constexpr int kGradPlain = 0;     // coef (p - [target])
+constexpr int kGradEntropy = 1;   // coef (p - [target]) + ecoef p (z - mu)
+constexpr int kGradSmooth = 2;    // ecoef p - mu - coef [target]   (label smoothing, z term)
 struct ChunkMaps {                   // bf16 maps have 64-column (128-byte) boxes
   CUtensorMap h128, w128;            // packed hidden rows and W, 128 rows
   CUtensorMap g128, g32;             // chunk buffers: 64-column panels of token rows; g32 stores
@@ -105,7 +111,8 @@ struct ChunkArgs {
   const int32_t* tok_p;
   const float* lse;
   const float* coef;
-  const float* ecoef;        // or nullptr
+  int form;                  // how z becomes g: kGradPlain, kGradEntropy, kGradSmooth
+  const float* ecoef;        // the forms' further row values (kGradPlain: none)
   const float* mu;
   const int32_t* counts;     // counts[3] = rows
   int V, H;
@@ -189,8 +196,8 @@ cudaError_t launch_finish(int H, int pad, bool with_ecoef, double denom, const W
 cudaError_t launch_seq_gate(int T, int Tcap, const LossEx& ex, const Workspace& ws, unsigned* err, cudaStream_t s);
 cudaError_t launch_loss_rows_ex(int Tcap, double denom, float clip_lo, float clip_hi, const LossEx& ex,
                                 const Workspace& ws, float* tokloss_out, cudaStream_t s);
-// dhidden_out[t] = bf16(the fp32 accumulator row of t)
-cudaError_t launch_cast_dh(const Workspace& ws, int T, int H, uint16_t* dh_out, int n_sm, cudaStream_t s);
+// dhidden_out[t] = bf16(the fp32 accumulator row of t); identity: packed rows are the backward rows
+cudaError_t launch_cast_dh(const Workspace& ws, bool identity, int T, int H, uint16_t* dh_out, int n_sm, cudaStream_t s);
 // vocabulary shards: one shard's per-row statistics (original order) from the
 // forward's split partials; the merge of all shards' statistics with the Eq. 2
 // terms; the rows of a shard's backward (coef != 0) and their packing; the
@@ -204,6 +211,25 @@ cudaError_t launch_vp_pack(int T, int H, int pad, const uint16_t* hidden, const 
                            const float* coef, int tok_shift, const Workspace& ws, int64_t ctl_words, int n_sm,
                            cudaStream_t s);
 cudaError_t launch_vp_dh_out(const Workspace& ws, int T, int H, float* out, int n_sm, cudaStream_t s);
+
+// ce.cu: cross entropy's row kernels
+struct CeArgs {
+  const int32_t* targets;
+  const float* weight;       // [T] or nullptr
+  int64_t ignore_index;
+  float smoothing, z_loss;
+  double denom;
+};
+// rows whose target is not ignore_index packed as launch_pack does (weights into ws.b_p),
+// padded with zero rows to whole K blocks; all packed rows are the backward's rows
+cudaError_t launch_ce_pack(const CeArgs& a, int T, int H, const uint16_t* hidden, const Workspace& ws, float* logp_out,
+                           float* lse_out, int64_t ctl_words, int n_sm, cudaStream_t s);
+// split partials -> lse, the loss and its stats, and the backward's row values; smooth:
+// partials hold the sum of z
+cudaError_t launch_ce_merge(const CeArgs& a, bool smooth, int Tcap, int V, int n_parts, const Workspace& ws, float* loss_out,
+                            float* logp_out, float* lse_out, molt_ce_stats* stats, unsigned* err, cudaStream_t s);
+// dst = bf16(src), n a multiple of 8
+cudaError_t launch_cast_bf16(const float* src, int64_t n, uint16_t* dst, int n_sm, cudaStream_t s);
 
 // lmhead_fwd.cu
 // (boxes of 128 rows x kBK columns of the packed hidden rows and of W)
