@@ -11,10 +11,10 @@
 namespace molt {
 namespace {
 
-constexpr int kSumCols = 32, kSumWarps = 16;
+constexpr int kSumCols = 32, kSumWarps = 32;
 
 // out[c] (+)= sum over blocks of part[block][which][c], blocks in a fixed order: warp w
-// takes every 16th, then the warps' sums are added one after the other.
+// takes every 32nd, eight loads at a time, then the warps' sums are added in order.
 __global__ void __launch_bounds__(kSumCols * kSumWarps) norm_part_sum_kernel(const float* __restrict__ part, int blocks, int H,
                                                                              float* o0, float* o1, float* o2, int accumulate) {
   __shared__ float sh[kSumWarps][kSumCols];
@@ -25,8 +25,16 @@ __global__ void __launch_bounds__(kSumCols * kSumWarps) norm_part_sum_kernel(con
   const int c = blockIdx.x * kSumCols + lane;
   float s = 0.f;
   if (c < H) {
-#pragma unroll 4
-    for (int b = warp; b < blocks; b += kSumWarps) s += part[(static_cast<int64_t>(b) * 3 + which) * H + c];
+    for (int b0 = warp; b0 < blocks; b0 += 8 * kSumWarps) {
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int b = b0 + i * kSumWarps;
+        v[i] = b < blocks ? part[(static_cast<int64_t>(b) * 3 + which) * H + c] : 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += v[i];
+    }
   }
   sh[warp][lane] = s;
   __syncthreads();
@@ -107,23 +115,61 @@ bool vectors(const molt_norm_desc* d, const NormArgs& a, std::initializer_list<c
   return true;
 }
 
+// Rows in registers, a block to each (or to four short ones): for the few rows of a
+// decoding step, and for vectors of more elements than the persistent kernels hold.
 NormShape row_shape(int H, bool vec) {
   NormShape s{};
   s.vec = vec ? 8 : 1;
-  s.elems = H <= 8 * kNormMaxThreads ? 8 : H <= 16 * kNormMaxThreads ? 16 : H <= kNormMaxH ? 32 : 0;
+  s.elems = !vec ? 0 : H <= 8 * kNormMaxThreads ? 8 : H <= 16 * kNormMaxThreads ? 16 : H <= kNormMaxH ? 32 : 0;
   s.threads = s.elems == 0 ? kNormMaxThreads : ((H + s.elems - 1) / s.elems + 31) / 32 * 32;
   s.rows = s.threads == 32 ? 4 : 1;
   return s;
 }
 
-constexpr int kMaxBlocksPerSM = 8;
 int64_t max_blocks(int n_sm) { return kMaxBlocksPerSM * static_cast<int64_t>(n_sm); }
 
-cudaError_t launch(const molt_norm_desc* d, const NormArgs& a, const NormShape& s, int grid, bool bwd, cudaStream_t stream) {
+// The persistent form of a call (in s and a), or false for rows that 16 elements to a
+// thread do not hold or shared memory does not.  A row's stage holds, side by side, what
+// is read of it.
+bool rows_shape(const molt_norm_desc* d, bool bwd, NormArgs& a, NormShape& s) {
+  if (a.H > 16 * kNormMaxThreads) return false;
+  // a row that begins inside a 16-byte word touches one more
+  const auto bytes = [&](int dt) { return a.H * dtype_bytes(dt) / 16 * 16 + (s.vec == 8 ? 0 : 32); };
+  const int xb = bytes(d->dtype), rb = bytes(d->residual_dtype);
+  int at = xb;
+  auto take = [&at](bool wanted, int n) {
+    const int r = at;
+    if (wanted) at += n;
+    return r;
+  };
+  a.at_r = take(bwd ? a.w_pre != nullptr : a.r != nullptr, rb);
+  a.at_dy = take(bwd && a.w_pre != nullptr, xb);
+  a.at_dr = take(bwd && a.dr != nullptr, rb);
+  a.at_gate = take(a.gate_kind == MOLT_GATE_FULL, xb);
+  a.stage_bytes = at;
+  // 16 elements to a thread where that makes a row one warp's, in the forward for longer
+  // rows too (32768 x 2048 with an fp32 stream: 8 elements 190 us, 16 132; 16001 x 5120 141
+  // and 110), not in the backward, whose sums then take too many registers (190 and 213, 189
+  // and 221), nor where elements come one by one (20000 x 2049 forward 115 and 135)
+  const int most8 = !bwd && s.vec == 8 ? 256 : 8 * 640;
+  const int elems = a.H <= 256 || (a.H > 512 && a.H <= most8) ? 8 : 16;
+  s.elems = elems;
+  s.threads = ((a.H + elems - 1) / elems + 31) / 32 * 32;
+  s.rows = s.threads == 32 ? kRingRows : 1;
+  a.stages = std::min(kRingStages, kRingSmem / (s.rows * a.stage_bytes));
+  s.persistent = a.stages >= 1;
+  if (!s.persistent) return false;
+  s.smem = static_cast<size_t>(s.rows) * a.stages * a.stage_bytes;
+  if (bwd && s.rows > 1) s.smem = std::max(s.smem, static_cast<size_t>(s.rows) * a.H * sizeof(float));
+  return true;
+}
+
+cudaError_t launch(const molt_norm_desc* d, const NormArgs& a, const NormShape& s, int* grid, bool bwd, cudaStream_t stream) {
+  const int n_sm = device_sm_count();
   const bool r_f32 = d->residual_dtype == MOLT_FP32;
-  if (d->dtype == MOLT_FP32) return launch_norm_fp32(a, s, grid, bwd, stream);
-  return d->dtype == MOLT_FP16 ? launch_norm_fp16(a, s, grid, r_f32, bwd, stream)
-                               : launch_norm_bf16(a, s, grid, r_f32, bwd, stream);
+  if (d->dtype == MOLT_FP32) return launch_norm_fp32(a, s, n_sm, grid, bwd, stream);
+  return d->dtype == MOLT_FP16 ? launch_norm_fp16(a, s, n_sm, grid, r_f32, bwd, stream)
+                               : launch_norm_bf16(a, s, n_sm, grid, r_f32, bwd, stream);
 }
 
 }  // namespace
@@ -165,10 +211,16 @@ molt_status molt_residual_norm_fwd(const molt_norm_desc* desc, const void* x, co
   a.r_out = residual_out;
   a.rstd_post = rstd_post;
   a.rstd_pre = rstd_pre;
-  const NormShape s = row_shape(a.H, vectors(desc, a, {x, residual, w_post, w_pre, y, residual_out,
-                                                       desc->gate_kind == MOLT_GATE_TOKEN ? nullptr : gate}));
-  const int grid = static_cast<int>((a.T + s.rows - 1) / s.rows);
-  if (const cudaError_t e = launch(desc, a, s, grid, false, stream); e != cudaSuccess) return cuda_fail(e, "residual norm");
+  molt_status st;
+  a.err = device_status_word(&st);
+  if (!a.err) return st;
+  NormShape s = row_shape(a.H, vectors(desc, a, {x, residual, w_post, w_pre, y, residual_out,
+                                                 desc->gate_kind == MOLT_GATE_TOKEN ? nullptr : gate}));
+  // rows that the SMs hold at once gain nothing from copies ahead
+  const NormShape few = s;
+  if ((s.vec == 1 || a.T > 16 * int64_t(device_sm_count())) && !rows_shape(desc, false, a, s)) s = few;
+  int grid;
+  if (const cudaError_t e = launch(desc, a, s, &grid, false, stream); e != cudaSuccess) return cuda_fail(e, "residual norm");
   note_launches(1);
   return MOLT_OK;
 }
@@ -239,14 +291,16 @@ molt_status molt_residual_norm_bwd(const molt_norm_desc* desc, const void* dy, c
   a.dr_out = dresidual_out;
   a.dgate = dgate;
   a.part = static_cast<float*>(sc.aligned());
-  const NormShape s =
+  molt_status st;
+  a.err = device_status_word(&st);
+  if (!a.err) return st;
+  NormShape s =
       row_shape(a.H, vectors(desc, a, {dy, dresidual, x, residual, w_post, w_pre, dx, dresidual_out,
                                        desc->gate_kind == MOLT_GATE_TOKEN ? nullptr : gate,
                                        desc->gate_kind == MOLT_GATE_FULL ? dgate : nullptr}));
-  const int per_sm = std::min(kMaxBlocksPerSM, std::max(1, 768 / (s.threads * s.rows)));
-  const int n_sm = device_sm_count();
-  const int grid = static_cast<int>(std::min<int64_t>((a.T + s.rows - 1) / s.rows, int64_t(n_sm) * per_sm));
-  if (const cudaError_t e = launch(desc, a, s, grid, true, stream); e != cudaSuccess)
+  if (!rows_shape(desc, true, a, s)) s = NormShape{kNormMaxThreads, 1, 0, 1, false, 0};
+  int grid;
+  if (const cudaError_t e = launch(desc, a, s, &grid, true, stream); e != cudaSuccess)
     return cuda_fail(e, "residual norm backward");
   note_launches(1);
   if (!sums[0] && !sums[1] && !sums[2]) return MOLT_OK;

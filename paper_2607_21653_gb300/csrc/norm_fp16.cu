@@ -3,10 +3,9 @@
 
 namespace molt {
 
-cudaError_t launch_norm_fp16(const NormArgs& a, const NormShape& s, int grid, bool r_f32, bool bwd, cudaStream_t stream) {
+cudaError_t launch_norm_fp16(const NormArgs& a, const NormShape& s, int n_sm, int* grid, bool r_f32, bool bwd, cudaStream_t stream) {
   using X = __half;
-  if (bwd) return r_f32 ? launch_norm_bwd_typed<X, float>(a, s, grid, stream) : launch_norm_bwd_typed<X, X>(a, s, grid, stream);
-  return r_f32 ? launch_norm_fwd_typed<X, float>(a, s, grid, stream) : launch_norm_fwd_typed<X, X>(a, s, grid, stream);
+  return r_f32 ? launch_norm_typed<X, float>(a, s, n_sm, grid, bwd, stream) : launch_norm_typed<X, X>(a, s, n_sm, grid, bwd, stream);
 }
 
 }  // namespace molt

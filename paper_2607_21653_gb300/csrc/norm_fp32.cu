@@ -3,8 +3,8 @@
 
 namespace molt {
 
-cudaError_t launch_norm_fp32(const NormArgs& a, const NormShape& s, int grid, bool bwd, cudaStream_t stream) {
-  return bwd ? launch_norm_bwd_typed<float, float>(a, s, grid, stream) : launch_norm_fwd_typed<float, float>(a, s, grid, stream);
+cudaError_t launch_norm_fp32(const NormArgs& a, const NormShape& s, int n_sm, int* grid, bool bwd, cudaStream_t stream) {
+  return launch_norm_typed<float, float>(a, s, n_sm, grid, bwd, stream);
 }
 
 }  // namespace molt

@@ -69,4 +69,61 @@ __device__ __forceinline__ void store_vec(T* p, const float (&v)[kV]) {
   }
 }
 
+// ------------------------------------------------- pairs of fp32
+// One instruction for both.  Kept as one 64-bit value: as two floats, packed for every
+// operation, the copies cost more than the pairs save.
+struct F2 {
+  unsigned long long v;
+  __device__ __forceinline__ float x() const { return __uint_as_float(static_cast<uint32_t>(v)); }
+  __device__ __forceinline__ float y() const { return __uint_as_float(static_cast<uint32_t>(v >> 32)); }
+};
+__device__ __forceinline__ F2 f2(float x, float y) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ F2 f2(float x) { return f2(x, x); }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+// 8 consecutive elements as pairs, 16-byte aligned
+template <class T>
+__device__ __forceinline__ void load_pairs(const T* p, F2* v) {
+  if constexpr (sizeof(T) == 4) {
+    const ulonglong2 a = reinterpret_cast<const ulonglong2*>(p)[0], b = reinterpret_cast<const ulonglong2*>(p)[1];
+    v[0].v = a.x, v[1].v = a.y, v[2].v = b.x, v[3].v = b.y;
+  } else {
+    const uint4 q = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float lo, hi;
+      unpack2(w[j], p, lo, hi);
+      v[j] = f2(lo, hi);
+    }
+  }
+}
+template <class T>
+__device__ __forceinline__ void store_pairs(T* p, const F2* v) {
+  if constexpr (sizeof(T) == 4) {
+    reinterpret_cast<ulonglong2*>(p)[0] = make_ulonglong2(v[0].v, v[1].v);
+    reinterpret_cast<ulonglong2*>(p)[1] = make_ulonglong2(v[2].v, v[3].v);
+  } else {
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack2(v[0].x(), v[0].y(), p), pack2(v[1].x(), v[1].y(), p),
+                                              pack2(v[2].x(), v[2].y(), p), pack2(v[3].x(), v[3].y(), p));
+  }
+}
+
 }  // namespace molt
