@@ -4,13 +4,27 @@ from __future__ import annotations
 
 import ctypes
 
-from . import _bf16_bits, _check, _ptr, _stream, _torch, _workspace, load
-from .stream import _dtype_code, _same_device, _shaped
+from . import _check, _stream, _torch, _workspace, load
+from .stream import _at, _cuda, _dtype_code, _shaped
 
 
 class CrossEntropyOptions(ctypes.Structure):
     """molt_ce_options."""
     _fields_ = [("ignore_index", ctypes.c_int64), ("label_smoothing", ctypes.c_float), ("z_loss", ctypes.c_float)]
+
+
+_options_cache: dict = {}
+
+
+def _options(ignore_index, label_smoothing, z_loss):
+    """Reference to the molt_ce_options of these values (read only)."""
+    key = (ignore_index, label_smoothing, z_loss)
+    ref = _options_cache.get(key)
+    if ref is None:
+        if len(_options_cache) >= 64:
+            _options_cache.clear()
+        ref = _options_cache[key] = ctypes.byref(CrossEntropyOptions(*key))
+    return ref
 
 
 def _prepare(hidden, weight, targets, token_weight):
@@ -21,7 +35,6 @@ def _prepare(hidden, weight, targets, token_weight):
     _shaped(targets, (T,), "targets")
     if token_weight is not None:
         _shaped(token_weight, (T,), "token_weight")
-    _same_device(hidden.device, weight=weight, targets=targets, token_weight=token_weight)
     return T, H, V
 
 
@@ -33,21 +46,23 @@ def cross_entropy_fwd(hidden, weight, targets, token_weight=None, denom=0.0, ign
     want_token_outputs; 0 on ignored rows), stats [5 x 8 bytes])."""
     torch = _torch()
     T, H, V = _prepare(hidden, weight, targets, token_weight)
-    dev, f32 = hidden.device, torch.float32
-    out = {"loss": torch.empty(1, dtype=f32, device=dev),
-           "logp": torch.empty(T, dtype=f32, device=dev) if want_token_outputs else None,
-           "lse": torch.empty(T, dtype=f32, device=dev) if want_token_outputs else None,
-           "stats": torch.empty(5, dtype=torch.float64, device=dev)}
-    opts = CrossEntropyOptions(int(ignore_index), float(label_smoothing), float(z_loss))
+    dev = _cuda(hidden, "hidden")
+    f32, bf16 = torch.float32, torch.bfloat16
+    loss = torch.empty(1, dtype=f32, device=dev)
+    stats = torch.empty(5, dtype=torch.float64, device=dev)
+    logp = lse = None
+    if want_token_outputs:
+        logp, lse = torch.empty(T, dtype=f32, device=dev), torch.empty(T, dtype=f32, device=dev)
     L = load()
     ws = workspace
     if ws is None:
-        ws = _workspace(int(L.molt_cross_entropy_workspace_bytes(T, H, V, 0, 2)), dev, "cross_entropy_fwd", stream)
+        ws = _workspace(L.molt_cross_entropy_workspace_bytes(T, H, V, 0, 2), dev, "cross_entropy_fwd", stream)
     _check(L.molt_cross_entropy_fwd(
-        _bf16_bits(hidden, "hidden"), _bf16_bits(weight, "weight"), _ptr(targets, torch.int32, "targets"),
-        _ptr(token_weight, f32, "token_weight"), T, H, V, float(denom), ctypes.byref(opts), _ptr(out["loss"]),
-        _ptr(out["logp"]), _ptr(out["lse"]), _ptr(out["stats"]), ws.data_ptr(), ws.numel(), _stream(stream, dev.index)))
-    return out
+        _at(hidden, bf16, dev, "hidden"), _at(weight, bf16, dev, "weight"), _at(targets, torch.int32, dev, "targets"),
+        _at(token_weight, f32, dev, "token_weight"), T, H, V, denom, _options(ignore_index, label_smoothing, z_loss),
+        loss.data_ptr(), _at(logp, f32, dev, "logp"), _at(lse, f32, dev, "lse"), stats.data_ptr(), ws.data_ptr(),
+        ws.numel(), _stream(stream, dev.index)))
+    return {"loss": loss, "logp": logp, "lse": lse, "stats": stats}
 
 
 def cross_entropy_fwd_bwd(hidden, weight, targets, token_weight=None, denom=0.0, ignore_index=-100,
@@ -59,30 +74,31 @@ def cross_entropy_fwd_bwd(hidden, weight, targets, token_weight=None, denom=0.0,
     added."""
     torch = _torch()
     T, H, V = _prepare(hidden, weight, targets, token_weight)
-    dev, f32 = hidden.device, torch.float32
+    if dW is not None:
+        _shaped(dW, (V, H), "dW")
+    dev = _cuda(hidden, "hidden")
+    f32, bf16 = torch.float32, torch.bfloat16
     if dW is None:
         dW = torch.empty(V, H, dtype=f32 if dW_dtype is None else dW_dtype, device=dev)
         accumulate_dW = False
-    else:
-        _shaped(dW, (V, H), "dW")
-        _same_device(dev, dW=dW)
-    out = {"loss": torch.empty(1, dtype=f32, device=dev),
-           "logp": torch.empty(T, dtype=f32, device=dev) if want_token_outputs else None,
-           "lse": torch.empty(T, dtype=f32, device=dev) if want_token_outputs else None,
-           "stats": torch.empty(5, dtype=torch.float64, device=dev),
-           "dhidden": torch.empty(T, H, dtype=torch.bfloat16, device=dev), "dW": dW}
     code = _dtype_code(dW.dtype, "dW")
-    opts = CrossEntropyOptions(int(ignore_index), float(label_smoothing), float(z_loss))
+    loss = torch.empty(1, dtype=f32, device=dev)
+    stats = torch.empty(5, dtype=torch.float64, device=dev)
+    dhidden = torch.empty(T, H, dtype=bf16, device=dev)
+    logp = lse = None
+    if want_token_outputs:
+        logp, lse = torch.empty(T, dtype=f32, device=dev), torch.empty(T, dtype=f32, device=dev)
     L = load()
     ws = workspace
     if ws is None:
-        ws = _workspace(int(L.molt_cross_entropy_workspace_bytes(T, H, V, 1, code)), dev, "cross_entropy", stream)
+        ws = _workspace(L.molt_cross_entropy_workspace_bytes(T, H, V, 1, code), dev, "cross_entropy", stream)
     _check(L.molt_cross_entropy_fwd_bwd(
-        _bf16_bits(hidden, "hidden"), _bf16_bits(weight, "weight"), _ptr(targets, torch.int32, "targets"),
-        _ptr(token_weight, f32, "token_weight"), T, H, V, float(denom), ctypes.byref(opts), _ptr(out["loss"]),
-        _ptr(out["dhidden"]), _ptr(dW, dW_dtype, "dW"), code, 1 if accumulate_dW else 0, _ptr(out["logp"]),
-        _ptr(out["lse"]), _ptr(out["stats"]), ws.data_ptr(), ws.numel(), _stream(stream, dev.index)))
-    return out
+        _at(hidden, bf16, dev, "hidden"), _at(weight, bf16, dev, "weight"), _at(targets, torch.int32, dev, "targets"),
+        _at(token_weight, f32, dev, "token_weight"), T, H, V, denom, _options(ignore_index, label_smoothing, z_loss),
+        loss.data_ptr(), dhidden.data_ptr(), _at(dW, dW_dtype or dW.dtype, dev, "dW"), code, 1 if accumulate_dW else 0,
+        _at(logp, f32, dev, "logp"), _at(lse, f32, dev, "lse"), stats.data_ptr(), ws.data_ptr(), ws.numel(),
+        _stream(stream, dev.index)))
+    return {"loss": loss, "logp": logp, "lse": lse, "stats": stats, "dhidden": dhidden, "dW": dW}
 
 
 def cross_entropy_stats(stats_tensor) -> dict:

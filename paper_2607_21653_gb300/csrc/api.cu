@@ -229,11 +229,32 @@ ChunkPlan chunk_shape(int64_t T, int64_t H, int64_t V, bool det) {
   const int64_t tiles = p.n_t * p.n_v + (p.n_t * n_vc + p.n_v * n_tc) * p.n_h;
   p.use = tiles < (int64_t(1) << 30);   // claimed with a 32-bit counter
   p.max_chunks = n_tc * n_vc;
-  const int64_t ct = std::min(p.n_t, p.chunk_t), cv = std::min(p.n_v, p.chunk_v);
+  const int64_t ct = std::max<int64_t>(1, std::min(p.n_t, p.chunk_t)), cv = std::min(p.n_v, p.chunk_v);   // T = 0: no tiles
   p.panel_rows = ct * 256;
   p.buf_panels = cv * 4;
   // all buffers together stay at 64 MB, half of L2
   p.n_buf = static_cast<int>(std::min<int64_t>(most_buf, std::max<int64_t>(2, 512 / (ct * cv))));
+  return p;
+}
+// As chunk_shape, for a dW that is stored in bf16: one chunk over up to 32 tiles of
+// tokens, of fewer columns, so that every dW tile has one contribution and is rounded as
+// it is stored.  Against several token chunks, fp32 sums and a pass that rounds them (us):
+// T = 8192 (30 % ignored), H = 4096, V = 151936 17190 and 17420; T = 5000, H = 2048, V =
+// 150000 4640 and 5020; T = 3000, H = 1024, V = 50000 820 and 890; but with H = 320, whose
+// tiles are short and wait for more of them, 810 and 610 (T = 5000, V = 50000).
+ChunkPlan chunk_shape_bf16(int64_t T, int64_t H, int64_t V) {
+  ChunkPlan p = chunk_shape(T, H, V, false);
+  if (p.n_t <= p.chunk_t || p.n_t > 32 || H < 1024) return p;
+  const int64_t tiles = p.chunk_t * p.chunk_v;
+  p.chunk_t = p.n_t;
+  p.chunk_v = std::max<int64_t>(1, tiles / p.chunk_t);
+  const int64_t n_vc = (p.n_v + p.chunk_v - 1) / p.chunk_v;
+  p.use = p.n_t * p.n_v + (p.n_t * n_vc + p.n_v) * p.n_h < (int64_t(1) << 30);
+  p.max_chunks = n_vc;
+  const int64_t cv = std::min(p.n_v, p.chunk_v);
+  p.panel_rows = p.n_t * 256;
+  p.buf_panels = cv * 4;
+  p.n_buf = static_cast<int>(std::min<int64_t>(16, std::max<int64_t>(2, 512 / (p.n_t * cv))));
   return p;
 }
 ChunkPlan chunk_plan(int64_t T, int64_t H, int64_t V, bool det) {
@@ -274,7 +295,8 @@ ChunkReserve chunk_reserve(int64_t T, int64_t H, int64_t V, bool det, bool alway
   const int64_t n_t = (T + 255) / 256, n_v = (V + 255) / 256;
   const ChunkPlan plain = chunk_plan(T, H, V, false), p = chunk_plan(T, H, V, det);
   if (always || plain.use || p.use) {
-    r.g = static_cast<size_t>(std::min<int64_t>(512, 16 * std::min<int64_t>(n_t, 16) * std::min<int64_t>(n_v, 16))) *
+    // (one chunk over all tokens: up to 32 tiles of them)
+    r.g = static_cast<size_t>(std::min<int64_t>(512, 16 * std::min<int64_t>(n_t, always ? 32 : 16) * std::min<int64_t>(n_v, 16))) *
           (256 * 256 * 2);
     r.ctl = static_cast<size_t>(kChunkCtlHead + 4 * ((n_t + 3) / 4) * ((n_v + 3) / 4)) * 4;
   }
@@ -292,7 +314,7 @@ int64_t part_rows(int64_t Tcap, int64_t V, int n_sm) {
 
 struct Layout {
   size_t counts, row_map, pos, tok_p, b_p, adv_p, h_p, part, zx, lse, coef, tile_list, red, dh32, turns, g, ctl;
-  size_t lp_p, ent_p, ecoef, mu, gate_p;
+  size_t lp_p, ent_p, ecoef, mu, gate_p, scale;
   size_t live_of, h_l, tok_l, lse_l, coef_l, ecoef_l, mu_l, total;
 };
 
@@ -418,17 +440,19 @@ Layout ce_layout(int64_t T, int64_t H, int64_t V, int n_sm, bool with_bwd, bool 
   L.h_p = take(Tcap * H * 2);
   L.part = take(static_cast<size_t>(part_rows(Tcap, V, n_sm)) * 16);
   L.zx = take(Tcap * 4);
+  L.adv_p = take(Tcap * 4);
   L.lse = take(Tcap * 4);
   L.coef = take(Tcap * 4);
   L.ecoef = take(Tcap * 4);
   L.mu = take(Tcap * 4);
-  L.red = take(Tcap / kRedRows * kRedSlots * 8);
+  L.scale = take(4);
+  L.red = take((Tcap + 7) / 8 * kRedSlots * 8);
   L.dh32 = with_bwd ? take(static_cast<size_t>(Tcap) * H * 4) : o;
   const ChunkReserve cr = chunk_reserve(T, H, V, false, true);
   L.g = with_bwd ? take(cr.g) : o;
   L.ctl = with_bwd ? take(cr.ctl) : o;
   *dW32_off = with_bwd && dW32 ? take(static_cast<size_t>(V) * H * 4) : o;
-  L.adv_p = L.tile_list = L.lp_p = L.ent_p = L.gate_p = L.live_of = o;
+  L.tile_list = L.lp_p = L.ent_p = L.gate_p = L.live_of = o;
   L.h_l = L.h_p;
   L.tok_l = L.tok_p;
   L.lse_l = L.lse;
@@ -453,6 +477,7 @@ Workspace carve(void* base, const Layout& L) {
   w.part = reinterpret_cast<float4*>(p + L.part);
   w.zx = reinterpret_cast<float*>(p + L.zx);
   w.lse = reinterpret_cast<float*>(p + L.lse);
+  w.scale = reinterpret_cast<float*>(p + L.scale);
   w.coef = reinterpret_cast<float*>(p + L.coef);
   w.tile_list = reinterpret_cast<int32_t*>(p + L.tile_list);
   w.red = reinterpret_cast<double*>(p + L.red);
@@ -664,10 +689,10 @@ molt_status zero_backward_targets(const Workspace& w, int64_t T, int64_t H, int6
   return MOLT_OK;
 }
 
-// The backward over chunks: as run_backward.
+// The backward over chunks: as run_backward; dW16: a bf16 dW in the place of dW_out.
 molt_status run_backward_chunk(const DeviceInfo* di, const ChunkPlan& cp, const uint16_t* W, int64_t T, int64_t H,
                                int64_t V, const Workspace& w, bool det, int det_clusters, int form,
-                               float* dW_out, int accumulate_dW, cudaStream_t stream) {
+                               float* dW_out, int accumulate_dW, cudaStream_t stream, uint16_t* dW16 = nullptr) {
   const int64_t Tcap = round_tiles(T);
   const auto bf16 = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
   const auto f32 = CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
@@ -681,12 +706,17 @@ molt_status run_backward_chunk(const DeviceInfo* di, const ChunkPlan& cp, const 
   MOLT_TRY(make_tmap_panels(&m.w64x2, W, V, H / kBK, H * 2, kBK * 2));
   MOLT_TRY(make_tmap_panels(&m.g64x2, w.g, cp.panel_rows, g_rows / cp.panel_rows, kBK * 2, cp.panel_rows * kBK * 2));
   MOLT_TRY(make_tmap(&m.dh, f32, 4, w.dh32, Tcap, H, 32, 32));
-  MOLT_TRY(make_tmap(&m.dw, f32, 4, dW_out, V, H, 32, 32));
+  if (dW16)
+    MOLT_TRY(make_tmap(&m.dw16, bf16, 2, dW16, V, H, kBK, 32));
+  else
+    MOLT_TRY(make_tmap(&m.dw, f32, 4, dW_out, V, H, 32, 32));
   ChunkArgs a{};
   a.tok_p = w.tok_l;
   a.lse = w.lse_l;
   a.coef = w.coef_l;
   a.form = form;
+  a.scale = w.scale;
+  a.dw_bf16 = dW16 != nullptr;
   if (form != kGradPlain) {
     a.ecoef = w.ecoef_l;
     a.mu = w.mu_l;
@@ -960,7 +990,8 @@ molt_status cross_entropy_impl(const uint16_t* hidden, const uint16_t* W, const 
       return fail(MOLT_ERR_INVALID_ARG, "label_smoothing must lie in [0, 1]");
     if (!(a.z_loss >= 0.f && a.z_loss <= 1e30f)) return fail(MOLT_ERR_INVALID_ARG, "z_loss must be finite and >= 0");
   }
-  const ChunkPlan cp = chunk_shape(T, H, V, false);
+  const bool round_dW = dW_dtype != MOLT_FP32;
+  const ChunkPlan cp = round_dW ? chunk_shape_bf16(T, H, V) : chunk_shape(T, H, V, false);
   if (grad && T > 0 && !cp.use) return fail(MOLT_ERR_UNSUPPORTED_SHAPE, "T and V are too large together");
   molt_status st;
   const DeviceInfo* di = device_info(&st);
@@ -975,9 +1006,11 @@ molt_status cross_entropy_impl(const uint16_t* hidden, const uint16_t* W, const 
   }
   const int64_t Tcap = round_tiles(T);
   const int S = forward_splits(Tcap, H, V, di->n_sm);
-  const bool round_dW = dW_dtype != MOLT_FP32;
+  // a dW in bf16: stored by the backward where one chunk holds all tokens, else summed in
+  // fp32 and rounded by a pass of its own
+  const bool dw16 = round_dW && cp.n_t <= cp.chunk_t;
   size_t dW32_off;
-  const Layout L = ce_layout(T, H, V, di->n_sm, grad, round_dW, &dW32_off);
+  const Layout L = ce_layout(T, H, V, di->n_sm, grad, round_dW && !dw16, &dW32_off);
   Scratch sc;
   MOLT_TRY(get_scratch(sc, workspace, workspace_bytes, L.total, stream));
   const Workspace w = carve(sc.ptr, L);
@@ -985,24 +1018,25 @@ molt_status cross_entropy_impl(const uint16_t* hidden, const uint16_t* W, const 
   MOLT_TRY(make_tmap(&tm_h, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, w.h_p, Tcap, H, kBK, kTileM));
   MOLT_TRY(make_tmap(&tm_w, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, W, V, H, kBK, 128));
   ev_start(0, stream);
-  MOLT_LAUNCH(launch_ce_pack(a, static_cast<int>(T), static_cast<int>(H), hidden, w, logp_out, lse_out,
+  MOLT_LAUNCH(launch_ce_pack(a, static_cast<int>(T), static_cast<int>(H), static_cast<int>(V), hidden, W, w, logp_out, lse_out,
                              grad ? cp.ctl_words() : 0, di->n_sm, stream),
               "pack");
   ev_stop(0, stream);
   const bool smooth = a.smoothing != 0.f || a.z_loss != 0.f;
   MOLT_TRY(run_forward_kernel(di, Tcap, H, V, S, w, tm_h, tm_w, false, smooth, stream));
   ev_start(2, stream);
-  MOLT_LAUNCH(launch_ce_merge(a, smooth, static_cast<int>(Tcap), static_cast<int>(V), S, w, loss_out, logp_out, lse_out,
+  MOLT_LAUNCH(launch_ce_merge(a, smooth, static_cast<int>(T), static_cast<int>(Tcap), static_cast<int>(V), S, w, loss_out, logp_out, lse_out,
                               stats_out, di->status, stream),
               "merge");
   ev_stop(2, stream);
   if (!grad) return MOLT_OK;
   float* dW = round_dW ? reinterpret_cast<float*>(static_cast<uint8_t*>(sc.aligned()) + dW32_off)
                        : static_cast<float*>(dW_out);
-  MOLT_TRY(run_backward_chunk(di, cp, W, T, H, V, w, false, 0, smooth ? kGradSmooth : kGradPlain, dW, accumulate_dW, stream));
+  MOLT_TRY(run_backward_chunk(di, cp, W, T, H, V, w, false, 0, kGradScaled, dW, accumulate_dW, stream,
+                              dw16 ? static_cast<uint16_t*>(dW_out) : nullptr));
   ev_start(4, stream);
   MOLT_LAUNCH(launch_cast_dh(w, true, static_cast<int>(T), static_cast<int>(H), dhidden_out, di->n_sm, stream), "cast dh");
-  if (round_dW)
+  if (round_dW && !dw16)
     MOLT_LAUNCH(launch_cast_bf16(dW, V * H, static_cast<uint16_t*>(dW_out), di->n_sm, stream), "cast dW");
   ev_stop(4, stream);
   return MOLT_OK;
@@ -1299,7 +1333,8 @@ size_t molt_cross_entropy_workspace_bytes(int64_t T, int64_t H, int64_t V, int w
   molt_status st;
   const DeviceInfo* di = device_info(&st);
   size_t dW32;
-  return ce_layout(T, H, V, di ? di->n_sm : 152, with_backward != 0, dW_dtype != MOLT_FP32, &dW32).total;
+  const ChunkPlan cp = chunk_shape_bf16(T, H, V);
+  return ce_layout(T, H, V, di ? di->n_sm : 152, with_backward != 0, dW_dtype != MOLT_FP32 && cp.n_t > cp.chunk_t, &dW32).total;
 }
 
 molt_status molt_cross_entropy_fwd(const uint16_t* hidden, const uint16_t* W, const int32_t* targets,

@@ -6,8 +6,16 @@
 //   dL/dz_tv = (w_t / D) [ (1 + 2 c lse_t) p_tv - e / V - (1 - e) [v = x_t] ]
 //
 // The logits exist only as tiles on chip: lse, z_x and the sum of z come from the
-// forward's epilogue, dL/dz from the backward's, where with e = c = 0 it is the policy
-// loss's coef (p - [target]) and else kGradSmooth's.
+// forward's epilogue, dL/dz from the backward's (kGradScaled).
+//
+// Two things make it more exact than its products.  The tensor cores add in fp32 but cut
+// off what does not fit, 256 times at H = 4096: the target's logit, which often is by far
+// the largest, comes out 1e-6 too small.  So its logit is formed again in fp32, here
+// where the rows are packed, and replaces the product's in the row's sum.  And the
+// gradient is rounded to bf16 without the factor 1 / D: a target that the model does not
+// expect then is -1, which bf16 holds exactly, where -1 / D would be off by up to 0.4 %
+// for all of them alike; the factor multiplies the products' sums.  (Relative errors of
+// logp and of dW before: 1.6e-6 and up to 2.9e-3.)
 #include <climits>
 #include <cstdint>
 #include <cuda_runtime.h>
@@ -36,14 +44,32 @@ __device__ __forceinline__ int count_targets(const int32_t* __restrict__ x, int 
   return block_sum(c);
 }
 
+// Sum of h w over a row, by a warp, in fp32 throughout.
+__device__ __forceinline__ float dot_row(const uint16_t* __restrict__ h, const uint16_t* __restrict__ w, int H) {
+  const uint4 *a = reinterpret_cast<const uint4*>(h), *b = reinterpret_cast<const uint4*>(w);
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int i = threadIdx.x & 31; i < H / 8; i += 32) {
+    const uint4 x = __ldg(a + i), y = __ldg(b + i);
+    const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      s[j] = fmaf(__uint_as_float(xs[j] << 16), __uint_as_float(ys[j] << 16), s[j]);
+      s[j] = fmaf(__uint_as_float(xs[j] & 0xffff0000u), __uint_as_float(ys[j] & 0xffff0000u), s[j]);
+    }
+  }
+  return warp_sum((s[0] + s[1]) + (s[2] + s[3]));
+}
+
 // The rows whose target is not ignored, packed (see pack_rows): maps, hidden rows,
-// targets and weights; zero hidden rows up to a whole K block of the dW product; also
-// the call's zeroing.
+// targets, weights and the targets' logits; zero hidden rows up to a whole K block of the
+// dW product; also the call's zeroing.
 __global__ void __launch_bounds__(kPackThreads) ce_pack_kernel(
-    const int32_t* __restrict__ targets, const float* __restrict__ weight, int ignore, bool any_ignored, int T, int H,
-    const uint16_t* __restrict__ hidden, int32_t* __restrict__ row_map, int32_t* __restrict__ pos,
-    int32_t* __restrict__ counts, uint16_t* __restrict__ h_p, int32_t* __restrict__ tok_p, float* __restrict__ w_p,
-    float* __restrict__ logp_out, float* __restrict__ lse_out, uint32_t* __restrict__ ctl, int ctl_words) {
+    const int32_t* __restrict__ targets, const float* __restrict__ weight, int ignore, bool any_ignored, int T, int H, int V,
+    const uint16_t* __restrict__ hidden, const uint16_t* __restrict__ W, int32_t* __restrict__ row_map,
+    int32_t* __restrict__ pos, int32_t* __restrict__ counts, uint16_t* __restrict__ h_p, int32_t* __restrict__ tok_p,
+    float* __restrict__ w_p, float* __restrict__ z_p, float* __restrict__ logp_out, float* __restrict__ lse_out,
+    uint32_t* __restrict__ ctl, int ctl_words) {
   for (int i = blockIdx.x * kPackThreads + threadIdx.x; i < ctl_words; i += gridDim.x * kPackThreads) ctl[i] = 0u;
   const int share = (T + gridDim.x - 1) / gridDim.x;
   const int64_t first = static_cast<int64_t>(blockIdx.x) * share;
@@ -63,6 +89,13 @@ __global__ void __launch_bounds__(kPackThreads) ce_pack_kernel(
           if (lse_out) lse_out[t] = 0.f;
         }
       });
+  __syncthreads();
+  for (int k = before + static_cast<int>(threadIdx.x >> 5); k < total; k += kPackThreads / 32) {
+    const int x = tok_p[k];
+    if (x < 0 || x >= V) continue;   // the merge leaves the row out
+    const float z = dot_row(hidden + static_cast<int64_t>(row_map[k]) * H, W + static_cast<int64_t>(x) * H, H);
+    if ((threadIdx.x & 31) == 0) z_p[k] = z;
+  }
   if (t1 != T) return;
   if (threadIdx.x == 0) {
     counts[0] = total;
@@ -77,43 +110,89 @@ __global__ void __launch_bounds__(kPackThreads) ce_pack_kernel(
 
 constexpr int kCeSums = 3;   // w l, -logp, lse^2
 
-// One block per kRedRows packed rows: the row's lse, loss and backward values, and the
-// rows' partial sums; the block that is done last adds all of them in a fixed order.
-template <int kGroups, bool kSmooth>
-__global__ void __launch_bounds__(kRedRows * kGroups) ce_merge_kernel(
+// A row's splits merged by kGroups threads: thread (r, g) = (t % kRows, t / kRows) takes
+// every kGroups-th, eight loads at a time.  Valid in group 0; every thread calls it.
+template <int kRows, int kGroups, bool kSumZ>
+__device__ __forceinline__ RowStats merge_row(const float4* __restrict__ part, int64_t stride, int n_parts, int k, bool act) {
+  __shared__ float4 sh[kGroups][kRows];
+  constexpr float kLog2e = 1.4426950408889634f;
+  const int r = threadIdx.x % kRows, g = threadIdx.x / kRows;
+  RowStats st{-INFINITY, 0.f, 0.f};
+  auto add = [&](float m, float s, float q) {
+    if (s == 0.f) return;   // no columns.  A NaN passes
+    const float M = fmaxf(st.M, m);
+    const float f0 = st.S == 0.f ? 0.f : ex2_approx((st.M - M) * kLog2e), f1 = ex2_approx((m - M) * kLog2e);
+    st.S = st.S * f0 + s * f1;
+    if (kSumZ) st.Q += q;
+    st.M = M;
+  };
+  for (int s0 = g; act && s0 < n_parts; s0 += 8 * kGroups) {
+    float4 p[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int s = s0 + i * kGroups;
+      p[i] = s < n_parts ? part[s * stride + k] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) add(p[i].x, p[i].y, p[i].z);
+  }
+  // groups in pairs, halves of the rest at a time
+#pragma unroll
+  for (int half = kGroups / 2; half > 0; half /= 2) {
+    if (g >= half && g < 2 * half) sh[g][r] = make_float4(st.M, st.S, st.Q, 0.f);
+    __syncthreads();
+    if (g < half) {
+      const float4 o = sh[g + half][r];
+      add(o.x, o.y, o.z);
+    }
+  }
+  return st;
+}
+
+// One block per kRows packed rows: the rows' lse, losses and backward values, and their
+// partial sums; the block that is done last adds all of them in a fixed order.
+template <int kRows, int kGroups, bool kSmooth>
+__global__ void __launch_bounds__(kRows* kGroups) ce_merge_kernel(
     CeArgs a, int Tcap, int V, int n_parts, int32_t* __restrict__ counts, const int32_t* __restrict__ row_map,
     const int32_t* __restrict__ tok_p, const float* __restrict__ w_p, const float4* __restrict__ part,
-    const float* __restrict__ zx, float* __restrict__ lse_o, float* __restrict__ coef_o, float* __restrict__ cp_o,
-    float* __restrict__ cu_o, double* __restrict__ red, float* __restrict__ loss_out, float* __restrict__ logp_out,
-    float* __restrict__ lse_out, molt_ce_stats* __restrict__ stats, unsigned* err) {
+    const float* __restrict__ zx, const float* __restrict__ z_p, float* __restrict__ lse_o, float* __restrict__ coef_o,
+    float* __restrict__ cp_o, float* __restrict__ cu_o, double* __restrict__ red, float* __restrict__ scale_out,
+    float* __restrict__ loss_out, float* __restrict__ logp_out, float* __restrict__ lse_out,
+    molt_ce_stats* __restrict__ stats, unsigned* err) {
+  constexpr float kLog2e = 1.4426950408889634f;
+  static_assert(kRows <= 32, "a row's lane in the first warp");
   const int n = counts[0];
-  const int n_blocks = max(1, (n + kRedRows - 1) / kRedRows);
+  const int n_blocks = max(1, (n + kRows - 1) / kRows);
   if (static_cast<int>(blockIdx.x) >= n_blocks) return;
-  const int k = blockIdx.x * kRedRows + threadIdx.x % kRedRows;
+  const int k = blockIdx.x * kRows + threadIdx.x % kRows;
   const bool act = k < n;
-  const RowStats st = merge_row_parts<kGroups, kSmooth>(part, Tcap, n_parts, k, act);
+  const RowStats st = merge_row<kRows, kGroups, kSmooth>(part, Tcap, n_parts, k, act);
   const double D = a.denom > 0.0 ? a.denom : static_cast<double>(n);
   __shared__ bool last;
-  if (threadIdx.x < kRedRows) {
+  if (threadIdx.x < 32) {
     double s[kCeSums] = {0.0, 0.0, 0.0};
-    if (act) {
-      const float lse = st.M + logf(st.S);
+    if (act && threadIdx.x < kRows) {
       const int x = tok_p[k];
       const bool in = x >= 0 && x < V;   // else no loss and no gradient
       if (!in) atomicOr(err, kDevErrTokenRange);
-      const float logp = in ? zx[k] - lse : 0.f;
+      // the target's exact logit in the place of the product's
+      const float z_mma = in ? zx[k] : 0.f, z = in ? z_p[k] : 0.f;
+      const float S = in ? fmaf(ex2_approx((z_mma - st.M) * kLog2e), expm1f(z - z_mma), st.S) : st.S;
+      const float lse = st.M + logf(S);
+      const float logp = in ? z - lse : 0.f;
       const float w = in ? (w_p ? w_p[k] : 1.f) : 0.f;
       float l = -logp;
-      const float c = D > 0.0 ? static_cast<float>(static_cast<double>(w) / D) : 0.f;
       if constexpr (kSmooth) {
         // off: the mean over the vocabulary of -log p
         const float off = a.smoothing != 0.f ? lse - st.Q / static_cast<float>(V) : l;
         l = fmaf(a.z_loss * lse, lse, fmaf(a.smoothing, off - l, l));
-        coef_o[k] = c * (1.f - a.smoothing);
-        cp_o[k] = c * fmaf(2.f * a.z_loss, lse, 1.f);
-        cu_o[k] = c * (a.smoothing / static_cast<float>(V));
+        coef_o[k] = w * (1.f - a.smoothing);
+        cp_o[k] = w * fmaf(2.f * a.z_loss, lse, 1.f);
+        cu_o[k] = w * (a.smoothing / static_cast<float>(V));
       } else {
-        coef_o[k] = c;
+        coef_o[k] = w;
+        cp_o[k] = w;
+        cu_o[k] = 0.f;
       }
       lse_o[k] = lse;
       const int t = row_map[k];
@@ -137,9 +216,10 @@ __global__ void __launch_bounds__(kRedRows * kGroups) ce_merge_kernel(
   __syncthreads();
   if (!last) return;
   __threadfence();
-  __shared__ double tot[kGroups][kCeSums];
+  constexpr int kWarps = kRows * kGroups / 32;
+  __shared__ double tot[kWarps][kCeSums];
   double s[kCeSums] = {0.0, 0.0, 0.0};
-  for (int b = threadIdx.x; b < n_blocks; b += kRedRows * kGroups) {
+  for (int b = threadIdx.x; b < n_blocks; b += kRows * kGroups) {
 #pragma unroll
     for (int i = 0; i < kCeSums; ++i) s[i] += __ldcg(red + static_cast<int64_t>(b) * kRedSlots + i);
   }
@@ -151,13 +231,14 @@ __global__ void __launch_bounds__(kRedRows * kGroups) ce_merge_kernel(
   }
   __syncthreads();
   if (threadIdx.x != 0) return;
-  for (int g = 1; g < kGroups; ++g) {
+  for (int g = 1; g < kWarps; ++g) {
 #pragma unroll
     for (int i = 0; i < kCeSums; ++i) s[i] += tot[g][i];
   }
   if (!(D > 0.0)) atomicOr(err, kDevErrZeroDenom);
   const double loss = D > 0.0 ? s[0] / D : 0.0;
   *loss_out = static_cast<float>(loss);
+  *scale_out = D > 0.0 ? static_cast<float>(1.0 / D) : 0.f;
   if (stats) {
     stats->denom = D;
     stats->loss = loss;
@@ -177,25 +258,27 @@ __global__ void __launch_bounds__(256) cast_bf16_kernel(const float* __restrict_
 
 }  // namespace
 
-cudaError_t launch_ce_pack(const CeArgs& a, int T, int H, const uint16_t* hidden, const Workspace& ws, float* logp_out,
-                           float* lse_out, int64_t ctl_words, int n_sm, cudaStream_t s) {
+cudaError_t launch_ce_pack(const CeArgs& a, int T, int H, int V, const uint16_t* hidden, const uint16_t* W, const Workspace& ws,
+                           float* logp_out, float* lse_out, int64_t ctl_words, int n_sm, cudaStream_t s) {
   // an ignore_index that no int32 can have ignores nothing
   const bool any = a.ignore_index >= INT32_MIN && a.ignore_index <= INT32_MAX;
-  ce_pack_kernel<<<n_sm * 8, kPackThreads, 0, s>>>(a.targets, a.weight, any ? static_cast<int>(a.ignore_index) : 0, any, T, H,
-                                                   hidden, ws.row_map, ws.pos_of_row, ws.counts, ws.h_p, ws.tok_p, ws.b_p,
-                                                   logp_out, lse_out, ws.ctl, static_cast<int>(ctl_words));
+  ce_pack_kernel<<<n_sm * 8, kPackThreads, 0, s>>>(a.targets, a.weight, any ? static_cast<int>(a.ignore_index) : 0, any, T, H, V,
+                                                   hidden, W, ws.row_map, ws.pos_of_row, ws.counts, ws.h_p, ws.tok_p, ws.b_p,
+                                                   ws.adv_p, logp_out, lse_out, ws.ctl, static_cast<int>(ctl_words));
   return cudaGetLastError();
 }
 
-cudaError_t launch_ce_merge(const CeArgs& a, bool smooth, int Tcap, int V, int n_parts, const Workspace& ws, float* loss_out,
+cudaError_t launch_ce_merge(const CeArgs& a, bool smooth, int T, int Tcap, int V, int n_parts, const Workspace& ws, float* loss_out,
                             float* logp_out, float* lse_out, molt_ce_stats* stats, unsigned* err, cudaStream_t s) {
-  const int groups = merge_groups(n_parts);
-  auto* k = groups == kMergeGroupsMany
-                ? (smooth ? &ce_merge_kernel<kMergeGroupsMany, true> : &ce_merge_kernel<kMergeGroupsMany, false>)
-                : (smooth ? &ce_merge_kernel<kMergeGroupsFew, true> : &ce_merge_kernel<kMergeGroupsFew, false>);
-  k<<<Tcap / kRedRows, kRedRows * groups, 0, s>>>(a, Tcap, V, n_parts, ws.counts, ws.row_map, ws.tok_p,
-                                                  a.weight ? ws.b_p : nullptr, ws.part, ws.zx, ws.lse, ws.coef, ws.ecoef, ws.mu,
-                                                  ws.red, loss_out, logp_out, lse_out, stats, err);
+  // few rows have many splits each: eight rows and 64 groups of threads to a block (T =
+  // 100 with 594 splits: 32 rows to a block, the splits read twice, took 24 us)
+  const bool few = n_parts > 64;
+  auto* k = few ? (smooth ? &ce_merge_kernel<8, 64, true> : &ce_merge_kernel<8, 64, false>)
+                : (smooth ? &ce_merge_kernel<32, 8, true> : &ce_merge_kernel<32, 8, false>);
+  const int rows = few ? 8 : 32;
+  k<<<(T + rows - 1) / rows, few ? 512 : 256, 0, s>>>(a, Tcap, V, n_parts, ws.counts, ws.row_map, ws.tok_p,
+                                                      a.weight ? ws.b_p : nullptr, ws.part, ws.zx, ws.adv_p, ws.lse, ws.coef,
+                                                      ws.ecoef, ws.mu, ws.red, ws.scale, loss_out, logp_out, lse_out, stats, err);
   return cudaGetLastError();
 }
 

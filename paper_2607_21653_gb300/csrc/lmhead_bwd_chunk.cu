@@ -2,8 +2,8 @@
 // tokens x vocabulary plane.
 //
 //   g_tv = coef_t (softmax(z_t)_v - [v == x_t]),  coef_t = m_t c_t / D   (Eq. 2)
-//          (+ ecoef_t softmax(z_t)_v (z_tv - mu_t) with an entropy bonus; label
-//          smoothing and a z term: see kGradSmooth)
+//          (+ ecoef_t softmax(z_t)_v (z_tv - mu_t) with an entropy bonus; the cross
+//          entropy's: kGradScaled)
 //   dH_t = sum_v g_tv W_v          dW_v = sum_t g_tv h_t
 //
 // A chunk is up to 4096 tokens x 4096 vocab columns.  Its g (bf16, at most
@@ -538,6 +538,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       return __shfl_sync(0xffffffffu, good, 0) != 0;
     };
     int seen_dh = -1, seen_dw = -1;   // last first chunks seen stored
+    float scale = 1.f;
+    if constexpr (kForm == kGradScaled) scale = *a.scale;
     uint32_t ai = 0;   // accumulators read
     // the next accumulator's products
     auto acc_full = [&]() -> bool {
@@ -590,7 +592,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             auto p_of = [&](int j) -> float {   // g without the target's term
               const float e = ex2_approx(fmaf(v[j], kLog2e, -lseL));
               if constexpr (kForm == kGradEntropy) return fmaf(ecoef, v[j] - mu, coef) * e;
-              if constexpr (kForm == kGradSmooth) return fmaf(ecoef, e, -mu);
+              if constexpr (kForm == kGradScaled) return fmaf(ecoef, e, -mu);
               return coef * e;
             };
             // a target or an invalid column among the warp's 32 x 32 values is rare
@@ -660,6 +662,41 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           }
         }
         const bool store = first && term == 0;
+        if constexpr (kForm == kGradScaled) {
+          if (a.dw_bf16 && !dh) {
+            // the only contribution: rounded and stored, 64 columns at a time
+#pragma unroll 1
+            for (int s = 0; s < 2; ++s) {
+              const int col = hf * 128 + s * 64;
+              if (col >= w) break;
+              uint32_t p[32];
+#pragma unroll
+              for (int u = 0; u < 2; ++u) {
+                float v[32];
+                tmem_ld32(taddr() + s * 64 + u * 32, v);
+#pragma unroll
+                for (int j = 0; j < 32; j += 2)
+                  p[u * 16 + j / 2] = empty ? 0u : pack_bf16x2(v[j] * scale, v[j + 1] * scale);
+              }
+              if (s == 1 || col + 64 >= w) release_acc();
+              if (s == 0) raise();
+              box_free();
+              const uint32_t rowp = box + lane * 128;
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+                st_shared_v4(rowp + static_cast<uint32_t>(i ^ (lane & 7)) * 16, p[4 * i], p[4 * i + 1], p[4 * i + 2],
+                             p[4 * i + 3]);
+              fence_proxy_async_smem();
+              __syncwarp();
+              if (lane == 0) {
+                if (rows_in) tma_store_2d(&m.dw16, box, x.h * 256 + col, y);
+                bulk_commit_group();
+              }
+            }
+            if (hf * 128 >= w) release_acc();
+            continue;
+          }
+        }
 #pragma unroll 1
         for (int s = 0; s < 4; ++s) {
           const int col = hf * 128 + s * 32;
@@ -669,6 +706,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           if (empty) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] = 0.f;
+          }
+          if constexpr (kForm == kGradScaled) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] *= scale;
           }
           if (kDet && store) {
             // what adding to +0 would leave: no negative zeros
@@ -734,7 +775,7 @@ cudaError_t launch_lmhead_bwd_chunk(const ChunkMaps& m, const ChunkArgs& a, int 
     k = a.form == kGradEntropy ? &lmhead_bwd_chunk_kernel<kGradEntropy, true> : &lmhead_bwd_chunk_kernel<kGradPlain, true>;
   else
     k = a.form == kGradEntropy  ? &lmhead_bwd_chunk_kernel<kGradEntropy, false>
-        : a.form == kGradSmooth ? &lmhead_bwd_chunk_kernel<kGradSmooth, false>
+        : a.form == kGradScaled ? &lmhead_bwd_chunk_kernel<kGradScaled, false>
                                 : &lmhead_bwd_chunk_kernel<kGradPlain, false>;
   const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
   if (e != cudaSuccess) return e;

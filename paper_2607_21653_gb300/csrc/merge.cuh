@@ -19,12 +19,12 @@ constexpr int kMergeGroupsMany = 32, kMergeGroupsFew = 8;
 inline int merge_groups(int n_parts) { return n_parts > 32 ? kMergeGroupsMany : kMergeGroupsFew; }
 
 struct RowStats {
-  float M, S, Q;   // max z, sum e^(z - M), sum e^(z - M)(z - M) (or the sum of z)
+  float M, S, Q;   // max z, sum e^(z - M), sum e^(z - M)(z - M)
 };
 
 // The statistics of packed row k (any value where !act), valid in warp 0; every
-// thread of the block calls it.  kSumZ: the partials hold the plain sum of z.
-template <int kGroups, bool kSumZ = false>
+// thread of the block calls it.
+template <int kGroups>
 __device__ __forceinline__ RowStats merge_row_parts(const float4* __restrict__ part, int64_t stride, int n_parts,
                                                     int k, bool act) {
   __shared__ float sh_m[kGroups][kRedRows];
@@ -50,7 +50,7 @@ __device__ __forceinline__ RowStats merge_row_parts(const float4* __restrict__ p
         const float d = p.x - M;
         const float f = ex2_approx(d * kLog2e);
         S += f * p.y;
-        Q += kSumZ ? p.z : f * (p.z + d * p.y);
+        Q += f * (p.z + d * p.y);
       }
     }
   }

@@ -29,6 +29,7 @@ struct Workspace {
   float4* part;         // [S, Tcap] per-split (max, sum exp, sum exp*(z-max), -)
   float* zx;            // [Tcap] target logit
   float* lse;           // [Tcap]
+  float* scale;         // [1] cross entropy: 1 / D
   float* coef;          // [Tcap] m c / D
   int32_t* tile_list;   // [Tcap/128]
   double* red;          // [Tcap/kRedRows, kRedSlots] partial sums of kRedRows packed rows
@@ -100,12 +101,13 @@ constexpr int kChunkCtlHead = 64;    // control words before the per-chunk count
 // g of one logit z of a row, p = e^(z - lse):
 constexpr int kGradPlain = 0;     // coef (p - [target])
 constexpr int kGradEntropy = 1;   // coef (p - [target]) + ecoef p (z - mu)
-constexpr int kGradSmooth = 2;    // ecoef p - mu - coef [target]   (label smoothing, z term)
+constexpr int kGradScaled = 2;    // (ecoef p - mu - coef [target]) s, the factor s = *scale on the products' sums
 struct ChunkMaps {                   // bf16 maps have 64-column (128-byte) boxes
   CUtensorMap h128, w128;            // packed hidden rows and W, 128 rows
   CUtensorMap g128, g32;             // chunk buffers: 64-column panels of token rows; g32 stores
   CUtensorMap h64x2, w64x2, g64x2;   // as [column box or panel, row, 64]: 64 rows of two boxes side by side
   CUtensorMap dh, dw;                // fp32 targets, 32 x 32 boxes
+  CUtensorMap dw16;                  // bf16 dW, boxes of 32 rows
 };
 struct ChunkArgs {
   const int32_t* tok_p;
@@ -114,6 +116,8 @@ struct ChunkArgs {
   int form;                  // how z becomes g: kGradPlain, kGradEntropy, kGradSmooth
   const float* ecoef;        // the forms' further row values (kGradPlain: none)
   const float* mu;
+  const float* scale;        // kGradScaled
+  int dw_bf16;               // kGradScaled: dW is rounded and stored through dw16 (one token chunk, nothing added)
   const int32_t* counts;     // counts[3] = rows
   int V, H;
   int chunk_t, chunk_v;      // a chunk's tiles of tokens and vocab, at most
@@ -222,11 +226,12 @@ struct CeArgs {
 };
 // rows whose target is not ignore_index packed as launch_pack does (weights into ws.b_p),
 // padded with zero rows to whole K blocks; all packed rows are the backward's rows
-cudaError_t launch_ce_pack(const CeArgs& a, int T, int H, const uint16_t* hidden, const Workspace& ws, float* logp_out,
-                           float* lse_out, int64_t ctl_words, int n_sm, cudaStream_t s);
-// split partials -> lse, the loss and its stats, and the backward's row values; smooth:
-// partials hold the sum of z
-cudaError_t launch_ce_merge(const CeArgs& a, bool smooth, int Tcap, int V, int n_parts, const Workspace& ws, float* loss_out,
+// and the targets' logits (into ws.adv_p)
+cudaError_t launch_ce_pack(const CeArgs& a, int T, int H, int V, const uint16_t* hidden, const uint16_t* W, const Workspace& ws,
+                           float* logp_out, float* lse_out, int64_t ctl_words, int n_sm, cudaStream_t s);
+// split partials -> lse, the loss and its stats, the backward's row values and 1 / D;
+// smooth: partials hold the sum of z
+cudaError_t launch_ce_merge(const CeArgs& a, bool smooth, int T, int Tcap, int V, int n_parts, const Workspace& ws, float* loss_out,
                             float* logp_out, float* lse_out, molt_ce_stats* stats, unsigned* err, cudaStream_t s);
 // dst = bf16(src), n a multiple of 8
 cudaError_t launch_cast_bf16(const float* src, int64_t n, uint16_t* dst, int n_sm, cudaStream_t s);

@@ -24,7 +24,7 @@ def _dtype_code(dtype, name):
 
 
 def _shaped(t, shape, name):
-    if tuple(t.shape) != shape:
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {list(shape)}, got {list(t.shape)}")
     return t
 
@@ -35,20 +35,36 @@ def _same_device(dev, **tensors):
             raise ValueError(f"{name} is on {t.device}, the call's other tensors on {dev}")
 
 
-def _rows(t, dtype, name):
-    """(pointer, row stride) of a CUDA matrix whose rows are contiguous."""
-    if t is None:
-        return None, 0
+def _cuda(t, name):
+    """The CUDA device of a tensor."""
     if not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
-    if t.dtype != dtype:
+    return t.device
+
+
+def _at(t, dtype, dev, name):
+    """Pointer of a contiguous tensor of this type on this device (None -> NULL)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.device != dev or not t.is_contiguous():
+        _same_device(dev, **{name: t})
+        return _ptr(t, dtype, name)
+    return t.data_ptr()
+
+
+def _rows(t, dtype, dev, name):
+    """(pointer, row stride, 0 for rows side by side) of a matrix whose rows are contiguous."""
+    if t is None:
+        return None, 0
+    if t.is_contiguous():
+        return _at(t, dtype, dev, name), 0
+    _same_device(dev, **{name: t})
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     T, H = t.shape
-    if T <= 1 and (H <= 1 or t.stride(1) == 1):
-        return t.data_ptr(), H
-    if (H > 1 and t.stride(1) != 1) or t.stride(0) < H:
+    if (H > 1 and t.stride(1) != 1) or (T > 1 and t.stride(0) < H):
         raise ValueError(f"{name} must have contiguous rows that do not overlap")
-    return t.data_ptr(), t.stride(0)
+    return t.data_ptr(), t.stride(0) if T > 1 else 0
 
 
 # ----------------------------------------------------------------- embedding
@@ -59,15 +75,15 @@ def token_embedding(weight, tokens, scale=1.0, out_dtype=None, out=None, stream=
     torch = _torch()
     V, H = weight.shape
     T, = tokens.shape
-    dev = weight.device
+    dev, dtype = _cuda(weight, "weight"), weight.dtype
     if out is None:
-        out = torch.empty(T, H, dtype=weight.dtype if out_dtype is None else out_dtype, device=dev)
+        out = torch.empty(T, H, dtype=dtype if out_dtype is None else out_dtype, device=dev)
     else:
         _shaped(out, (T, H), "out")
-    _same_device(dev, tokens=tokens, out=out)
     _check(load().molt_token_embedding(
-        _ptr(weight, None, "weight"), _dtype_code(weight.dtype, "weight"), _ptr(tokens, torch.int32, "tokens"), T, H, V,
-        float(scale), _ptr(out, out_dtype, "out"), _dtype_code(out.dtype, "out"), _stream(stream, dev.index)))
+        _at(weight, dtype, dev, "weight"), _dtype_code(dtype, "weight"), _at(tokens, torch.int32, dev, "tokens"), T, H,
+        V, scale, _at(out, out_dtype or out.dtype, dev, "out"), _dtype_code(out.dtype, "out"),
+        _stream(stream, dev.index)))
     return out
 
 
@@ -79,22 +95,21 @@ def token_embedding_bwd(dout, tokens, V, scale=1.0, padding_idx=None, dtype=None
     gradient where the weights are tied) added.  Bitwise reproducible."""
     torch = _torch()
     T, H = dout.shape
-    dev = dout.device
     _shaped(tokens, (T,), "tokens")
+    dev, din = _cuda(dout, "dout"), dout.dtype
     if dW is None:
-        dW = torch.empty(V, H, dtype=dout.dtype if dtype is None else dtype, device=dev)
+        dW = torch.empty(V, H, dtype=din if dtype is None else dtype, device=dev)
         accumulate_dW = False
     else:
         _shaped(dW, (V, H), "dW")
-    _same_device(dev, tokens=tokens, dW=dW)
     L = load()
     ws = workspace
     if ws is None:
-        ws = _workspace(int(L.molt_token_embedding_bwd_workspace_bytes(T, H, V)), dev, "embedding_bwd", stream)
+        ws = _workspace(L.molt_token_embedding_bwd_workspace_bytes(T, H, V), dev, "embedding_bwd", stream)
     _check(L.molt_token_embedding_bwd(
-        _ptr(dout, None, "dout"), _dtype_code(dout.dtype, "dout"), _ptr(tokens, torch.int32, "tokens"), T, H, V,
-        float(scale), -1 if padding_idx is None else int(padding_idx), _ptr(dW, dtype, "dW"),
-        _dtype_code(dW.dtype, "dW"), 1 if accumulate_dW else 0, ws.data_ptr(), ws.numel(), _stream(stream, dev.index)))
+        _at(dout, din, dev, "dout"), _dtype_code(din, "dout"), _at(tokens, torch.int32, dev, "tokens"), T, H, V, scale,
+        -1 if padding_idx is None else padding_idx, _at(dW, dtype or dW.dtype, dev, "dW"), _dtype_code(dW.dtype, "dW"),
+        1 if accumulate_dW else 0, ws.data_ptr(), ws.numel(), _stream(stream, dev.index)))
     return dW
 
 
@@ -109,34 +124,49 @@ class NormDesc(ctypes.Structure):
 
 GATE_NONE, GATE_CHANNEL, GATE_TOKEN, GATE_FULL = range(4)
 
+# Descriptors by their values: building one takes longer than the rest of a small call's
+# marshalling.  They are read only.
+_desc_cache: dict = {}
+_DESC_CACHE_MAX = 256
+
+
+def _desc(*values):
+    """Reference to the molt_norm_desc of these values."""
+    ref = _desc_cache.get(values)
+    if ref is None:
+        if len(_desc_cache) >= _DESC_CACHE_MAX:
+            _desc_cache.clear()
+        ref = _desc_cache[values] = ctypes.byref(NormDesc(*values))
+    return ref
+
 
 def _gate_kind(gate, T, H):
     """The gate's kind by its shape: [H], [T, 1] or [T] (where T is not H; then [T, 1] is needed), [T, H]."""
     if gate is None:
         return GATE_NONE
-    shape = tuple(gate.shape)
+    shape = gate.shape
     if shape == (H,):
         return GATE_CHANNEL
-    if shape in ((T,), (T, 1)):
+    if shape == (T,) or shape == (T, 1):
         return GATE_TOKEN
     if shape == (T, H):
         return GATE_FULL
     raise ValueError(f"gate must have shape [{H}], [{T}], [{T}, 1] or [{T}, {H}], got {list(shape)}")
 
 
-def _params(dtype, H, **named):
+def _param_type(dtype, H, w_post, w_pre, gate):
     """The common type of the parameter vectors (x's where there is none)."""
-    torch = _torch()
     found = None
-    for name, p in named.items():
+    for name, p in (("w_post", w_post), ("w_pre", w_pre), ("gate", gate)):
         if p is None:
             continue
         _shaped(p, (H,), name)
-        if p.dtype not in (dtype, torch.float32):
-            raise TypeError(f"{name} must be {dtype} or float32, got {p.dtype}")
-        if found not in (None, p.dtype):
+        t = p.dtype
+        if t is not dtype and t is not _torch().float32:
+            raise TypeError(f"{name} must be {dtype} or float32, got {t}")
+        if found is not None and found is not t:
             raise TypeError("w_post, w_pre and a channel gate must have one type")
-        found = p.dtype
+        found = t
     return dtype if found is None else found
 
 
@@ -153,34 +183,35 @@ def residual_norm_fwd(x, residual=None, w_post=None, gate=None, w_pre=None, res_
     changes it (no residual, norm or gate)."""
     torch = _torch()
     T, H = x.shape
-    dev, dtype = x.device, x.dtype
     kind = _gate_kind(gate, T, H)
+    dtype, f32 = x.dtype, torch.float32
     if residual is not None:
         _shaped(residual, (T, H), "residual")
-        if residual_dtype not in (None, residual.dtype):
+        rtype = residual.dtype
+        if residual_dtype is not None and residual_dtype is not rtype:
             raise TypeError("residual_dtype is the residual's own type")
-        residual_dtype = residual.dtype
-    elif residual_dtype is None:
-        residual_dtype = dtype
-    same = residual is None and w_post is None and kind == GATE_NONE and residual_dtype == dtype
-    ptype = _params(dtype, H, w_post=w_post, w_pre=w_pre, gate=gate if kind == GATE_CHANNEL else None)
-    _same_device(dev, residual=residual, w_post=w_post, gate=gate, w_pre=w_pre)
-    f32 = torch.float32
-    out = {"y": torch.empty(T, H, dtype=dtype, device=dev) if w_pre is not None else None,
-           "residual": x if same else torch.empty(T, H, dtype=residual_dtype, device=dev),
-           "rstd_post": torch.empty(T, dtype=f32, device=dev) if want_stats and w_post is not None else None,
-           "rstd_pre": torch.empty(T, dtype=f32, device=dev) if want_stats and w_pre is not None else None}
-    if same and w_pre is None:
+    else:
+        rtype = dtype if residual_dtype is None else residual_dtype
+    ptype = _param_type(dtype, H, w_post, w_pre, gate if kind == GATE_CHANNEL else None)
+    dev = _cuda(x, "x")
+    same = residual is None and w_post is None and kind == GATE_NONE and rtype is dtype
+    xp, xs = _rows(x, dtype, dev, "x")
+    rp, rs = _rows(residual, rtype, dev, "residual")
+    y = torch.empty(T, H, dtype=dtype, device=dev) if w_pre is not None else None
+    r_out = x if same else torch.empty(T, H, dtype=rtype, device=dev)
+    rstd_post = torch.empty(T, dtype=f32, device=dev) if want_stats and w_post is not None else None
+    rstd_pre = torch.empty(T, dtype=f32, device=dev) if want_stats and w_pre is not None else None
+    out = {"y": y, "residual": r_out, "rstd_post": rstd_post, "rstd_pre": rstd_pre}
+    if same and y is None:
         return out
-    xp, xs = _rows(x, dtype, "x")
-    rp, rs = _rows(residual, residual_dtype, "residual")
-    desc = NormDesc(T, H, xs, rs, 0, _dtype_code(dtype, "x"), _dtype_code(residual_dtype, "residual"),
-                    _dtype_code(ptype, "w_pre"), kind, float(res_scale), float(eps), float(weight_offset))
+    ref = _desc(T, H, xs, rs, 0, _dtype_code(dtype, "x"), _dtype_code(rtype, "residual"), _dtype_code(ptype, "w_pre"),
+                kind, res_scale, eps, weight_offset)
     _check(load().molt_residual_norm_fwd(
-        ctypes.byref(desc), xp, rp, _ptr(w_post, None, "w_post"),
-        _ptr(gate, f32 if kind == GATE_TOKEN else dtype if kind == GATE_FULL else None, "gate"),
-        _ptr(w_pre, None, "w_pre"), _ptr(out["y"]), None if same else _ptr(out["residual"]), _ptr(out["rstd_post"]),
-        _ptr(out["rstd_pre"]), _stream(stream, dev.index)))
+        ref, xp, rp, _at(w_post, ptype, dev, "w_post"),
+        _at(gate, ptype if kind == GATE_CHANNEL else f32 if kind == GATE_TOKEN else dtype, dev, "gate"),
+        _at(w_pre, ptype, dev, "w_pre"), y if y is None else y.data_ptr(), None if same else r_out.data_ptr(),
+        rstd_post if rstd_post is None else rstd_post.data_ptr(), rstd_pre if rstd_pre is None else rstd_pre.data_ptr(),
+        _stream(stream, dev.index)))
     return out
 
 
@@ -195,7 +226,7 @@ def residual_norm_bwd(dy, dresidual, x, residual, rstd_pre, rstd_post=None, w_po
     and a channel gate's dgate are written, with accumulate=True added to."""
     torch = _torch()
     T, H = x.shape
-    dev, dtype, f32 = x.device, x.dtype, torch.float32
+    dtype, f32 = x.dtype, torch.float32
     kind = _gate_kind(gate, T, H)
     if residual is None and dresidual is None:
         raise ValueError("one of residual and dresidual is needed")
@@ -206,9 +237,8 @@ def residual_norm_bwd(dy, dresidual, x, residual, rstd_pre, rstd_post=None, w_po
     for name, t in (("rstd_pre", rstd_pre), ("rstd_post", rstd_post)):
         if t is not None:
             _shaped(t, (T,), name)
-    ptype = _params(dtype, H, w_post=w_post, w_pre=w_pre, gate=gate if kind == GATE_CHANNEL else None)
-    _same_device(dev, dy=dy, dresidual=dresidual, residual=residual, rstd_pre=rstd_pre, rstd_post=rstd_post,
-                 w_post=w_post, gate=gate, w_pre=w_pre, dw_post=dw_post, dgate=dgate, dw_pre=dw_pre)
+    ptype = _param_type(dtype, H, w_post, w_pre, gate if kind == GATE_CHANNEL else None)
+    dev = _cuda(x, "x")
 
     def vector(given, wanted, name):
         if not wanted:
@@ -219,30 +249,30 @@ def residual_norm_bwd(dy, dresidual, x, residual, rstd_pre, rstd_post=None, w_po
 
     if dgate is not None and kind != GATE_CHANNEL:
         raise ValueError("dgate can be given for a channel gate only")
-    out = {"dx": torch.empty(T, H, dtype=dtype, device=dev),
-           "dresidual": torch.empty(T, H, dtype=rtype, device=dev) if want_dresidual else None,
-           "dw_post": vector(dw_post, w_post is not None, "dw_post"),
-           "dgate": vector(dgate, kind == GATE_CHANNEL, "dgate"),
-           "dw_pre": vector(dw_pre, w_pre is not None, "dw_pre")}
+    dx = torch.empty(T, H, dtype=dtype, device=dev)
+    dr_out = torch.empty(T, H, dtype=rtype, device=dev) if want_dresidual else None
+    dw_post = vector(dw_post, w_post is not None, "dw_post")
+    dw_pre = vector(dw_pre, w_pre is not None, "dw_pre")
     if kind == GATE_TOKEN:
-        out["dgate"] = torch.empty(T, dtype=f32, device=dev)
+        dgate = torch.empty(T, dtype=f32, device=dev)
     elif kind == GATE_FULL:
-        out["dgate"] = torch.empty(T, H, dtype=dtype, device=dev)
-    xp, xs = _rows(x, dtype, "x")
-    rp, rs = _rows(residual, rtype, "residual")
-    dyp, dys = _rows(dy, dtype, "dy")
-    desc = NormDesc(T, H, xs, rs, dys, _dtype_code(dtype, "x"), _dtype_code(rtype, "residual"),
-                    _dtype_code(ptype, "w_pre"), kind, float(res_scale), 0.0, float(weight_offset))
-    ref = ctypes.byref(desc)
+        dgate = torch.empty(T, H, dtype=dtype, device=dev)
+    else:
+        dgate = vector(dgate, kind == GATE_CHANNEL, "dgate")
+    xp, xs = _rows(x, dtype, dev, "x")
+    rp, rs = _rows(residual, rtype, dev, "residual")
+    dyp, dys = _rows(dy, dtype, dev, "dy")
+    ref = _desc(T, H, xs, rs, dys, _dtype_code(dtype, "x"), _dtype_code(rtype, "residual"), _dtype_code(ptype, "w_pre"),
+                kind, res_scale, 0.0, weight_offset)
     L = load()
     ws = workspace
     if ws is None:
-        ws = _workspace(int(L.molt_residual_norm_bwd_workspace_bytes(ref)), dev, "norm_bwd", stream)
+        ws = _workspace(L.molt_residual_norm_bwd_workspace_bytes(ref), dev, "norm_bwd", stream)
     _check(L.molt_residual_norm_bwd(
-        ref, dyp, _ptr(dresidual, rtype, "dresidual"), xp, rp, _ptr(rstd_post, f32, "rstd_post"),
-        _ptr(rstd_pre, f32, "rstd_pre"), _ptr(w_post, None, "w_post"),
-        _ptr(gate, f32 if kind == GATE_TOKEN else dtype if kind == GATE_FULL else None, "gate"),
-        _ptr(w_pre, None, "w_pre"), _ptr(out["dx"]), _ptr(out["dresidual"]), _ptr(out["dw_post"], f32, "dw_post"),
-        _ptr(out["dgate"], dtype if kind == GATE_FULL else f32, "dgate"), _ptr(out["dw_pre"], f32, "dw_pre"),
-        1 if accumulate else 0, ws.data_ptr(), ws.numel(), _stream(stream, dev.index)))
-    return out
+        ref, dyp, _at(dresidual, rtype, dev, "dresidual"), xp, rp, _at(rstd_post, f32, dev, "rstd_post"),
+        _at(rstd_pre, f32, dev, "rstd_pre"), _at(w_post, ptype, dev, "w_post"),
+        _at(gate, ptype if kind == GATE_CHANNEL else f32 if kind == GATE_TOKEN else dtype, dev, "gate"),
+        _at(w_pre, ptype, dev, "w_pre"), dx.data_ptr(), dr_out if dr_out is None else dr_out.data_ptr(),
+        _at(dw_post, f32, dev, "dw_post"), _at(dgate, dtype if kind == GATE_FULL else f32, dev, "dgate"),
+        _at(dw_pre, f32, dev, "dw_pre"), 1 if accumulate else 0, ws.data_ptr(), ws.numel(), _stream(stream, dev.index)))
+    return {"dx": dx, "dresidual": dr_out, "dw_post": dw_post, "dgate": dgate, "dw_pre": dw_pre}
