@@ -68,8 +68,8 @@ def cross_entropy_fwd(hidden, weight, targets, token_weight=None, denom=0.0, ign
 def cross_entropy_fwd_bwd(hidden, weight, targets, token_weight=None, denom=0.0, ignore_index=-100,
                           label_smoothing=0.0, z_loss=0.0, dW=None, accumulate_dW=False, dW_dtype=None,
                           want_token_outputs=True, stream=None, workspace=None):
-    """Cross entropy of the next token over the LM head with its gradient, the [T, V]
-    logits never kept.  As cross_entropy_fwd, and dhidden [T, H] bf16 and dW [V, H]: fp32,
+    """Cross entropy of the next token over the LM head with its gradient, without a
+    [T, V] tensor of logits or of their gradient.  As cross_entropy_fwd, and dhidden [T, H] bf16 and dW [V, H]: fp32,
     or `dW_dtype` = bfloat16.  With `dW` it is written there, with accumulate_dW (fp32)
     added."""
     torch = _torch()

@@ -148,10 +148,10 @@ struct ChunkPlan {
   int64_t ctl_words() const { return use ? kChunkCtlHead + 4 * max_chunks : 0; }
   int64_t turn_words() const { return use ? (n_t + n_v) * n_h * 16 : 0; }
   // list steps between a chunk's logit tiles and those that read them
-  int lag(int64_t H, int64_t pairs) const {
+  int lag(int64_t H, int64_t pairs, bool kept = false) const {
     if (max_chunks <= n_buf) return n_buf - 1;   // no buffer is used twice: logits first
     const int64_t ct = std::min(n_t, chunk_t), cv = std::min(n_v, chunk_v);
-    const int64_t step = ct * cv * (std::max<int64_t>(H / kBK, 9) + 8 * n_h);
+    const int64_t step = ct * cv * (std::max<int64_t>(kept ? 0 : H / kBK, 9) + 8 * n_h);
     const int64_t hold = (4 * ct + 4 * cv + 18) * pairs;
     return static_cast<int>(std::min<int64_t>(n_buf - 1, std::max<int64_t>(2, hold / step + 1)));
   }
@@ -239,9 +239,9 @@ ChunkPlan chunk_shape(int64_t T, int64_t H, int64_t V, bool det) {
 // As chunk_shape, for a dW that is stored in bf16: one chunk over up to 32 tiles of
 // tokens, of fewer columns, so that every dW tile has one contribution and is rounded as
 // it is stored.  Against several token chunks, fp32 sums and a pass that rounds them (us):
-// T = 8192 (30 % ignored), H = 4096, V = 151936 17190 and 17420; T = 5000, H = 2048, V =
-// 150000 4640 and 5020; T = 3000, H = 1024, V = 50000 820 and 890; but with H = 320, whose
-// tiles are short and wait for more of them, 810 and 610 (T = 5000, V = 50000).
+// T = 8192 (20 % ignored), H = 2048, V = 32000 1870 and 1890; T = 3000, H = 1024, V = 50000
+// 710 and 790; but with H = 320, whose tiles are short and wait for more of them, 810 and
+// 610 (T = 5000, V = 50000).
 ChunkPlan chunk_shape_bf16(int64_t T, int64_t H, int64_t V) {
   ChunkPlan p = chunk_shape(T, H, V, false);
   if (p.n_t <= p.chunk_t || p.n_t > 32 || H < 1024) return p;
@@ -315,7 +315,7 @@ int64_t part_rows(int64_t Tcap, int64_t V, int n_sm) {
 struct Layout {
   size_t counts, row_map, pos, tok_p, b_p, adv_p, h_p, part, zx, lse, coef, tile_list, red, dh32, turns, g, ctl;
   size_t lp_p, ent_p, ecoef, mu, gate_p, scale;
-  size_t live_of, h_l, tok_l, lse_l, coef_l, ecoef_l, mu_l, total;
+  size_t live_of, h_l, tok_l, lse_l, coef_l, ecoef_l, mu_l, keep, total;
 };
 
 constexpr size_t kNoRegion = ~size_t(0);   // a Layout region that is not allocated
@@ -421,6 +421,26 @@ Layout vp_backward_layout(int64_t T, int64_t H, int64_t V) {
   return L;
 }
 
+// The cross entropy's forward keeps the logits of its first so many token tiles in 16 bits
+// (kKeepTile), and the backward needs no product to form them again: 2.1 bytes written and
+// read for 2 H operations, under the products of other tiles.  Kept and formed again (ms,
+// whole calls): H = 4096 T = 8192 (30 % ignored), V = 151936 14.0 and 17.9, T = 1031 2.9 and
+// 3.7; H = 2048 T = 8192 (20 %), V = 32000 1.83 and 2.20; H = 1024 T = 16000, V = 32000 2.34
+// and 2.77; H = 640 T = 16000, V = 32000 1.76 and 1.87, T = 5000, V = 50000 0.92 and 0.93, T
+// = 400, V = 47000 0.146 and 0.140; H = 576 T = 5000, V = 50000 0.92 and 0.89; H = 512 0.79
+// and 0.76: from 640 on.  At most kKeepBytes of them, 1.5 % of the memory; the rows past it
+// (T V above 2^31) are formed again.
+constexpr int64_t kKeepBytes = int64_t(4) << 30, kKeepFromH = 640;
+int64_t keep_tiles(int64_t T, int64_t H, int64_t V) {
+  if (H < kKeepFromH) return 0;
+  return std::min((T + 255) / 256, kKeepBytes / ((V + 255) / 256 * kKeepTile));
+}
+// what the workspace holds for them: never less for a larger T or V
+int64_t keep_bytes(int64_t T, int64_t H, int64_t V) {
+  if (H < kKeepFromH) return 0;
+  return std::min(kKeepBytes, (T + 255) / 256 * ((V + 255) / 256) * kKeepTile);
+}
+
 // Workspace of the cross entropy: the active rows packed, which are the backward's rows
 // too; `dW32`: an fp32 dW that is rounded at the end.
 Layout ce_layout(int64_t T, int64_t H, int64_t V, int n_sm, bool with_bwd, bool dW32, size_t* dW32_off) {
@@ -451,6 +471,7 @@ Layout ce_layout(int64_t T, int64_t H, int64_t V, int n_sm, bool with_bwd, bool 
   const ChunkReserve cr = chunk_reserve(T, H, V, false, true);
   L.g = with_bwd ? take(cr.g) : o;
   L.ctl = with_bwd ? take(cr.ctl) : o;
+  L.keep = with_bwd ? take(static_cast<size_t>(keep_bytes(T, H, V))) : o;
   *dW32_off = with_bwd && dW32 ? take(static_cast<size_t>(V) * H * 4) : o;
   L.tile_list = L.lp_p = L.ent_p = L.gate_p = L.live_of = o;
   L.h_l = L.h_p;
@@ -485,6 +506,7 @@ Workspace carve(void* base, const Layout& L) {
   w.turns = L.turns != kNoRegion ? reinterpret_cast<uint32_t*>(p + L.turns) : nullptr;
   w.g = reinterpret_cast<uint16_t*>(p + L.g);
   w.ctl = reinterpret_cast<uint32_t*>(p + L.ctl);
+  w.keep = p + L.keep;
   w.lp_p = reinterpret_cast<float*>(p + L.lp_p);
   w.ent_p = reinterpret_cast<float*>(p + L.ent_p);
   w.ecoef = reinterpret_cast<float*>(p + L.ecoef);
@@ -633,7 +655,8 @@ struct ZeroJoin {
 
 // The forward kernel over the packed rows.
 molt_status run_forward_kernel(const DeviceInfo* di, int64_t Tcap, int64_t H, int64_t V, int S, const Workspace& w,
-                               const CUtensorMap& tm_h, const CUtensorMap& tm_w, bool ordered, bool sum_z, cudaStream_t s) {
+                               const CUtensorMap& tm_h, const CUtensorMap& tm_w, bool ordered, bool sum_z, cudaStream_t s,
+                               int64_t keep_t = 0) {
   FwdArgs fa{};
   fa.tok_p = w.tok_p;
   fa.counts = w.counts;
@@ -647,6 +670,8 @@ molt_status run_forward_kernel(const DeviceInfo* di, int64_t Tcap, int64_t H, in
   fa.next_unit = w.counts + 4;
   fa.part = w.part;
   fa.zx = w.zx;
+  fa.keep = keep_t > 0 ? w.keep : nullptr;
+  fa.keep_t = static_cast<int>(keep_t);
   fa.err = di->status;
   ev_start(1, s);
   MOLT_LAUNCH(launch_lmhead_fwd(tm_h, tm_w, fa, di->n_sm, s), "lmhead forward");
@@ -692,7 +717,8 @@ molt_status zero_backward_targets(const Workspace& w, int64_t T, int64_t H, int6
 // The backward over chunks: as run_backward; dW16: a bf16 dW in the place of dW_out.
 molt_status run_backward_chunk(const DeviceInfo* di, const ChunkPlan& cp, const uint16_t* W, int64_t T, int64_t H,
                                int64_t V, const Workspace& w, bool det, int det_clusters, int form,
-                               float* dW_out, int accumulate_dW, cudaStream_t stream, uint16_t* dW16 = nullptr) {
+                               float* dW_out, int accumulate_dW, cudaStream_t stream, uint16_t* dW16 = nullptr,
+                               int64_t keep_t = 0) {
   const int64_t Tcap = round_tiles(T);
   const auto bf16 = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
   const auto f32 = CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
@@ -721,6 +747,8 @@ molt_status run_backward_chunk(const DeviceInfo* di, const ChunkPlan& cp, const 
     a.ecoef = w.ecoef_l;
     a.mu = w.mu_l;
   }
+  a.keep = w.keep;
+  a.keep_t = static_cast<int>(keep_t);
   a.counts = w.counts;
   a.V = static_cast<int>(V);
   a.H = static_cast<int>(H);
@@ -736,7 +764,7 @@ molt_status run_backward_chunk(const DeviceInfo* di, const ChunkPlan& cp, const 
   a.det_turns = det ? w.turns : nullptr;
   a.err = di->status;
   const int ctas = det_clusters > 0 ? 4 * det_clusters : di->n_sm;
-  a.lag = cp.lag(H, std::max(1, ctas / 2));
+  a.lag = cp.lag(H, std::max(1, ctas / 2), keep_t > 0);
   ev_start(3, stream);
   MOLT_LAUNCH(launch_lmhead_bwd_chunk(m, a, ctas, stream), "lmhead backward");
   ev_stop(3, stream);
@@ -1023,7 +1051,8 @@ molt_status cross_entropy_impl(const uint16_t* hidden, const uint16_t* W, const 
               "pack");
   ev_stop(0, stream);
   const bool smooth = a.smoothing != 0.f || a.z_loss != 0.f;
-  MOLT_TRY(run_forward_kernel(di, Tcap, H, V, S, w, tm_h, tm_w, false, smooth, stream));
+  const int64_t keep_t = grad ? keep_tiles(T, H, V) : 0;
+  MOLT_TRY(run_forward_kernel(di, Tcap, H, V, S, w, tm_h, tm_w, false, smooth, stream, keep_t));
   ev_start(2, stream);
   MOLT_LAUNCH(launch_ce_merge(a, smooth, static_cast<int>(T), static_cast<int>(Tcap), static_cast<int>(V), S, w, loss_out, logp_out, lse_out,
                               stats_out, di->status, stream),
@@ -1033,7 +1062,7 @@ molt_status cross_entropy_impl(const uint16_t* hidden, const uint16_t* W, const 
   float* dW = round_dW ? reinterpret_cast<float*>(static_cast<uint8_t*>(sc.aligned()) + dW32_off)
                        : static_cast<float*>(dW_out);
   MOLT_TRY(run_backward_chunk(di, cp, W, T, H, V, w, false, 0, kGradScaled, dW, accumulate_dW, stream,
-                              dw16 ? static_cast<uint16_t*>(dW_out) : nullptr));
+                              dw16 ? static_cast<uint16_t*>(dW_out) : nullptr, keep_t));
   ev_start(4, stream);
   MOLT_LAUNCH(launch_cast_dh(w, true, static_cast<int>(T), static_cast<int>(H), dhidden_out, di->n_sm, stream), "cast dh");
   if (round_dW && !dw16)

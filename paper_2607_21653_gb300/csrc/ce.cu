@@ -5,8 +5,9 @@
 //   L    = sum_t w_t l_t / D,  D = denom, or the number of active rows
 //   dL/dz_tv = (w_t / D) [ (1 + 2 c lse_t) p_tv - e / V - (1 - e) [v = x_t] ]
 //
-// The logits exist only as tiles on chip: lse, z_x and the sum of z come from the
-// forward's epilogue, dL/dz from the backward's (kGradScaled).
+// lse, z_x and the sum of z come from the forward's epilogue on tiles of logits on chip,
+// dL/dz from the backward's (kGradScaled), which forms the tiles again, or from H = 640 on
+// reads what the forward's epilogue kept of them in 16 bits (kKeepTile).
 //
 // Two things make it more exact than its products.  The tensor cores add in fp32 but cut
 // off what does not fit, 256 times at H = 4096: the target's logit, which often is by far

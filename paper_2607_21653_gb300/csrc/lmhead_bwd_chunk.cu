@@ -44,6 +44,12 @@
 // through a ring of two slots.  TMEM holds two 256-column accumulators, so a
 // tile's epilogue runs under the next tile's products.
 //
+// The cross entropy's forward may have kept the logits in 16 bits (kKeepTile): a Z tile
+// then has no products, its epilogue loads them, a quarter of the columns ahead, and two
+// products are left of three.  Its own share of the time is small (a step's Z tiles spread
+// between its dW tiles took up to 17 % more: the run of them is over sooner than the
+// tiles in flight).
+//
 // What bounds it, measured on T = 16384, H = 4096, V = 151936 (61.2 TFLOP in
 // three products): 36.8 ms, 1.66 PFLOP/s, at the board's power cap (1.49 GHz of
 // 2.07, 1375 W), where a cuBLAS 8192^3 product reaches 1.72 at the same clock; the
@@ -66,6 +72,7 @@
 #include <cstdint>
 #include <cuda.h>
 #include <cuda_runtime.h>
+#include <type_traits>
 
 #include "molt_internal.cuh"
 #include "ptx.cuh"
@@ -115,7 +122,7 @@ template <int kAlign>
 struct TileList {
   int n_rows, V, H;
   bool add_dw;
-  int n_t, n_v, n_h, n_tc, n_vc, n_chunks, nb, lag;
+  int n_t, n_v, n_h, n_tc, n_vc, n_chunks, nb, lag, keep_t;
   int total;                             // tiles in the list
   int step, base;                        // list step and its first index
   int n_dh, n_z, n_dw;                   // tiles of the step
@@ -137,6 +144,7 @@ struct TileList {
     total = n_t * n_v + (n_t * n_vc + n_v * n_tc) * n_h;   // Z + dH + dW tiles of all chunks
     nb = a.n_buf;
     lag = a.lag;
+    keep_t = a.keep_t;
     step = 0;
     base = 0;
     fill();
@@ -189,9 +197,9 @@ struct TileList {
     if (z) {
       i -= n_dh;
       x.kind = kTileZ;
-      x.nk = H / kBK;
       x.v += i / z_ct;
       x.t += i % z_ct;
+      x.nk = x.t < keep_t ? 0 : H / kBK;   // 0: its logits were kept
       nr = 0;
       if (x.chunk >= nb) chunk_counts(x.chunk - nb, nz, nr);
       x.need = static_cast<int>(nr);
@@ -420,6 +428,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       Tile x;
       for (uint32_t ji = 0; ok && next_tile(ji, x); ++ji) {
         const int nk = x.nk;
+        if (nk == 0 && x.kind == kTileZ) continue;
         // K-major operands advance 32 bytes per K = 16, MN-major ones 16 rows of 128
         const bool a_mn = x.kind == kTileDW, b_mn = x.kind != kTileZ;
         const uint32_t idesc = idesc_bf16_f32(256, b_mn ? mma_n(x.h) : 256, a_mn, b_mn);
@@ -560,7 +569,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         if (lane == 0) mbar_arrive_cluster_relaxed(acce_lead0 + (ai & 1u) * 8);
         ++ai;
       };
-      if (x.kind == kTileZ) {
+      // a logit tile: g from the products, or from the logits that the forward kept
+      auto z_tile = [&](auto kept_c) -> bool {
+        constexpr bool kept = decltype(kept_c)::value;
+        // 32 of the lane's columns, and their reference
+        const uint8_t* slab = nullptr;
+        uint4 kq[4];
+        float kref;
+        auto load_kept = [&](int c) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) kq[i] = __ldcs(reinterpret_cast<const uint4*>(slab + (c * 4 + i) * 512 + lane * 16));
+          kref = __ldcs(reinterpret_cast<const float*>(slab + 16 * 512 + c * 128 + lane * 4));
+        };
+        if (kept && x.t * 256 + r0 < n_rows) {
+          slab = a.keep + (static_cast<int64_t>(x.t) * ((V + 255) / 256) + x.v) * kKeepTile +
+                 (static_cast<int>(rank) * kEpiWarps + hf * 4 + q) * kKeepSlab;
+          load_kept(0);   // under the wait for the buffer
+        }
         const int row = x.t * 256 + r0 + lane;
         const bool in = row < n_rows;
         const float coef = in ? a.coef[row] : 0.f;
@@ -576,57 +601,85 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const int lx = in ? a.tok_p[row] - vbase : -1;
         const int nvalid = in ? V - vbase : 0;
         // the buffer's previous chunk must have been read
-        if (x.need > 0 && !(ok = wait_count(cdone + x.chunk - a.n_buf, x.need))) break;
-        if (!(ok = acc_full())) break;
+        if (x.need > 0 && !wait_count(cdone + x.chunk - a.n_buf, x.need)) return false;
+        if (!kept && !acc_full()) return false;
         const int p0 = (x.v - x.v0) * 4 + hf * 2;
         const int gy = (x.buf * a.buf_panels + p0) * a.panel_rows + (x.t - x.t0) * 256 + r0;
+        const uint32_t rowp = box + lane * 128;
 #pragma unroll 1
-        for (int c = 0; c < 2; ++c) {
-          uint32_t w[32];
+        for (int c = 0; c < 4; ++c) {
+          float v[32];
+          if constexpr (!kept) {
+            tmem_ld32(taddr() + c * 32, v);
+            if (c == 3) release_acc();
+          } else if (slab != nullptr) {
+            const float ref = kref - lseL;   // v: (z - lse) log2 e
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            float v[32];
-            tmem_ld32(taddr() + c * 64 + u * 32, v);
-            const int lxc = lx - c * 64 - u * 32;
-            const int nv = nvalid - c * 64 - u * 32;
-            auto p_of = [&](int j) -> float {   // g without the target's term
-              const float e = ex2_approx(fmaf(v[j], kLog2e, -lseL));
-              if constexpr (kForm == kGradEntropy) return fmaf(ecoef, v[j] - mu, coef) * e;
-              if constexpr (kForm == kGradScaled) return fmaf(ecoef, e, -mu);
-              return coef * e;
-            };
-            // a target or an invalid column among the warp's 32 x 32 values is rare
-            if (__any_sync(0xffffffffu, static_cast<unsigned>(lxc) < 32u || nv < 32)) {
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t ks[4] = {kq[i].x, kq[i].y, kq[i].z, kq[i].w};
 #pragma unroll
-              for (int j = 0; j < 32; j += 2) {
-                float g0 = p_of(j), g1 = p_of(j + 1);
-                if (j == lxc) g0 -= coef;
-                if (j + 1 == lxc) g1 -= coef;
-                if (j >= nv) g0 = 0.f;
-                if (j + 1 >= nv) g1 = 0.f;
-                w[u * 16 + j / 2] = pack_bf16x2(g0, g1);
+              for (int j = 0; j < 4; ++j) {
+                const float k0 = __uint_as_float(__byte_perm(ks[j], __float_as_uint(kKeepZero), 0x7610)) - kKeepZero;
+                const float k1 = __uint_as_float(__byte_perm(ks[j], __float_as_uint(kKeepZero), 0x7632)) - kKeepZero;
+                v[8 * i + 2 * j] = fmaf(k0, -1.f / kKeepStep, ref);
+                v[8 * i + 2 * j + 1] = fmaf(k1, -1.f / kKeepStep, ref);
               }
-            } else {
-#pragma unroll
-              for (int j = 0; j < 32; j += 2) w[u * 16 + j / 2] = pack_bf16x2(p_of(j), p_of(j + 1));
             }
-          }
-          if (c == 1) release_acc();
-          if (c == 0) raise();   // of the tile before, long stored
-          box_free();
-          const uint32_t rowp = box + lane * 128;
+            if (c < 3) load_kept(c + 1);
+          } else {
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            st_shared_v4(rowp + static_cast<uint32_t>(i ^ (lane & 7)) * 16, w[4 * i], w[4 * i + 1], w[4 * i + 2],
+            for (int j = 0; j < 32; ++j) v[j] = 0.f;   // rows past the end
+          }
+          const int lxc = lx - c * 32;
+          const int nv = nvalid - c * 32;
+          auto p_of = [&](int j) -> float {   // g without the target's term
+            const float e = ex2_approx(kept ? v[j] : fmaf(v[j], kLog2e, -lseL));
+            if constexpr (kForm == kGradEntropy) return fmaf(ecoef, v[j] - mu, coef) * e;
+            if constexpr (kForm == kGradScaled) return fmaf(ecoef, e, -mu);
+            return coef * e;
+          };
+          uint32_t w[16];
+          // a target or an invalid column among the warp's 32 x 32 values is rare
+          if (__any_sync(0xffffffffu, static_cast<unsigned>(lxc) < 32u || nv < 32)) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) {
+              float g0 = p_of(j), g1 = p_of(j + 1);
+              if (j == lxc) g0 -= coef;
+              if (j + 1 == lxc) g1 -= coef;
+              if (j >= nv) g0 = 0.f;
+              if (j + 1 >= nv) g1 = 0.f;
+              w[j / 2] = pack_bf16x2(g0, g1);
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) w[j / 2] = pack_bf16x2(p_of(j), p_of(j + 1));
+          }
+          const int u = c & 1;
+          if (u == 0) {
+            if (c == 0) raise();   // of the tile before, long stored
+            box_free();
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            st_shared_v4(rowp + static_cast<uint32_t>((u * 4 + i) ^ (lane & 7)) * 16, w[4 * i], w[4 * i + 1], w[4 * i + 2],
                          w[4 * i + 3]);
+          if (u == 0) continue;
           fence_proxy_async_smem();
           __syncwarp();
           if (lane == 0) {
-            tma_store_2d(&m.g32, box, 0, gy + c * a.panel_rows);
+            tma_store_2d(&m.g32, box, 0, gy + (c >> 1) * a.panel_rows);
             bulk_commit_group();
           }
         }
         pending = zdone + x.chunk;
+        return true;
+      };
+      if (x.kind == kTileZ) {
+        if constexpr (kForm == kGradScaled)
+          ok = x.nk == 0 ? z_tile(std::true_type{}) : z_tile(std::false_type{});
+        else
+          ok = z_tile(std::false_type{});
+        if (!ok) break;
         continue;
       }
       const bool dh = x.kind == kTileDH;

@@ -103,6 +103,27 @@ struct Stats {
   }
 };
 
+// Keeps 32 logits of a row under the reference mL = log2 e times a maximum that none of
+// them exceeds; `slab` is the lane's first vector for them, `ref` its reference.
+__device__ __forceinline__ void keep_logits(const float (&v)[32], float mL, uint8_t* slab, uint8_t* ref) {
+  const float base = fmaf(mL, kKeepStep, kKeepZero);
+  uint32_t w[16];
+#pragma unroll
+  for (int j = 0; j < 32; j += 2) {
+    uint32_t k[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float t = fmaf(v[j + i], -kLog2e * kKeepStep, base);
+      k[i] = __float_as_uint(fmaxf(fminf(t, kKeepZero + 65535.f), kKeepZero));
+    }
+    w[j / 2] = __byte_perm(k[0], k[1], 0x5410);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    __stcs(reinterpret_cast<uint4*>(slab + i * 512), make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
+  __stcs(reinterpret_cast<float*>(ref), mL);
+}
+
 // fold 32 logits (all columns valid) into the row's statistics
 template <int kMode>
 __device__ __forceinline__ void fold_full(const float (&v)[32], Stats& r) {
@@ -172,7 +193,8 @@ __device__ __forceinline__ void unit_of(int u, int n_mt, int S, int& mt, int& s)
 // (api.cu) and merged in their order.  T = 16384, V = 65536: 0.49 against
 // 0.38 ms at H = 256, 0.73 and 0.62 at H = 512, 1.33 and 1.21 at H = 1024; at H = 4096
 // the products hide it (4.94 and 4.93).
-template <int kMode>
+// kKeep: the logits of the first keep_t token tiles are kept (see kKeepTile).
+template <int kMode, bool kKeep>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     lmhead_fwd_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__ CUtensorMap tm_w,
                       const FwdArgs a) {
@@ -396,6 +418,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             fold_full<kMode>(v, st);
           else
             fold_partial<kMode>(v, ncols - c0, st);
+          if constexpr (kKeep) {
+            // (a quarter of rows past the end keeps nothing)
+            if (mt < a.keep_t && mt * 256 + r_in_tile - lane < n_rows) {
+              uint8_t* slab = a.keep + (static_cast<int64_t>(mt) * a.n_vtiles + vt) * kKeepTile +
+                              (static_cast<int>(rank) * kEpiWarps + hf * 4 + q) * kKeepSlab;
+              keep_logits(v, st.m * kLog2e, slab + c0 * 64 + lane * 16, slab + 16 * 512 + c0 * 4 + lane * 4);
+            }
+          }
         }
         // every lane's TMEM reads are complete: one arrival per warp hands it back
         tc_fence_before();
@@ -458,12 +488,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 cudaError_t launch_lmhead_fwd(const CUtensorMap& tm_h, const CUtensorMap& tm_w, const FwdArgs& a, int grid,
                               cudaStream_t s) {
   // the shared-memory attribute is per device: set it on each device once
-  static std::atomic<unsigned long long> attr_set[3] = {};
+  static std::atomic<unsigned long long> attr_set[6] = {};
   const int mode = a.ordered ? kOrdered : a.sum_z ? kSumZ : kStats;
-  auto* const k = mode == kOrdered ? &lmhead_fwd_kernel<kOrdered>
-                  : mode == kSumZ  ? &lmhead_fwd_kernel<kSumZ>
-                                   : &lmhead_fwd_kernel<kStats>;
-  auto& set = attr_set[mode];
+  const bool keep = a.keep != nullptr;
+  auto* const k = mode == kOrdered ? &lmhead_fwd_kernel<kOrdered, false>
+                  : mode == kSumZ  ? (keep ? &lmhead_fwd_kernel<kSumZ, true> : &lmhead_fwd_kernel<kSumZ, false>)
+                                   : (keep ? &lmhead_fwd_kernel<kStats, true> : &lmhead_fwd_kernel<kStats, false>);
+  auto& set = attr_set[2 * mode + keep];
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;

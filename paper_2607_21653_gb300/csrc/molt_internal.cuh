@@ -46,6 +46,7 @@ struct Workspace {
   // backward over chunks
   uint16_t* g;          // chunk buffers of the softmax gradient (bf16 bits)
   uint32_t* ctl;        // tile counter, abort word, per-chunk counters
+  uint8_t* keep;        // cross entropy: kept logits
   // extended objective (loss call only)
   float* lp_p;          // [Tcap] packed log-probs
   float* ent_p;         // [Tcap] packed entropies
@@ -57,6 +58,17 @@ constexpr int kRedRows = 32, kRedSlots = 8;
 
 // advantage estimators (values of molt_adv_estimator)
 constexpr int kAdvGrpo = 0, kAdvGroupMean = 1, kAdvDrGrpo = 2, kAdvRloo = 3, kAdvReinforcePP = 4;
+
+// Kept logits of the cross entropy: per 256 x 256 tile (tokens first) a slab for each
+// of its 16 epilogue warps (CTA, column half, lane quarter): sixteen vectors of eight
+// columns by 32 rows, 16 bits each, then four references by 32 rows.  A logit is
+//   z log2 e = reference - k / 1024,
+// the reference being the row's running maximum at its 32 columns; k ends at 65535, a
+// factor of 2^-64.
+constexpr int kKeepSlab = 16 * 512 + 4 * 128;
+constexpr int kKeepTile = 16 * kKeepSlab;
+constexpr float kKeepStep = 1024.f;
+constexpr float kKeepZero = 8388608.f;   // 2^23: k in a float's low bits
 
 struct FwdArgs {
   const int32_t* tok_p;
@@ -70,6 +82,8 @@ struct FwdArgs {
   int32_t* next_unit;   // zeroed
   float4* part;         // [n_split, rows_cap]
   float* zx;
+  uint8_t* keep;        // where the logits of the first keep_t token tiles go, or nullptr
+  int keep_t;
   unsigned* err;
 };
 
@@ -113,11 +127,13 @@ struct ChunkArgs {
   const int32_t* tok_p;
   const float* lse;
   const float* coef;
-  int form;                  // how z becomes g: kGradPlain, kGradEntropy, kGradSmooth
+  int form;                  // how z becomes g: kGradPlain, kGradEntropy, kGradScaled
   const float* ecoef;        // the forms' further row values (kGradPlain: none)
   const float* mu;
   const float* scale;        // kGradScaled
   int dw_bf16;               // kGradScaled: dW is rounded and stored through dw16 (one token chunk, nothing added)
+  const uint8_t* keep;       // kGradScaled: kept logits of the first keep_t token tiles
+  int keep_t;
   const int32_t* counts;     // counts[3] = rows
   int V, H;
   int chunk_t, chunk_v;      // a chunk's tiles of tokens and vocab, at most

@@ -108,6 +108,54 @@ def test_rounded_weight_gradient(T, H, V, masked):
     assert molt.device_status() == 0
 
 
+@pytest.mark.parametrize("spread", [1.0, 40.0, 2000.0])
+@pytest.mark.parametrize("H", [576, 640])
+def test_logits_far_apart(H, spread):
+    """Rows whose logits lie up to `spread` apart, at widths whose logits are formed again
+    and kept.  The products' fp32 sums of H terms of up to z / 4 are good to 1e-5 z at the
+    most, so logp is held to that where it is more than LOGP_ATOL."""
+    T, V = 300, 1300
+    h, W, x, _ = make(T, H, V, 0.1, seed=11, known=False)
+    h = (h.float() * (torch.rand(T, 1, device=h.device, generator=torch.Generator(device=h.device).manual_seed(1)) * spread)).to(torch.bfloat16)
+    out, ref = molt.cross_entropy_fwd_bwd(h, W, x), reference(h, W, x)
+    size = float((h.double() @ W.double().t()).abs().max())
+    assert (out["logp"].double() - ref["logp"]).abs().max() <= max(LOGP_ATOL, 1e-5 * size)
+    assert abs(float(out["loss"]) - float(ref["loss"])) <= LOSS_RTOL * ref["size"]
+    for k in ("dhidden", "dW"):
+        assert_grad_close(out[k].double().cpu().numpy(), ref[k].cpu().numpy(), k)
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_kept_logits_show_a_bad_row(value):
+    """As without keeping: the row's dhidden and dW are NaN, the other rows' dhidden is not."""
+    h, W, x, _ = make(300, 640, 700, seed=12)
+    h[17, 3] = value
+    out = molt.cross_entropy_fwd_bwd(h, W, x)
+    assert torch.isnan(out["dhidden"][17]).all() and torch.isnan(out["dW"]).all() and torch.isnan(out["loss"]).all()
+    rest = torch.arange(300, device=h.device) != 17
+    good = molt.cross_entropy_fwd_bwd(h[rest], W, x[rest], denom=300.0)
+    # an upper tile's K blocks may hold the bad row's zeros only: rows are independent
+    assert torch.isfinite(out["dhidden"][rest]).all()
+    assert (out["dhidden"][rest].float() - good["dhidden"].float()).abs().max() <= 2e-2 * good["dhidden"].float().abs().max()
+
+
+def test_more_logits_than_are_kept():
+    """The last token tiles' logits are formed again; against two calls of half the rows,
+    which keep all of theirs (each side is good to 2e-2, so they agree to 4e-2)."""
+    T, H, V = 8300, 640, 262149
+    h, W, x, _ = make(T, H, V, seed=13)
+    out = molt.cross_entropy_fwd_bwd(h, W, x, denom=float(T))
+    dW = None
+    for rows in (slice(0, 4150), slice(4150, T)):
+        part = molt.cross_entropy_fwd_bwd(h[rows], W, x[rows], denom=float(T), dW=dW, accumulate_dW=dW is not None)
+        dW = part["dW"]
+        assert (out["logp"][rows] - part["logp"]).abs().max() <= 2 * LOGP_ATOL
+        far = (out["dhidden"][rows].float() - part["dhidden"].float()).abs().max()
+        assert far <= 4e-2 * part["dhidden"].float().abs().max()
+    assert (out["dW"] - dW).abs().max() <= 4e-2 * dW.abs().max()
+    assert molt.device_status() == 0
+
+
 def test_one_column_has_no_loss():
     h, W, x, _ = make(10, 64, 1, known=False)
     out = molt.cross_entropy_fwd_bwd(h, W, x)
