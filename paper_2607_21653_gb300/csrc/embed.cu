@@ -313,19 +313,31 @@ __device__ __forceinline__ void zero_rows(const EmbedGradArgs& a, int64_t v0) {
     const int next = i + 32;
     i = next < a.T && a.keys[next] == last ? max(next, warp_lower_bound(a.keys, a.T, last + 1)) : next;
   }
-  for (unsigned m = ~occur & (rows == 32 ? 0xffffffffu : (1u << rows) - 1u); m != 0; m &= m - 1)
-    zero_span(static_cast<O*>(a.dE) + (v0 + __ffs(m) - 1) * a.H, a.H);
+  // neighbours together: short rows of any length then are few unaligned ends
+  for (unsigned m = ~occur & (rows == 32 ? 0xffffffffu : (1u << rows) - 1u); m != 0;) {
+    const int at = __ffs(m) - 1, n = __ffs(~(m >> at)) - 1;   // n < 0: all 32
+    const int len = n < 0 ? 32 : n;
+    zero_span(static_cast<O*>(a.dE) + (v0 + at) * a.H, len * a.H);
+    m = at + len >= 32 ? 0u : m & (0xffffffffu << (at + len));
+  }
 }
 
 // kV elements as they are in memory, so that a batch of rows in flight takes few registers
 template <class X, int kV>
 struct Raw {
-  uint4 q[kV * sizeof(X) / 16];
+  static constexpr int kWords = kV * sizeof(X) / 4;
+  alignas(16) uint32_t w[kWords];
   __device__ __forceinline__ void load(const X* p) {
+    if constexpr (kWords == 1) {
+      w[0] = *reinterpret_cast<const uint32_t*>(p);
+    } else if constexpr (kWords == 2) {
+      *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(p);
+    } else {
 #pragma unroll
-    for (int i = 0; i < static_cast<int>(kV * sizeof(X) / 16); ++i) q[i] = reinterpret_cast<const uint4*>(p)[i];
+      for (int i = 0; i < kWords / 4; ++i) reinterpret_cast<uint4*>(w)[i] = reinterpret_cast<const uint4*>(p)[i];
+    }
   }
-  __device__ __forceinline__ void get(float (&v)[kV]) const { load_vec<kV>(reinterpret_cast<const X*>(q), v); }
+  __device__ __forceinline__ void get(float (&v)[kV]) const { load_vec<kV>(reinterpret_cast<const X*>(w), v); }
 };
 template <class X>
 struct Raw<X, 1> {
@@ -519,6 +531,17 @@ molt_status check(int64_t T, int64_t H, int64_t V, int narrow, int wide, float s
   return MOLT_OK;
 }
 
+// Elements to a load or store of rows of H side by side: as many as divide H, up to 8,
+// and the two bases are aligned to.  (us, where only multiples of eight were read in
+// vectors and now: T = 30000, H = 1566 forward 49 and 37; gradient, absent rows then also
+// zeroed one by one, T = 26064, H = 4554, V = 49523 246 and 193.)
+int vec_of(int64_t H, const void* p, int p_dtype, const void* q, int q_dtype) {
+  for (int v = 8; v > 1; v /= 2)
+    if (H % v == 0 && aligned(p, std::min(16, v * dtype_bytes(p_dtype))) && aligned(q, std::min(16, v * dtype_bytes(q_dtype))))
+      return v;
+  return 1;
+}
+
 // f(X, O): the types as values of their own
 template <class F>
 cudaError_t with_types(int x, int o, F f) {
@@ -588,8 +611,8 @@ molt_status molt_token_embedding(const void* E, int E_dtype, const int32_t* toke
   molt_status st;
   EmbedArgs a{E, tokens, T, static_cast<int>(V), static_cast<int>(H), scale, out, device_status_word(&st)};
   if (!a.err) return st;
-  const bool vec = H % 8 == 0 && aligned(E, 16) && aligned(out, 16);
-  const Group g = group_of(vec ? H / 8 : H);
+  const int vec = vec_of(H, E, E_dtype, out, out_dtype);
+  const Group g = group_of(H / vec);
   // four rows to a thread keep enough loads in flight; where that leaves SMs idle, one
   const int rows = T >= 4 * int64_t(device_sm_count()) * g.per_block ? 4 : 1;
   const int grid = static_cast<int>((T + rows * g.per_block - 1) / (rows * g.per_block));
@@ -597,8 +620,10 @@ molt_status molt_token_embedding(const void* E, int E_dtype, const int32_t* toke
   const cudaError_t e = with_types(E_dtype, out_dtype, [&](auto x, auto o) {
     using X = decltype(x);
     using O = decltype(o);
-    auto* k = vec ? (rows == 4 ? embed_kernel<X, O, 8, 4> : embed_kernel<X, O, 8, 1>)
-                  : (rows == 4 ? embed_kernel<X, O, 1, 4> : embed_kernel<X, O, 1, 1>);
+    auto* k = vec == 8   ? (rows == 4 ? embed_kernel<X, O, 8, 4> : embed_kernel<X, O, 8, 1>)
+              : vec == 4 ? (rows == 4 ? embed_kernel<X, O, 4, 4> : embed_kernel<X, O, 4, 1>)
+              : vec == 2 ? (rows == 4 ? embed_kernel<X, O, 2, 4> : embed_kernel<X, O, 2, 1>)
+                         : (rows == 4 ? embed_kernel<X, O, 1, 4> : embed_kernel<X, O, 1, 1>);
     k<<<grid, block, 0, stream>>>(a);
     return cudaGetLastError();
   });
@@ -656,7 +681,7 @@ molt_status molt_token_embedding_bwd(const void* dout, int dout_dtype, const int
     at = 1 - at;
   }
 
-  const bool vec = H % 8 == 0 && aligned(dout, 16) && aligned(dE, 16);
+  const int vec = vec_of(H, dout, dout_dtype, dE, dE_dtype);
   const Group g = group_of((H + 7) / 8);
   EmbedGradArgs a{};
   a.dout = dout;
@@ -684,7 +709,10 @@ molt_status molt_token_embedding_bwd(const void* dout, int dout_dtype, const int
   e = with_types(dout_dtype, dE_dtype, [&](auto x, auto o) {
     using X = decltype(x);
     using O = decltype(o);
-    auto* k = vec ? embed_grad_kernel<X, O, 8> : embed_grad_kernel<X, O, 1>;
+    auto* k = vec == 8   ? embed_grad_kernel<X, O, 8>
+              : vec == 4 ? embed_grad_kernel<X, O, 4>
+              : vec == 2 ? embed_grad_kernel<X, O, 2>
+                         : embed_grad_kernel<X, O, 1>;
     k<<<a.sum_blocks + a.zero_blocks, dim3(g.threads, g.per_block), 0, stream>>>(a);
     return cudaGetLastError();
   });

@@ -104,23 +104,29 @@ NormArgs base_args(const molt_norm_desc* d) {
   return a;
 }
 
-// Whether rows can be read 16 bytes at a time: the row length in whole vectors, and
-// every row and parameter on a 16-byte boundary.
-bool vectors(const molt_norm_desc* d, const NormArgs& a, std::initializer_list<const void*> ptrs) {
-  if (a.H % 8 != 0) return false;
+// Elements that rows can be read at a time: eight, where the rows' length is in whole
+// vectors and every row and parameter on a 16-byte boundary; two, where they are in whole
+// pairs (20000 x 1566 with an fp32 stream, one and two at a time: forward 137 and 76 us,
+// backward 188 and 178); or one.
+int vector_of(const molt_norm_desc* d, const NormArgs& a, std::initializer_list<const void*> ptrs) {
   const int b = dtype_bytes(d->dtype), rb = dtype_bytes(d->residual_dtype);
-  if (a.x_ld * b % 16 != 0 || a.r_ld * rb % 16 != 0 || a.dy_ld * b % 16 != 0) return false;
-  for (const void* p : ptrs)
-    if (!aligned(p, 16)) return false;
-  return true;
+  const auto based = [&](int bytes) {
+    for (const void* p : ptrs)
+      if (!aligned(p, bytes)) return false;
+    return true;
+  };
+  if (a.H % 8 == 0 && a.x_ld * b % 16 == 0 && a.r_ld * rb % 16 == 0 && a.dy_ld * b % 16 == 0 && based(16)) return 8;
+  // (bases for pairs of the widest type among them)
+  const bool wide = b == 4 || rb == 4 || dtype_bytes(d->param_dtype) == 4;
+  return a.H % 2 == 0 && a.x_ld % 2 == 0 && a.r_ld % 2 == 0 && a.dy_ld % 2 == 0 && based(wide ? 8 : 4) ? 2 : 1;
 }
 
 // Rows in registers, a block to each (or to four short ones): for the few rows of a
 // decoding step, and for vectors of more elements than the persistent kernels hold.
-NormShape row_shape(int H, bool vec) {
+NormShape row_shape(int H, int vec) {
   NormShape s{};
-  s.vec = vec ? 8 : 1;
-  s.elems = !vec ? 0 : H <= 8 * kNormMaxThreads ? 8 : H <= 16 * kNormMaxThreads ? 16 : H <= kNormMaxH ? 32 : 0;
+  s.vec = vec;
+  s.elems = vec != 8 ? 0 : H <= 8 * kNormMaxThreads ? 8 : H <= 16 * kNormMaxThreads ? 16 : H <= kNormMaxH ? 32 : 0;
   s.threads = s.elems == 0 ? kNormMaxThreads : ((H + s.elems - 1) / s.elems + 31) / 32 * 32;
   s.rows = s.threads == 32 ? 4 : 1;
   return s;
@@ -151,7 +157,7 @@ bool rows_shape(const molt_norm_desc* d, bool bwd, NormArgs& a, NormShape& s) {
   // rows too (32768 x 2048 with an fp32 stream: 8 elements 190 us, 16 132; 16001 x 5120 141
   // and 110), not in the backward, whose sums then take too many registers (190 and 213, 189
   // and 221), nor where elements come one by one (20000 x 2049 forward 115 and 135)
-  const int most8 = !bwd && s.vec == 8 ? 256 : 8 * 640;
+  const int most8 = !bwd && s.vec > 1 ? 256 : 8 * 640;
   const int elems = a.H <= 256 || (a.H > 512 && a.H <= most8) ? 8 : 16;
   s.elems = elems;
   s.threads = ((a.H + elems - 1) / elems + 31) / 32 * 32;
@@ -214,11 +220,11 @@ molt_status molt_residual_norm_fwd(const molt_norm_desc* desc, const void* x, co
   molt_status st;
   a.err = device_status_word(&st);
   if (!a.err) return st;
-  NormShape s = row_shape(a.H, vectors(desc, a, {x, residual, w_post, w_pre, y, residual_out,
+  NormShape s = row_shape(a.H, vector_of(desc, a, {x, residual, w_post, w_pre, y, residual_out,
                                                  desc->gate_kind == MOLT_GATE_TOKEN ? nullptr : gate}));
   // rows that the SMs hold at once gain nothing from copies ahead
   const NormShape few = s;
-  if ((s.vec == 1 || a.T > 16 * int64_t(device_sm_count())) && !rows_shape(desc, false, a, s)) s = few;
+  if ((s.vec != 8 || a.T > 16 * int64_t(device_sm_count())) && !rows_shape(desc, false, a, s)) s = few;
   int grid;
   if (const cudaError_t e = launch(desc, a, s, &grid, false, stream); e != cudaSuccess) return cuda_fail(e, "residual norm");
   note_launches(1);
@@ -295,7 +301,7 @@ molt_status molt_residual_norm_bwd(const molt_norm_desc* desc, const void* dy, c
   a.err = device_status_word(&st);
   if (!a.err) return st;
   NormShape s =
-      row_shape(a.H, vectors(desc, a, {dy, dresidual, x, residual, w_post, w_pre, dx, dresidual_out,
+      row_shape(a.H, vector_of(desc, a, {dy, dresidual, x, residual, w_post, w_pre, dx, dresidual_out,
                                        desc->gate_kind == MOLT_GATE_TOKEN ? nullptr : gate,
                                        desc->gate_kind == MOLT_GATE_FULL ? dgate : nullptr}));
   if (!rows_shape(desc, true, a, s)) s = NormShape{kNormMaxThreads, 1, 0, 1, false, 0};

@@ -241,6 +241,7 @@ __global__ void __launch_bounds__(kNormMaxThreads) norm_fwd_kernel(const NormArg
 // that begins inside a word brings the words it touches and is read at its offset; words
 // that reach outside the matrix (its first and last row) are filled in element by element.
 //   kV = 8: rows of whole vectors; a thread holds E / 8 vectors of 8 elements.
+//   kV = 2: rows of whole pairs; a thread holds E / 2 pairs, blockDim.x pairs apart.
 //   kV = 1: any row; a thread holds elements blockDim.x apart.
 // Multiplications and additions are done two at a time (f32x2: a tenth fewer instructions).
 // ---------------------------------------------------------------------------
@@ -276,7 +277,7 @@ __device__ __forceinline__ void ring_fetch(Stream& s, uint8_t* stage, uint32_t b
   const uint8_t *src = s.next, *end = src + s.bytes;
   uint8_t* dst = stage + s.at;
   int n = s.bytes;
-  if constexpr (kV == 1) {
+  if constexpr (kV != 8) {
     const uint8_t* w0 = reinterpret_cast<const uint8_t*>(reinterpret_cast<uintptr_t>(src) & ~uintptr_t(15));
     const uint8_t* w1 = reinterpret_cast<const uint8_t*>((reinterpret_cast<uintptr_t>(end) + 15) & ~uintptr_t(15));
     if (n > 0) {
@@ -343,10 +344,9 @@ template <int kV, int E>
 struct Share {
   static constexpr int kPairs = E / 2;
   int H;
-  // of element e; kV = 8: of the vector that e begins
+  // of the vector that element e begins
   __device__ __forceinline__ int col(int e) const {
-    return kV == 8 ? (e / 8 * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x)) * 8
-                   : e * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x);
+    return (e / kV * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x)) * kV;
   }
   __device__ __forceinline__ bool has(int e) const { return col(e) < H; }
   // elements past the row's end read as 0
@@ -362,6 +362,13 @@ struct Share {
           for (int j = 0; j < 4; ++j) v[e / 2 + j] = f2(0.f);
         }
       }
+    } else if constexpr (kV == 2) {
+#pragma unroll
+      for (int e = 0; e < E; e += 2) {
+        float p[2] = {0.f, 0.f};
+        if (has(e)) load_vec<2>(row + col(e), p);
+        v[e / 2] = f2(p[0], p[1]);
+      }
     } else {
 #pragma unroll
       for (int e = 0; e < E; e += 2)
@@ -374,6 +381,12 @@ struct Share {
 #pragma unroll
       for (int e = 0; e < E; e += 8)
         if (has(e)) store_pairs(row + col(e), v + e / 2);
+    } else if constexpr (kV == 2) {
+#pragma unroll
+      for (int e = 0; e < E; e += 2) {
+        const float p[2] = {v[e / 2].x(), v[e / 2].y()};
+        if (has(e)) store_vec<2>(row + col(e), p);
+      }
     } else {
 #pragma unroll
       for (int e = 0; e < E; e += 2) {
@@ -646,7 +659,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) norm_bwd_rows_kernel(const 
     param<X, kV, E>(factor, a.param_f32, add, 1.f, sh, f);
 #pragma unroll
     for (int j = 0; j < P; ++j) f[j] = mul2(f[j], v[j]);
-    if (blockDim.y == 1) {   // (a row of the parts is on a vector boundary where kV = 8)
+    if (blockDim.y == 1) {   // (a row of the parts is on a boundary of kV elements)
       sh.store(out, f);
       return;
     }
@@ -838,12 +851,12 @@ cudaError_t launch_norm_rows(const NormArgs& a, const NormShape& s, int n_sm, in
    {MOLT_FWD(V, 16, 192, 1), MOLT_BWD(V, 16, 128, 3)},                                                        \
    {MOLT_FWD(V, 16, 320, 2), MOLT_BWD(V, 16, 512, 1)},                                                       \
    {MOLT_FWD(V, 16, 512, 1), MOLT_BWD(V, 16, 512, 1)}}
-  static constexpr Kernel kernels[2][4][4] = {MOLT_ROWS(1), MOLT_ROWS(8)};
+  static constexpr Kernel kernels[3][4][4] = {MOLT_ROWS(1), MOLT_ROWS(2), MOLT_ROWS(8)};
 #undef MOLT_ROWS
 #undef MOLT_BWD
 #undef MOLT_FWD
-  static KernelInfo info[2][4][4];
-  const int vec = s.vec == 8 ? 1 : 0, size = s.elems == 8 ? 0 : s.threads <= 192 ? 1 : s.threads <= 320 ? 2 : 3;
+  static KernelInfo info[3][4][4];
+  const int vec = s.vec == 8 ? 2 : s.vec == 2 ? 1 : 0, size = s.elems == 8 ? 0 : s.threads <= 192 ? 1 : s.threads <= 320 ? 2 : 3;
   const int which = (bwd ? 2 : 0) + (a.gate_kind == MOLT_GATE_FULL ? 1 : 0);
   const Kernel k = kernels[vec][size][which];
   int warp_regs;

@@ -38,11 +38,23 @@ __device__ __forceinline__ uint32_t pack2(float a, float b, const __half*) {
   return *reinterpret_cast<const uint32_t*>(&p);
 }
 
-// kV consecutive elements; kV = 8 needs 16-byte alignment
+// kV = 1, 2, 4 or 8 consecutive elements, aligned to their size (at most 16 bytes)
 template <int kV, class T>
 __device__ __forceinline__ void load_vec(const T* p, float (&v)[kV]) {
   if constexpr (kV == 1) {
     v[0] = to_float(*p);
+  } else if constexpr (kV == 2 && sizeof(T) == 4) {
+    const float2 a = *reinterpret_cast<const float2*>(p);
+    v[0] = a.x, v[1] = a.y;
+  } else if constexpr (kV == 4 && sizeof(T) == 4) {
+    const float4 a = *reinterpret_cast<const float4*>(p);
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
+  } else if constexpr (kV == 2) {
+    unpack2(*reinterpret_cast<const uint32_t*>(p), p, v[0], v[1]);
+  } else if constexpr (kV == 4) {
+    const uint2 a = *reinterpret_cast<const uint2*>(p);
+    unpack2(a.x, p, v[0], v[1]);
+    unpack2(a.y, p, v[2], v[3]);
   } else if constexpr (sizeof(T) == 4) {
     static_assert(kV == 8);
     const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
@@ -60,6 +72,14 @@ template <int kV, class T>
 __device__ __forceinline__ void store_vec(T* p, const float (&v)[kV]) {
   if constexpr (kV == 1) {
     from_float(v[0], *p);
+  } else if constexpr (kV == 2 && sizeof(T) == 4) {
+    *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
+  } else if constexpr (kV == 4 && sizeof(T) == 4) {
+    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+  } else if constexpr (kV == 2) {
+    *reinterpret_cast<uint32_t*>(p) = pack2(v[0], v[1], p);
+  } else if constexpr (kV == 4) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack2(v[0], v[1], p), pack2(v[2], v[3], p));
   } else if constexpr (sizeof(T) == 4) {
     reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
     reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);

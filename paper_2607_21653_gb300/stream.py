@@ -124,20 +124,22 @@ class NormDesc(ctypes.Structure):
 
 GATE_NONE, GATE_CHANNEL, GATE_TOKEN, GATE_FULL = range(4)
 
-# Descriptors by their values: building one takes longer than the rest of a small call's
-# marshalling.  They are read only.
+# Descriptors by their values, with the backward's workspace bytes: building one takes
+# longer than the rest of a small call's marshalling.  They are read only.
 _desc_cache: dict = {}
 _DESC_CACHE_MAX = 256
 
 
-def _desc(*values):
-    """Reference to the molt_norm_desc of these values."""
-    ref = _desc_cache.get(values)
-    if ref is None:
+def _desc(device, *values):
+    """Reference to the molt_norm_desc of these values, and its backward's workspace bytes."""
+    key = (device, values)
+    entry = _desc_cache.get(key)
+    if entry is None:
         if len(_desc_cache) >= _DESC_CACHE_MAX:
             _desc_cache.clear()
-        ref = _desc_cache[values] = ctypes.byref(NormDesc(*values))
-    return ref
+        ref = ctypes.byref(NormDesc(*values))
+        entry = _desc_cache[key] = ref, load().molt_residual_norm_bwd_workspace_bytes(ref)
+    return entry
 
 
 def _gate_kind(gate, T, H):
@@ -204,8 +206,8 @@ def residual_norm_fwd(x, residual=None, w_post=None, gate=None, w_pre=None, res_
     out = {"y": y, "residual": r_out, "rstd_post": rstd_post, "rstd_pre": rstd_pre}
     if same and y is None:
         return out
-    ref = _desc(T, H, xs, rs, 0, _dtype_code(dtype, "x"), _dtype_code(rtype, "residual"), _dtype_code(ptype, "w_pre"),
-                kind, res_scale, eps, weight_offset)
+    ref, _ = _desc(dev, T, H, xs, rs, 0, _dtype_code(dtype, "x"), _dtype_code(rtype, "residual"),
+                   _dtype_code(ptype, "w_pre"), kind, res_scale, eps, weight_offset)
     _check(load().molt_residual_norm_fwd(
         ref, xp, rp, _at(w_post, ptype, dev, "w_post"),
         _at(gate, ptype if kind == GATE_CHANNEL else f32 if kind == GATE_TOKEN else dtype, dev, "gate"),
@@ -262,13 +264,12 @@ def residual_norm_bwd(dy, dresidual, x, residual, rstd_pre, rstd_post=None, w_po
     xp, xs = _rows(x, dtype, dev, "x")
     rp, rs = _rows(residual, rtype, dev, "residual")
     dyp, dys = _rows(dy, dtype, dev, "dy")
-    ref = _desc(T, H, xs, rs, dys, _dtype_code(dtype, "x"), _dtype_code(rtype, "residual"), _dtype_code(ptype, "w_pre"),
-                kind, res_scale, 0.0, weight_offset)
-    L = load()
+    ref, nbytes = _desc(dev, T, H, xs, rs, dys, _dtype_code(dtype, "x"), _dtype_code(rtype, "residual"),
+                        _dtype_code(ptype, "w_pre"), kind, res_scale, 0.0, weight_offset)
     ws = workspace
     if ws is None:
-        ws = _workspace(L.molt_residual_norm_bwd_workspace_bytes(ref), dev, "norm_bwd", stream)
-    _check(L.molt_residual_norm_bwd(
+        ws = _workspace(nbytes, dev, "norm_bwd", stream)
+    _check(load().molt_residual_norm_bwd(
         ref, dyp, _at(dresidual, rtype, dev, "dresidual"), xp, rp, _at(rstd_post, f32, dev, "rstd_post"),
         _at(rstd_pre, f32, dev, "rstd_pre"), _at(w_post, ptype, dev, "w_post"),
         _at(gate, ptype if kind == GATE_CHANNEL else f32 if kind == GATE_TOKEN else dtype, dev, "gate"),

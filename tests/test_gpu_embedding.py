@@ -102,6 +102,24 @@ def test_gradient_padding_and_alignment(T, H, V):
     check_grad(np.full(T, 4, dtype=np.int32), V, H, torch.float32, torch.float32, 1.0, 4, 3)   # nothing left
 
 
+@pytest.mark.parametrize("dtype,out", PAIRS)
+@pytest.mark.parametrize("T,H,V", [(1, 76, 3001), (2, 1566, 700), (700, 34, 5000), (5, 33, 4100), (1500, 2052, 60), (40, 2, 100000)])
+def test_rows_of_every_vector_length(T, H, V, dtype, out):
+    """Even rows that are no multiple of eight; few tokens of many, so that rows are zeroed in long runs."""
+    rng = np.random.default_rng(T + H)
+    ids = ids_of("zipf", T, V, rng)
+    for unaligned in (False, True):
+        check_grad(ids, V, H, dtype, out, 1.5, None, 6, unaligned=unaligned)
+    E = torch.from_numpy(rng.normal(size=(V, H))).to(dev(), dtype)
+    x = torch.from_numpy(ids).to(dev())
+    ref = E.double()[x.long()] * 1.5
+    for at in (0, 1, 2, 4):   # rows that start at any element
+        buf = torch.empty(T * H + 8, dtype=out, device=dev())[at:at + T * H].view(T, H)
+        got = molt.token_embedding(E, x, scale=1.5, out_dtype=out, out=buf)
+        assert ((got.double() - ref).abs() <= (U[out] + 2.0**-23) * ref.abs() + TINY[out]).all()
+    assert molt.device_status() == 0
+
+
 @pytest.mark.parametrize("T", [300, 9001])
 def test_tokens_out_of_range(T):
     V, H = 70, 40

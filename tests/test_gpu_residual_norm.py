@@ -171,6 +171,14 @@ def test_many_rows(T, H):
     run_both(make(T, H, BF, F, BF, True, "channel", True, True, 0.0, seed=1), T)
 
 
+@pytest.mark.parametrize("dtype,res,ptype,gate", [(BF, F, BF, "channel"), (HF, HF, F, "full"), (F, F, F, "token"), (BF, BF, BF, "none")])
+@pytest.mark.parametrize("T,H,stride", [(1, 2, 0), (900, 34, 0), (700, 250, 2), (5000, 1566, 0), (300, 514, 6), (40, 2050, 0),
+                                        (9, 5122, 2), (7, 8190, 0), (3, 8198, 0), (3, 16386, 0)])
+def test_rows_of_whole_pairs(T, H, stride, dtype, res, ptype, gate):
+    """Even rows that are no multiple of eight, rows that begin at a pair but not at a vector."""
+    run_both(make(T, H, dtype, res, ptype, True, gate, True, True, 0.0, seed=T + H, stride=stride), T)
+
+
 @pytest.mark.parametrize("stride", [1, 8, 64])
 @pytest.mark.parametrize("H", [64, 1024, 1025])
 def test_strided_rows(H, stride):
