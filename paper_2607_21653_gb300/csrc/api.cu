@@ -438,7 +438,8 @@ int64_t keep_tiles(int64_t T, int64_t H, int64_t V) {
 // what the workspace holds for them: never less for a larger T or V
 int64_t keep_bytes(int64_t T, int64_t H, int64_t V) {
   if (H < kKeepFromH) return 0;
-  return std::min(kKeepBytes, (T + 255) / 256 * ((V + 255) / 256) * kKeepTile);
+  const int64_t tiles = std::min((T + 255) / 256 * ((V + 255) / 256), kKeepBytes / kKeepTile + 1);   // (no overflow)
+  return std::min(kKeepBytes, tiles * kKeepTile);
 }
 
 // Workspace of the cross entropy: the active rows packed, which are the backward's rows

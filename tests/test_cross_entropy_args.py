@@ -56,6 +56,15 @@ def test_workspace_never_shrinks_as_tokens_grow(lib, H):
             assert sizes == sorted(sizes) and sizes[-1] > 0
 
 
+@pytest.mark.parametrize("V", [1, 151936, (1 << 31) - 300])
+def test_workspace_of_the_largest_calls(lib, V):
+    """Sizes whose products pass 64 bits where they are not held back."""
+    Ts = [1 << k for k in range(20, 31)] + [(1 << 31) - 1000]
+    sizes = [lib.molt_cross_entropy_workspace_bytes(T, 1024, V, 1, 2) for T in Ts]
+    assert sizes == sorted(sizes)
+    assert all(T * 1024 * 2 < n < 1 << 62 for T, n in zip(Ts, sizes))
+
+
 def test_binding_refuses():
     h, W, x = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(9, 64, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int32)
     with pytest.raises(ValueError, match="weight"):
