@@ -109,6 +109,37 @@ __global__ void __launch_bounds__(kPackThreads) ce_pack_kernel(
   for (int64_t v = v0 + threadIdx.x; v < v1; v += kPackThreads) reinterpret_cast<uint4*>(h_p)[v] = make_uint4(0, 0, 0, 0);
 }
 
+// A sum as two floats, good to about 48 bits.  FP64 runs at a 64th of the rate here: an
+// addition takes a warp 60 clocks, and the merge kernel's sums in it took half of its time
+// (16200 clocks at T = 512, of which the last block's 7400).
+struct Sum2 {
+  float h = 0.f, l = 0.f;
+  __device__ __forceinline__ void add(float bh, float bl) {
+    const float s = h + bh, b = s - h;
+    float e = (h - (s - b)) + (bh - b) + (l + bl);
+    if (!(fabsf(s) < INFINITY)) e = 0.f;   // infinities stay what they are
+    h = s + e;
+    l = e - (h - s);
+    if (!(fabsf(h) < INFINITY)) l = 0.f;
+  }
+  __device__ __forceinline__ void add(Sum2 o) { add(o.h, o.l); }
+  // a product, whole
+  static __device__ __forceinline__ Sum2 product(float a, float b) {
+    Sum2 p;
+    p.h = a * b;
+    p.l = fabsf(p.h) < INFINITY ? fmaf(a, b, -p.h) : 0.f;
+    return p;
+  }
+  __device__ __forceinline__ void warp_sum() {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const float oh = __shfl_xor_sync(0xffffffffu, h, o), ol = __shfl_xor_sync(0xffffffffu, l, o);
+      add(oh, ol);
+    }
+  }
+  __device__ __forceinline__ double value() const { return static_cast<double>(h) + static_cast<double>(l); }
+};
+
 constexpr int kCeSums = 3;   // w l, -logp, lse^2
 
 // A row's splits merged by kGroups threads: thread (r, g) = (t % kRows, t / kRows) takes
@@ -154,34 +185,36 @@ __device__ __forceinline__ RowStats merge_row(const float4* __restrict__ part, i
 // partial sums; the block that is done last adds all of them in a fixed order.
 template <int kRows, int kGroups, bool kSmooth>
 __global__ void __launch_bounds__(kRows* kGroups) ce_merge_kernel(
-    CeArgs a, int Tcap, int V, int n_parts, int32_t* __restrict__ counts, const int32_t* __restrict__ row_map,
+    CeArgs a, int T, int Tcap, int V, int n_parts, int32_t* __restrict__ counts, const int32_t* __restrict__ row_map,
     const int32_t* __restrict__ tok_p, const float* __restrict__ w_p, const float4* __restrict__ part,
     const float* __restrict__ zx, const float* __restrict__ z_p, float* __restrict__ lse_o, float* __restrict__ coef_o,
-    float* __restrict__ cp_o, float* __restrict__ cu_o, double* __restrict__ red, float* __restrict__ scale_out,
+    float* __restrict__ cp_o, float* __restrict__ cu_o, float2* __restrict__ red, float* __restrict__ scale_out,
     float* __restrict__ loss_out, float* __restrict__ logp_out, float* __restrict__ lse_out,
     molt_ce_stats* __restrict__ stats, unsigned* err) {
   constexpr float kLog2e = 1.4426950408889634f;
   static_assert(kRows <= 32, "a row's lane in the first warp");
+  const int k = blockIdx.x * kRows + threadIdx.x % kRows;
+  // the row's other values beside the count and the splits (a row past the count: any value)
+  const bool lead = threadIdx.x < kRows && k < Tcap;
   const int n = counts[0];
+  const int x = lead ? tok_p[k] : 0, t = lead ? row_map[min(k, T - 1)] : 0;
+  const float z_mma = lead ? zx[k] : 0.f, z_row = lead ? z_p[k] : 0.f, w_row = lead && w_p ? w_p[k] : 1.f;
   const int n_blocks = max(1, (n + kRows - 1) / kRows);
   if (static_cast<int>(blockIdx.x) >= n_blocks) return;
-  const int k = blockIdx.x * kRows + threadIdx.x % kRows;
   const bool act = k < n;
   const RowStats st = merge_row<kRows, kGroups, kSmooth>(part, Tcap, n_parts, k, act);
-  const double D = a.denom > 0.0 ? a.denom : static_cast<double>(n);
   __shared__ bool last;
   if (threadIdx.x < 32) {
-    double s[kCeSums] = {0.0, 0.0, 0.0};
+    Sum2 s[kCeSums];
     if (act && threadIdx.x < kRows) {
-      const int x = tok_p[k];
       const bool in = x >= 0 && x < V;   // else no loss and no gradient
       if (!in) atomicOr(err, kDevErrTokenRange);
       // the target's exact logit in the place of the product's
-      const float z_mma = in ? zx[k] : 0.f, z = in ? z_p[k] : 0.f;
+      const float z = in ? z_row : 0.f;
       const float S = in ? fmaf(ex2_approx((z_mma - st.M) * kLog2e), expm1f(z - z_mma), st.S) : st.S;
       const float lse = st.M + logf(S);
       const float logp = in ? z - lse : 0.f;
-      const float w = in ? (w_p ? w_p[k] : 1.f) : 0.f;
+      const float w = in ? w_row : 0.f;
       float l = -logp;
       if constexpr (kSmooth) {
         // off: the mean over the vocabulary of -log p
@@ -196,20 +229,19 @@ __global__ void __launch_bounds__(kRows* kGroups) ce_merge_kernel(
         cu_o[k] = 0.f;
       }
       lse_o[k] = lse;
-      const int t = row_map[k];
       if (logp_out) logp_out[t] = logp;
       if (lse_out) lse_out[t] = lse;
       if (in) {
-        s[0] = static_cast<double>(w) * static_cast<double>(l);
-        s[1] = -static_cast<double>(logp);
-        s[2] = static_cast<double>(lse) * static_cast<double>(lse);
+        s[0] = Sum2::product(w, l);
+        s[1].h = -logp;
+        s[2] = Sum2::product(lse, lse);
       }
     }
 #pragma unroll
-    for (int i = 0; i < kCeSums; ++i) s[i] = warp_sum<double>(s[i]);
+    for (int i = 0; i < kCeSums; ++i) s[i].warp_sum();
     if (threadIdx.x == 0) {
 #pragma unroll
-      for (int i = 0; i < kCeSums; ++i) red[static_cast<int64_t>(blockIdx.x) * kRedSlots + i] = s[i];
+      for (int i = 0; i < kCeSums; ++i) red[static_cast<int64_t>(blockIdx.x) * kRedSlots + i] = make_float2(s[i].h, s[i].l);
       __threadfence();
       last = atomicAdd(counts + 5, 1) == n_blocks - 1;
     }
@@ -218,33 +250,40 @@ __global__ void __launch_bounds__(kRows* kGroups) ce_merge_kernel(
   if (!last) return;
   __threadfence();
   constexpr int kWarps = kRows * kGroups / 32;
-  __shared__ double tot[kWarps][kCeSums];
-  double s[kCeSums] = {0.0, 0.0, 0.0};
+  __shared__ float2 tot[kWarps][kCeSums];
+  Sum2 s[kCeSums];
   for (int b = threadIdx.x; b < n_blocks; b += kRows * kGroups) {
 #pragma unroll
-    for (int i = 0; i < kCeSums; ++i) s[i] += __ldcg(red + static_cast<int64_t>(b) * kRedSlots + i);
+    for (int i = 0; i < kCeSums; ++i) {
+      const float2 v = __ldcg(red + static_cast<int64_t>(b) * kRedSlots + i);
+      s[i].add(v.x, v.y);
+    }
   }
+  // (warps without a block have nothing to add)
+  const int warps = min(kWarps, (n_blocks + 31) / 32);
+  if (static_cast<int>(threadIdx.x) / 32 < warps) {
 #pragma unroll
-  for (int i = 0; i < kCeSums; ++i) s[i] = warp_sum<double>(s[i]);
-  if (threadIdx.x % 32 == 0) {
-#pragma unroll
-    for (int i = 0; i < kCeSums; ++i) tot[threadIdx.x / 32][i] = s[i];
+    for (int i = 0; i < kCeSums; ++i) {
+      s[i].warp_sum();
+      if (threadIdx.x % 32 == 0) tot[threadIdx.x / 32][i] = make_float2(s[i].h, s[i].l);
+    }
   }
   __syncthreads();
   if (threadIdx.x != 0) return;
-  for (int g = 1; g < kWarps; ++g) {
+  for (int g = 1; g < warps; ++g) {
 #pragma unroll
-    for (int i = 0; i < kCeSums; ++i) s[i] += tot[g][i];
+    for (int i = 0; i < kCeSums; ++i) s[i].add(tot[g][i].x, tot[g][i].y);
   }
+  const double D = a.denom > 0.0 ? a.denom : static_cast<double>(n);
   if (!(D > 0.0)) atomicOr(err, kDevErrZeroDenom);
-  const double loss = D > 0.0 ? s[0] / D : 0.0;
+  const double inv_D = D > 0.0 ? 1.0 / D : 0.0, loss = D > 0.0 ? s[0].value() * inv_D : 0.0;
   *loss_out = static_cast<float>(loss);
-  *scale_out = D > 0.0 ? static_cast<float>(1.0 / D) : 0.f;
+  *scale_out = static_cast<float>(inv_D);
   if (stats) {
     stats->denom = D;
     stats->loss = loss;
-    stats->sum_nll = s[1];
-    stats->sum_lse_sq = s[2];
+    stats->sum_nll = s[1].value();
+    stats->sum_lse_sq = s[2].value();
     stats->n_active = n;
   }
 }
@@ -277,9 +316,9 @@ cudaError_t launch_ce_merge(const CeArgs& a, bool smooth, int T, int Tcap, int V
   auto* k = few ? (smooth ? &ce_merge_kernel<8, 64, true> : &ce_merge_kernel<8, 64, false>)
                 : (smooth ? &ce_merge_kernel<32, 8, true> : &ce_merge_kernel<32, 8, false>);
   const int rows = few ? 8 : 32;
-  k<<<(T + rows - 1) / rows, few ? 512 : 256, 0, s>>>(a, Tcap, V, n_parts, ws.counts, ws.row_map, ws.tok_p,
+  k<<<(T + rows - 1) / rows, few ? 512 : 256, 0, s>>>(a, T, Tcap, V, n_parts, ws.counts, ws.row_map, ws.tok_p,
                                                       a.weight ? ws.b_p : nullptr, ws.part, ws.zx, ws.adv_p, ws.lse, ws.coef,
-                                                      ws.ecoef, ws.mu, ws.red, ws.scale, loss_out, logp_out, lse_out, stats, err);
+                                                      ws.ecoef, ws.mu, reinterpret_cast<float2*>(ws.red), ws.scale, loss_out, logp_out, lse_out, stats, err);
   return cudaGetLastError();
 }
 
