@@ -515,8 +515,10 @@ molt_status molt_residual_norm_bwd(const molt_norm_desc* desc, const void* dy, c
  * MOLT_DEV_ZERO_DENOM is set.
  * Outputs: loss_out (device fp32 scalar); optional (may be NULL) logp_out [T] =
  * z_{t,x_t} - lse_t and lse_out [T], 0 on ignored rows, and stats_out (device
- * molt_ce_stats).  dW_out of dW_dtype: MOLT_FP32, or MOLT_BF16 (summed in fp32 in the
- * workspace and rounded once); accumulate_dW = 1 adds to an fp32 dW.
+ * molt_ce_stats).  dW_out of dW_dtype: MOLT_FP32, or MOLT_BF16 (summed in fp32 and rounded
+ * once); accumulate_dW = 1 adds to an fp32 dW.  The contributions of several pieces of the
+ * vocabulary to dhidden, and of the tokens to dW, are added as they come, so the last bits of
+ * the gradients can differ from run to run; the forward's outputs do not.
  */
 typedef struct {
   int64_t ignore_index;   /* rows with this target are left out; a value that no int32 has: none are */

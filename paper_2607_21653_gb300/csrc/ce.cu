@@ -236,7 +236,8 @@ __global__ void __launch_bounds__(kRows* kGroups) ce_merge_kernel(
       if (!in) atomicOr(err, kDevErrTokenRange);
       // the target's exact logit in the place of the product's
       const float z = in ? z_row : 0.f;
-      const float S = in ? fmaf(ex2_approx((z_mma - st.M) * kLog2e), expm1f(z - z_mma), st.S) : st.S;
+      const float dz = z - z_mma;   // (NaN where both are infinite)
+      const float S = in && fabsf(dz) < INFINITY ? fmaf(ex2_approx((z_mma - st.M) * kLog2e), expm1f(dz), st.S) : st.S;
       const float lse = st.M + logf(S);
       const float logp = in ? z - lse : 0.f;
       const float w = in ? w_row : 0.f;

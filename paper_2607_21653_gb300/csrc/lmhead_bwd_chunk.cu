@@ -46,9 +46,8 @@
 //
 // The cross entropy's forward may have kept the logits in 16 bits (kKeepTile): a Z tile
 // then has no products, its epilogue loads them, a quarter of the columns ahead, and two
-// products are left of three.  Its own share of the time is small (a step's Z tiles spread
-// between its dW tiles took up to 17 % more: the run of them is over sooner than the
-// tiles in flight).
+// products are left of three.  (A step's Z tiles spread among its other tiles, over all of the
+// step or parts of it: 0 to 17 % slower.)
 //
 // What bounds it, measured on T = 16384, H = 4096, V = 151936 (61.2 TFLOP in
 // three products): 36.8 ms, 1.66 PFLOP/s, at the board's power cap (1.49 GHz of

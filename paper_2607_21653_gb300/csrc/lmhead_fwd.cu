@@ -1,7 +1,8 @@
 // Forward pass of the LM head with a fused online log-softmax (Sec. 4.5: the
 // actor's recomputed log-probabilities of the generated tokens, plus entropy).
 //
-// z = h W^T is never written to global memory.  Each work unit is one tile of
+// z = h W^T is not written to global memory in fp32 (for the cross entropy's backward it is
+// kept in 16 bits, see kKeepTile).  Each work unit is one tile of
 // 256 packed token rows times one contiguous split of the vocabulary.  For
 // every 256-column vocab tile of the split, the tensor cores of a CTA pair
 // accumulate the 256 x 256 fp32 logit tile in TMEM (128 rows in each CTA; K = H

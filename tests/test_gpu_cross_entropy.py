@@ -125,6 +125,27 @@ def test_logits_far_apart(H, spread):
         assert_grad_close(out[k].double().cpu().numpy(), ref[k].cpu().numpy(), k)
 
 
+def test_a_column_of_minus_infinity():
+    """A column whose logit is -inf in every row: no part of the others' sums; a row that has
+    it as its target has logp -inf and makes the loss +inf."""
+    h, W, x, _ = make(300, 128, 700, seed=14, known=False)
+    h[:, 5] = h[:, 5].abs() + 0.1
+    W[7, 5] = float("-inf")
+    x[x == 7] = 8
+    keep = torch.arange(700, device=h.device) != 7
+    xr = torch.where(x > 7, x - 1, x)
+    for targets, bad in ((x, False), (torch.where(torch.arange(300, device=h.device) == 17, 7, x).to(torch.int32), True)):
+        out = molt.cross_entropy_fwd(h, W, targets)
+        ref = reference(h, W[keep], xr)
+        rows = torch.arange(300, device=h.device) != 17
+        assert (out["logp"].double() - ref["logp"])[rows].abs().max() <= LOGP_ATOL
+        assert (out["lse"].double() - ref["lse"]).abs().max() <= LOGP_ATOL
+        if bad:
+            assert out["logp"][17] == float("-inf") and out["loss"][0] == float("inf")
+        else:
+            assert abs(float(out["loss"]) - float(ref["loss"])) <= LOSS_RTOL * ref["size"]
+
+
 @pytest.mark.parametrize("value", [float("nan"), float("inf")])
 def test_kept_logits_show_a_bad_row(value):
     """As without keeping: the row's dhidden and dW are NaN, the other rows' dhidden is not."""
