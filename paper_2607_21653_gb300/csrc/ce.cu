@@ -12,11 +12,13 @@
 // Two things make it more exact than its products.  The tensor cores add in fp32 but cut
 // off what does not fit, 256 times at H = 4096: the target's logit, which often is by far
 // the largest, comes out 1e-6 too small.  So its logit is formed again in fp32, here
-// where the rows are packed, and replaces the product's in the row's sum.  And the
-// gradient is rounded to bf16 without the factor 1 / D: a target that the model does not
-// expect then is -1, which bf16 holds exactly, where -1 / D would be off by up to 0.4 %
-// for all of them alike; the factor multiplies the products' sums.  (Relative errors of
-// logp and of dW before: 1.6e-6 and up to 2.9e-3.)
+// where the rows are packed, and replaces the product's in the row's sum and in the
+// gradient: the target's entry of dL/dz is finished where the rows are merged, from what
+// the row's other columns sum to, and the backward's tiles take it as it is (see finish_row).
+// And the gradient is rounded to bf16 without the factor 1 / D: a target that the model
+// does not expect then is -1, which bf16 holds exactly, where -1 / D would be off by up to
+// 0.4 % for all of them alike; the factor multiplies the products' sums.  (Relative errors
+// of logp and of dW before: 1.6e-6 and up to 2.9e-3.)
 #include <climits>
 #include <cstdint>
 #include <cuda_runtime.h>
@@ -166,13 +168,13 @@ struct Sum2 {
 };
 
 constexpr int kCeSums = 3;   // w l, -logp, lse^2
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // A row's splits merged by kGroups threads: thread (r, g) = (t % kRows, t / kRows) takes
 // every kGroups-th, eight loads at a time.  Valid in group 0; every thread calls it.
 template <int kRows, int kGroups, bool kSumZ>
 __device__ __forceinline__ RowStats merge_row(const float4* __restrict__ part, int64_t stride, int n_parts, int k, bool act) {
   __shared__ float4 sh[kGroups][kRows];
-  constexpr float kLog2e = 1.4426950408889634f;
   const int r = threadIdx.x % kRows, g = threadIdx.x / kRows;
   RowStats st{-INFINITY, 0.f, 0.f};
   auto add = [&](float m, float s, float q) {
@@ -191,7 +193,14 @@ __device__ __forceinline__ RowStats merge_row(const float4* __restrict__ part, i
       p[i] = s < n_parts ? part[s * stride + k] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) add(p[i].x, p[i].y, p[i].z);
+    for (int i = 0; i < 8; ++i) {
+      // The forward's exponentials are 2^(z log2e - mL) with mL = m log2e rounded to fp32: all of
+      // them 2^rho too large, rho up to 1e-6 at m = 20, which is a loss of 1e-6 too much
+      // or too little.  s takes 2^-rho = 1 - a + a^2 / 2 (rho is small wherever logits mean anything).
+      const float rho = fmaf(p[i].x, kLog2e, -__fmul_rn(p[i].x, kLog2e));
+      const float a = kLn2 * fminf(fmaxf(rho, -0.01f), 0.01f);
+      add(p[i].x, fmaf(p[i].y, a * fmaf(0.5f, a, -1.f), p[i].y), p[i].z);
+    }
   }
   // groups in pairs, halves of the rest at a time
 #pragma unroll
@@ -206,17 +215,35 @@ __device__ __forceinline__ RowStats merge_row(const float4* __restrict__ part, i
   return st;
 }
 
+// A row's lse and log p of its target, whose logit is z where the products had z_mma:
+// with R the others' sum over e^z, log p = -log(1 + R), without lse's rounding (2^-20 at
+// z = 20, which is all of the loss of a row that the model predicts that well) and without a
+// difference of logits.  What R is off by is the sum's rounding and that of the
+// exponentials, a few 2^-24.
+struct RowEnd {
+  float lse, logp;
+};
+__device__ __forceinline__ RowEnd finish_row(const RowStats& st, float z, float z_mma) {
+  float rest = st.S - ex2_approx((z_mma - st.M) * kLog2e);
+  if (rest < 0.f) rest = 0.f;   // (rounding.  A NaN passes)
+  if (z > st.M - 1.f) {
+    const float l = log1pf(rest * ex2_approx((st.M - z) * kLog2e));
+    return {z + l, -l};
+  }
+  const float d = z - st.M, l = logf(rest + ex2_approx(d * kLog2e));
+  return {st.M + l, d - l};
+}
+
 // One block per kRows packed rows: the rows' lse, losses and backward values, and their
 // partial sums; the block that is done last adds all of them in a fixed order.
 template <int kRows, int kGroups, bool kSmooth>
 __global__ void __launch_bounds__(kRows* kGroups) ce_merge_kernel(
     CeArgs a, int T, int Tcap, int V, int n_parts, int32_t* __restrict__ counts, const int32_t* __restrict__ row_map,
     const int32_t* __restrict__ tok_p, const float* __restrict__ w_p, const float4* __restrict__ part,
-    const float* __restrict__ zx, const float* __restrict__ z_p, float* __restrict__ lse_o, float* __restrict__ coef_o,
+    const float* __restrict__ zx, const float* __restrict__ z_p, float* __restrict__ lse_o, float* __restrict__ target_o,
     float* __restrict__ cp_o, float* __restrict__ cu_o, float2* __restrict__ red, float* __restrict__ scale_out,
     float* __restrict__ loss_out, float* __restrict__ logp_out, float* __restrict__ lse_out,
     molt_ce_stats* __restrict__ stats, unsigned* err) {
-  constexpr float kLog2e = 1.4426950408889634f;
   static_assert(kRows <= 32, "a row's lane in the first warp");
   const int k = blockIdx.x * kRows + threadIdx.x % kRows;
   // the row's other values beside the count and the splits (a row past the count: any value)
@@ -234,26 +261,24 @@ __global__ void __launch_bounds__(kRows* kGroups) ce_merge_kernel(
     if (act && threadIdx.x < kRows) {
       const bool in = x >= 0 && x < V;   // else no loss and no gradient
       if (!in) atomicOr(err, kDevErrTokenRange);
-      // the target's exact logit in the place of the product's
-      const float z = in ? z_row : 0.f;
-      const float dz = z - z_mma;   // (NaN where both are infinite)
-      const float S = in && fabsf(dz) < INFINITY ? fmaf(ex2_approx((z_mma - st.M) * kLog2e), expm1f(dz), st.S) : st.S;
-      const float lse = st.M + logf(S);
-      const float logp = in ? z - lse : 0.f;
+      // (no target: the sum as it is)
+      const RowEnd end = in ? finish_row(st, z_row, z_mma) : RowEnd{st.M + logf(st.S), 0.f};
+      const float lse = end.lse, logp = end.logp;
       const float w = in ? w_row : 0.f;
-      float l = -logp;
+      float l = -logp, minus = expm1f(logp);   // minus: p - 1
       if constexpr (kSmooth) {
         // off: the mean over the vocabulary of -log p
         const float off = a.smoothing != 0.f ? lse - st.Q / static_cast<float>(V) : l;
         l = fmaf(a.z_loss * lse, lse, fmaf(a.smoothing, off - l, l));
-        coef_o[k] = w * (1.f - a.smoothing);
-        cp_o[k] = w * fmaf(2.f * a.z_loss, lse, 1.f);
-        cu_o[k] = w * (a.smoothing / static_cast<float>(V));
+        const float e_V = a.smoothing / static_cast<float>(V), zl = 2.f * a.z_loss;
+        minus += fmaf(zl * lse, 1.f + minus, a.smoothing - e_V);
+        cp_o[k] = w * fmaf(zl, lse, 1.f);
+        cu_o[k] = w * e_V;
       } else {
-        coef_o[k] = w;
         cp_o[k] = w;
         cu_o[k] = 0.f;
       }
+      target_o[k] = w * minus;
       lse_o[k] = lse;
       if (logp_out) logp_out[t] = logp;
       if (lse_out) lse_out[t] = lse;

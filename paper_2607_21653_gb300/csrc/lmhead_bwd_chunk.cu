@@ -643,8 +643,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int j = 0; j < 32; j += 2) {
               float g0 = p_of(j), g1 = p_of(j + 1);
-              if (j == lxc) g0 -= coef;
-              if (j + 1 == lxc) g1 -= coef;
+              if (j == lxc) g0 = kForm == kGradScaled ? coef : g0 - coef;
+              if (j + 1 == lxc) g1 = kForm == kGradScaled ? coef : g1 - coef;
               if (j >= nv) g0 = 0.f;
               if (j + 1 >= nv) g1 = 0.f;
               w[j / 2] = pack_bf16x2(g0, g1);

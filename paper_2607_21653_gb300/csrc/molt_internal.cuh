@@ -30,7 +30,7 @@ struct Workspace {
   float* zx;            // [Tcap] target logit
   float* lse;           // [Tcap]
   float* scale;         // [1] cross entropy: 1 / D
-  float* coef;          // [Tcap] m c / D
+  float* coef;          // [Tcap] m c / D; cross entropy: the target's entry of dL/dz times D
   int32_t* tile_list;   // [Tcap/128]
   double* red;          // [Tcap/kRedRows, kRedSlots] partial sums of kRedRows packed rows
   float* dh32;          // [Tcap, H] fp32 dhidden accumulator, by backward row (loss call only)
@@ -115,7 +115,7 @@ constexpr int kChunkCtlHead = 64;    // control words before the per-chunk count
 // g of one logit z of a row, p = e^(z - lse):
 constexpr int kGradPlain = 0;     // coef (p - [target])
 constexpr int kGradEntropy = 1;   // coef (p - [target]) + ecoef p (z - mu)
-constexpr int kGradScaled = 2;    // (ecoef p - mu - coef [target]) s, the factor s = *scale on the products' sums
+constexpr int kGradScaled = 2;    // (target ? coef : ecoef p - mu) s, the factor s = *scale on the products' sums
 struct ChunkMaps {                   // bf16 maps have 64-column (128-byte) boxes
   CUtensorMap h128, w128;            // packed hidden rows and W, 128 rows
   CUtensorMap g128, g32;             // chunk buffers: 64-column panels of token rows; g32 stores
