@@ -499,7 +499,8 @@ molt_status molt_residual_norm_bwd(const molt_norm_desc* desc, const void* dy, c
  * Softmax cross entropy over the LM head, forward and backward, without keeping the
  * logits in 32 bits (the backward forms them again in pieces of the vocabulary; from H =
  * 640 on the forward keeps up to 4 GB of them in the workspace, as 16-bit steps of 2^-10
- * in log2 below their row's running maximum, an error of 2^-11 ln 2 in the softmax):
+ * in log2 below their row's running maximum: half a step, a relative error of 2^-11 ln 2 in
+ * the gradient's softmax, beside that of the maximum's and lse's rounding to fp32):
  *   z_tv = sum_k hidden[t,k] W[v,k];  lse_t = log sum_v exp z_tv;  x_t = targets[t]
  *   l_t  = lse_t - (1 - e) z_{t,x_t} - e mean_v z_tv + c lse_t^2
  *   loss = sum_t w_t l_t / D    over the active rows, targets[t] != ignore_index

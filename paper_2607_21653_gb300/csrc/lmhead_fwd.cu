@@ -105,16 +105,18 @@ struct Stats {
 };
 
 // Keeps 32 logits of a row under the reference mL = log2 e times a maximum that none of
-// them exceeds; `slab` is the lane's first vector for them, `ref` its reference.
+// them exceeds; `slab` is the lane's first vector for them, `ref` its reference.  The
+// difference to the reference comes first, so that what is rounded to a whole step is the
+// step count alone: half a step.  (With the reference scaled and rounded to steps beforehand an
+// instruction less, but up to a whole step, half of it shared by the row's 32 columns.)
 __device__ __forceinline__ void keep_logits(const float (&v)[32], float mL, uint8_t* slab, uint8_t* ref) {
-  const float base = fmaf(mL, kKeepStep, kKeepZero);
   uint32_t w[16];
 #pragma unroll
   for (int j = 0; j < 32; j += 2) {
     uint32_t k[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const float t = fmaf(v[j + i], -kLog2e * kKeepStep, base);
+      const float t = fmaf(fmaf(v[j + i], kLog2e, -mL), -kKeepStep, kKeepZero);
       k[i] = __float_as_uint(fmaxf(fminf(t, kKeepZero + 65535.f), kKeepZero));
     }
     w[j / 2] = __byte_perm(k[0], k[1], 0x5410);
