@@ -462,7 +462,7 @@ molt_status molt_token_embedding_bwd(const void* dout, int dout_dtype, const int
 #define MOLT_GATE_TOKEN 2     /* gate [T] fp32 */
 #define MOLT_GATE_FULL 3      /* gate [T,H] of dtype */
 typedef struct {
-  int64_t T, H;               /* T >= 0, 1 <= H <= 65536 */
+  int64_t T, H;               /* 0 <= T <= 2^31 - 2^17, 1 <= H <= 65536 */
   int64_t x_stride, residual_stride, dy_stride;   /* elements between rows of x, of the residual
                                  stream read, and of dy; 0: H (all other rows lie side by side) */
   int dtype;                  /* molt_dtype of x, y and their gradients, and of a full gate */

@@ -57,11 +57,16 @@ molt_status cuda_fail(cudaError_t e, const char* what) {
 bool known_type(int dt) { return dt == MOLT_BF16 || dt == MOLT_FP16 || dt == MOLT_FP32; }
 bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
+// Rows are counted in 32 bits and the persistent kernels go on by a grid's rows, at most
+// kMaxBlocksPerSM * kRingRows to an SM, past the last one: 2^17 are those of 4096 SMs.
+constexpr int64_t kMaxRows = (int64_t(1) << 31) - (int64_t(1) << 17);
+static_assert(kMaxBlocksPerSM * kRingRows * 4096 <= 1 << 17);
+
 molt_status check_desc(const molt_norm_desc* d) {
   if (!d) return fail(MOLT_ERR_INVALID_ARG, "desc is NULL");
   if (d->T < 0 || d->H < 1) return fail(MOLT_ERR_INVALID_ARG, "sizes must satisfy T >= 0, H >= 1");
-  if (d->T >= (int64_t(1) << 31) || d->H > 65536)
-    return fail(MOLT_ERR_UNSUPPORTED_SHAPE, "T must be below 2^31 and H at most 65536");
+  if (d->T > kMaxRows || d->H > 65536)
+    return fail(MOLT_ERR_UNSUPPORTED_SHAPE, "T must be at most 2^31 - 2^17 and H at most 65536");
   if (!known_type(d->dtype) || !known_type(d->residual_dtype) || !known_type(d->param_dtype))
     return fail(MOLT_ERR_INVALID_ARG, "unknown element type");
   if (d->residual_dtype != d->dtype && d->residual_dtype != MOLT_FP32)
