@@ -280,13 +280,15 @@ __device__ __forceinline__ void ring_fetch(Stream& s, uint8_t* stage, uint32_t b
   if constexpr (kV != 8) {
     const uint8_t* w0 = reinterpret_cast<const uint8_t*>(reinterpret_cast<uintptr_t>(src) & ~uintptr_t(15));
     const uint8_t* w1 = reinterpret_cast<const uint8_t*>((reinterpret_cast<uintptr_t>(end) + 15) & ~uintptr_t(15));
+    __syncwarp();   // a row of one warp: all lanes have read what the stage held
     if (n > 0) {
       // words that reach outside the matrix: their bytes inside it, two at a time (elements
-      // are of two or four bytes)
+      // are of two or four bytes), ordered before the copies that will fill the stage again
       auto edge = [&](const uint8_t* w) {
         for (int b = 0; b < 16; b += 2)
           if (w + b >= s.lo && w + b < s.hi)
             *reinterpret_cast<uint16_t*>(dst + (w - w0) + b) = *reinterpret_cast<const uint16_t*>(w + b);
+        fence_proxy_async_smem();
       };
       const uint8_t* first = w0;
       if (first < s.lo) {
