@@ -62,7 +62,8 @@ class Policy:
             y = s["y"]
             h = torch.relu(y @ w[f"A{i}"])
             o = h @ w[f"B{i}"]
-            s = molt.residual_norm_fwd(o, s["residual"], w_post=w[f"post{i}"], gate=w[f"gate{i}"], w_pre=w[f"norm{i + 1}"])
+            s = molt.residual_norm_fwd(o, s["residual"], w_post=w[f"post{i}"], gate=w[f"gate{i}"], w_pre=w[f"norm{i + 1}"],
+                                       gate_kind="channel")
             kept.append((o, y, h, s))
         return s["y"], kept
 
@@ -75,7 +76,7 @@ class Policy:
         for i in reversed(range(self.blocks)):
             o, y, h, s = kept[i + 1]
             b = molt.residual_norm_bwd(dy, dr, o, s["residual"], s["rstd_pre"], s["rstd_post"], w_post=w[f"post{i}"],
-                                       gate=w[f"gate{i}"], w_pre=w[f"norm{i + 1}"])
+                                       gate=w[f"gate{i}"], w_pre=w[f"norm{i + 1}"], gate_kind="channel")
             do, dr = b["dx"], b["dresidual"]
             grads[f"post{i}"], grads[f"gate{i}"], grads[f"norm{i + 1}"] = b["dw_post"], b["dgate"], b["dw_pre"]
             grads[f"B{i}"] = h.t() @ do

@@ -142,12 +142,26 @@ def _desc(device, *values):
     return entry
 
 
-def _gate_kind(gate, T, H):
-    """The gate's kind by its shape: [H], [T, 1] or [T] (where T is not H; then [T, 1] is needed), [T, H]."""
+_KINDS = {"channel": GATE_CHANNEL, "token": GATE_TOKEN, "full": GATE_FULL}
+
+
+def _gate_kind(gate, T, H, stated=None):
+    """The gate's kind, by its shape or as stated: [H], [T, 1] or [T], [T, H].  A float32 vector
+    of T = H could be a gate per channel or per token: its kind has to be stated."""
     if gate is None:
+        if stated is not None:
+            raise ValueError(f"gate_kind is {stated!r}, but there is no gate")
         return GATE_NONE
     shape = gate.shape
+    if stated is not None:
+        shapes = {"channel": ((H,),), "token": ((T, 1), (T,)), "full": ((T, H),)}.get(stated, ())
+        if shape not in shapes:
+            raise ValueError(f"a gate of shape {list(shape)} is not of kind {stated!r} (channel [{H}], token [{T}, 1], full [{T}, {H}])")
+        return _KINDS[stated]
     if shape == (H,):
+        if T == H > 1 and gate.dtype is _torch().float32:
+            raise ValueError(f"a gate of shape [{H}] with {T} rows could be of a channel or of a token: state its "
+                             "gate_kind, or give a token's as [T, 1]")
         return GATE_CHANNEL
     if shape == (T,) or shape == (T, 1):
         return GATE_TOKEN
@@ -173,19 +187,20 @@ def _param_type(dtype, H, w_post, w_pre, gate):
 
 
 def residual_norm_fwd(x, residual=None, w_post=None, gate=None, w_pre=None, res_scale=1.0, eps=1e-6, weight_offset=0.0,
-                      residual_dtype=None, want_stats=True, stream=None):
+                      residual_dtype=None, want_stats=True, stream=None, gate_kind=None):
     """A block's output x into the residual stream, and out of it again
     (molt_residual_norm_fwd):
         u = x, or RMS norm of x with weight w_post;  r' = res_scale residual + gate u;
         y = RMS norm of r' with weight w_pre.
-    x, residual [T, H] (rows may be strided); gate [H], [T, 1] (fp32), [T, H] or None;
-    w_post, w_pre [H] or None.  residual_dtype (without a residual: x's type or
-    float32) is the stream's type.  Returns dict(y, residual = r', rstd_post,
-    rstd_pre); what a call has no use for is None, and r' is x itself where nothing
-    changes it (no residual, norm or gate)."""
+    x, residual [T, H] (rows may be strided); w_post, w_pre [H] or None; gate [H], [T, 1] or
+    [T] (fp32), [T, H] or None.  gate_kind = "channel", "token" or "full" states what the
+    gate is; a float32 vector needs it where T = H, and a program whose T changes gives it
+    always.  residual_dtype (without a residual: x's type or float32) is the stream's
+    type.  Returns dict(y, residual = r', rstd_post, rstd_pre); what a call has no use for
+    is None, and r' is x itself where nothing changes it (no residual, norm or gate)."""
     torch = _torch()
     T, H = x.shape
-    kind = _gate_kind(gate, T, H)
+    kind = _gate_kind(gate, T, H, gate_kind)
     dtype, f32 = x.dtype, torch.float32
     if residual is not None:
         _shaped(residual, (T, H), "residual")
@@ -219,17 +234,17 @@ def residual_norm_fwd(x, residual=None, w_post=None, gate=None, w_pre=None, res_
 
 def residual_norm_bwd(dy, dresidual, x, residual, rstd_pre, rstd_post=None, w_post=None, gate=None, w_pre=None,
                       res_scale=1.0, weight_offset=0.0, want_dresidual=True, dw_post=None, dgate=None, dw_pre=None,
-                      accumulate=False, stream=None, workspace=None):
+                      accumulate=False, stream=None, workspace=None, gate_kind=None):
     """Gradients of residual_norm_fwd (molt_residual_norm_bwd) from dy (the gradient
     of y, None without w_pre) and dresidual (that of r' from later blocks, or None).
-    x, gate and weights as there; residual is its r', rstd_* its statistics.  Returns
+    x, gate, gate_kind and weights as there; residual is its r', rstd_* its statistics.  Returns
     dict(dx, dresidual, dw_post, dgate, dw_pre): weights' gradients fp32 [H], the
     gate's fp32 [H] or [T], or [T, H] of x's type.  Buffers given for dw_post, dw_pre
     and a channel gate's dgate are written, with accumulate=True added to."""
     torch = _torch()
     T, H = x.shape
     dtype, f32 = x.dtype, torch.float32
-    kind = _gate_kind(gate, T, H)
+    kind = _gate_kind(gate, T, H, gate_kind)
     if residual is None and dresidual is None:
         raise ValueError("one of residual and dresidual is needed")
     rtype = (residual if residual is not None else dresidual).dtype
