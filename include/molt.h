@@ -473,7 +473,8 @@ typedef struct {
 } molt_norm_desc;
 
 /* rstd_post [T], rstd_pre [T] fp32: what the backward needs of the row sums, each
- * NULL where it is not wanted (serving).  residual_out may be the residual itself. */
+ * NULL where it is not wanted (serving).  residual_out may be the residual itself where
+ * that one's rows lie side by side. */
 molt_status molt_residual_norm_fwd(const molt_norm_desc* desc, const void* x, const void* residual, const void* w_post,
                                    const void* gate, const void* w_pre, void* y, void* residual_out, float* rstd_post,
                                    float* rstd_pre, cudaStream_t stream);

@@ -198,6 +198,8 @@ molt_status molt_residual_norm_fwd(const molt_norm_desc* desc, const void* x, co
   if (!x || (desc->gate_kind != MOLT_GATE_NONE && !gate)) return fail(MOLT_ERR_INVALID_ARG, "null pointer");
   if ((w_pre == nullptr) != (y == nullptr)) return fail(MOLT_ERR_INVALID_ARG, "w_pre and y come together");
   if (!y && !residual_out) return fail(MOLT_ERR_INVALID_ARG, "neither y nor residual_out is wanted");
+  if (residual && residual == residual_out && desc->T > 1 && desc->residual_stride != 0 && desc->residual_stride != desc->H)
+    return fail(MOLT_ERR_INVALID_ARG, "a residual is updated in place where its rows lie side by side");
   const int gate_type = desc->gate_kind == MOLT_GATE_TOKEN     ? MOLT_FP32
                         : desc->gate_kind == MOLT_GATE_CHANNEL ? desc->param_dtype
                                                                : desc->dtype;

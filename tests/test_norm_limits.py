@@ -40,3 +40,18 @@ def test_rows_at_the_limit(lib):
     st = lib.molt_residual_norm_fwd(d, None, FAKE, None, None, FAKE, FAKE, FAKE, None, None, None)
     assert molt.STATUS[st] == "MOLT_ERR_INVALID_ARG"
     assert lib.molt_residual_norm_bwd_workspace_bytes(d) > 0
+
+
+def test_in_place_residual_needs_rows_side_by_side(lib):
+    """r' is written with its rows side by side: over a residual whose rows are not, it would
+    overwrite rows that are still to be read."""
+    def call(T, stride, r, r_out):
+        d = S.NormDesc(T, 64, 0, stride, 0, 0, 0, 0, S.GATE_NONE, 1.0, 1e-6, 0.0)
+        return molt.STATUS[lib.molt_residual_norm_fwd(ctypes.byref(d), FAKE, r, None, None, None, None, r_out, None, None, None)]
+
+    n0 = lib.molt_kernel_launches()
+    assert call(4, 72, FAKE, FAKE) == "MOLT_ERR_INVALID_ARG"
+    assert b"in place" in lib.molt_last_error()
+    assert lib.molt_kernel_launches() == n0
+    # no rows: nothing to overwrite
+    assert call(0, 72, FAKE, FAKE) == "MOLT_OK"
