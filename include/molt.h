@@ -497,11 +497,12 @@ molt_status molt_residual_norm_bwd(const molt_norm_desc* desc, const void* dy, c
                                    void* workspace, size_t workspace_bytes, cudaStream_t stream);
 
 /*
- * Softmax cross entropy over the LM head, forward and backward, without keeping the
- * logits in 32 bits (the backward forms them again in pieces of the vocabulary; from H =
- * 640 on the forward keeps up to 4 GB of them in the workspace, as 16-bit steps of 2^-10
- * in log2 below their row's running maximum: half a step, a relative error of 2^-11 ln 2 in
- * the gradient's softmax, beside that of the maximum's and lse's rounding to fp32):
+ * Softmax cross entropy over the LM head, forward and backward, without logits in 32 bits.
+ * The backward forms them again in pieces of the vocabulary; or, from H = 640 on, the
+ * forward keeps them in the workspace, up to max_kept_bytes (4 GB unless told otherwise;
+ * about 2.1 bytes a logit), as 16-bit steps of 2^-10 in log2 below their row's running
+ * maximum: half a step, a relative error of 2^-11 ln 2 in the gradient's softmax, beside that
+ * of the maximum's and lse's rounding to fp32.  The forward alone keeps none.
  *   z_tv = sum_k hidden[t,k] W[v,k];  lse_t = log sum_v exp z_tv;  x_t = targets[t]
  *   l_t  = lse_t - (1 - e) z_{t,x_t} - e mean_v z_tv + c lse_t^2
  *   loss = sum_t w_t l_t / D    over the active rows, targets[t] != ignore_index
@@ -526,7 +527,9 @@ typedef struct {
   int64_t ignore_index;   /* rows with this target are left out; a value that no int32 has: none are */
   float label_smoothing;  /* in [0, 1] */
   float z_loss;           /* >= 0 */
-} molt_ce_options;        /* NULL: { -100, 0, 0 } */
+  int64_t max_kept_bytes; /* of logits in the workspace between forward and backward; 0: 4 GB, which
+                             is also the most; negative: none, every logit is formed twice */
+} molt_ce_options;        /* NULL: { -100, 0, 0, 0 } */
 typedef struct {
   double denom;           /* D actually used */
   double loss;            /* sum w l / D */
@@ -535,6 +538,9 @@ typedef struct {
   int64_t n_active;
 } molt_ce_stats;
 size_t molt_cross_entropy_workspace_bytes(int64_t T, int64_t H, int64_t V, int with_backward, int dW_dtype);
+/* the same for a call with these options (NULL: as above) */
+size_t molt_cross_entropy_workspace_bytes_ex(int64_t T, int64_t H, int64_t V, int with_backward, int dW_dtype,
+                                             const molt_ce_options* opts);
 molt_status molt_cross_entropy_fwd(const uint16_t* hidden, const uint16_t* W, const int32_t* targets,
                                    const float* token_weight, int64_t T, int64_t H, int64_t V, double denom,
                                    const molt_ce_options* opts, float* loss_out, float* logp_out, float* lse_out,

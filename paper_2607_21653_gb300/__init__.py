@@ -149,6 +149,7 @@ def load():
         "molt_residual_norm_bwd_workspace_bytes": (SZ, [P]),
         "molt_residual_norm_bwd": (I32, [P] * 15 + [I32, P, SZ, P]),
         "molt_cross_entropy_workspace_bytes": (SZ, [I64, I64, I64, I32, I32]),
+        "molt_cross_entropy_workspace_bytes_ex": (SZ, [I64, I64, I64, I32, I32, P]),
         "molt_cross_entropy_fwd": (I32, [P, P, P, P, I64, I64, I64, D, P, P, P, P, P, P, SZ, P]),
         "molt_cross_entropy_fwd_bwd": (I32, [P, P, P, P, I64, I64, I64, D, P, P, P, P, I32, I32, P, P, P, P, SZ, P]),
     }

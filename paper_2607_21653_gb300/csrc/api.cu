@@ -424,27 +424,32 @@ Layout vp_backward_layout(int64_t T, int64_t H, int64_t V) {
 // The cross entropy's forward keeps the logits of its first so many token tiles in 16 bits
 // (kKeepTile), and the backward needs no product to form them again: 2.1 bytes written and
 // read for 2 H operations, under the products of other tiles.  Kept and formed again (ms,
-// whole calls): H = 4096 T = 8192 (30 % ignored), V = 151936 14.0 and 17.9, T = 1031 2.9 and
-// 3.7; H = 2048 T = 8192 (20 %), V = 32000 1.83 and 2.20; H = 1024 T = 16000, V = 32000 2.34
-// and 2.77; H = 640 T = 16000, V = 32000 1.76 and 1.87, T = 5000, V = 50000 0.92 and 0.93, T
-// = 400, V = 47000 0.146 and 0.140; H = 576 T = 5000, V = 50000 0.92 and 0.89; H = 512 0.79
-// and 0.76: from 640 on.  At most kKeepBytes of them, 1.5 % of the memory; the rows past it
-// (T V above 2^31) are formed again.
+// whole calls): H = 4096 T = 8192 (30 % ignored), V = 151936 13.5 and 16.9, T = 1031 2.2 and
+// 2.9; H = 2048 T = 8192 (20 %), V = 32000 1.83 and 2.11; H = 1024 T = 16000, V = 32000 2.36
+// and 2.70; H = 896 T = 5000, V = 50000 1.12 and 1.26; H = 768 1.01 and 1.04; H = 640 0.927
+// and 0.915, T = 16000, V = 32000 1.74 and 1.78, T = 400, V = 47000 0.145 and 0.160 or 0.137;
+// H = 576 T = 5000, V = 50000 0.92 and 0.89; H = 512 0.79 and 0.76: from 640 on.  At most
+// kKeepBytes of them, 1.5 % of the memory, or as many as the caller allows
+// (molt_ce_options); the rows past it (by default T V above 2^31) are formed again.
 constexpr int64_t kKeepBytes = int64_t(4) << 30, kKeepFromH = 640;
-int64_t keep_tiles(int64_t T, int64_t H, int64_t V) {
+int64_t keep_limit(const molt_ce_options* opts) {
+  const int64_t n = opts ? opts->max_kept_bytes : 0;
+  return n == 0 ? kKeepBytes : std::max<int64_t>(0, std::min(n, kKeepBytes));
+}
+int64_t keep_tiles(int64_t T, int64_t H, int64_t V, int64_t limit) {
   if (H < kKeepFromH) return 0;
-  return std::min((T + 255) / 256, kKeepBytes / ((V + 255) / 256 * kKeepTile));
+  return std::min((T + 255) / 256, limit / ((V + 255) / 256 * kKeepTile));
 }
 // what the workspace holds for them: never less for a larger T or V
-int64_t keep_bytes(int64_t T, int64_t H, int64_t V) {
+int64_t keep_bytes(int64_t T, int64_t H, int64_t V, int64_t limit) {
   if (H < kKeepFromH) return 0;
-  const int64_t tiles = std::min((T + 255) / 256 * ((V + 255) / 256), kKeepBytes / kKeepTile + 1);   // (no overflow)
-  return std::min(kKeepBytes, tiles * kKeepTile);
+  const int64_t tiles = std::min((T + 255) / 256 * ((V + 255) / 256), limit / kKeepTile + 1);   // (no overflow)
+  return std::min(limit, tiles * kKeepTile);
 }
 
 // Workspace of the cross entropy: the active rows packed, which are the backward's rows
-// too; `dW32`: an fp32 dW that is rounded at the end.
-Layout ce_layout(int64_t T, int64_t H, int64_t V, int n_sm, bool with_bwd, bool dW32, size_t* dW32_off) {
+// too; `dW32`: an fp32 dW that is rounded at the end; `keep`: bytes of kept logits at most.
+Layout ce_layout(int64_t T, int64_t H, int64_t V, int n_sm, bool with_bwd, bool dW32, int64_t keep, size_t* dW32_off) {
   const int64_t Tcap = round_tiles(T);
   Layout L{};
   size_t o = 0;
@@ -472,7 +477,7 @@ Layout ce_layout(int64_t T, int64_t H, int64_t V, int n_sm, bool with_bwd, bool 
   const ChunkReserve cr = chunk_reserve(T, H, V, false, true);
   L.g = with_bwd ? take(cr.g) : o;
   L.ctl = with_bwd ? take(cr.ctl) : o;
-  L.keep = with_bwd ? take(static_cast<size_t>(keep_bytes(T, H, V))) : o;
+  L.keep = with_bwd ? take(static_cast<size_t>(keep_bytes(T, H, V, keep))) : o;
   *dW32_off = with_bwd && dW32 ? take(static_cast<size_t>(V) * H * 4) : o;
   L.tile_list = L.lp_p = L.ent_p = L.gate_p = L.live_of = o;
   L.h_l = L.h_p;
@@ -1039,7 +1044,7 @@ molt_status cross_entropy_impl(const uint16_t* hidden, const uint16_t* W, const 
   // fp32 and rounded by a pass of its own
   const bool dw16 = round_dW && cp.n_t <= cp.chunk_t;
   size_t dW32_off;
-  const Layout L = ce_layout(T, H, V, di->n_sm, grad, round_dW && !dw16, &dW32_off);
+  const Layout L = ce_layout(T, H, V, di->n_sm, grad, round_dW && !dw16, keep_limit(opts), &dW32_off);
   Scratch sc;
   MOLT_TRY(get_scratch(sc, workspace, workspace_bytes, L.total, stream));
   const Workspace w = carve(sc.ptr, L);
@@ -1052,7 +1057,7 @@ molt_status cross_entropy_impl(const uint16_t* hidden, const uint16_t* W, const 
               "pack");
   ev_stop(0, stream);
   const bool smooth = a.smoothing != 0.f || a.z_loss != 0.f;
-  const int64_t keep_t = grad ? keep_tiles(T, H, V) : 0;
+  const int64_t keep_t = grad ? keep_tiles(T, H, V, keep_limit(opts)) : 0;
   MOLT_TRY(run_forward_kernel(di, Tcap, H, V, S, w, tm_h, tm_w, false, smooth, stream, keep_t));
   ev_start(2, stream);
   MOLT_LAUNCH(launch_ce_merge(a, smooth, static_cast<int>(T), static_cast<int>(Tcap), static_cast<int>(V), S, w, loss_out, logp_out, lse_out,
@@ -1359,12 +1364,19 @@ molt_status molt_policy_loss_fwd_bwd_ex(const uint16_t* hidden, const uint16_t* 
 
 // ------------------------------------------------------------ cross entropy
 size_t molt_cross_entropy_workspace_bytes(int64_t T, int64_t H, int64_t V, int with_backward, int dW_dtype) {
+  return molt_cross_entropy_workspace_bytes_ex(T, H, V, with_backward, dW_dtype, nullptr);
+}
+
+size_t molt_cross_entropy_workspace_bytes_ex(int64_t T, int64_t H, int64_t V, int with_backward, int dW_dtype,
+                                             const molt_ce_options* opts) {
   if (check_shape(T, H, V) != MOLT_OK) return 0;
   molt_status st;
   const DeviceInfo* di = device_info(&st);
   size_t dW32;
   const ChunkPlan cp = chunk_shape_bf16(T, H, V);
-  return ce_layout(T, H, V, di ? di->n_sm : 152, with_backward != 0, dW_dtype != MOLT_FP32 && cp.n_t > cp.chunk_t, &dW32).total;
+  return ce_layout(T, H, V, di ? di->n_sm : 152, with_backward != 0, dW_dtype != MOLT_FP32 && cp.n_t > cp.chunk_t,
+                   keep_limit(opts), &dW32)
+      .total;
 }
 
 molt_status molt_cross_entropy_fwd(const uint16_t* hidden, const uint16_t* W, const int32_t* targets,
