@@ -844,23 +844,28 @@ template <class X, class R>
 cudaError_t launch_norm_rows(const NormArgs& a, const NormShape& s, int n_sm, int* grid, bool bwd, cudaStream_t stream) {
   using Kernel = void (*)(const NormArgs);
   // by the elements and threads of a row: 8 and up to 640, 16 and up to 192, 320 and 512
+  // (rows_shape gives 16 elements to 193 to 320 threads in the forward of vectors and pairs only)
 #define MOLT_FWD(V, E, THREADS, BLOCKS) \
   norm_fwd_rows_kernel<X, R, V, E, THREADS, BLOCKS, false>, norm_fwd_rows_kernel<X, R, V, E, THREADS, BLOCKS, true>
 #define MOLT_BWD(V, E, THREADS, BLOCKS) \
   norm_bwd_rows_kernel<X, R, V, E, THREADS, BLOCKS, false>, norm_bwd_rows_kernel<X, R, V, E, THREADS, BLOCKS, true>
-#define MOLT_ROWS(V)                                                                                      \
-  {{MOLT_FWD(V, 8, 640, 1), MOLT_BWD(V, 8, 640, 1)},                                                         \
-   {MOLT_FWD(V, 16, 192, 1), MOLT_BWD(V, 16, 128, 3)},                                                        \
-   {MOLT_FWD(V, 16, 320, 2), MOLT_BWD(V, 16, 512, 1)},                                                       \
+#define MOLT_NONE nullptr, nullptr
+#define MOLT_ROWS(V, FWD_320)                           \
+  {{MOLT_FWD(V, 8, 640, 1), MOLT_BWD(V, 8, 640, 1)},    \
+   {MOLT_FWD(V, 16, 192, 1), MOLT_BWD(V, 16, 128, 3)},  \
+   {FWD_320, MOLT_NONE},                                \
    {MOLT_FWD(V, 16, 512, 1), MOLT_BWD(V, 16, 512, 1)}}
-  static constexpr Kernel kernels[3][4][4] = {MOLT_ROWS(1), MOLT_ROWS(2), MOLT_ROWS(8)};
+  static constexpr Kernel kernels[3][4][4] = {MOLT_ROWS(1, MOLT_NONE), MOLT_ROWS(2, MOLT_FWD(2, 16, 320, 2)),
+                                              MOLT_ROWS(8, MOLT_FWD(8, 16, 320, 2))};
 #undef MOLT_ROWS
+#undef MOLT_NONE
 #undef MOLT_BWD
 #undef MOLT_FWD
   static KernelInfo info[3][4][4];
   const int vec = s.vec == 8 ? 2 : s.vec == 2 ? 1 : 0, size = s.elems == 8 ? 0 : s.threads <= 192 ? 1 : s.threads <= 320 ? 2 : 3;
   const int which = (bwd ? 2 : 0) + (a.gate_kind == MOLT_GATE_FULL ? 1 : 0);
   const Kernel k = kernels[vec][size][which];
+  if (k == nullptr) return cudaErrorInvalidValue;   // a shape that rows_shape does not give
   int warp_regs;
   const cudaError_t e = info[vec][size][which].get(k, &warp_regs);
   if (e != cudaSuccess) return e;
