@@ -194,9 +194,10 @@ __device__ __forceinline__ RowStats merge_row(const float4* __restrict__ part, i
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      // The forward's exponentials are 2^(z log2e - mL) with mL = m log2e rounded to fp32: all of
-      // them 2^rho too large, rho up to 1e-6 at m = 20, which is a loss of 1e-6 too much
-      // or too little.  s takes 2^-rho = 1 - a + a^2 / 2 (rho is small wherever logits mean anything).
+      // The forward's exponentials are 2^(z log2e - mL) with mL = m log2e rounded to fp32: all
+      // of them 2^rho too large, rho up to 1e-6 at m = 20, which is a loss of 1e-6 too much or
+      // too little.  s takes 2^-rho = 1 - a + a^2 / 2 (rho is small wherever logits mean
+      // anything).
       const float rho = fmaf(p[i].x, kLog2e, -__fmul_rn(p[i].x, kLog2e));
       const float a = kLn2 * fminf(fmaxf(rho, -0.01f), 0.01f);
       add(p[i].x, fmaf(p[i].y, a * fmaf(0.5f, a, -1.f), p[i].y), p[i].z);

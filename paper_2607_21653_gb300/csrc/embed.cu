@@ -98,8 +98,9 @@ constexpr int kSortElems = 128, kSortSplit = 4, kSortThreads = kSortElems * kSor
 constexpr int kSortBits = 9, kSortChunk = 1 << kSortBits;
 
 // Tokens that give no gradient (outside [0, V), or the padding token) get the key V and
-// so come last.  Word: token << kSortBits | place in the chunk (64 bits where V needs them).  A block places kSortElems elements of a chunk, kSortSplit threads to an
-// element, each comparing it with a part of the chunk.
+// so come last.  Word: token << kSortBits | place in the chunk (64 bits where V needs
+// them).  A block places kSortElems elements of a chunk, kSortSplit threads to an element,
+// each comparing it with a part of the chunk.
 template <class Word>
 __global__ void __launch_bounds__(kSortThreads) sort_chunks_kernel(const int32_t* __restrict__ tok, int T, int V, int padding,
                                                                    uint32_t* __restrict__ keys_out,

@@ -159,9 +159,10 @@ bool rows_shape(const molt_norm_desc* d, bool bwd, NormArgs& a, NormShape& s) {
   a.at_gate = take(a.gate_kind == MOLT_GATE_FULL, xb);
   a.stage_bytes = at;
   // 16 elements to a thread where that makes a row one warp's, in the forward for longer
-  // rows too (32768 x 2048 with an fp32 stream: 8 elements 190 us, 16 132; 16001 x 5120 141
-  // and 110), not in the backward, whose sums then take too many registers (190 and 213, 189
-  // and 221), nor where elements come one by one (20000 x 2049 forward 115 and 135)
+  // rows too (32768 x 2048 with an fp32 stream: 8 elements 151 us, 16 142; 16001 x 5120 148
+  // and 114), not in the backward, whose sums then take too many registers (191 and 213, 189
+  // and 309), nor where elements come one by one (20000 x 2049 forward 122 and 126, but
+  // 20000 x 1563 136 and 87: a rule by the length has not been looked for)
   const int most8 = !bwd && s.vec > 1 ? 256 : 8 * 640;
   const int elems = a.H <= 256 || (a.H > 512 && a.H <= most8) ? 8 : 16;
   s.elems = elems;
