@@ -554,6 +554,123 @@ molt_status molt_cross_entropy_fwd_bwd(const uint16_t* hidden, const uint16_t* W
                                        size_t workspace_bytes, cudaStream_t stream);
 
 /*
+ * ---------------------------------------------------------------------------
+ * Inside a block (no paper counterpart): what stands between two norms of the
+ * residual stream.
+ * ---------------------------------------------------------------------------
+ */
+
+/*
+ * Gated feed-forward block:
+ *   g = x w_gate^T, u = x w_up^T  [T,F];   h = act(g) u;   y = h w_down^T  [T,H]
+ * x [T,H], w_gate, w_up [F,H], w_down [H,F] (nn.Linear layouts) and y of one 16-bit type;
+ * sums in fp32, h rounded once to the type for the second product, g and u kept (or not)
+ * rounded once.  Rows of the operands may be strided; the outputs' rows lie side by side.  All
+ * pointers 16-byte aligned; outputs overlap neither one another nor the inputs.
+ */
+#define MOLT_ACT_SILU 0       /* g / (1 + e^-g) */
+#define MOLT_ACT_GELU 1       /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2 */
+#define MOLT_ACT_RELU 2       /* max(g, 0); its derivative at 0 is 0 */
+typedef struct {
+  int64_t T, H, F;            /* 0 <= T <= 2^24; H, F multiples of 8 up to 2^17 */
+  int64_t x_stride, w_gate_stride, w_up_stride, w_down_stride, dy_stride;   /* elements between
+                                 rows, multiples of 8; 0: side by side */
+  int dtype;                  /* MOLT_BF16 or MOLT_FP16 */
+  int activation;             /* MOLT_ACT_* */
+} molt_ffn_desc;
+
+/* gate_out, up_out [T,F]: g and u for the backward, both or neither. */
+size_t molt_gated_ffn_fwd_workspace_bytes(const molt_ffn_desc* desc);
+molt_status molt_gated_ffn_fwd(const molt_ffn_desc* desc, const void* x, const void* w_gate, const void* w_up,
+                               const void* w_down, void* y, void* gate_out, void* up_out, void* workspace,
+                               size_t workspace_bytes, cudaStream_t stream);
+
+/*
+ * Backward from dy [T,H]:
+ *   dh = dy w_down;  dg = dh u act'(g);  du = dh act(g)   (rounded once each, as h is)
+ *   dx = dg w_gate + du w_up;  dw_gate (+)= dg^T x;  dw_up (+)= du^T x;  dw_down (+)= dy^T h
+ * gate, up: what the forward kept, or both NULL: then they are formed again in fp32, which
+ * takes a third more operations and 8 T F bytes of workspace (kept = 0 in the query).
+ * dx [T,H] of the block's type; weights' gradients of dw_dtype (the block's type, or MOLT_FP32;
+ * accumulate = 1 adds to them and needs MOLT_FP32).  Bitwise reproducible on one kind of device.
+ */
+size_t molt_gated_ffn_bwd_workspace_bytes(const molt_ffn_desc* desc, int kept);
+molt_status molt_gated_ffn_bwd(const molt_ffn_desc* desc, const void* dy, const void* x, const void* w_gate,
+                               const void* w_up, const void* w_down, const void* gate, const void* up, void* dx,
+                               void* dw_gate, void* dw_up, void* dw_down, int dw_dtype, int accumulate,
+                               void* workspace, size_t workspace_bytes, cudaStream_t stream);
+
+/*
+ * Gated linear recurrence over packed sequences, channel by channel:
+ *   MOLT_SCAN_SIGMOID  h_t = a_t h_{t-1} + (1 - a_t) value_t,  a_t = 1 / (1 + e^-gate_t)
+ *   MOLT_SCAN_LOG      h_t = a_t h_{t-1} + value_t,            a_t = e^gate_t
+ * gate, value, y [T,H] of one type (rows of gate and value may be strided, as the halves of one
+ * projection are); states fp32.  Sequence b is rows cu_seqlens[b] .. cu_seqlens[b+1] - 1 (device
+ * int32 [B+1], ascending, within [0, T]; sequences may be empty), or with cu_seqlens NULL the b-th
+ * T / B rows.  It begins with initial_state[b] ([B,H], NULL: 0).  Rows of y outside of every
+ * sequence are left as they were, or with fill_outside 0; their gradients are 0.  cu_seqlens that descend or leave [0, T] set
+ * MOLT_DEV_UNSORTED_GROUPS; what is then written is unspecified, but lies inside the outputs.
+ * Nothing of a sequence, not even an infinity or a NaN, reaches another.
+ */
+#define MOLT_SCAN_SIGMOID 0
+#define MOLT_SCAN_LOG 1
+#define MOLT_SCAN_STATE_ROWS 128
+typedef struct {
+  int64_t T, H, B;            /* 0 <= T, B < 2^31 - 256; 1 <= H <= 65536 */
+  int64_t gate_stride, value_stride, dy_stride;   /* elements between rows; 0: H */
+  int dtype;                  /* molt_dtype of gate, value, y and their gradients */
+  int form;                   /* MOLT_SCAN_* */
+  int fill_outside;           /* forward: 1 writes zeros to the rows of y that no sequence has */
+} molt_scan_desc;
+
+/* final_state [B,H] (NULL: not wanted): h of each sequence's last row (an empty one's initial
+ * state).  states [ceil(T / 128), H] (NULL: no backward follows): h of the row before each 128th,
+ * for the backward. */
+molt_status molt_gated_scan_fwd(const molt_scan_desc* desc, const void* gate, const void* value,
+                                const float* initial_state, const int32_t* cu_seqlens, void* y, float* final_state,
+                                float* states, cudaStream_t stream);
+
+/*
+ * Backward from dy [T,H] and dfinal_state [B,H] (NULL: 0), with the forward's inputs and
+ * states: dgate, dvalue [T,H], dinitial_state [B,H] (NULL: not wanted).  Both directions are
+ * bitwise reproducible.
+ */
+molt_status molt_gated_scan_bwd(const molt_scan_desc* desc, const void* dy, const void* gate, const void* value,
+                                const float* states, const float* initial_state, const int32_t* cu_seqlens,
+                                const float* dfinal_state, void* dgate, void* dvalue, float* dinitial_state,
+                                cudaStream_t stream);
+
+/* One row of each of B = T sequences (decoding): y = state_out = the recurrence from state [B,H].
+ * state_out may be state. */
+molt_status molt_gated_scan_step(const molt_scan_desc* desc, const void* gate, const void* value, const float* state,
+                                 void* y, float* state_out, cudaStream_t stream);
+
+/*
+ * Dropout without a stored mask:
+ *   out = res_scale residual + keep x / (1 - q),   q = round(2^16 p) / 2^16
+ * keep of an element depends on (seed, offset, first_row + row, column) alone: 16 bits of
+ * Philox4x32-10 with key seed and counter (column / 8, row, offset), not below 2^16 q; half
+ * j % 2 (low first) of word j / 2 for column 8 g + j.  So a batch may be cut by rows
+ * (first_row), and the backward is the same call on the gradient: dx = dropout of dout (its
+ * residual's gradient is res_scale dout).  Dropped values are left out, whatever they are.
+ * x [T,H] of dtype, residual (NULL: none) and out of out_dtype: dtype, or one of the two is
+ * MOLT_FP32.  out may be x or the residual where rows lie side by side and the type is the same.
+ * seed_offset: device uint64 [2], read when the call runs, in the place of seed and offset (a
+ * captured graph draws a new mask at every replay when the program changes them), or NULL.
+ */
+typedef struct {
+  int64_t T, H;               /* 0 <= T, 1 <= H <= 65536 */
+  int64_t x_stride, residual_stride;   /* elements between rows; 0: H */
+  int64_t first_row;          /* first_row + T <= 2^32 */
+  uint64_t seed, offset;
+  double p;                   /* in [0, 1]; 1 drops everything */
+  float res_scale;
+  int dtype, out_dtype;       /* molt_dtype */
+} molt_dropout_desc;
+molt_status molt_dropout(const molt_dropout_desc* desc, const void* x, const void* residual,
+                         const uint64_t* seed_offset, void* out, cudaStream_t stream);
+
+/*
  * Per-kernel timing hook for benchmarks.  While set, every LM-head call made
  * from the calling thread records starts[k] / stops[k] (caller-created CUDA
  * events) on its stream around kernel group k:

@@ -22,7 +22,8 @@ __all__ = [
     "token_logprobs_workspace_bytes", "policy_loss_workspace_bytes", "header_functions", "backward_plan",
     "vp_partials", "vp_loss", "vp_backward", "vocab_shard_bounds", "gather_shard_partials", "sum_dhidden",
     "policy_loss_vocab_parallel", "token_embedding", "token_embedding_bwd", "residual_norm_fwd", "residual_norm_bwd",
-    "cross_entropy_fwd", "cross_entropy_fwd_bwd", "cross_entropy_stats",
+    "cross_entropy_fwd", "cross_entropy_fwd_bwd", "cross_entropy_stats", "gated_ffn_fwd", "gated_ffn_bwd",
+    "gated_scan_fwd", "gated_scan_bwd", "gated_scan_step", "dropout_fwd", "dropout_bwd",
 ]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -32,7 +33,8 @@ _INCLUDE = os.path.join(_ROOT, "include")
 _BUILD = os.path.join(_ROOT, "_build")
 _LIB = os.path.join(_PKG, "libmolt.so")
 _SOURCES = ["rows.cu", "lmhead_fwd.cu", "lmhead_bwd.cu", "lmhead_bwd4.cu", "lmhead_bwd_chunk.cu", "api.cu", "noalloc.cu",
-            "ce.cu", "embed.cu", "norm.cu", "norm_bf16.cu", "norm_fp16.cu", "norm_fp32.cu"]
+            "ce.cu", "embed.cu", "norm.cu", "norm_bf16.cu", "norm_fp16.cu", "norm_fp32.cu", "ffn.cu", "ffn_gemm.cu",
+            "scan.cu", "dropout.cu"]
 ARCH_FLAGS = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 STATUS = {
@@ -152,6 +154,14 @@ def load():
         "molt_cross_entropy_workspace_bytes_ex": (SZ, [I64, I64, I64, I32, I32, P]),
         "molt_cross_entropy_fwd": (I32, [P, P, P, P, I64, I64, I64, D, P, P, P, P, P, P, SZ, P]),
         "molt_cross_entropy_fwd_bwd": (I32, [P, P, P, P, I64, I64, I64, D, P, P, P, P, I32, I32, P, P, P, P, SZ, P]),
+        "molt_gated_ffn_fwd_workspace_bytes": (SZ, [P]),
+        "molt_gated_ffn_fwd": (I32, [P] * 9 + [SZ, P]),
+        "molt_gated_ffn_bwd_workspace_bytes": (SZ, [P, I32]),
+        "molt_gated_ffn_bwd": (I32, [P] * 12 + [I32, I32, P, SZ, P]),
+        "molt_gated_scan_fwd": (I32, [P] * 9),
+        "molt_gated_scan_bwd": (I32, [P] * 12),
+        "molt_gated_scan_step": (I32, [P] * 7),
+        "molt_dropout": (I32, [P] * 6),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -631,5 +641,7 @@ def policy_loss_vocab_parallel(hidden, weight_shard, v_begin, tokens, behavior_l
     return out
 
 
+from .blocks import (dropout_bwd, dropout_fwd, gated_ffn_bwd, gated_ffn_fwd, gated_scan_bwd,  # noqa: E402
+                     gated_scan_fwd, gated_scan_step)
 from .cross_entropy import cross_entropy_fwd, cross_entropy_fwd_bwd, cross_entropy_stats  # noqa: E402
 from .stream import residual_norm_bwd, residual_norm_fwd, token_embedding, token_embedding_bwd  # noqa: E402

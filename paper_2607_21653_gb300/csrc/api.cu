@@ -96,14 +96,15 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
   return fn;
 }
 
-// 2-D row-major tensor map: `rows` x `cols` elements, box `box_cols` x `box_rows`
+// 2-D row-major tensor map: `rows` x `cols` elements, rows `ld` elements apart (0: side by
+// side), box `box_cols` x `box_rows`
 molt_status make_tmap(CUtensorMap* m, CUtensorMapDataType dt, int elem_bytes, const void* base, uint64_t rows,
                       uint64_t cols, uint32_t box_cols, uint32_t box_rows,
-                      CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
+                      CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B, uint64_t ld = 0) {
   auto fn = encode_fn();
   if (!fn) return fail(MOLT_ERR_CUDA, "cuTensorMapEncodeTiled entry point unavailable");
   cuuint64_t dims[2] = {cols, rows};
-  cuuint64_t strides[1] = {cols * static_cast<uint64_t>(elem_bytes)};
+  cuuint64_t strides[1] = {(ld ? ld : cols) * static_cast<uint64_t>(elem_bytes)};
   cuuint32_t box[2] = {box_cols, box_rows};
   cuuint32_t estr[2] = {1, 1};
   CUresult r = fn(m, dt, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
@@ -1139,6 +1140,11 @@ int ordered_splits(int64_t Tcap, int64_t V, int n_sm) {
 molt_status encode_tmap_2d(CUtensorMap* m, CUtensorMapDataType dt, int elem_bytes, const void* base, uint64_t rows,
                            uint64_t cols, uint32_t box_cols, uint32_t box_rows) {
   return make_tmap(m, dt, elem_bytes, base, rows, cols, box_cols, box_rows);
+}
+
+molt_status encode_tmap_rows(CUtensorMap* m, CUtensorMapDataType dt, int elem_bytes, const void* base, uint64_t rows,
+                             uint64_t cols, uint64_t ld, uint32_t box_cols, uint32_t box_rows) {
+  return make_tmap(m, dt, elem_bytes, base, rows, cols, box_cols, box_rows, CU_TENSOR_MAP_SWIZZLE_128B, ld);
 }
 
 }  // namespace molt

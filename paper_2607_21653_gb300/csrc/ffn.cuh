@@ -1,0 +1,68 @@
+// Gated feed-forward block: what the C-ABI layer (ffn.cu) hands to its kernels.
+#pragma once
+
+#include <cstdint>
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+namespace molt {
+
+// activations (values of MOLT_ACT_*)
+constexpr int kActSilu = 0, kActGelu = 1, kActRelu = 2;
+
+// What becomes of a unit's accumulator.
+enum FfnEpilogue : int {
+  kEpiStore16 = 0,   // rounded, stored through out[0]
+  kEpiStore32 = 1,   // stored through out[0] in fp32 (add: reduce-added to it)
+  kEpiGlu = 2,       // gate | up columns: h = act(g) u through out[0]; keep: g, u through out[1], out[2]
+  kEpiGlu32 = 3,     // g and u in fp32 through out[0], out[1]
+  kEpiDglu = 4,      // dh: dg, du and h through out[0], out[1], out[2], from gate and up
+  kEpiPart = 5       // fp32 part of a split K through out[0]
+};
+
+// One product C[m,n] = sum_k A[m,k] B[n,k] in tiles of 256 x 256 (kEpiGlu*: 256 rows by 128
+// columns of g and the same of u).  K is a series of blocks of 64, the first nk0 from a[0]
+// and b[0], the others from a[1] and b[1]; it is cut into `splits` units of unit_k blocks.
+struct FfnProblem {
+  CUtensorMap a[2], b[2], out[3];
+  const void* gate;     // kEpiDglu: [m, n], of the operands' type or fp32 (wide)
+  const void* up;
+  int m, n;
+  int n_m, n_n;         // tiles
+  int nk0, nk;
+  int splits, unit_k;
+  int first;            // the first of its units in the launch
+  int a_mn, b_mn;       // operand is MN-major (its rows run along K)
+  int epi;              // FfnEpilogue
+  int glu;              // b[0] and b[1] are W_gate and W_up, brought by one CTA of the pair each
+  int add;              // kEpiStore32
+  int keep;             // kEpiGlu
+  int wide;             // kEpiDglu: gate and up are fp32
+};
+constexpr int kFfnProblems = 4;
+struct FfnBatch {
+  FfnProblem p[kFfnProblems];
+  int n;                // problems
+  int total;            // units
+  int act;
+  unsigned* err;
+};
+
+// Sums of a split K: out = sum_s part[s], as the problem's epilogue.
+struct FfnReduce {
+  const float* part;    // [splits][rows][ld]
+  int64_t split_stride;
+  int splits, ld;
+  int m, n;
+  int epi;              // the unsplit problem's
+  int act, add, keep, wide;
+  const void* gate;
+  const void* up;
+  void* out[3];
+};
+
+int ffn_pairs(int n_sm);   // CTA pairs of a launch
+cudaError_t launch_ffn_gemm(const FfnBatch& b, bool fp16, int n_sm, cudaStream_t s);
+cudaError_t launch_ffn_reduce(const FfnReduce& r, bool fp16, int n_sm, cudaStream_t s);
+
+}  // namespace molt

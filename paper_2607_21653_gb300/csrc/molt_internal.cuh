@@ -182,6 +182,9 @@ int forward_splits(int64_t Tcap, int64_t H, int64_t V, int n_sm);
 int ordered_splits(int64_t Tcap, int64_t V, int n_sm);   // the reproducible loss call's
 molt_status encode_tmap_2d(CUtensorMap* m, CUtensorMapDataType dt, int elem_bytes, const void* base, uint64_t rows,
                            uint64_t cols, uint32_t box_cols, uint32_t box_rows);
+// the same for rows that lie ld elements apart
+molt_status encode_tmap_rows(CUtensorMap* m, CUtensorMapDataType dt, int elem_bytes, const void* base, uint64_t rows,
+                             uint64_t cols, uint64_t ld, uint32_t box_cols, uint32_t box_rows);
 
 // rows.cu
 // one bounded turn wait on a counter nothing raises (words: 3 zeroed uint32)
