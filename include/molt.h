@@ -626,9 +626,10 @@ typedef struct {
 /* final_state [B,H] (NULL: not wanted): h of each sequence's last row (an empty one's initial
  * state).  states [ceil(T / 128), H] (NULL: no backward follows): h of the row before each 128th,
  * for the backward. */
+size_t molt_gated_scan_workspace_bytes(const molt_scan_desc* desc);   /* of either direction */
 molt_status molt_gated_scan_fwd(const molt_scan_desc* desc, const void* gate, const void* value,
                                 const float* initial_state, const int32_t* cu_seqlens, void* y, float* final_state,
-                                float* states, cudaStream_t stream);
+                                float* states, void* workspace, size_t workspace_bytes, cudaStream_t stream);
 
 /*
  * Backward from dy [T,H] and dfinal_state [B,H] (NULL: 0), with the forward's inputs and
@@ -638,7 +639,7 @@ molt_status molt_gated_scan_fwd(const molt_scan_desc* desc, const void* gate, co
 molt_status molt_gated_scan_bwd(const molt_scan_desc* desc, const void* dy, const void* gate, const void* value,
                                 const float* states, const float* initial_state, const int32_t* cu_seqlens,
                                 const float* dfinal_state, void* dgate, void* dvalue, float* dinitial_state,
-                                cudaStream_t stream);
+                                void* workspace, size_t workspace_bytes, cudaStream_t stream);
 
 /* One row of each of B = T sequences (decoding): y = state_out = the recurrence from state [B,H].
  * state_out may be state. */

@@ -158,8 +158,9 @@ def load():
         "molt_gated_ffn_fwd": (I32, [P] * 9 + [SZ, P]),
         "molt_gated_ffn_bwd_workspace_bytes": (SZ, [P, I32]),
         "molt_gated_ffn_bwd": (I32, [P] * 12 + [I32, I32, P, SZ, P]),
-        "molt_gated_scan_fwd": (I32, [P] * 9),
-        "molt_gated_scan_bwd": (I32, [P] * 12),
+        "molt_gated_scan_workspace_bytes": (SZ, [P]),
+        "molt_gated_scan_fwd": (I32, [P] * 9 + [SZ, P]),
+        "molt_gated_scan_bwd": (I32, [P] * 12 + [SZ, P]),
         "molt_gated_scan_step": (I32, [P] * 7),
         "molt_dropout": (I32, [P] * 6),
     }

@@ -191,7 +191,7 @@ def _packed(t, like, name):
 
 
 def gated_scan_fwd(gate, value, initial_state=None, cu_seqlens=None, kind="sigmoid", want_states=False,
-                   want_final_state=True, out=None, stream=None):
+                   want_final_state=True, out=None, stream=None, workspace=None):
     """Gated linear recurrence over sequences, channel by channel (molt_gated_scan_fwd):
         "sigmoid":  h_t = a_t h_{t-1} + (1 - a_t) value_t,  a_t = sigmoid(gate_t)
         "log":      h_t = a_t h_{t-1} + value_t,            a_t = exp(gate_t)
@@ -213,15 +213,17 @@ def gated_scan_fwd(gate, value, initial_state=None, cu_seqlens=None, kind="sigmo
         out = torch.empty(gate.shape, dtype=dtype, device=dev)
     final = torch.empty(B, H, dtype=f32, device=dev) if want_final_state else None
     states = torch.empty((T + STATE_ROWS - 1) // STATE_ROWS, H, dtype=f32, device=dev) if want_states else None
-    ref, _ = _desc(ScanDesc, (T, H, B, gs, vs, 0, _dtype_code(dtype, "gate"), _form(kind), fill))
+    ref, nbytes = _desc(ScanDesc, (T, H, B, gs, vs, 0, _dtype_code(dtype, "gate"), _form(kind), fill),
+                        "molt_gated_scan_workspace_bytes")
+    ws = workspace if workspace is not None else _scratch(nbytes, dev, "gated_scan", stream)
     _call(load().molt_gated_scan_fwd, dev, ref, gp, vp, _at(initial_state, f32, dev, "initial_state"), cu,
           _at(_shaped(out, gate.shape, "out"), dtype, dev, "out"), final if final is None else final.data_ptr(),
-          states if states is None else states.data_ptr(), _stream(stream, dev.index))
+          states if states is None else states.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream, dev.index))
     return {"y": out, "final_state": final, "states": states}
 
 
 def gated_scan_bwd(dy, gate, value, states, initial_state=None, cu_seqlens=None, dfinal_state=None, kind="sigmoid",
-                   stream=None):
+                   stream=None, workspace=None):
     """Gradients of gated_scan_fwd (molt_gated_scan_bwd) from dy and dfinal_state [B, H]
     (float32, or None: the final state is not used), with the forward's inputs and its `states`.
     Returns dict(dgate, dvalue, dinitial_state), the last one None without an initial state.
@@ -239,10 +241,13 @@ def gated_scan_bwd(dy, gate, value, states, initial_state=None, cu_seqlens=None,
             _shaped(t, (B, H), name)
     dgate, dvalue = (torch.empty(gate.shape, dtype=dtype, device=dev) for _ in range(2))
     dinit = None if initial_state is None else torch.empty(B, H, dtype=f32, device=dev)
-    ref, _ = _desc(ScanDesc, (T, H, B, gs, vs, ds, _dtype_code(dtype, "gate"), _form(kind), 0))
+    ref, nbytes = _desc(ScanDesc, (T, H, B, gs, vs, ds, _dtype_code(dtype, "gate"), _form(kind), 0),
+                        "molt_gated_scan_workspace_bytes")
+    ws = workspace if workspace is not None else _scratch(nbytes, dev, "gated_scan", stream)
     _call(load().molt_gated_scan_bwd, dev, ref, dp, gp, vp, _at(states, f32, dev, "states"),
           _at(initial_state, f32, dev, "initial_state"), cu, _at(dfinal_state, f32, dev, "dfinal_state"),
-          dgate.data_ptr(), dvalue.data_ptr(), dinit if dinit is None else dinit.data_ptr(), _stream(stream, dev.index))
+          dgate.data_ptr(), dvalue.data_ptr(), dinit if dinit is None else dinit.data_ptr(), ws.data_ptr(), ws.numel(),
+          _stream(stream, dev.index))
     return {"dgate": dgate, "dvalue": dvalue, "dinitial_state": dinit}
 
 

@@ -1146,6 +1146,10 @@ molt_status encode_tmap_rows(CUtensorMap* m, CUtensorMapDataType dt, int elem_by
                              uint64_t cols, uint64_t ld, uint32_t box_cols, uint32_t box_rows) {
   return make_tmap(m, dt, elem_bytes, base, rows, cols, box_cols, box_rows, CU_TENSOR_MAP_SWIZZLE_128B, ld);
 }
+molt_status encode_tmap_plain(CUtensorMap* m, CUtensorMapDataType dt, int elem_bytes, const void* base, uint64_t rows,
+                              uint64_t cols, uint64_t ld, uint32_t box_cols, uint32_t box_rows) {
+  return make_tmap(m, dt, elem_bytes, base, rows, cols, box_cols, box_rows, CU_TENSOR_MAP_SWIZZLE_NONE, ld);
+}
 
 }  // namespace molt
 

@@ -185,6 +185,9 @@ molt_status encode_tmap_2d(CUtensorMap* m, CUtensorMapDataType dt, int elem_byte
 // the same for rows that lie ld elements apart
 molt_status encode_tmap_rows(CUtensorMap* m, CUtensorMapDataType dt, int elem_bytes, const void* base, uint64_t rows,
                              uint64_t cols, uint64_t ld, uint32_t box_cols, uint32_t box_rows);
+// and row after row in shared memory, without the swizzle
+molt_status encode_tmap_plain(CUtensorMap* m, CUtensorMapDataType dt, int elem_bytes, const void* base, uint64_t rows,
+                              uint64_t cols, uint64_t ld, uint32_t box_cols, uint32_t box_rows);
 
 // rows.cu
 // one bounded turn wait on a counter nothing raises (words: 3 zeroed uint32)

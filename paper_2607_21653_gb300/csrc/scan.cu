@@ -10,16 +10,27 @@
 //
 // What a row does to h is an affine map (a, b), and maps compose, so rows can be taken
 // together: a tile is 128 rows by 64 channels, a warp has 16 rows of it, a lane two channels.
-// Every warp composes its rows' maps, adds its predecessors' in order, and then goes
-// through its rows again from the state that it now knows; the tile's own map carries the
-// state on.  A row that begins a sequence cuts: what comes before is not multiplied
-// by zero but left out, so that an infinite or NaN state stays in its sequence.
+// Every warp composes its rows' maps; the maps of a tile's warps, and of the tiles of a
+// cluster, are folded in order; and then every warp goes through its rows again from the
+// state that it now knows.  The backward's E is the same from the other end; h it forms
+// again from the states that the forward kept at every 128th row.  A row that begins a
+// sequence cuts: what comes before is not multiplied by zero but left out, so that an
+// infinite or NaN state stays in its sequence.
 //
-// Everything is held as 1 - a: with a as a float near 1 the memory 1 / (1 - a) of a channel
-// would be off by 2^-24 / (1 - a), and h - (1 - a) (h - v) needs no a at all.
+// Everything is held as m = a - 1: with a as a float near 1 the memory 1 / (1 - a) of a
+// channel would be off by 2^-24 / (1 - a); h + m (h - v) and h + m h + v need no a at all.
+//
+// Layout: a strip of channels belongs to a cluster of up to eight blocks, which take a
+// tile each, exchange their maps through one another's shared memory (512 bytes to each
+// peer) and go on together, so that the inputs are read once and a super step of 1024 rows
+// costs one exchange.  A ninth warp brings the tiles ahead (TMA, and from cu_seqlens which rows
+// begin and end a sequence).  Few strips and many rows are cut into segments besides: a first
+// launch folds each segment's map, the second starts from what precedes its own.
 #include <algorithm>
 #include <cstdint>
+#include <cuda.h>
 #include <cuda_runtime.h>
+#include <initializer_list>
 
 #include "molt_internal.cuh"
 #include "ptx.cuh"
@@ -30,7 +41,9 @@ namespace {
 
 constexpr int kTile = 128;               // rows of a tile, and between kept states
 constexpr int kWarps = 8, kRows = kTile / kWarps;
+constexpr int kThreads = 32 * (kWarps + 1);
 constexpr int kStrip = 64;               // channels of a block
+constexpr int kMaxCluster = 8;
 constexpr int kFormSigmoid = 0, kFormLog = 1;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -49,7 +62,12 @@ struct ScanArgs {
   float* states;           // [tiles, H], written by the forward (or nullptr), read by the backward
   void *dgate, *dvalue;    // backward
   float* dinit;            // [B, H] or nullptr
+  int tiles, seg_tiles;    // tiles in all, and of a segment
+  float4* seg_maps;        // [segments, strips, 32]: (A, b) of two channels, A < 0: cut
   unsigned* err;
+};
+struct ScanMaps {
+  CUtensorMap gate, value, dy;   // boxes of 64 channels by 128 rows
 };
 
 __device__ __forceinline__ float rcp_approx(float x) {
@@ -57,36 +75,40 @@ __device__ __forceinline__ float rcp_approx(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ F2 zero2() { return f2(0.f, 0.f); }
+__device__ __forceinline__ F2 sub2(F2 a, F2 b) { return fma2(b, f2(-1.f), a); }
 
-// 1 - a of a gate's value
+// m = a - 1 of two gates.  sigmoid: -1 / (1 + e^f), no digits lost on either side.  log: e^f - 1,
+// by its series where the difference would lose digits (the first term left out is
+// 0.35^7 / 8! of the first, 1.6e-8)
 template <int kForm>
-__device__ __forceinline__ float one_minus_a(float f) {
+__device__ __forceinline__ F2 decay(F2 f) {
   if constexpr (kForm == kFormSigmoid) {
-    const float e = ex2_approx(-kLog2e * fabsf(f)), r = rcp_approx(1.f + e);
-    return f >= 0.f ? e * r : f < 0.f ? r : f;
+    const F2 x = mul2(f, f2(kLog2e));
+    return f2(rcp_approx(-1.f - ex2_approx(x.x())), rcp_approx(-1.f - ex2_approx(x.y())));
   } else {
-    // -(e^f - 1): by its series where the difference would lose digits (the first
-    // term left out is 0.35^7 / 8! of the first, 1.6e-8)
-    float p = 1.f / 5040.f;
-    p = fmaf(p, f, 1.f / 720.f);
-    p = fmaf(p, f, 1.f / 120.f);
-    p = fmaf(p, f, 1.f / 24.f);
-    p = fmaf(p, f, 1.f / 6.f);
-    p = fmaf(p, f, 0.5f);
-    p = fmaf(p, f, 1.f);
-    return fabsf(f) < 0.35f ? -f * p : 1.f - ex2_approx(kLog2e * f);
+    F2 p = f2(1.f / 5040.f);
+    p = fma2(p, f, f2(1.f / 720.f));
+    p = fma2(p, f, f2(1.f / 120.f));
+    p = fma2(p, f, f2(1.f / 24.f));
+    p = fma2(p, f, f2(1.f / 6.f));
+    p = fma2(p, f, f2(0.5f));
+    p = fma2(p, f, f2(1.f));
+    p = mul2(p, f);
+    const F2 x = mul2(f, f2(kLog2e));
+    return f2(fabsf(f.x()) < 0.35f ? p.x() : ex2_approx(x.x()) - 1.f, fabsf(f.y()) < 0.35f ? p.y() : ex2_approx(x.y()) - 1.f);
   }
 }
 // h_t from h_{t-1}
 template <int kForm>
-__device__ __forceinline__ float step(float h, float na, float v) {
-  if constexpr (kForm == kFormSigmoid) return fmaf(na, v - h, h);
-  return fmaf(-na, h, h) + v;
+__device__ __forceinline__ F2 step(F2 h, F2 m, F2 v) {
+  if constexpr (kForm == kFormSigmoid) return fma2(m, sub2(h, v), h);
+  return add2(fma2(m, h, h), v);
 }
 
-// two neighbouring channels of a row, of which `left` exist
+// two neighbouring channels of a row, of which `left` exist; kPair: both or none, aligned
 template <bool kPair, class T>
-__device__ __forceinline__ float2 load2(const T* p, int left) {
+__device__ __forceinline__ F2 load2(const T* p, int left) {
   float v[2] = {0.f, 0.f};
   if constexpr (kPair) {
     if (left > 1) load_vec<2>(p, v);
@@ -94,289 +116,434 @@ __device__ __forceinline__ float2 load2(const T* p, int left) {
     if (left > 0) v[0] = to_float(p[0]);
     if (left > 1) v[1] = to_float(p[1]);
   }
-  return make_float2(v[0], v[1]);
+  return f2(v[0], v[1]);
 }
 template <bool kPair, class T>
-__device__ __forceinline__ void store2(T* p, float a, float b, int left) {
+__device__ __forceinline__ void store2(T* p, F2 x, int left) {
   if constexpr (kPair) {
-    const float v[2] = {a, b};
+    const float v[2] = {x.x(), x.y()};
     if (left > 1) store_vec<2>(p, v);
   } else {
-    if (left > 0) from_float(a, p[0]);
-    if (left > 1) from_float(b, p[1]);
+    if (left > 0) from_float(x.x(), p[0]);
+    if (left > 1) from_float(x.y(), p[1]);
   }
 }
 
-// Which rows of a tile begin or end a sequence, and which one: -1 for none.  lo and hi: the
-// tile's rows that are in any.
+// Which rows of a tile begin or end a sequence (a bit each), and which one (of those rows);
+// lo and hi: the tile's rows that are in any.
 struct TileRows {
-  int start[kTile], end[kTile];
+  uint32_t starts[kTile / 32], ends[kTile / 32];
+  int seq[kTile];
   int lo, hi;
 };
 
-// first b in [0, B] with cu[b] >= row (B + 1: none)
-__device__ __forceinline__ int64_t first_bound(const int32_t* cu, int64_t B, int64_t row) {
-  int64_t a = 0, z = B + 1;
-  while (a < z) {
-    const int64_t m = (a + z) / 2;
-    if (cu[m] >= row)
-      z = m;
-    else
-      a = m + 1;
-  }
-  return a;
-}
-
-// Fills `t` for the rows from row0 on; by one warp.
-__device__ __forceinline__ void mark_rows(const ScanArgs& a, int64_t row0, TileRows& t, int lane) {
+// Fills `t` for the rows from row0 on; by one warp.  Returns the first bound that is not below
+// row0; `at` is what it returned for the tile before in the walk (at first 0, backwards
+// B + 1).
+template <bool kBwd>
+__device__ __forceinline__ int64_t mark_rows(const ScanArgs& a, int64_t row0, TileRows& t, int64_t at, int lane) {
   const int n = static_cast<int>(a.T - row0 < kTile ? a.T - row0 : kTile);
-#pragma unroll
-  for (int i = lane; i < kTile; i += 32) t.start[i] = t.end[i] = -1;
+  if (lane < kTile / 32) t.starts[lane] = t.ends[lane] = 0u;
   __syncwarp();
   if (a.cu == nullptr) {
     if (lane == 0) {
       t.lo = 0;
       t.hi = n;
     }
-    for (int i = lane; i < n; i += 32) {
-      const int64_t r = row0 + i, b = r / a.L;
-      const int64_t in = r - b * a.L;
-      if (in == 0) t.start[i] = static_cast<int>(b);
-      if (in == a.L - 1) t.end[i] = static_cast<int>(b);
+    int64_t b = row0 / a.L;
+    int64_t v = b * a.L - row0;   // where sequence b begins
+    for (b += lane, v += int64_t(lane) * a.L; v < n; b += 32, v += int64_t(32) * a.L) {
+      if (v >= 0) {
+        t.seq[v] = static_cast<int>(b);
+        atomicOr(&t.starts[v >> 5], 1u << (v & 31));
+      }
+      const int64_t e = v + a.L - 1;
+      if (e < n) {
+        t.seq[e] = static_cast<int>(b);
+        atomicOr(&t.ends[e >> 5], 1u << (e & 31));
+      }
     }
-    return;
+    __syncwarp();
+    return 0;
   }
   if (lane == 0) {
     const int64_t first = a.cu[0] - row0, last = a.cu[a.B] - row0;
     t.lo = static_cast<int>(first < 0 ? 0 : first > n ? n : first);
     t.hi = static_cast<int>(last < 0 ? 0 : last > n ? n : last);
   }
+  // the first bound that is not below row0: among the 32 next to the last one's, or by 32
+  // probes at a time
+  int64_t lo, hi;
+  if constexpr (!kBwd) {
+    const int64_t b = at + lane;
+    const int n_below = __popc(__ballot_sync(0xffffffffu, b <= a.B && a.cu[b] < row0));
+    lo = at + n_below;
+    hi = n_below == 32 ? a.B + 1 : lo;
+  } else {
+    const int64_t b = at - 1 - lane;
+    const int n_above = __popc(__ballot_sync(0xffffffffu, b >= 0 && a.cu[b] >= row0));
+    hi = at - n_above;
+    lo = n_above == 32 ? 0 : hi;
+  }
+  while (lo < hi) {
+    const int64_t stride = (hi - lo + 31) / 32, b = lo + lane * stride;
+    const unsigned below = __ballot_sync(0xffffffffu, b < hi && a.cu[b] < row0);
+    const int k = __popc(below);   // probes below row0: a prefix of them
+    const int64_t base = lo;
+    if (k == 0) break;
+    lo = base + (k - 1) * stride + 1;
+    hi = min(hi, base + k * stride);
+  }
+  const int64_t found = lo;
   // bounds in [row0, row0 + n]: each ends the sequence before it and begins the one after
-  for (int64_t b0 = first_bound(a.cu, a.B, row0);; b0 += 32) {
+  for (int64_t b0 = found;; b0 += 32) {
     const int64_t b = b0 + lane;
     const int64_t v = b <= a.B ? a.cu[b] - row0 : int64_t(n) + 1;
     const bool in = v >= 0 && v <= n;
-    if (in && v < n && b < a.B && a.cu[b + 1] - row0 > v) t.start[v] = static_cast<int>(b);
-    if (in && v > 0 && b > 0 && a.cu[b - 1] - row0 < v) t.end[v - 1] = static_cast<int>(b - 1);
+    if (in && v < n && b < a.B && a.cu[b + 1] - row0 > v) {
+      t.seq[v] = static_cast<int>(b);
+      atomicOr(&t.starts[v >> 5], 1u << (v & 31));
+    }
+    if (in && v > 0 && b > 0 && a.cu[b - 1] - row0 < v) {
+      t.seq[v - 1] = static_cast<int>(b - 1);
+      atomicOr(&t.ends[(v - 1) >> 5], 1u << ((v - 1) & 31));
+    }
     if (!__all_sync(0xffffffffu, in)) break;
   }
+  __syncwarp();
+  return found;
 }
 
-// Sequences without rows keep their state: out = in (0 where there is none).  By one block.
+// Sequences without rows keep their state: out = in (0 where there is none).
 __device__ __forceinline__ void pass_empty(const ScanArgs& a, const float* in, float* out, int c0, int block, int blocks) {
   if (out == nullptr || (a.cu == nullptr && a.L > 0)) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   for (int64_t b = int64_t(block) * kWarps + warp; b < a.B; b += int64_t(blocks) * kWarps) {
-    bool empty = a.cu == nullptr && a.L == 0;
-    if (a.cu != nullptr) {
-      const int32_t lo = a.cu[b], hi = a.cu[b + 1];
-      empty = hi <= lo;
-      if ((hi < lo || lo < 0 || hi > a.T) && lane == 0 && c0 == 0) atomicOr(a.err, kDevErrUnsortedGroups);
-    }
-    if (!empty) continue;
+    if (a.cu != nullptr && a.cu[b + 1] > a.cu[b]) continue;
     for (int c = c0 + lane; c < min(c0 + kStrip, a.H); c += 32) out[b * a.H + c] = in ? in[b * a.H + c] : 0.f;
   }
 }
-
-template <class T, int kForm, bool kPair>
-__global__ void __launch_bounds__(kWarps * 32) scan_fwd_kernel(const ScanArgs a) {
-  __shared__ TileRows rows;
-  __shared__ float2 map_a[kWarps][32], map_b[kWarps][32];
-  __shared__ int cut[kWarps];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int c0 = blockIdx.x * kStrip, c = c0 + 2 * lane, left = a.H - c;
-  const T* gate = static_cast<const T*>(a.gate);
-  const T* value = static_cast<const T*>(a.value);
-  T* y = static_cast<T*>(a.y);
-  float2 carry = make_float2(0.f, 0.f);
-  const auto initial = [&](int b) {
-    return a.h0 ? load2<kPair>(a.h0 + int64_t(b) * a.H + c, left) : make_float2(0.f, 0.f);
-  };
-  pass_empty(a, a.h0, a.final_state, c0, 0, 1);
-  for (int64_t row0 = 0; row0 < a.T; row0 += kTile) {
-    if (warp == 0) mark_rows(a, row0, rows, lane);
-    if (a.states && warp == kWarps - 1)
-      store2<kPair>(a.states + row0 / kTile * a.H + c, carry.x, carry.y, left);
-    const int r = warp * kRows;
-    const int n = static_cast<int>(min(int64_t(kRows), a.T - row0 - r));   // may be negative
-    float2 na[kRows], v[kRows];
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      na[i] = v[i] = make_float2(0.f, 0.f);
-      if (i < n) {
-        na[i] = load2<kPair>(gate + (row0 + r + i) * a.gate_ld + c, left);
-        v[i] = load2<kPair>(value + (row0 + r + i) * a.value_ld + c, left);
-      }
-    }
-    __syncthreads();   // rows
-    float2 A = make_float2(1.f, 1.f), h = make_float2(0.f, 0.f);
-    bool has_cut = false;
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      na[i].x = one_minus_a<kForm>(na[i].x);
-      na[i].y = one_minus_a<kForm>(na[i].y);
-      if (r + i < rows.lo || r + i >= rows.hi) continue;
-      const int b = rows.start[r + i];
-      if (b >= 0) {
-        h = initial(b);
-        has_cut = true;
-      }
-      h.x = step<kForm>(h.x, na[i].x, v[i].x);
-      h.y = step<kForm>(h.y, na[i].y, v[i].y);
-      A.x = fmaf(-na[i].x, A.x, A.x);
-      A.y = fmaf(-na[i].y, A.y, A.y);
-    }
-    map_a[warp][lane] = A;
-    map_b[warp][lane] = h;
-    if (lane == 0) cut[warp] = has_cut;
-    __syncthreads();
-    float2 in = carry;   // the state that enters this warp's rows
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      if (w == warp) in = carry;
-      const float2 pa = map_a[w][lane], pb = map_b[w][lane];
-      carry.x = cut[w] ? pb.x : fmaf(pa.x, carry.x, pb.x);
-      carry.y = cut[w] ? pb.y : fmaf(pa.y, carry.y, pb.y);
-    }
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      if (r + i < rows.lo || r + i >= rows.hi) {
-        if (a.fill && i < n) store2<kPair>(y + (row0 + r + i) * a.H + c, 0.f, 0.f, left);
-        continue;
-      }
-      const int b = rows.start[r + i], e = rows.end[r + i];
-      if (b >= 0) in = initial(b);
-      in.x = step<kForm>(in.x, na[i].x, v[i].x);
-      in.y = step<kForm>(in.y, na[i].y, v[i].y);
-      store2<kPair>(y + (row0 + r + i) * a.H + c, in.x, in.y, left);
-      if (e >= 0 && a.final_state) store2<kPair>(a.final_state + int64_t(e) * a.H + c, in.x, in.y, left);
-    }
-    __syncthreads();   // rows and maps are free
-  }
+// cu_seqlens that descend or leave the rows are reported.
+__device__ __forceinline__ void check_bounds(const ScanArgs& a, int block, int blocks) {
+  if (a.cu == nullptr) return;
+  bool bad = false;
+  for (int64_t b = int64_t(block) * (kWarps * 32) + threadIdx.x; b <= a.B; b += int64_t(blocks) * (kWarps * 32))
+    bad |= a.cu[b] < 0 || a.cu[b] > a.T || (b > 0 && a.cu[b] < a.cu[b - 1]);
+  if (bad) atomicOr(a.err, kDevErrUnsortedGroups);
 }
 
-template <class T, int kForm, bool kPair>
-__global__ void __launch_bounds__(kWarps * 32) scan_bwd_kernel(const ScanArgs a) {
-  __shared__ TileRows rows;
-  __shared__ float2 map_a[kWarps][32], map_b[kWarps][32], map_e[kWarps][32];
-  __shared__ int cut_h[kWarps], cut_e[kWarps];
+// An affine map of two channels' states, h -> A h + b, with a cut in A's sign (A of a map
+// that has none is not negative).
+struct Map {
+  F2 A, b;
+};
+__device__ __forceinline__ float4 pack(Map m, bool cut) {
+  return make_float4(cut ? -1.f : m.A.x(), cut ? -1.f : m.A.y(), m.b.x(), m.b.y());
+}
+// m applied to h
+__device__ __forceinline__ F2 apply(const float4& m, F2 h) {
+  return f2(m.x < 0.f ? m.z : fmaf(m.x, h.x(), m.z), m.y < 0.f ? m.w : fmaf(m.y, h.y(), m.w));
+}
+// first m, then n
+__device__ __forceinline__ float4 compose(const float4& m, const float4& n) {
+  const F2 b = apply(n, f2(m.z, m.w));
+  const bool cut = n.x < 0.f || m.x < 0.f || n.y < 0.f || m.y < 0.f;   // in both channels at once
+  return make_float4(cut ? -1.f : m.x * n.x, cut ? -1.f : m.y * n.y, b.x(), b.y());
+}
+
+// What the warps of a block and the blocks of a cluster tell one another in a step.  Two
+// slots for the peers, so that one a step ahead does not write what is still read.
+struct Exchange {
+  float4 warps[kWarps][32];
+  float4 peers[2][kMaxCluster - 1][32];
+};
+
+__device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory"); }
+
+// A stage is the tile's rows of each tensor.  As many as leave room for two blocks to an SM (one
+// of fp32).
+template <class T, int kTensors>
+constexpr int kStageBytesOf = kTensors * kTile * kStrip * static_cast<int>(sizeof(T));
+template <int kTensors>
+constexpr int kStagesOf = kTensors == 2 ? 3 : 2;
+
+// kBwd: rows from the last one backwards.  kMapOnly: a segment's map alone.  kFast: tiles by TMA
+// and pairs of channels; else elements one by one from any address.
+template <class T, int kForm, bool kBwd, bool kMapOnly, bool kFast>
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) scan_kernel(const __grid_constant__ ScanMaps maps,
+                                                                              const ScanArgs a) {
+  // tensors of a tile: gate, value (the backward's map needs none), dy
+  constexpr bool kValue = !(kBwd && kMapOnly);
+  constexpr int kTensors = kBwd && !kMapOnly ? 3 : 2, kV = 1, kD = kValue ? 2 : 1;
+  constexpr int kStages = kStagesOf<kTensors>;
+  constexpr int kStageBytes = kStageBytesOf<T, kTensors>, kTensorBytes = kStageBytes / kTensors;
+  extern __shared__ __align__(128) uint8_t smem_raw[];
+  __shared__ __align__(16) Exchange ex;
+  __shared__ float4 h_maps[kBwd && !kMapOnly ? kWarps : 1][32];
+  __shared__ TileRows rows_sh[kStages];
+  __shared__ __align__(8) uint64_t full_bar[kStages], empty_bar[kStages], peer_bar[2];
+  __shared__ int abort_sh;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int c0 = blockIdx.x * kStrip, c = c0 + 2 * lane, left = a.H - c;
-  const T* gate = static_cast<const T*>(a.gate);
-  const T* value = static_cast<const T*>(a.value);
-  const T* dy = static_cast<const T*>(a.dy);
-  T* dgate = static_cast<T*>(a.dgate);
-  T* dvalue = static_cast<T*>(a.dvalue);
-  float2 back = make_float2(0.f, 0.f);   // E of the row after the tile
-  const auto of_seq = [&](const float* p, int b) {
-    return p ? load2<kPair>(p + int64_t(b) * a.H + c, left) : make_float2(0.f, 0.f);
+  volatile int* abort_flag = &abort_sh;
+  uint32_t size;
+  asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(size));
+  const int S = static_cast<int>(size), rank = static_cast<int>(cluster_ctarank());
+  const int strip = blockIdx.x / S, strips = gridDim.x / S;
+  const int c0 = strip * kStrip, c = c0 + 2 * lane, left = a.H - c;
+  const int seg = blockIdx.y, seg0 = seg * a.seg_tiles, seg_n = min(a.seg_tiles, a.tiles - seg0);
+  const int n_steps = (seg_n + S - 1) / S;
+  // the tile of step k, or -1
+  auto tile_of = [&](int k) -> int {
+    const int i = k * S + rank;
+    return i >= seg_n ? -1 : kBwd ? seg0 + seg_n - 1 - i : seg0 + i;
   };
-  pass_empty(a, a.dfinal, a.dinit, c0, 0, 1);
-  const int64_t tiles = (a.T + kTile - 1) / kTile;
-  for (int64_t tile = tiles - 1; tile >= 0; --tile) {
-    const int64_t row0 = tile * kTile;
-    if (warp == 0) mark_rows(a, row0, rows, lane);
-    const int r = warp * kRows;
-    const int n = static_cast<int>(min(int64_t(kRows), a.T - row0 - r));   // may be negative
-    float2 na[kRows], v[kRows], d[kRows], hp[kRows];
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      na[i] = v[i] = d[i] = make_float2(0.f, 0.f);
-      if (i < n) {
-        na[i] = load2<kPair>(gate + (row0 + r + i) * a.gate_ld + c, left);
-        v[i] = load2<kPair>(value + (row0 + r + i) * a.value_ld + c, left);
-        d[i] = load2<kPair>(dy + (row0 + r + i) * a.dy_ld + c, left);
-      }
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(smem_u32(&full_bar[s]), kFast ? 2 : 1);
+      mbar_init(smem_u32(&empty_bar[s]), kWarps);
     }
-    __syncthreads();   // rows
-    float2 A = make_float2(1.f, 1.f), h = make_float2(0.f, 0.f), E = make_float2(0.f, 0.f);
-    bool ch = false, ce = false;
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      na[i].x = one_minus_a<kForm>(na[i].x);
-      na[i].y = one_minus_a<kForm>(na[i].y);
-      if (r + i < rows.lo || r + i >= rows.hi) continue;
-      const int b = rows.start[r + i];
-      if (b >= 0) {
-        h = of_seq(a.h0, b);
-        ch = true;
-      }
-      h.x = step<kForm>(h.x, na[i].x, v[i].x);
-      h.y = step<kForm>(h.y, na[i].y, v[i].y);
-      A.x = fmaf(-na[i].x, A.x, A.x);
-      A.y = fmaf(-na[i].y, A.y, A.y);
-    }
-#pragma unroll
-    for (int i = kRows - 1; i >= 0; --i) {
-      if (r + i < rows.lo || r + i >= rows.hi) continue;
-      const int e = rows.end[r + i];
-      if (e >= 0) {
-        E = of_seq(a.dfinal, e);
-        ce = true;
-      }
-      E.x += d[i].x;
-      E.y += d[i].y;
-      E.x = fmaf(-na[i].x, E.x, E.x);
-      E.y = fmaf(-na[i].y, E.y, E.y);
-    }
-    map_a[warp][lane] = A;
-    map_b[warp][lane] = h;
-    map_e[warp][lane] = E;
-    if (lane == 0) {
-      cut_h[warp] = ch;
-      cut_e[warp] = ce;
-    }
-    __syncthreads();
-    float2 in = load2<kPair>(a.states + tile * a.H + c, left);
-    for (int w = 0; w < warp; ++w) {
-      const float2 pa = map_a[w][lane], pb = map_b[w][lane];
-      in.x = cut_h[w] ? pb.x : fmaf(pa.x, in.x, pb.x);
-      in.y = cut_h[w] ? pb.y : fmaf(pa.y, in.y, pb.y);
-    }
-    float2 out = back;
-#pragma unroll
-    for (int w = kWarps - 1; w >= 0; --w) {
-      if (w == warp) out = back;
-      const float2 pa = map_a[w][lane], pe = map_e[w][lane];
-      back.x = cut_e[w] ? pe.x : fmaf(pa.x, back.x, pe.x);
-      back.y = cut_e[w] ? pe.y : fmaf(pa.y, back.y, pe.y);
-    }
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      if (r + i < rows.lo || r + i >= rows.hi) continue;
-      const int b = rows.start[r + i];
-      if (b >= 0) in = of_seq(a.h0, b);
-      hp[i] = in;
-      in.x = step<kForm>(in.x, na[i].x, v[i].x);
-      in.y = step<kForm>(in.y, na[i].y, v[i].y);
-    }
-#pragma unroll
-    for (int i = kRows - 1; i >= 0; --i) {
-      if (r + i < rows.lo || r + i >= rows.hi) {
-        if (i < n) {
-          store2<kPair>(dgate + (row0 + r + i) * a.H + c, 0.f, 0.f, left);
-          store2<kPair>(dvalue + (row0 + r + i) * a.H + c, 0.f, 0.f, left);
-        }
-        continue;
-      }
-      const int b = rows.start[r + i], e = rows.end[r + i];
-      if (e >= 0) out = of_seq(a.dfinal, e);
-      const float2 D = make_float2(d[i].x + out.x, d[i].y + out.y);
-      out.x = fmaf(-na[i].x, D.x, D.x);   // E
-      out.y = fmaf(-na[i].y, D.y, D.y);
-      float2 df, dv = D;
-      if constexpr (kForm == kFormSigmoid) {
-        dv = make_float2(D.x * na[i].x, D.y * na[i].y);
-        df = make_float2(out.x * na[i].x * (hp[i].x - v[i].x), out.y * na[i].y * (hp[i].y - v[i].y));
-      } else {
-        df = make_float2(out.x * hp[i].x, out.y * hp[i].y);
-      }
-      store2<kPair>(dgate + (row0 + r + i) * a.H + c, df.x, df.y, left);
-      store2<kPair>(dvalue + (row0 + r + i) * a.H + c, dv.x, dv.y, left);
-      if (b >= 0 && a.dinit) store2<kPair>(a.dinit + int64_t(b) * a.H + c, out.x, out.y, left);
-    }
-    __syncthreads();   // rows and maps are free
+    for (int s = 0; s < 2; ++s) mbar_init(smem_u32(&peer_bar[s]), 1);
+    abort_sh = 0;
+    fence_mbar_init();
   }
+  __syncthreads();
+  cluster_sync_all();   // every block's barriers exist before a peer's message
+
+  if (warp == kWarps) {
+    // tiles, and their rows' bounds, ahead of the others
+    int64_t at = kBwd ? a.B + 1 : 0;
+    int issued = 0;
+    for (int k = 0; k < n_steps; ++k) {
+      const int tile = tile_of(k), st = k % kStages;
+      if (tile < 0) break;
+      if (!mbar_wait(smem_u32(&empty_bar[st]), ((k / kStages) & 1u) ^ 1u, abort_flag, a.err)) break;
+      if (kFast && lane == 0) {
+        const uint32_t bar = smem_u32(&full_bar[st]), dst = smem_u32(smem_raw) + st * kStageBytes;
+        mbar_arrive_expect_tx(bar, kStageBytes);
+        tma_load_2d(dst, &maps.gate, bar, c0, tile * kTile);
+        if constexpr (kValue) tma_load_2d(dst + kV * kTensorBytes, &maps.value, bar, c0, tile * kTile);
+        if constexpr (kBwd) tma_load_2d(dst + kD * kTensorBytes, &maps.dy, bar, c0, tile * kTile);
+      }
+      ++issued;
+      at = mark_rows<kBwd>(a, int64_t(tile) * kTile, rows_sh[st], at, lane);
+      if (lane == 0) mbar_arrive(smem_u32(&full_bar[st]));
+    }
+    // copies land in this block's memory: wait for the last ones before it may exit
+    if (lane == 0)
+      for (int k = max(0, issued - kStages); k < issued; ++k)
+        mbar_wait_drain(smem_u32(&full_bar[k % kStages]), (k / kStages) & 1u, a.err);
+  } else {
+    if (!kMapOnly && seg == 0) {
+      pass_empty(a, kBwd ? a.dfinal : a.h0, kBwd ? a.dinit : a.final_state, c0, rank, S);
+      if (strip == 0) check_bounds(a, rank, S);
+    }
+    const int r0 = warp * kRows;
+    const auto of_seq = [&](const float* p, int b) { return p ? load2<kFast>(p + int64_t(b) * a.H + c, left) : zero2(); };
+    const float4 identity = make_float4(1.f, 1.f, 0.f, 0.f);
+    // the state before the segment (E after it)
+    F2 carry = zero2();
+    float4 total = identity;
+    if constexpr (!kMapOnly) {
+      for (int s = kBwd ? static_cast<int>(gridDim.y) - 1 : 0; s != seg; s += kBwd ? -1 : 1)
+        carry = apply(a.seg_maps[(int64_t(s) * strips + strip) * 32 + lane], carry);
+    }
+    bool alive = true;   // no wait has run out; else the loop goes on without work, for the barriers' sake
+    for (int k = 0; k < n_steps; ++k) {
+      const int st = k % kStages, slot = k & 1;
+      int tile = alive ? tile_of(k) : -1;
+      const TileRows& rows = rows_sh[st];
+      if (threadIdx.x == 0 && S > 1) mbar_arrive_expect_tx(smem_u32(&peer_bar[slot]), (S - 1) * 512);
+      F2 h = zero2();      // backward: the state before the tile, then before the warp's rows
+      if (tile >= 0) {
+        if constexpr (kBwd && !kMapOnly) h = load2<kFast>(a.states + int64_t(tile) * a.H + c, left);
+        if (!mbar_wait(smem_u32(&full_bar[st]), (k / kStages) & 1u, abort_flag, a.err)) {
+          alive = false;
+          tile = -1;
+        }
+      }
+      const int64_t row = int64_t(tile) * kTile + r0;   // the warp's first
+      uint32_t starts = 0, ends = 0;
+      bool whole = true;                                // all of its rows are in sequences
+      if (tile >= 0) {
+        starts = rows.starts[r0 >> 5] >> (r0 & 31) & 0xffffu;
+        ends = rows.ends[r0 >> 5] >> (r0 & 31) & 0xffffu;
+        whole = rows.lo <= r0 && rows.hi >= r0 + kRows;
+      }
+      const bool simple = whole && (starts | ends) == 0;
+      auto inside = [&](int i) { return r0 + i >= rows.lo && r0 + i < rows.hi; };
+      const T* const stage = reinterpret_cast<const T*>(smem_raw + st * kStageBytes) + r0 * kStrip + 2 * lane;
+      auto get = [&](int tensor, int i) -> F2 {
+        if constexpr (kFast) return load2<true>(stage + tensor * (kTile * kStrip) + i * kStrip, 2);
+        if (row + i >= a.T) return zero2();
+        const void* const p = tensor == 0 ? a.gate : kValue && tensor == kV ? a.value : a.dy;
+        const int64_t ld = tensor == 0 ? a.gate_ld : kValue && tensor == kV ? a.value_ld : a.dy_ld;
+        return load2<false>(static_cast<const T*>(p) + (row + i) * ld + c, left);
+      };
+
+      // ---- the maps of the warp's rows
+      F2 m[kRows];
+      float4 mine = identity, mine_h = identity;
+      if (tile >= 0) {
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) m[i] = decay<kForm>(get(0, i));
+        F2 A = f2(1.f), x = zero2(), z = zero2();   // x: the walk's, z: h in a backward walk
+        bool cut = false, cut_z = false;
+        if (simple) {
+#pragma unroll
+          for (int i = 0; i < kRows; ++i) {
+            A = fma2(m[i], A, A);
+            if constexpr (!kBwd) x = step<kForm>(x, m[i], get(kV, i));
+            if constexpr (kBwd && !kMapOnly) z = step<kForm>(z, m[i], get(kV, i));
+          }
+          if constexpr (kBwd) {
+#pragma unroll
+            for (int i = kRows - 1; i >= 0; --i) {
+              x = add2(x, get(kD, i));
+              x = fma2(m[i], x, x);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < kRows; ++i) {
+            if (!inside(i)) continue;
+            A = fma2(m[i], A, A);
+            if constexpr (!kBwd || !kMapOnly) {
+              F2& w = kBwd ? z : x;
+              if (starts >> i & 1u) {
+                w = of_seq(a.h0, rows.seq[r0 + i]);
+                (kBwd ? cut_z : cut) = true;
+              }
+              w = step<kForm>(w, m[i], get(kV, i));
+            }
+          }
+          if constexpr (kBwd) {
+#pragma unroll
+            for (int i = kRows - 1; i >= 0; --i) {
+              if (!inside(i)) continue;
+              if (ends >> i & 1u) {
+                x = of_seq(a.dfinal, rows.seq[r0 + i]);
+                cut = true;
+              }
+              x = add2(x, get(kD, i));
+              x = fma2(m[i], x, x);
+            }
+          }
+        }
+        mine = pack(Map{A, x}, cut);
+        if constexpr (kBwd && !kMapOnly) mine_h = pack(Map{A, z}, cut_z);
+      }
+      ex.warps[warp][lane] = mine;
+      if constexpr (kBwd && !kMapOnly) h_maps[warp][lane] = mine_h;
+      consumer_sync();
+      // ---- the tile's map, to all blocks of the cluster
+      auto tile_map = [&]() {
+        float4 t = identity;
+#pragma unroll
+        for (int j = 0; j < kWarps; ++j) t = compose(t, ex.warps[kBwd ? kWarps - 1 - j : j][lane]);
+        return t;
+      };
+      if (S > 1) {
+        if (warp == 0) {
+          const float4 t = tile_map();
+          const int4 bits = make_int4(__float_as_int(t.x), __float_as_int(t.y), __float_as_int(t.z), __float_as_int(t.w));
+          const uint32_t bar = smem_u32(&peer_bar[slot]);
+          for (int p = 0; p < S; ++p)
+            if (p != rank) st_async_v4(mapa_shared(smem_u32(&ex.peers[slot][rank < p ? rank : rank - 1][lane]), p),
+                                       mapa_shared(bar, p), bits);
+        }
+        if (!mbar_wait(smem_u32(&peer_bar[slot]), (k >> 1) & 1u, abort_flag, a.err)) {
+          alive = false;
+          tile = -1;
+        }
+      }
+      // ---- what enters the warp's rows, and the step after
+      F2 in = carry;
+      for (int p = 0; p < S; ++p) {
+        const float4* const peer = &ex.peers[slot][p < rank ? p : p - 1][lane];
+        if constexpr (kMapOnly) {
+          total = compose(total, p == rank ? tile_map() : *peer);
+        } else if (p != rank) {
+          carry = apply(*peer, carry);
+        } else {
+          if (!kBwd && tile >= 0 && a.states && warp == 0) store2<kFast>(a.states + int64_t(tile) * a.H + c, carry, left);
+#pragma unroll
+          for (int j = 0; j < kWarps; ++j) {
+            const int w = kBwd ? kWarps - 1 - j : j;
+            if (w == warp) in = carry;
+            carry = apply(ex.warps[w][lane], carry);
+          }
+        }
+      }
+      if constexpr (kBwd && !kMapOnly)
+        for (int w = 0; w < warp; ++w) h = apply(h_maps[w][lane], h);
+      consumer_sync();   // the warps' maps are read
+
+      // ---- the rows again
+      if (tile >= 0) {
+        if constexpr (!kBwd && !kMapOnly) {
+          T* y = static_cast<T*>(a.y) + row * a.H + c;
+          if (simple) {
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+              in = step<kForm>(in, m[i], get(kV, i));
+              store2<kFast>(y + int64_t(i) * a.H, in, left);
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+              if (!inside(i)) {
+                if (a.fill && row + i < a.T) store2<kFast>(y + int64_t(i) * a.H, zero2(), left);
+                continue;
+              }
+              if (starts >> i & 1u) in = of_seq(a.h0, rows.seq[r0 + i]);
+              in = step<kForm>(in, m[i], get(kV, i));
+              store2<kFast>(y + int64_t(i) * a.H, in, left);
+              if ((ends >> i & 1u) && a.final_state) store2<kFast>(a.final_state + int64_t(rows.seq[r0 + i]) * a.H + c, in, left);
+            }
+          }
+        } else if constexpr (!kMapOnly) {
+          T* dg = static_cast<T*>(a.dgate) + row * a.H + c;
+          T* dv = static_cast<T*>(a.dvalue) + row * a.H + c;
+          F2 hp[kRows];   // h of the row before
+#pragma unroll
+          for (int i = 0; i < kRows; ++i) {
+            if (!simple && !inside(i)) continue;
+            if (starts >> i & 1u) h = of_seq(a.h0, rows.seq[r0 + i]);
+            hp[i] = h;
+            h = step<kForm>(h, m[i], get(kV, i));
+          }
+#pragma unroll
+          for (int i = kRows - 1; i >= 0; --i) {
+            if (!simple && !inside(i)) {
+              if (row + i < a.T) {
+                store2<kFast>(dg + int64_t(i) * a.H, zero2(), left);
+                store2<kFast>(dv + int64_t(i) * a.H, zero2(), left);
+              }
+              continue;
+            }
+            if (ends >> i & 1u) in = of_seq(a.dfinal, rows.seq[r0 + i]);
+            const F2 D = add2(get(kD, i), in);
+            in = fma2(m[i], D, D);   // E
+            if constexpr (kForm == kFormSigmoid) {
+              const F2 w = mul2(m[i], f2(-1.f));
+              store2<kFast>(dg + int64_t(i) * a.H, mul2(mul2(in, w), sub2(hp[i], get(kV, i))), left);
+              store2<kFast>(dv + int64_t(i) * a.H, mul2(D, w), left);
+            } else {
+              store2<kFast>(dg + int64_t(i) * a.H, mul2(in, hp[i]), left);
+              store2<kFast>(dv + int64_t(i) * a.H, D, left);
+            }
+            if ((starts >> i & 1u) && a.dinit) store2<kFast>(a.dinit + int64_t(rows.seq[r0 + i]) * a.H + c, in, left);
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&empty_bar[st]));
+      }
+    }
+    if (kMapOnly && warp == 0 && rank == 0) a.seg_maps[(int64_t(seg) * strips + strip) * 32 + lane] = total;
+  }
+  __syncthreads();
+  cluster_sync_all();   // no block leaves while a peer may still write to it
 }
 
 template <class T, int kForm>
@@ -386,10 +553,10 @@ __global__ void __launch_bounds__(256) scan_step_kernel(const T* gate, const T* 
   for (int64_t i = blockIdx.x * int64_t(256) + threadIdx.x; i < n; i += gridDim.x * int64_t(256)) {
     const int64_t b = i / H;
     const int c = static_cast<int>(i - b * H);
-    const float h = step<kForm>(state[i], one_minus_a<kForm>(to_float(gate[b * gate_ld + c])),
-                                to_float(value[b * value_ld + c]));
-    state_out[i] = h;
-    from_float(h, y[i]);
+    const F2 h = step<kForm>(f2(state[i]), decay<kForm>(f2(to_float(gate[b * gate_ld + c]))),
+                             f2(to_float(value[b * value_ld + c])));
+    state_out[i] = h.x();
+    from_float(h.x(), y[i]);
   }
 }
 
@@ -441,44 +608,108 @@ ScanArgs base_args(const molt_scan_desc* d, const int32_t* cu) {
   return a;
 }
 
-// rows and vectors can be read two channels at a time
-bool pairs_of(const ScanArgs& a, int dtype) {
-  const size_t n = 2 * static_cast<size_t>(dtype_bytes(dtype));
+// Tiles can come by TMA and vectors be read two channels at a time.
+bool fast_of(const ScanArgs& a, int dtype) {
+  const size_t e = static_cast<size_t>(dtype_bytes(dtype));
   const auto at = [](const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; };
-  for (const void* p : {a.gate, a.value, a.dy, static_cast<const void*>(a.y), static_cast<const void*>(a.dgate),
-                        static_cast<const void*>(a.dvalue)})
-    if (!at(p, n)) return false;
-  for (const void* p : {static_cast<const void*>(a.h0), static_cast<const void*>(a.dfinal),
-                        static_cast<const void*>(a.final_state), static_cast<const void*>(a.states),
-                        static_cast<const void*>(a.dinit)})
+  for (const void* p : {a.gate, a.value, a.dy})
+    if (!at(p, 16)) return false;
+  for (const void* p : {a.y, a.dgate, a.dvalue})
+    if (!at(p, 2 * e)) return false;
+  for (const float* p : {a.h0, a.dfinal, static_cast<const float*>(a.final_state), static_cast<const float*>(a.states),
+                         static_cast<const float*>(a.dinit)})
     if (!at(p, 8)) return false;
-  return a.H % 2 == 0 && a.gate_ld % 2 == 0 && a.value_ld % 2 == 0 && a.dy_ld % 2 == 0;
+  return a.H % 2 == 0 && a.gate_ld * e % 16 == 0 && a.value_ld * e % 16 == 0 && a.dy_ld * e % 16 == 0;
 }
 
-template <class T, int kForm>
-cudaError_t launch_scan(const ScanArgs& a, bool bwd, bool pair, cudaStream_t s) {
-  const int grid = (a.H + kStrip - 1) / kStrip;
+constexpr int kMaxSegments = 32;
+int64_t strips_of(const molt_scan_desc* d) { return (d->H + kStrip - 1) / kStrip; }
+size_t seg_bytes(const molt_scan_desc* d) { return static_cast<size_t>(kMaxSegments) * strips_of(d) * 32 * sizeof(float4) + 256; }
+
+struct ScanPlan {
+  int cluster, segments;
+};
+ScanPlan plan_of(const molt_scan_desc* d, int tiles, int n_sm) {
+  const int64_t strips = strips_of(d), slots = int64_t(n_sm) * (d->dtype == MOLT_FP32 ? 1 : 2);
+  ScanPlan p;
+  p.cluster = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({kMaxCluster, slots / strips, tiles})));
+  const int64_t room = slots / (strips * p.cluster), steps = (tiles + p.cluster - 1) / p.cluster;
+  p.segments = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({kMaxSegments, room, steps / 8})));
+  return p;
+}
+
+template <class T, int kForm, bool kBwd, bool kMapOnly, bool kFast>
+cudaError_t launch_kernel(const ScanMaps& m, const ScanArgs& a, int strips, int cluster, int segments, cudaStream_t s) {
+  constexpr int kTensors = kBwd && !kMapOnly ? 3 : 2;
+  constexpr int smem = kFast ? kStagesOf<kTensors> * kStageBytesOf<T, kTensors> : 0;
+  const auto k = &scan_kernel<T, kForm, kBwd, kMapOnly, kFast>;
+  if (const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem); e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(strips * cluster, segments);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = cluster;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, k, m, a);
+}
+template <class T, int kForm, bool kFast>
+cudaError_t launch_form(const ScanMaps& m, const ScanArgs& a, bool bwd, bool map_only, int strips, int cluster, int segments,
+                        cudaStream_t s) {
   if (bwd)
-    (pair ? scan_bwd_kernel<T, kForm, true> : scan_bwd_kernel<T, kForm, false>)<<<grid, kWarps * 32, 0, s>>>(a);
-  else
-    (pair ? scan_fwd_kernel<T, kForm, true> : scan_fwd_kernel<T, kForm, false>)<<<grid, kWarps * 32, 0, s>>>(a);
-  return cudaGetLastError();
+    return map_only ? launch_kernel<T, kForm, true, true, kFast>(m, a, strips, cluster, segments, s)
+                    : launch_kernel<T, kForm, true, false, kFast>(m, a, strips, cluster, segments, s);
+  return map_only ? launch_kernel<T, kForm, false, true, kFast>(m, a, strips, cluster, segments, s)
+                  : launch_kernel<T, kForm, false, false, kFast>(m, a, strips, cluster, segments, s);
 }
 template <class T>
-cudaError_t launch_scan(const ScanArgs& a, int form, bool bwd, bool pair, cudaStream_t s) {
-  return form == kFormSigmoid ? launch_scan<T, kFormSigmoid>(a, bwd, pair, s) : launch_scan<T, kFormLog>(a, bwd, pair, s);
+cudaError_t launch_type(const ScanMaps& m, const ScanArgs& a, int form, bool fast, bool bwd, bool map_only, int strips, int cluster,
+                        int segments, cudaStream_t s) {
+  const auto k = form == kFormSigmoid ? (fast ? launch_form<T, kFormSigmoid, true> : launch_form<T, kFormSigmoid, false>)
+                                      : (fast ? launch_form<T, kFormLog, true> : launch_form<T, kFormLog, false>);
+  return k(m, a, bwd, map_only, strips, cluster, segments, s);
 }
 
-molt_status launch(const molt_scan_desc* d, ScanArgs& a, bool bwd, cudaStream_t s) {
+molt_status launch(const molt_scan_desc* d, ScanArgs& a, bool bwd, void* workspace, size_t workspace_bytes, cudaStream_t s) {
   molt_status st;
   a.err = device_status_word(&st);
   if (!a.err) return st;
-  const bool pair = pairs_of(a, d->dtype);
-  const cudaError_t e = d->dtype == MOLT_FP32   ? launch_scan<float>(a, d->form, bwd, pair, s)
-                        : d->dtype == MOLT_FP16 ? launch_scan<__half>(a, d->form, bwd, pair, s)
-                                                : launch_scan<__nv_bfloat16>(a, d->form, bwd, pair, s);
-  if (e != cudaSuccess) return cuda_fail(e, "gated scan");
-  note_launches(1);
+  const int strips = static_cast<int>(strips_of(d));
+  a.tiles = static_cast<int>((a.T + kTile - 1) / kTile);
+  const ScanPlan plan = plan_of(d, a.tiles, device_sm_count());
+  a.seg_tiles = (a.tiles + plan.segments - 1) / plan.segments;
+  const int segments = a.tiles > 0 ? (a.tiles + a.seg_tiles - 1) / a.seg_tiles : 1;
+  Scratch sc;
+  if (segments > 1) {
+    if (const molt_status e = get_scratch(sc, workspace, workspace_bytes, seg_bytes(d), s); e != MOLT_OK) return e;
+    a.seg_maps = static_cast<float4*>(sc.aligned());
+  }
+  const bool fast = a.tiles > 0 && fast_of(a, d->dtype);
+  ScanMaps m{};
+  if (fast) {
+    const int e = dtype_bytes(d->dtype);
+    const auto encode = [&](CUtensorMap* t, const void* p, int64_t ld) {
+      return encode_tmap_plain(t, e == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, e, p, a.T, a.H, ld,
+                               kStrip, kTile);
+    };
+    if (const molt_status q = encode(&m.gate, a.gate, a.gate_ld); q != MOLT_OK) return q;
+    if (const molt_status q = encode(&m.value, a.value, a.value_ld); q != MOLT_OK) return q;
+    if (bwd)
+      if (const molt_status q = encode(&m.dy, a.dy, a.dy_ld); q != MOLT_OK) return q;
+  }
+  for (int pass = segments > 1 ? 0 : 1; pass < 2; ++pass) {
+    const bool map_only = pass == 0;
+    const cudaError_t e =
+        d->dtype == MOLT_FP32   ? launch_type<float>(m, a, d->form, fast, bwd, map_only, strips, plan.cluster, segments, s)
+        : d->dtype == MOLT_FP16 ? launch_type<__half>(m, a, d->form, fast, bwd, map_only, strips, plan.cluster, segments, s)
+                                : launch_type<__nv_bfloat16>(m, a, d->form, fast, bwd, map_only, strips, plan.cluster, segments, s);
+    if (e != cudaSuccess) return cuda_fail(e, "gated scan");
+    note_launches(1);
+  }
   return MOLT_OK;
 }
 
@@ -497,9 +728,13 @@ using namespace molt;
 
 extern "C" {
 
+size_t molt_gated_scan_workspace_bytes(const molt_scan_desc* desc) {
+  return check_desc(desc, true) == MOLT_OK ? seg_bytes(desc) : 0;
+}
+
 molt_status molt_gated_scan_fwd(const molt_scan_desc* desc, const void* gate, const void* value, const float* initial_state,
-                                const int32_t* cu_seqlens, void* y, float* final_state, float* states,
-                                cudaStream_t stream) {
+                                const int32_t* cu_seqlens, void* y, float* final_state, float* states, void* workspace,
+                                size_t workspace_bytes, cudaStream_t stream) {
   if (const molt_status st = check_desc(desc, cu_seqlens != nullptr); st != MOLT_OK) return st;
   if (desc->T > 0 && (!gate || !value || !y)) return fail(MOLT_ERR_INVALID_ARG, "null pointer");
   if (const molt_status st = check_elements({{gate, desc->dtype},
@@ -512,6 +747,7 @@ molt_status molt_gated_scan_fwd(const molt_scan_desc* desc, const void* gate, co
       st != MOLT_OK)
     return st;
   if (desc->T == 0 && (desc->B == 0 || !final_state)) return MOLT_OK;
+  if (workspace && workspace_bytes < seg_bytes(desc)) return fail(MOLT_ERR_WORKSPACE, "workspace too small");
   ScanArgs a = base_args(desc, cu_seqlens);
   a.gate = gate;
   a.value = value;
@@ -520,13 +756,13 @@ molt_status molt_gated_scan_fwd(const molt_scan_desc* desc, const void* gate, co
   a.final_state = final_state;
   a.states = states;
   a.fill = desc->fill_outside != 0;
-  return launch(desc, a, false, stream);
+  return launch(desc, a, false, workspace, workspace_bytes, stream);
 }
 
 molt_status molt_gated_scan_bwd(const molt_scan_desc* desc, const void* dy, const void* gate, const void* value,
                                 const float* states, const float* initial_state, const int32_t* cu_seqlens,
                                 const float* dfinal_state, void* dgate, void* dvalue, float* dinitial_state,
-                                cudaStream_t stream) {
+                                void* workspace, size_t workspace_bytes, cudaStream_t stream) {
   if (const molt_status st = check_desc(desc, cu_seqlens != nullptr); st != MOLT_OK) return st;
   if (desc->T > 0 && (!dy || !gate || !value || !states || !dgate || !dvalue)) return fail(MOLT_ERR_INVALID_ARG, "null pointer");
   if (const molt_status st = check_elements({{dy, desc->dtype},
@@ -542,6 +778,7 @@ molt_status molt_gated_scan_bwd(const molt_scan_desc* desc, const void* dy, cons
       st != MOLT_OK)
     return st;
   if (desc->T == 0 && (desc->B == 0 || !dinitial_state)) return MOLT_OK;
+  if (workspace && workspace_bytes < seg_bytes(desc)) return fail(MOLT_ERR_WORKSPACE, "workspace too small");
   ScanArgs a = base_args(desc, cu_seqlens);
   a.dy = dy;
   a.gate = gate;
@@ -552,7 +789,7 @@ molt_status molt_gated_scan_bwd(const molt_scan_desc* desc, const void* dy, cons
   a.dgate = dgate;
   a.dvalue = dvalue;
   a.dinit = dinitial_state;
-  return launch(desc, a, true, stream);
+  return launch(desc, a, true, workspace, workspace_bytes, stream);
 }
 
 molt_status molt_gated_scan_step(const molt_scan_desc* desc, const void* gate, const void* value, const float* state,

@@ -101,13 +101,13 @@ def test_ffn_workspaces_never_shrink_as_tokens_grow(lib):
 def scan_fwd(lib, d, **kw):
     names = ("gate", "value", "h0", "cu", "y", "final", "states")
     ptr = {**{n: FAKE for n in names}, **kw}
-    return status(lib.molt_gated_scan_fwd(ctypes.byref(d), *[ptr[n] for n in names], None))
+    return status(lib.molt_gated_scan_fwd(ctypes.byref(d), *[ptr[n] for n in names], FAKE, 16, None))
 
 
 def scan_bwd(lib, d, **kw):
     names = ("dy", "gate", "value", "states", "h0", "cu", "dfinal", "dgate", "dvalue", "dinit")
     ptr = {**{n: FAKE for n in names}, **kw}
-    return status(lib.molt_gated_scan_bwd(ctypes.byref(d), *[ptr[n] for n in names], None))
+    return status(lib.molt_gated_scan_bwd(ctypes.byref(d), *[ptr[n] for n in names], FAKE, 16, None))
 
 
 def scan_step(lib, d, **kw):
@@ -151,6 +151,9 @@ def test_scan_refuses_pointers(lib):
     assert scan_step(lib, scan(T=0, B=0), gate=None) == "MOLT_OK"
     for f in (lib.molt_gated_scan_fwd, lib.molt_gated_scan_bwd, lib.molt_gated_scan_step):
         assert status(f(None, *[FAKE] * (len(f.argtypes) - 2), None)) == BAD
+    assert scan_fwd(lib, scan()) == scan_bwd(lib, scan()) == "MOLT_ERR_WORKSPACE"
+    assert lib.molt_gated_scan_workspace_bytes(ctypes.byref(scan())) > 0
+    assert lib.molt_gated_scan_workspace_bytes(ctypes.byref(scan(H=0))) == 0
 
 
 def dropout(lib, d, x=FAKE, r=None, words=None, out=2 * FAKE):
