@@ -23,8 +23,8 @@
 // Layout: a strip of channels belongs to a cluster of up to eight blocks, which take a
 // tile each, exchange their maps through one another's shared memory (512 bytes to each
 // peer) and go on together, so that the inputs are read once and a super step of 1024 rows
-// costs one exchange.  A ninth warp brings the tiles ahead (TMA, and from cu_seqlens which rows
-// begin and end a sequence).  Few strips and many rows are cut into segments besides: a first
+// costs one exchange.  Of two further warps one brings the tiles ahead (TMA, and from
+// cu_seqlens which rows begin and end a sequence), the other folds the maps.  Few strips and many rows are cut into segments besides: a first
 // launch folds each segment's map, the second starts from what precedes its own.
 #include <algorithm>
 #include <cstdint>
@@ -41,7 +41,7 @@ namespace {
 
 constexpr int kTile = 128;               // rows of a tile, and between kept states
 constexpr int kWarps = 8, kRows = kTile / kWarps;
-constexpr int kThreads = 32 * (kWarps + 1);
+constexpr int kThreads = 32 * (kWarps + 2);
 constexpr int kStrip = 64;               // channels of a block
 constexpr int kMaxCluster = 8;
 constexpr int kFormSigmoid = 0, kFormLog = 1;
@@ -68,6 +68,7 @@ struct ScanArgs {
 };
 struct ScanMaps {
   CUtensorMap gate, value, dy;   // boxes of 64 channels by 128 rows
+  CUtensorMap out0, out1;        // y, or dgate and dvalue: boxes of 64 channels by 16 rows
 };
 
 __device__ __forceinline__ float rcp_approx(float x) {
@@ -251,14 +252,17 @@ __device__ __forceinline__ float4 compose(const float4& m, const float4& n) {
   return make_float4(cut ? -1.f : m.x * n.x, cut ? -1.f : m.y * n.y, b.x(), b.y());
 }
 
-// What the warps of a block and the blocks of a cluster tell one another in a step.  Two
-// slots for the peers, so that one a step ahead does not write what is still read.
+// What the warps of a block and the blocks of a cluster tell one another in a step.  warps:
+// the map of each warp's rows, then that of all the warps before it.  Two slots for the
+// peers, so that one a step ahead does not write what is still read.
 struct Exchange {
   float4 warps[kWarps][32];
+  float4 tile[32];
   float4 peers[2][kMaxCluster - 1][32];
 };
 
-__device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory"); }
+// the eight warps with rows, and the one that folds
+__device__ __forceinline__ void maps_sync() { asm volatile("bar.sync 1, %0;" ::"n"((kWarps + 1) * 32) : "memory"); }
 
 // A stage is the tile's rows of each tensor.  As many as leave room for two blocks to an SM (one
 // of fp32).
@@ -279,7 +283,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) scan_kernel(
   constexpr int kStageBytes = kStageBytesOf<T, kTensors>, kTensorBytes = kStageBytes / kTensors;
   extern __shared__ __align__(128) uint8_t smem_raw[];
   __shared__ __align__(16) Exchange ex;
-  __shared__ float4 h_maps[kBwd && !kMapOnly ? kWarps : 1][32];
+  __shared__ float4 h_maps[kBwd && !kMapOnly ? kWarps : 1][32];   // then, in x and y, h before each warp's rows
   __shared__ TileRows rows_sh[kStages];
   __shared__ __align__(8) uint64_t full_bar[kStages], empty_bar[kStages], peer_bar[2];
   __shared__ int abort_sh;
@@ -307,6 +311,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) scan_kernel(
     abort_sh = 0;
     fence_mbar_init();
   }
+  const float4 identity = make_float4(1.f, 1.f, 0.f, 0.f);
   __syncthreads();
   cluster_sync_all();   // every block's barriers exist before a peer's message
 
@@ -333,6 +338,43 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) scan_kernel(
     if (lane == 0)
       for (int k = max(0, issued - kStages); k < issued; ++k)
         mbar_wait_drain(smem_u32(&full_bar[k % kStages]), (k / kStages) & 1u, a.err);
+  } else if (warp == kWarps + 1) {
+    // a step's maps: the tile's, for all blocks of the cluster, and what precedes each warp's rows
+    for (int k = 0; k < n_steps; ++k) {
+      const int tile = tile_of(k), slot = k & 1;
+      F2 h = zero2();   // backward: the state before the tile
+      if constexpr (kBwd && !kMapOnly)
+        if (tile >= 0) h = load2<kFast>(a.states + int64_t(tile) * a.H + c, left);
+      maps_sync();
+      float4 before[kWarps], t = identity;
+#pragma unroll
+      for (int j = 0; j < kWarps; ++j) before[j] = ex.warps[kBwd ? kWarps - 1 - j : j][lane];
+#pragma unroll
+      for (int j = 0; j < kWarps; ++j) {
+        const float4 own = before[j];
+        before[j] = t;
+        t = compose(t, own);
+      }
+      const uint32_t bar = smem_u32(&peer_bar[slot]);
+      const int4 bits = make_int4(__float_as_int(t.x), __float_as_int(t.y), __float_as_int(t.z), __float_as_int(t.w));
+      for (int p = 0; p < S; ++p)
+        if (p != rank)
+          st_async_v4(mapa_shared(smem_u32(&ex.peers[slot][rank < p ? rank : rank - 1][lane]), p), mapa_shared(bar, p), bits);
+      ex.tile[lane] = t;
+#pragma unroll
+      for (int j = 0; j < kWarps; ++j) ex.warps[kBwd ? kWarps - 1 - j : j][lane] = before[j];
+      if constexpr (kBwd && !kMapOnly) {
+#pragma unroll
+        for (int j = 0; j < kWarps; ++j) before[j] = h_maps[j][lane];
+#pragma unroll
+        for (int j = 0; j < kWarps; ++j) {
+          *reinterpret_cast<float2*>(&h_maps[j][lane]) = make_float2(h.x(), h.y());
+          h = apply(before[j], h);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive_expect_tx(bar, (S - 1) * 512);
+    }
   } else {
     if (!kMapOnly && seg == 0) {
       pass_empty(a, kBwd ? a.dfinal : a.h0, kBwd ? a.dinit : a.final_state, c0, rank, S);
@@ -340,7 +382,6 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) scan_kernel(
     }
     const int r0 = warp * kRows;
     const auto of_seq = [&](const float* p, int b) { return p ? load2<kFast>(p + int64_t(b) * a.H + c, left) : zero2(); };
-    const float4 identity = make_float4(1.f, 1.f, 0.f, 0.f);
     // the state before the segment (E after it)
     F2 carry = zero2();
     float4 total = identity;
@@ -349,14 +390,21 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) scan_kernel(
         carry = apply(a.seg_maps[(int64_t(s) * strips + strip) * 32 + lane], carry);
     }
     bool alive = true;   // no wait has run out; else the loop goes on without work, for the barriers' sake
+    // a stage whose rows are still read by this warp's copies: given back in the next step
+    int held = -1;
+    auto give_back = [&]() {
+      if (held < 0) return;
+      if (lane == 0) {
+        bulk_wait_group_read<0>();
+        mbar_arrive(smem_u32(&empty_bar[held]));
+      }
+      held = -1;
+    };
     for (int k = 0; k < n_steps; ++k) {
       const int st = k % kStages, slot = k & 1;
       int tile = alive ? tile_of(k) : -1;
       const TileRows& rows = rows_sh[st];
-      if (threadIdx.x == 0 && S > 1) mbar_arrive_expect_tx(smem_u32(&peer_bar[slot]), (S - 1) * 512);
-      F2 h = zero2();      // backward: the state before the tile, then before the warp's rows
       if (tile >= 0) {
-        if constexpr (kBwd && !kMapOnly) h = load2<kFast>(a.states + int64_t(tile) * a.H + c, left);
         if (!mbar_wait(smem_u32(&full_bar[st]), (k / kStages) & 1u, abort_flag, a.err)) {
           alive = false;
           tile = -1;
@@ -372,7 +420,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) scan_kernel(
       }
       const bool simple = whole && (starts | ends) == 0;
       auto inside = [&](int i) { return r0 + i >= rows.lo && r0 + i < rows.hi; };
-      const T* const stage = reinterpret_cast<const T*>(smem_raw + st * kStageBytes) + r0 * kStrip + 2 * lane;
+      T* const stage = reinterpret_cast<T*>(smem_raw + st * kStageBytes) + r0 * kStrip + 2 * lane;
       auto get = [&](int tensor, int i) -> F2 {
         if constexpr (kFast) return load2<true>(stage + tensor * (kTile * kStrip) + i * kStrip, 2);
         if (row + i >= a.T) return zero2();
@@ -435,87 +483,105 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) scan_kernel(
       }
       ex.warps[warp][lane] = mine;
       if constexpr (kBwd && !kMapOnly) h_maps[warp][lane] = mine_h;
-      consumer_sync();
-      // ---- the tile's map, to all blocks of the cluster
-      auto tile_map = [&]() {
-        float4 t = identity;
-#pragma unroll
-        for (int j = 0; j < kWarps; ++j) t = compose(t, ex.warps[kBwd ? kWarps - 1 - j : j][lane]);
-        return t;
-      };
-      if (S > 1) {
-        if (warp == 0) {
-          const float4 t = tile_map();
-          const int4 bits = make_int4(__float_as_int(t.x), __float_as_int(t.y), __float_as_int(t.z), __float_as_int(t.w));
-          const uint32_t bar = smem_u32(&peer_bar[slot]);
-          for (int p = 0; p < S; ++p)
-            if (p != rank) st_async_v4(mapa_shared(smem_u32(&ex.peers[slot][rank < p ? rank : rank - 1][lane]), p),
-                                       mapa_shared(bar, p), bits);
-        }
-        if (!mbar_wait(smem_u32(&peer_bar[slot]), (k >> 1) & 1u, abort_flag, a.err)) {
-          alive = false;
-          tile = -1;
-        }
+      maps_sync();
+      give_back();
+      if (!mbar_wait(smem_u32(&peer_bar[slot]), (k >> 1) & 1u, abort_flag, a.err)) {
+        alive = false;
+        tile = -1;
       }
       // ---- what enters the warp's rows, and the step after
       F2 in = carry;
       for (int p = 0; p < S; ++p) {
-        const float4* const peer = &ex.peers[slot][p < rank ? p : p - 1][lane];
+        const float4 of_tile = p == rank ? ex.tile[lane] : ex.peers[slot][p < rank ? p : p - 1][lane];
         if constexpr (kMapOnly) {
-          total = compose(total, p == rank ? tile_map() : *peer);
-        } else if (p != rank) {
-          carry = apply(*peer, carry);
+          if (warp == 0) total = compose(total, of_tile);
         } else {
-          if (!kBwd && tile >= 0 && a.states && warp == 0) store2<kFast>(a.states + int64_t(tile) * a.H + c, carry, left);
-#pragma unroll
-          for (int j = 0; j < kWarps; ++j) {
-            const int w = kBwd ? kWarps - 1 - j : j;
-            if (w == warp) in = carry;
-            carry = apply(ex.warps[w][lane], carry);
+          if (p == rank) {
+            in = apply(ex.warps[warp][lane], carry);
+            if (!kBwd && tile >= 0 && a.states && warp == 0) store2<kFast>(a.states + int64_t(tile) * a.H + c, carry, left);
           }
+          carry = apply(of_tile, carry);
         }
       }
-      if constexpr (kBwd && !kMapOnly)
-        for (int w = 0; w < warp; ++w) h = apply(h_maps[w][lane], h);
-      consumer_sync();   // the warps' maps are read
 
       // ---- the rows again
-      if (tile >= 0) {
-        if constexpr (!kBwd && !kMapOnly) {
-          T* y = static_cast<T*>(a.y) + row * a.H + c;
-          if (simple) {
-#pragma unroll
-            for (int i = 0; i < kRows; ++i) {
-              in = step<kForm>(in, m[i], get(kV, i));
-              store2<kFast>(y + int64_t(i) * a.H, in, left);
-            }
-          } else {
-#pragma unroll
-            for (int i = 0; i < kRows; ++i) {
-              if (!inside(i)) {
-                if (a.fill && row + i < a.T) store2<kFast>(y + int64_t(i) * a.H, zero2(), left);
-                continue;
-              }
-              if (starts >> i & 1u) in = of_seq(a.h0, rows.seq[r0 + i]);
-              in = step<kForm>(in, m[i], get(kV, i));
-              store2<kFast>(y + int64_t(i) * a.H, in, left);
-              if ((ends >> i & 1u) && a.final_state) store2<kFast>(a.final_state + int64_t(rows.seq[r0 + i]) * a.H + c, in, left);
-            }
-          }
-        } else if constexpr (!kMapOnly) {
-          T* dg = static_cast<T*>(a.dgate) + row * a.H + c;
-          T* dv = static_cast<T*>(a.dvalue) + row * a.H + c;
-          F2 hp[kRows];   // h of the row before
+      if (tile < 0) continue;
+      // results of a warp whose rows are all in sequences go out as a box, from where its gates
+      // (and dy) have been
+      bool boxed = false;
+      if constexpr (!kBwd && !kMapOnly) {
+        T* y = static_cast<T*>(a.y) + row * a.H + c;
+        if (simple) {
+          boxed = kFast;
 #pragma unroll
           for (int i = 0; i < kRows; ++i) {
-            if (!simple && !inside(i)) continue;
+            in = step<kForm>(in, m[i], get(kV, i));
+            if constexpr (kFast)
+              store2<true>(stage + i * kStrip, in, 2);
+            else
+              store2<false>(y + int64_t(i) * a.H, in, left);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < kRows; ++i) {
+            if (!inside(i)) {
+              if (a.fill && row + i < a.T) store2<kFast>(y + int64_t(i) * a.H, zero2(), left);
+              continue;
+            }
+            if (starts >> i & 1u) in = of_seq(a.h0, rows.seq[r0 + i]);
+            in = step<kForm>(in, m[i], get(kV, i));
+            store2<kFast>(y + int64_t(i) * a.H, in, left);
+            if ((ends >> i & 1u) && a.final_state) store2<kFast>(a.final_state + int64_t(rows.seq[r0 + i]) * a.H + c, in, left);
+          }
+        }
+      } else if constexpr (!kMapOnly) {
+        T* dg = static_cast<T*>(a.dgate) + row * a.H + c;
+        T* dv = static_cast<T*>(a.dvalue) + row * a.H + c;
+        const float2 before = *reinterpret_cast<const float2*>(&h_maps[warp][lane]);
+        F2 h = f2(before.x, before.y);
+        // dgate and dvalue of a row from D and E, h of the row before and its value
+        auto grads = [&](int i, F2 D, F2 E, F2 hp, F2& df, F2& dval) {
+          if constexpr (kForm == kFormSigmoid) {
+            const F2 w = mul2(m[i], f2(-1.f));
+            df = mul2(mul2(E, w), sub2(hp, get(kV, i)));
+            dval = mul2(D, w);
+          } else {
+            df = mul2(E, hp);
+            dval = D;
+          }
+        };
+        F2 hp[kRows], df, dval;   // hp: h of the row before
+        if (simple) {
+          boxed = kFast;
+#pragma unroll
+          for (int i = 0; i < kRows; ++i) {
+            hp[i] = h;
+            h = step<kForm>(h, m[i], get(kV, i));
+          }
+#pragma unroll
+          for (int i = kRows - 1; i >= 0; --i) {
+            const F2 D = add2(get(kD, i), in);
+            in = fma2(m[i], D, D);   // E
+            grads(i, D, in, hp[i], df, dval);
+            if constexpr (kFast) {
+              store2<true>(stage + i * kStrip, df, 2);
+              store2<true>(stage + kD * (kTile * kStrip) + i * kStrip, dval, 2);
+            } else {
+              store2<false>(dg + int64_t(i) * a.H, df, left);
+              store2<false>(dv + int64_t(i) * a.H, dval, left);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < kRows; ++i) {
+            if (!inside(i)) continue;
             if (starts >> i & 1u) h = of_seq(a.h0, rows.seq[r0 + i]);
             hp[i] = h;
             h = step<kForm>(h, m[i], get(kV, i));
           }
 #pragma unroll
           for (int i = kRows - 1; i >= 0; --i) {
-            if (!simple && !inside(i)) {
+            if (!inside(i)) {
               if (row + i < a.T) {
                 store2<kFast>(dg + int64_t(i) * a.H, zero2(), left);
                 store2<kFast>(dv + int64_t(i) * a.H, zero2(), left);
@@ -524,22 +590,31 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) scan_kernel(
             }
             if (ends >> i & 1u) in = of_seq(a.dfinal, rows.seq[r0 + i]);
             const F2 D = add2(get(kD, i), in);
-            in = fma2(m[i], D, D);   // E
-            if constexpr (kForm == kFormSigmoid) {
-              const F2 w = mul2(m[i], f2(-1.f));
-              store2<kFast>(dg + int64_t(i) * a.H, mul2(mul2(in, w), sub2(hp[i], get(kV, i))), left);
-              store2<kFast>(dv + int64_t(i) * a.H, mul2(D, w), left);
-            } else {
-              store2<kFast>(dg + int64_t(i) * a.H, mul2(in, hp[i]), left);
-              store2<kFast>(dv + int64_t(i) * a.H, D, left);
-            }
+            in = fma2(m[i], D, D);
+            grads(i, D, in, hp[i], df, dval);
+            store2<kFast>(dg + int64_t(i) * a.H, df, left);
+            store2<kFast>(dv + int64_t(i) * a.H, dval, left);
             if ((starts >> i & 1u) && a.dinit) store2<kFast>(a.dinit + int64_t(rows.seq[r0 + i]) * a.H + c, in, left);
           }
         }
+      }
+      if (boxed) {
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          const uint32_t box = smem_u32(smem_raw) + st * kStageBytes + r0 * kStrip * static_cast<int>(sizeof(T));
+          tma_store_2d(&maps.out0, box, c0, static_cast<int>(row));
+          if constexpr (kBwd && !kMapOnly) tma_store_2d(&maps.out1, box + kD * kTensorBytes, c0, static_cast<int>(row));
+          bulk_commit_group();
+        }
+        held = st;
+      } else {
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&empty_bar[st]));
       }
     }
+    give_back();
+    if (lane == 0) bulk_wait_group<0>();
     if (kMapOnly && warp == 0 && rank == 0) a.seg_maps[(int64_t(seg) * strips + strip) * 32 + lane] = total;
   }
   __syncthreads();
@@ -612,14 +687,13 @@ ScanArgs base_args(const molt_scan_desc* d, const int32_t* cu) {
 bool fast_of(const ScanArgs& a, int dtype) {
   const size_t e = static_cast<size_t>(dtype_bytes(dtype));
   const auto at = [](const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; };
-  for (const void* p : {a.gate, a.value, a.dy})
+  for (const void* p : {a.gate, a.value, a.dy, static_cast<const void*>(a.y), static_cast<const void*>(a.dgate),
+                        static_cast<const void*>(a.dvalue)})
     if (!at(p, 16)) return false;
-  for (const void* p : {a.y, a.dgate, a.dvalue})
-    if (!at(p, 2 * e)) return false;
   for (const float* p : {a.h0, a.dfinal, static_cast<const float*>(a.final_state), static_cast<const float*>(a.states),
                          static_cast<const float*>(a.dinit)})
     if (!at(p, 8)) return false;
-  return a.H % 2 == 0 && a.gate_ld * e % 16 == 0 && a.value_ld * e % 16 == 0 && a.dy_ld * e % 16 == 0;
+  return a.H * e % 16 == 0 && a.gate_ld * e % 16 == 0 && a.value_ld * e % 16 == 0 && a.dy_ld * e % 16 == 0;
 }
 
 constexpr int kMaxSegments = 32;
@@ -692,14 +766,17 @@ molt_status launch(const molt_scan_desc* d, ScanArgs& a, bool bwd, void* workspa
   ScanMaps m{};
   if (fast) {
     const int e = dtype_bytes(d->dtype);
-    const auto encode = [&](CUtensorMap* t, const void* p, int64_t ld) {
+    const auto encode = [&](CUtensorMap* t, const void* p, int64_t ld, int rows = kTile) {
       return encode_tmap_plain(t, e == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, e, p, a.T, a.H, ld,
-                               kStrip, kTile);
+                               kStrip, rows);
     };
     if (const molt_status q = encode(&m.gate, a.gate, a.gate_ld); q != MOLT_OK) return q;
     if (const molt_status q = encode(&m.value, a.value, a.value_ld); q != MOLT_OK) return q;
     if (bwd)
       if (const molt_status q = encode(&m.dy, a.dy, a.dy_ld); q != MOLT_OK) return q;
+    if (const molt_status q = encode(&m.out0, bwd ? a.dgate : a.y, a.H, kRows); q != MOLT_OK) return q;
+    if (bwd)
+      if (const molt_status q = encode(&m.out1, a.dvalue, a.H, kRows); q != MOLT_OK) return q;
   }
   for (int pass = segments > 1 ? 0 : 1; pass < 2; ++pass) {
     const bool map_only = pass == 0;
