@@ -43,7 +43,7 @@ constexpr int kTile = 128;               // rows of a tile, and between kept sta
 constexpr int kWarps = 8, kRows = kTile / kWarps;
 constexpr int kThreads = 32 * (kWarps + 2);
 constexpr int kStrip = 64;               // channels of a block
-constexpr int kMaxCluster = 8;
+constexpr int kMaxCluster = 8;           // 4 where tiles do not come by TMA (shared memory for two blocks to an SM)
 constexpr int kFormSigmoid = 0, kFormLog = 1;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -255,21 +255,60 @@ __device__ __forceinline__ float4 compose(const float4& m, const float4& n) {
 // What the warps of a block and the blocks of a cluster tell one another in a step.  warps:
 // the map of each warp's rows, then that of all the warps before it.  Two slots for the
 // peers, so that one a step ahead does not write what is still read.
+template <int kCluster>
 struct Exchange {
   float4 warps[kWarps][32];
   float4 tile[32];
-  float4 peers[2][kMaxCluster - 1][32];
+  float4 peers[2][kCluster - 1][32];
 };
 
 // the eight warps with rows, and the one that folds
 __device__ __forceinline__ void maps_sync() { asm volatile("bar.sync 1, %0;" ::"n"((kWarps + 1) * 32) : "memory"); }
 
 // A stage is the tile's rows of each tensor.  As many as leave room for two blocks to an SM (one
-// of fp32).
-template <class T, int kTensors>
-constexpr int kStageBytesOf = kTensors * kTile * kStrip * static_cast<int>(sizeof(T));
+// of fp32).  Rows that do not come by TMA begin inside a word and may need one more.
+template <class T, bool kFast>
+constexpr int kPitch = kStrip * static_cast<int>(sizeof(T)) + (kFast || sizeof(T) == 4 ? 0 : 4);
+template <class T, int kTensors, bool kFast>
+constexpr int kStageBytesOf = kTensors * kTile * kPitch<T, kFast>;
 template <int kTensors>
 constexpr int kStagesOf = kTensors == 2 ? 3 : 2;
+
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// A row's channels c0 .. c0 + n - 1 to shared memory, by words, from any address; first, last:
+// no element lies before or behind them that may be read along.
+template <class T>
+__device__ __forceinline__ void copy_row(uint32_t dst, const T* row, int n, bool first, bool last, int lane) {
+  if constexpr (sizeof(T) == 4) {
+    if (lane < n) cp_async4(dst + 4 * lane, row + lane);
+    if (lane + 32 < n) cp_async4(dst + 4 * (lane + 32), row + lane + 32);
+  } else {
+    const int off = static_cast<int>(reinterpret_cast<uintptr_t>(row) >> 1 & 1);
+    auto word = [&](int l) {
+      const int e = 2 * l - off;   // its first element
+      if (e >= n) return;
+      if ((e < 0 && first) || (e + 1 >= n && last)) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          if (e + j >= 0 && e + j < n)
+            asm volatile("st.shared.u16 [%0], %1;" ::"r"(dst + 4 * l + 2 * j), "h"(reinterpret_cast<const uint16_t*>(row)[e + j])
+                         : "memory");
+        return;
+      }
+      cp_async4(dst + 4 * l, row + e);
+    };
+    word(lane);
+    if (off && lane == 0) word(32);
+  }
+}
 
 // kBwd: rows from the last one backwards.  kMapOnly: a segment's map alone.  kFast: tiles by TMA
 // and pairs of channels; else elements one by one from any address.
@@ -280,9 +319,10 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) scan_kernel(
   constexpr bool kValue = !(kBwd && kMapOnly);
   constexpr int kTensors = kBwd && !kMapOnly ? 3 : 2, kV = 1, kD = kValue ? 2 : 1;
   constexpr int kStages = kStagesOf<kTensors>;
-  constexpr int kStageBytes = kStageBytesOf<T, kTensors>, kTensorBytes = kStageBytes / kTensors;
+  constexpr int kRowBytes = kPitch<T, kFast>;
+  constexpr int kStageBytes = kStageBytesOf<T, kTensors, kFast>, kTensorBytes = kStageBytes / kTensors;
   extern __shared__ __align__(128) uint8_t smem_raw[];
-  __shared__ __align__(16) Exchange ex;
+  __shared__ __align__(16) Exchange<kFast ? kMaxCluster : kMaxCluster / 2> ex;
   __shared__ float4 h_maps[kBwd && !kMapOnly ? kWarps : 1][32];   // then, in x and y, h before each warp's rows
   __shared__ TileRows rows_sh[kStages];
   __shared__ __align__(8) uint64_t full_bar[kStages], empty_bar[kStages], peer_bar[2];
@@ -389,6 +429,36 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) scan_kernel(
       for (int s = kBwd ? static_cast<int>(gridDim.y) - 1 : 0; s != seg; s += kBwd ? -1 : 1)
         carry = apply(a.seg_maps[(int64_t(s) * strips + strip) * 32 + lane], carry);
     }
+    // rows that do not come by TMA: every warp copies its own, all stages but one ahead
+    const void* const tensor_of[3] = {a.gate, kValue ? a.value : a.dy, a.dy};
+    const int64_t ld_of[3] = {a.gate_ld, kValue ? a.value_ld : a.dy_ld, a.dy_ld};
+    uint32_t odd_base = 0, odd_ld = 0;   // whether a tensor's rows begin inside a word: at row 0, and for odd rows besides
+    auto load_rows = [&](int k) {
+      const int t = k < n_steps ? tile_of(k) : -1;
+      if (t >= 0) {
+#pragma unroll
+        for (int j = 0; j < kTensors; ++j) {
+          const uint32_t dst = smem_u32(smem_raw) + (k % kStages) * kStageBytes + j * kTensorBytes + r0 * kRowBytes;
+#pragma unroll 4
+          for (int i = 0; i < kRows; ++i) {
+            const int64_t r = int64_t(t) * kTile + r0 + i;
+            if (r >= a.T) break;
+            copy_row(dst + i * kRowBytes, static_cast<const T*>(tensor_of[j]) + r * ld_of[j] + c0, min(kStrip, a.H - c0),
+                     r == 0 && c0 == 0, r == a.T - 1 && c0 + kStrip >= a.H, lane);
+          }
+        }
+      }
+      cp_async_commit();
+    };
+    if constexpr (!kFast) {
+#pragma unroll
+      for (int j = 0; j < kTensors; ++j) {
+        odd_base |= static_cast<uint32_t>(reinterpret_cast<uintptr_t>(tensor_of[j]) >> 1 & 1) << j;   // (c0 is even)
+        odd_ld |= static_cast<uint32_t>(ld_of[j] & 1) << j;
+      }
+#pragma unroll
+      for (int k = 0; k < kStages - 1; ++k) load_rows(k);
+    }
     bool alive = true;   // no wait has run out; else the loop goes on without work, for the barriers' sake
     // a stage whose rows are still read by this warp's copies: given back in the next step
     int held = -1;
@@ -411,22 +481,34 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) scan_kernel(
         }
       }
       const int64_t row = int64_t(tile) * kTile + r0;   // the warp's first
-      uint32_t starts = 0, ends = 0;
-      bool whole = true;                                // all of its rows are in sequences
+      uint32_t starts = 0, ends = 0, valid = 0;         // a bit for each of its rows; valid: in a sequence
       if (tile >= 0) {
         starts = rows.starts[r0 >> 5] >> (r0 & 31) & 0xffffu;
         ends = rows.ends[r0 >> 5] >> (r0 & 31) & 0xffffu;
-        whole = rows.lo <= r0 && rows.hi >= r0 + kRows;
+        const int lo = min(max(rows.lo - r0, 0), kRows), hi = min(max(rows.hi - r0, 0), kRows);
+        valid = (1u << hi) - 1u & ~((1u << lo) - 1u);
+        if constexpr (!kFast) {
+          load_rows(k + kStages - 1);
+          cp_async_wait<kStages - 1>();
+          __syncwarp();
+        }
       }
-      const bool simple = whole && (starts | ends) == 0;
-      auto inside = [&](int i) { return r0 + i >= rows.lo && r0 + i < rows.hi; };
-      T* const stage = reinterpret_cast<T*>(smem_raw + st * kStageBytes) + r0 * kStrip + 2 * lane;
+      const bool simple = valid == (1u << kRows) - 1u && (starts | ends) == 0;
+      auto inside = [&](int i) -> bool { return valid >> i & 1u; };
+      uint8_t* const stage8 = smem_raw + st * kStageBytes + r0 * kRowBytes;
+      T* const stage = reinterpret_cast<T*>(stage8) + 2 * lane;
       auto get = [&](int tensor, int i) -> F2 {
-        if constexpr (kFast) return load2<true>(stage + tensor * (kTile * kStrip) + i * kStrip, 2);
-        if (row + i >= a.T) return zero2();
-        const void* const p = tensor == 0 ? a.gate : kValue && tensor == kV ? a.value : a.dy;
-        const int64_t ld = tensor == 0 ? a.gate_ld : kValue && tensor == kV ? a.value_ld : a.dy_ld;
-        return load2<false>(static_cast<const T*>(p) + (row + i) * ld + c, left);
+        if constexpr (kFast || sizeof(T) == 4) {
+          return load2<true>(reinterpret_cast<const T*>(reinterpret_cast<const uint8_t*>(stage) + tensor * kTensorBytes +
+                                                        i * kRowBytes), 2);
+        } else {
+          const uint32_t* const w = reinterpret_cast<const uint32_t*>(stage8 + tensor * kTensorBytes + i * kRowBytes) + lane;
+          const bool odd = (odd_base >> tensor ^ (odd_ld >> tensor & static_cast<uint32_t>(row + i))) & 1u;
+          const uint32_t w0 = w[0], w1 = w[1];
+          float lo, hi;
+          unpack2(odd ? __byte_perm(w0, w1, 0x5432) : w0, static_cast<const T*>(nullptr), lo, hi);
+          return f2(lo, hi);
+        }
       };
 
       // ---- the maps of the warp's rows
@@ -615,6 +697,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) scan_kernel(
     }
     give_back();
     if (lane == 0) bulk_wait_group<0>();
+    if constexpr (!kFast) cp_async_wait<0>();
     if (kMapOnly && warp == 0 && rank == 0) a.seg_maps[(int64_t(seg) * strips + strip) * 32 + lane] = total;
   }
   __syncthreads();
@@ -703,10 +786,10 @@ size_t seg_bytes(const molt_scan_desc* d) { return static_cast<size_t>(kMaxSegme
 struct ScanPlan {
   int cluster, segments;
 };
-ScanPlan plan_of(const molt_scan_desc* d, int tiles, int n_sm) {
+ScanPlan plan_of(const molt_scan_desc* d, int tiles, int n_sm, bool fast) {
   const int64_t strips = strips_of(d), slots = int64_t(n_sm) * (d->dtype == MOLT_FP32 ? 1 : 2);
   ScanPlan p;
-  p.cluster = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({kMaxCluster, slots / strips, tiles})));
+  p.cluster = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({fast ? kMaxCluster : kMaxCluster / 2, slots / strips, tiles})));
   const int64_t room = slots / (strips * p.cluster), steps = (tiles + p.cluster - 1) / p.cluster;
   p.segments = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({kMaxSegments, room, steps / 8})));
   return p;
@@ -715,7 +798,7 @@ ScanPlan plan_of(const molt_scan_desc* d, int tiles, int n_sm) {
 template <class T, int kForm, bool kBwd, bool kMapOnly, bool kFast>
 cudaError_t launch_kernel(const ScanMaps& m, const ScanArgs& a, int strips, int cluster, int segments, cudaStream_t s) {
   constexpr int kTensors = kBwd && !kMapOnly ? 3 : 2;
-  constexpr int smem = kFast ? kStagesOf<kTensors> * kStageBytesOf<T, kTensors> : 0;
+  constexpr int smem = kStagesOf<kTensors> * kStageBytesOf<T, kTensors, kFast>;
   const auto k = &scan_kernel<T, kForm, kBwd, kMapOnly, kFast>;
   if (const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem); e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
@@ -754,7 +837,8 @@ molt_status launch(const molt_scan_desc* d, ScanArgs& a, bool bwd, void* workspa
   if (!a.err) return st;
   const int strips = static_cast<int>(strips_of(d));
   a.tiles = static_cast<int>((a.T + kTile - 1) / kTile);
-  const ScanPlan plan = plan_of(d, a.tiles, device_sm_count());
+  const bool fast = a.tiles > 0 && fast_of(a, d->dtype);
+  const ScanPlan plan = plan_of(d, a.tiles, device_sm_count(), fast);
   a.seg_tiles = (a.tiles + plan.segments - 1) / plan.segments;
   const int segments = a.tiles > 0 ? (a.tiles + a.seg_tiles - 1) / a.seg_tiles : 1;
   Scratch sc;
@@ -762,7 +846,6 @@ molt_status launch(const molt_scan_desc* d, ScanArgs& a, bool bwd, void* workspa
     if (const molt_status e = get_scratch(sc, workspace, workspace_bytes, seg_bytes(d), s); e != MOLT_OK) return e;
     a.seg_maps = static_cast<float4*>(sc.aligned());
   }
-  const bool fast = a.tiles > 0 && fast_of(a, d->dtype);
   ScanMaps m{};
   if (fast) {
     const int e = dtype_bytes(d->dtype);

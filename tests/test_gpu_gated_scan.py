@@ -145,6 +145,23 @@ def test_long_memory(dtype, kind):
         check(out[k], ref[k], torch.float32, k)
 
 
+@pytest.mark.parametrize("dtype,H", [(torch.bfloat16, 72), (torch.bfloat16, 65), (torch.float32, 40), (torch.float16, 33)])
+def test_long_and_narrow(dtype, H):
+    """Few channels and many rows: segments of rows, each of them several tiles to a block."""
+    T = 18000
+    s = make(T, H, 5, dtype, "sigmoid", 2, long=3.0)
+    cu = [100, 100, 2500, 2600, 17000, T - 50]
+    ref, out = reference(s, cu, "sigmoid"), run(s, cu, "sigmoid")
+    rows = slice(cu[0], cu[-1])
+    for k in ("y", "dgate", "dvalue"):
+        check(out[k], ref[k], dtype, k, rows)
+    for k in ("final_state", "dinitial_state"):
+        check(out[k], ref[k], torch.float32, k)
+    again = run(s, cu, "sigmoid")
+    for k, v in out.items():
+        assert torch.equal(v, again[k]), k
+
+
 @pytest.mark.parametrize("L", [1, 16, 100, 128, 200])
 def test_equal_sequences(L):
     """[B, L, H] is the same as packed rows."""
