@@ -9,8 +9,8 @@
 // of its initial one.
 //
 // What a row does to h is an affine map (a, b), and maps compose, so rows can be taken
-// together: a tile is 128 rows by 64 channels, a warp has 16 rows of it, a lane two channels.
-// Every warp composes its rows' maps; the maps of a tile's warps, and of the tiles of a
+// together: a tile is 128 rows (64 of the forward in fp32) by 64 channels, a warp has 16 (8)
+// rows of it, a lane two channels.  Every warp composes its rows' maps; the maps of a tile's warps, and of the tiles of a
 // cluster, are folded in order; and then every warp goes through its rows again from the
 // state that it now knows.  The backward's E is the same from the other end; h it forms
 // again from the states that the forward kept at every 128th row.  A row that begins a
@@ -27,7 +27,10 @@
 // cu_seqlens which rows begin and end a sequence), the other folds the maps.  Few strips and many rows are cut into segments besides: a first
 // launch folds each segment's map, the second starts from what precedes its own.
 #include <algorithm>
+#include <atomic>
 #include <cstdint>
+#include <cstdio>
+#include <cstdlib>
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <initializer_list>
@@ -39,8 +42,16 @@
 namespace molt {
 namespace {
 
-constexpr int kTile = 128;               // rows of a tile, and between kept states
-constexpr int kWarps = 8, kRows = kTile / kWarps;
+constexpr int kStateRows = 128;          // rows between kept states
+constexpr int kWarps = 8;
+constexpr int kHalf = 8;                 // rows that a warp brings into registers at a time
+// Halves of a warp's rows: two, or one of the forward in fp32, whose tiles have twice the
+// bytes.  The backward's tile is the rows between two kept states.
+template <class T, bool kBwd>
+constexpr int kHalves = kBwd || sizeof(T) == 2 ? 2 : 1;
+template <class T, bool kBwd>
+constexpr int kTile = kWarps * kHalves<T, kBwd> * kHalf;
+static_assert(kTile<float, true> == kStateRows && kStateRows % kTile<float, false> == 0);
 constexpr int kThreads = 32 * (kWarps + 2);
 constexpr int kStrip = 64;               // channels of a block
 constexpr int kMaxCluster = 8;           // 4 where tiles do not come by TMA (shared memory for two blocks to an SM)
@@ -67,8 +78,8 @@ struct ScanArgs {
   unsigned* err;
 };
 struct ScanMaps {
-  CUtensorMap gate, value, dy;   // boxes of 64 channels by 128 rows
-  CUtensorMap out0, out1;        // y, or dgate and dvalue: boxes of 64 channels by 16 rows
+  CUtensorMap gate, value, dy;   // boxes of 64 channels by a tile's rows
+  CUtensorMap out0, out1;        // y, or dgate and dvalue: boxes of 64 channels by a warp's rows
 };
 
 __device__ __forceinline__ float rcp_approx(float x) {
@@ -132,19 +143,20 @@ __device__ __forceinline__ void store2(T* p, F2 x, int left) {
 
 // Which rows of a tile begin or end a sequence (a bit each), and which one (of those rows);
 // lo and hi: the tile's rows that are in any.
+template <int kN>
 struct TileRows {
-  uint32_t starts[kTile / 32], ends[kTile / 32];
-  int seq[kTile];
+  uint32_t starts[kN / 32], ends[kN / 32];
+  int seq[kN];
   int lo, hi;
 };
 
 // Fills `t` for the rows from row0 on; by one warp.  Returns the first bound that is not below
 // row0; `at` is what it returned for the tile before in the walk (at first 0, backwards
 // B + 1).
-template <bool kBwd>
-__device__ __forceinline__ int64_t mark_rows(const ScanArgs& a, int64_t row0, TileRows& t, int64_t at, int lane) {
-  const int n = static_cast<int>(a.T - row0 < kTile ? a.T - row0 : kTile);
-  if (lane < kTile / 32) t.starts[lane] = t.ends[lane] = 0u;
+template <int kN, bool kBwd>
+__device__ __forceinline__ int64_t mark_rows(const ScanArgs& a, int64_t row0, TileRows<kN>& t, int64_t at, int lane) {
+  const int n = static_cast<int>(a.T - row0 < kN ? a.T - row0 : kN);
+  if (lane < kN / 32) t.starts[lane] = t.ends[lane] = 0u;
   __syncwarp();
   if (a.cu == nullptr) {
     if (lane == 0) {
@@ -253,26 +265,25 @@ __device__ __forceinline__ float4 compose(const float4& m, const float4& n) {
 }
 
 // What the warps of a block and the blocks of a cluster tell one another in a step.  warps:
-// the map of each warp's rows, then that of all the warps before it.  Two slots for the
-// peers, so that one a step ahead does not write what is still read.
+// the map of each warp's rows, then in x and y what enters them.  Two slots for the peers, so
+// that one a step ahead does not write what is still read.
 template <int kCluster>
 struct Exchange {
   float4 warps[kWarps][32];
-  float4 tile[32];
   float4 peers[2][kCluster - 1][32];
 };
 
 // the eight warps with rows, and the one that folds
 __device__ __forceinline__ void maps_sync() { asm volatile("bar.sync 1, %0;" ::"n"((kWarps + 1) * 32) : "memory"); }
 
-// A stage is the tile's rows of each tensor.  As many as leave room for two blocks to an SM (one
-// of fp32).  Rows that do not come by TMA begin inside a word and may need one more.
+// A stage is the tile's rows of each tensor.  As many as leave room for two blocks to an SM (fp32
+// backward: one).  Rows that do not come by TMA begin inside a word and may need one more.
 template <class T, bool kFast>
 constexpr int kPitch = kStrip * static_cast<int>(sizeof(T)) + (kFast || sizeof(T) == 4 ? 0 : 4);
 template <class T, int kTensors, bool kFast>
-constexpr int kStageBytesOf = kTensors * kTile * kPitch<T, kFast>;
-template <int kTensors>
-constexpr int kStagesOf = kTensors == 2 ? 3 : 2;
+constexpr int kRowsBytesOf = kTensors * kPitch<T, kFast>;   // of one row of all tensors
+template <bool kBwd, bool kMapOnly>
+constexpr int kStagesOf = kBwd && !kMapOnly ? 2 : 3;
 
 __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
@@ -310,22 +321,42 @@ __device__ __forceinline__ void copy_row(uint32_t dst, const T* row, int n, bool
   }
 }
 
+// Two values of a row as they are in memory.
+template <class T>
+struct Raw {
+  uint32_t w;
+  __device__ __forceinline__ F2 f() const {
+    float lo, hi;
+    unpack2(w, static_cast<const T*>(nullptr), lo, hi);
+    return f2(lo, hi);
+  }
+};
+template <>
+struct Raw<float> {
+  F2 w;
+  __device__ __forceinline__ F2 f() const { return w; }
+};
+
+template <class T, bool kBwd>
+constexpr int kBlocksPerSM = kBwd && sizeof(T) == 4 ? 1 : 2;
+
 // kBwd: rows from the last one backwards.  kMapOnly: a segment's map alone.  kFast: tiles by TMA
-// and pairs of channels; else elements one by one from any address.
+// and pairs of channels; else words and elements one by one from any address.
 template <class T, int kForm, bool kBwd, bool kMapOnly, bool kFast>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) scan_kernel(const __grid_constant__ ScanMaps maps,
-                                                                              const ScanArgs a) {
+__global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel(const __grid_constant__ ScanMaps maps,
+                                                                               const ScanArgs a) {
   // tensors of a tile: gate, value (the backward's map needs none), dy
-  constexpr bool kValue = !(kBwd && kMapOnly);
-  constexpr int kTensors = kBwd && !kMapOnly ? 3 : 2, kV = 1, kD = kValue ? 2 : 1;
-  constexpr int kStages = kStagesOf<kTensors>;
+  constexpr bool kGrads = kBwd && !kMapOnly, kValue = !kBwd || !kMapOnly;
+  constexpr int kTensors = kGrads ? 3 : 2, kV = 1, kD = kValue ? 2 : 1;
+  constexpr int kStages = kStagesOf<kBwd, kMapOnly>, kN = kTile<T, kBwd>, kParts = kHalves<T, kBwd>, kRows = kParts * kHalf;
+  constexpr uint32_t kAll = (1u << kHalf) - 1u;
   constexpr int kRowBytes = kPitch<T, kFast>;
-  constexpr int kStageBytes = kStageBytesOf<T, kTensors, kFast>, kTensorBytes = kStageBytes / kTensors;
+  constexpr int kTensorBytes = kN * kRowBytes, kStageBytes = kTensors * kTensorBytes;
   extern __shared__ __align__(128) uint8_t smem_raw[];
   __shared__ __align__(16) Exchange<kFast ? kMaxCluster : kMaxCluster / 2> ex;
-  __shared__ float4 h_maps[kBwd && !kMapOnly ? kWarps : 1][32];   // then, in x and y, h before each warp's rows
-  __shared__ TileRows rows_sh[kStages];
-  __shared__ __align__(8) uint64_t full_bar[kStages], empty_bar[kStages], peer_bar[2];
+  __shared__ float4 h_maps[kGrads ? kWarps : 1][32];   // then, in x and y, h before each warp's rows
+  __shared__ TileRows<kN> rows_sh[kStages];
+  __shared__ __align__(8) uint64_t full_bar[kStages], empty_bar[kStages], peer_bar[2], in_bar[2];
   __shared__ int abort_sh;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   volatile int* abort_flag = &abort_sh;
@@ -347,7 +378,10 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) scan_kernel(
       mbar_init(smem_u32(&full_bar[s]), kFast ? 2 : 1);
       mbar_init(smem_u32(&empty_bar[s]), kWarps);
     }
-    for (int s = 0; s < 2; ++s) mbar_init(smem_u32(&peer_bar[s]), 1);
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(smem_u32(&peer_bar[s]), 1);
+      mbar_init(smem_u32(&in_bar[s]), 1);
+    }
     abort_sh = 0;
     fence_mbar_init();
   }
@@ -366,12 +400,12 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) scan_kernel(
       if (kFast && lane == 0) {
         const uint32_t bar = smem_u32(&full_bar[st]), dst = smem_u32(smem_raw) + st * kStageBytes;
         mbar_arrive_expect_tx(bar, kStageBytes);
-        tma_load_2d(dst, &maps.gate, bar, c0, tile * kTile);
-        if constexpr (kValue) tma_load_2d(dst + kV * kTensorBytes, &maps.value, bar, c0, tile * kTile);
-        if constexpr (kBwd) tma_load_2d(dst + kD * kTensorBytes, &maps.dy, bar, c0, tile * kTile);
+        tma_load_2d(dst, &maps.gate, bar, c0, tile * kN);
+        if constexpr (kValue) tma_load_2d(dst + kV * kTensorBytes, &maps.value, bar, c0, tile * kN);
+        if constexpr (kBwd) tma_load_2d(dst + kD * kTensorBytes, &maps.dy, bar, c0, tile * kN);
       }
       ++issued;
-      at = mark_rows<kBwd>(a, int64_t(tile) * kTile, rows_sh[st], at, lane);
+      at = mark_rows<kN, kBwd>(a, int64_t(tile) * kN, rows_sh[st], at, lane);
       if (lane == 0) mbar_arrive(smem_u32(&full_bar[st]));
     }
     // copies land in this block's memory: wait for the last ones before it may exit
@@ -379,56 +413,95 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) scan_kernel(
       for (int k = max(0, issued - kStages); k < issued; ++k)
         mbar_wait_drain(smem_u32(&full_bar[k % kStages]), (k / kStages) & 1u, a.err);
   } else if (warp == kWarps + 1) {
-    // a step's maps: the tile's, for all blocks of the cluster, and what precedes each warp's rows
+    // folds a step's maps: the tile's, for all blocks of the cluster, and what enters each warp's rows
+    F2 carry = zero2();           // the state before the step (E after it)
+    float4 total = identity;
+    if constexpr (!kMapOnly) {
+      for (int s = kBwd ? static_cast<int>(gridDim.y) - 1 : 0; s != seg; s += kBwd ? -1 : 1)
+        carry = apply(a.seg_maps[(int64_t(s) * strips + strip) * 32 + lane], carry);
+    }
     for (int k = 0; k < n_steps; ++k) {
       const int tile = tile_of(k), slot = k & 1;
+      const uint32_t bar = smem_u32(&peer_bar[slot]);
+      if (S > 1 && lane == 0) mbar_arrive_expect_tx(bar, (S - 1) * 512);
       F2 h = zero2();   // backward: the state before the tile
-      if constexpr (kBwd && !kMapOnly)
+      if constexpr (kGrads)
         if (tile >= 0) h = load2<kFast>(a.states + int64_t(tile) * a.H + c, left);
       maps_sync();
-      float4 before[kWarps], t = identity;
+      float4 m[kWarps], pair[4], quad[2];   // in the order of the walk
+      float4(*const warps)[32] = ex.warps;
 #pragma unroll
-      for (int j = 0; j < kWarps; ++j) before[j] = ex.warps[kBwd ? kWarps - 1 - j : j][lane];
+      for (int j = 0; j < kWarps; ++j) m[j] = warps[kBwd ? kWarps - 1 - j : j][lane];
 #pragma unroll
-      for (int j = 0; j < kWarps; ++j) {
-        const float4 own = before[j];
-        before[j] = t;
-        t = compose(t, own);
-      }
-      const uint32_t bar = smem_u32(&peer_bar[slot]);
-      const int4 bits = make_int4(__float_as_int(t.x), __float_as_int(t.y), __float_as_int(t.z), __float_as_int(t.w));
+      for (int j = 0; j < 4; ++j) pair[j] = compose(m[2 * j], m[2 * j + 1]);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) quad[j] = compose(pair[2 * j], pair[2 * j + 1]);
+      const float4 own = compose(quad[0], quad[1]);
+      const int4 bits = make_int4(__float_as_int(own.x), __float_as_int(own.y), __float_as_int(own.z), __float_as_int(own.w));
       for (int p = 0; p < S; ++p)
         if (p != rank)
           st_async_v4(mapa_shared(smem_u32(&ex.peers[slot][rank < p ? rank : rank - 1][lane]), p), mapa_shared(bar, p), bits);
-      ex.tile[lane] = t;
+      if constexpr (kGrads) {   // while the peers' are on their way
+        float4 w[kWarps];
 #pragma unroll
-      for (int j = 0; j < kWarps; ++j) ex.warps[kBwd ? kWarps - 1 - j : j][lane] = before[j];
-      if constexpr (kBwd && !kMapOnly) {
-#pragma unroll
-        for (int j = 0; j < kWarps; ++j) before[j] = h_maps[j][lane];
+        for (int j = 0; j < kWarps; ++j) w[j] = h_maps[j][lane];
 #pragma unroll
         for (int j = 0; j < kWarps; ++j) {
           *reinterpret_cast<float2*>(&h_maps[j][lane]) = make_float2(h.x(), h.y());
-          h = apply(before[j], h);
+          h = apply(w[j], h);
         }
       }
+      // (a wait that runs out raises the block's flag; what follows is then of no use, but ends)
+      if (S > 1) mbar_wait(bar, (k >> 1) & 1u, abort_flag, a.err);
+      constexpr int kPeers = (kFast ? kMaxCluster : kMaxCluster / 2) - 1;
+      float4 peer[kPeers];
+#pragma unroll
+      for (int p = 0; p < kPeers; ++p)
+        if (p < S - 1) peer[p] = ex.peers[slot][p][lane];
+      F2 here = carry;
+      float4 upto = identity;
+#pragma unroll
+      for (int p = 0; p <= kPeers; ++p) {
+        if (p == rank) {
+          here = carry;
+          if constexpr (kMapOnly) upto = compose(upto, own);
+          carry = apply(own, carry);
+        }
+        if (p < kPeers && p < S - 1) {
+          if constexpr (kMapOnly) upto = compose(upto, peer[p]);
+          carry = apply(peer[p], carry);
+        }
+      }
+      if constexpr (kMapOnly) {
+        total = compose(total, upto);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&in_bar[slot]));
+        continue;
+      }
+      auto put = [&](int j, F2 x) {
+        *reinterpret_cast<float2*>(&warps[kBwd ? kWarps - 1 - j : j][lane]) = make_float2(x.x(), x.y());
+      };
+      const F2 two = apply(pair[0], here), four = apply(quad[0], here), six = apply(pair[2], four);
+      put(0, here);
+      put(1, apply(m[0], here));
+      put(2, two);
+      put(3, apply(m[2], two));
+      put(4, four);
+      put(5, apply(m[4], four));
+      put(6, six);
+      put(7, apply(m[6], six));
       __syncwarp();
-      if (lane == 0) mbar_arrive_expect_tx(bar, (S - 1) * 512);
+      if (lane == 0) mbar_arrive(smem_u32(&in_bar[slot]));
+      if (!kBwd && a.states && tile >= 0 && tile % (kStateRows / kN) == 0)
+        store2<kFast>(a.states + int64_t(tile / (kStateRows / kN)) * a.H + c, here, left);
     }
+    if (kMapOnly && rank == 0) a.seg_maps[(int64_t(seg) * strips + strip) * 32 + lane] = total;
   } else {
     if (!kMapOnly && seg == 0) {
       pass_empty(a, kBwd ? a.dfinal : a.h0, kBwd ? a.dinit : a.final_state, c0, rank, S);
       if (strip == 0) check_bounds(a, rank, S);
     }
     const int r0 = warp * kRows;
-    const auto of_seq = [&](const float* p, int b) { return p ? load2<kFast>(p + int64_t(b) * a.H + c, left) : zero2(); };
-    // the state before the segment (E after it)
-    F2 carry = zero2();
-    float4 total = identity;
-    if constexpr (!kMapOnly) {
-      for (int s = kBwd ? static_cast<int>(gridDim.y) - 1 : 0; s != seg; s += kBwd ? -1 : 1)
-        carry = apply(a.seg_maps[(int64_t(s) * strips + strip) * 32 + lane], carry);
-    }
     // rows that do not come by TMA: every warp copies its own, all stages but one ahead
     const void* const tensor_of[3] = {a.gate, kValue ? a.value : a.dy, a.dy};
     const int64_t ld_of[3] = {a.gate_ld, kValue ? a.value_ld : a.dy_ld, a.dy_ld};
@@ -441,7 +514,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) scan_kernel(
           const uint32_t dst = smem_u32(smem_raw) + (k % kStages) * kStageBytes + j * kTensorBytes + r0 * kRowBytes;
 #pragma unroll 4
           for (int i = 0; i < kRows; ++i) {
-            const int64_t r = int64_t(t) * kTile + r0 + i;
+            const int64_t r = int64_t(t) * kN + r0 + i;
             if (r >= a.T) break;
             copy_row(dst + i * kRowBytes, static_cast<const T*>(tensor_of[j]) + r * ld_of[j] + c0, min(kStrip, a.H - c0),
                      r == 0 && c0 == 0, r == a.T - 1 && c0 + kStrip >= a.H, lane);
@@ -470,213 +543,261 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) scan_kernel(
       }
       held = -1;
     };
+    // a half's rows: m, and the tensors' values.  The forward keeps m of both halves from the maps to
+    // the results (its exponentials and reciprocals take as long as half of its bytes), the
+    // backward that of the last.
+    constexpr int kKept = kBwd ? 1 : kParts;
+    F2 kept[kKept][kHalf];
+    Raw<T> v[kHalf], d[kHalf];
     for (int k = 0; k < n_steps; ++k) {
-      const int st = k % kStages, slot = k & 1;
+      const int st = k % kStages;
       int tile = alive ? tile_of(k) : -1;
-      const TileRows& rows = rows_sh[st];
+      const TileRows<kN>& rows = rows_sh[st];
       if (tile >= 0) {
         if (!mbar_wait(smem_u32(&full_bar[st]), (k / kStages) & 1u, abort_flag, a.err)) {
           alive = false;
           tile = -1;
         }
       }
-      const int64_t row = int64_t(tile) * kTile + r0;   // the warp's first
-      uint32_t starts = 0, ends = 0, valid = 0;         // a bit for each of its rows; valid: in a sequence
+      const int64_t row = int64_t(tile) * kN + r0;   // the warp's first
+      // a bit for each of its rows: begins, ends a sequence; valid: is in one
+      uint32_t starts = 0, ends = 0, valid = 0;
       if (tile >= 0) {
-        starts = rows.starts[r0 >> 5] >> (r0 & 31) & 0xffffu;
-        ends = rows.ends[r0 >> 5] >> (r0 & 31) & 0xffffu;
+        starts = rows.starts[r0 >> 5] >> (r0 & 31) & ((1u << kRows) - 1u);
+        ends = rows.ends[r0 >> 5] >> (r0 & 31) & ((1u << kRows) - 1u);
         const int lo = min(max(rows.lo - r0, 0), kRows), hi = min(max(rows.hi - r0, 0), kRows);
-        valid = (1u << hi) - 1u & ~((1u << lo) - 1u);
+        valid = ((1u << hi) - 1u) & ~((1u << lo) - 1u);
         if constexpr (!kFast) {
           load_rows(k + kStages - 1);
           cp_async_wait<kStages - 1>();
           __syncwarp();
         }
       }
-      const bool simple = valid == (1u << kRows) - 1u && (starts | ends) == 0;
-      auto inside = [&](int i) -> bool { return valid >> i & 1u; };
-      uint8_t* const stage8 = smem_raw + st * kStageBytes + r0 * kRowBytes;
-      T* const stage = reinterpret_cast<T*>(stage8) + 2 * lane;
-      auto get = [&](int tensor, int i) -> F2 {
-        if constexpr (kFast || sizeof(T) == 4) {
-          return load2<true>(reinterpret_cast<const T*>(reinterpret_cast<const uint8_t*>(stage) + tensor * kTensorBytes +
-                                                        i * kRowBytes), 2);
+      uint8_t* const stage = smem_raw + st * kStageBytes + r0 * kRowBytes;
+      auto get = [&](int tensor, int i) -> Raw<T> {
+        const uint8_t* const p = stage + tensor * kTensorBytes + i * kRowBytes;
+        Raw<T> r;
+        if constexpr (sizeof(T) == 4) {
+          r.w.v = *reinterpret_cast<const unsigned long long*>(p + 8 * lane);
         } else {
-          const uint32_t* const w = reinterpret_cast<const uint32_t*>(stage8 + tensor * kTensorBytes + i * kRowBytes) + lane;
-          const bool odd = (odd_base >> tensor ^ (odd_ld >> tensor & static_cast<uint32_t>(row + i))) & 1u;
-          const uint32_t w0 = w[0], w1 = w[1];
-          float lo, hi;
-          unpack2(odd ? __byte_perm(w0, w1, 0x5432) : w0, static_cast<const T*>(nullptr), lo, hi);
-          return f2(lo, hi);
+          r.w = *reinterpret_cast<const uint32_t*>(p + 4 * lane);
+          if constexpr (!kFast) {
+            const uint32_t next = *reinterpret_cast<const uint32_t*>(p + 4 * lane + 4);
+            if ((odd_base >> tensor ^ (odd_ld >> tensor & static_cast<uint32_t>(row + i))) & 1u) r.w = __byte_perm(r.w, next, 0x5432);
+          }
         }
+        return r;
+      };
+
+      auto load_gates = [&](F2 (&m)[kHalf], int q) {
+#pragma unroll
+        for (int i = 0; i < kHalf; ++i) m[i] = decay<kForm>(get(0, q * kHalf + i).f());
+        const uint32_t in = valid >> (q * kHalf) & kAll;
+        if (in != kAll) {
+          // rows outside of every sequence change nothing (no h behind the last one is used)
+#pragma unroll
+          for (int i = 0; i < kHalf; ++i)
+            if (!(in >> i & 1u)) m[i] = zero2();
+        }
+      };
+      auto load_values = [&](int q) {
+#pragma unroll
+        for (int i = 0; i < kHalf; ++i) {
+          if constexpr (kValue) v[i] = get(kV, q * kHalf + i);
+          if constexpr (kBwd) d[i] = get(kD, q * kHalf + i);
+        }
+        const uint32_t in = valid >> (q * kHalf) & kAll;
+        if (in != kAll) {
+#pragma unroll
+          for (int i = 0; i < kHalf; ++i)
+            if (!(in >> i & 1u)) v[i] = d[i] = Raw<T>{};
+        }
+      };
+      // what the rows of these bits start from
+      auto start_half = [&](const float* p, uint32_t bits, int q, F2 (&x)[kHalf]) {
+#pragma unroll
+        for (int i = 0; i < kHalf; ++i) x[i] = zero2();
+        if (p == nullptr || bits == 0) return;
+#pragma unroll
+        for (int i = 0; i < kHalf; ++i)
+          if (bits >> i & 1u) x[i] = load2<kFast>(p + int64_t(rows.seq[r0 + q * kHalf + i]) * a.H + c, left);
+      };
+      auto pick = [](uint32_t bits, int i, F2 x, F2 y) -> F2 { return F2{bits >> i & 1u ? x.v : y.v}; };
+      // the half's map of h (A, x), and in a backward walk of E (A, x) and of h (A, z)
+      auto map_half = [&](const F2 (&m)[kHalf], int q, float4& of_walk, float4& of_h) {
+        const uint32_t s = starts >> (q * kHalf) & kAll, e = ends >> (q * kHalf) & kAll;
+        F2 A = f2(1.f), x = zero2(), z = zero2();
+        if ((s | e) == 0) {
+#pragma unroll
+          for (int i = 0; i < kHalf; ++i) {
+            A = fma2(m[i], A, A);
+            if constexpr (kValue) z = step<kForm>(z, m[i], v[i].f());
+          }
+          if constexpr (kBwd) {
+#pragma unroll
+            for (int i = kHalf - 1; i >= 0; --i) {
+              x = add2(x, d[i].f());
+              x = fma2(m[i], x, x);
+            }
+          }
+        } else {
+          F2 from[kHalf];
+          if constexpr (kValue) start_half(a.h0, s, q, from);
+#pragma unroll
+          for (int i = 0; i < kHalf; ++i) {
+            A = fma2(m[i], A, A);
+            if constexpr (kValue) z = step<kForm>(pick(s, i, from[i], z), m[i], v[i].f());
+          }
+          if constexpr (kBwd) {
+            start_half(a.dfinal, e, q, from);
+#pragma unroll
+            for (int i = kHalf - 1; i >= 0; --i) {
+              x = add2(pick(e, i, from[i], x), d[i].f());
+              x = fma2(m[i], x, x);
+            }
+          }
+        }
+        of_h = pack(Map{A, z}, s != 0);
+        of_walk = kBwd ? pack(Map{A, x}, e != 0) : of_h;
       };
 
       // ---- the maps of the warp's rows
-      F2 m[kRows];
-      float4 mine = identity, mine_h = identity;
+      float4 mine = identity, mine_h = identity, first_h = identity;   // first_h: the first half's
       if (tile >= 0) {
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) m[i] = decay<kForm>(get(0, i));
-        F2 A = f2(1.f), x = zero2(), z = zero2();   // x: the walk's, z: h in a backward walk
-        bool cut = false, cut_z = false;
-        if (simple) {
-#pragma unroll
-          for (int i = 0; i < kRows; ++i) {
-            A = fma2(m[i], A, A);
-            if constexpr (!kBwd) x = step<kForm>(x, m[i], get(kV, i));
-            if constexpr (kBwd && !kMapOnly) z = step<kForm>(z, m[i], get(kV, i));
-          }
-          if constexpr (kBwd) {
-#pragma unroll
-            for (int i = kRows - 1; i >= 0; --i) {
-              x = add2(x, get(kD, i));
-              x = fma2(m[i], x, x);
-            }
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < kRows; ++i) {
-            if (!inside(i)) continue;
-            A = fma2(m[i], A, A);
-            if constexpr (!kBwd || !kMapOnly) {
-              F2& w = kBwd ? z : x;
-              if (starts >> i & 1u) {
-                w = of_seq(a.h0, rows.seq[r0 + i]);
-                (kBwd ? cut_z : cut) = true;
-              }
-              w = step<kForm>(w, m[i], get(kV, i));
-            }
-          }
-          if constexpr (kBwd) {
-#pragma unroll
-            for (int i = kRows - 1; i >= 0; --i) {
-              if (!inside(i)) continue;
-              if (ends >> i & 1u) {
-                x = of_seq(a.dfinal, rows.seq[r0 + i]);
-                cut = true;
-              }
-              x = add2(x, get(kD, i));
-              x = fma2(m[i], x, x);
-            }
-          }
+        float4 w, h;
+        load_gates(kept[0], 0);
+        load_values(0);
+        map_half(kept[0], 0, mine, mine_h);
+        if constexpr (kParts == 2) {
+          first_h = mine_h;
+          load_gates(kept[kKept - 1], 1);
+          load_values(1);
+          map_half(kept[kKept - 1], 1, w, h);
+          mine = kBwd ? compose(w, mine) : compose(mine, w);
+          if constexpr (kGrads) mine_h = compose(mine_h, h);
         }
-        mine = pack(Map{A, x}, cut);
-        if constexpr (kBwd && !kMapOnly) mine_h = pack(Map{A, z}, cut_z);
       }
       ex.warps[warp][lane] = mine;
-      if constexpr (kBwd && !kMapOnly) h_maps[warp][lane] = mine_h;
-      maps_sync();
+      if constexpr (kGrads) h_maps[warp][lane] = mine_h;
       give_back();
-      if (!mbar_wait(smem_u32(&peer_bar[slot]), (k >> 1) & 1u, abort_flag, a.err)) {
+      maps_sync();
+      if constexpr (kMapOnly) {
+        if (tile >= 0 && lane == 0) mbar_arrive(smem_u32(&empty_bar[st]));   // (behind the sync)
+      }
+      // what enters the warp's rows (or: the maps have been read)
+      if (!mbar_wait(smem_u32(&in_bar[k & 1]), (k >> 1) & 1u, abort_flag, a.err)) {
         alive = false;
         tile = -1;
       }
-      // ---- what enters the warp's rows, and the step after
-      F2 in = carry;
-      for (int p = 0; p < S; ++p) {
-        const float4 of_tile = p == rank ? ex.tile[lane] : ex.peers[slot][p < rank ? p : p - 1][lane];
-        if constexpr (kMapOnly) {
-          if (warp == 0) total = compose(total, of_tile);
-        } else {
-          if (p == rank) {
-            in = apply(ex.warps[warp][lane], carry);
-            if (!kBwd && tile >= 0 && a.states && warp == 0) store2<kFast>(a.states + int64_t(tile) * a.H + c, carry, left);
-          }
-          carry = apply(of_tile, carry);
-        }
-      }
+      if (kMapOnly || tile < 0) continue;
+      const float2 entering = *reinterpret_cast<const float2*>(&ex.warps[warp][lane]);
+      F2 in = f2(entering.x, entering.y);
 
-      // ---- the rows again
-      if (tile < 0) continue;
-      // results of a warp whose rows are all in sequences go out as a box, from where its gates
-      // (and dy) have been
-      bool boxed = false;
-      if constexpr (!kBwd && !kMapOnly) {
-        T* y = static_cast<T*>(a.y) + row * a.H + c;
-        if (simple) {
-          boxed = kFast;
+      // ---- the rows again.  Where all of the warp's are in sequences their results go out as a box,
+      // from where the gates (and dy) have been
+      const bool boxed = kFast && valid == (1u << kRows) - 1u;
+      auto out_row = [&](T* base, int tensor, int i, F2 x) {
+        if (boxed)
+          store2<true>(reinterpret_cast<T*>(stage + tensor * kTensorBytes + i * kRowBytes) + 2 * lane, x, 2);
+        else
+          store2<kFast>(base + (row + i) * a.H + c, x, left);
+      };
+      if constexpr (!kBwd) {
+        T* const y = static_cast<T*>(a.y);
 #pragma unroll
-          for (int i = 0; i < kRows; ++i) {
-            in = step<kForm>(in, m[i], get(kV, i));
-            if constexpr (kFast)
-              store2<true>(stage + i * kStrip, in, 2);
-            else
-              store2<false>(y + int64_t(i) * a.H, in, left);
-          }
-        } else {
+        for (int q = 0; q < kParts; ++q) {
+          const uint32_t s = starts >> (q * kHalf) & kAll, e = ends >> (q * kHalf) & kAll, is = valid >> (q * kHalf) & kAll;
+          if (kParts > 1) load_values(q);
+          if (boxed && (s | e) == 0) {
 #pragma unroll
-          for (int i = 0; i < kRows; ++i) {
-            if (!inside(i)) {
-              if (a.fill && row + i < a.T) store2<kFast>(y + int64_t(i) * a.H, zero2(), left);
-              continue;
+            for (int i = 0; i < kHalf; ++i) {
+              in = step<kForm>(in, kept[q][i], v[i].f());
+              store2<true>(reinterpret_cast<T*>(stage + (q * kHalf + i) * kRowBytes) + 2 * lane, in, 2);
             }
-            if (starts >> i & 1u) in = of_seq(a.h0, rows.seq[r0 + i]);
-            in = step<kForm>(in, m[i], get(kV, i));
-            store2<kFast>(y + int64_t(i) * a.H, in, left);
-            if ((ends >> i & 1u) && a.final_state) store2<kFast>(a.final_state + int64_t(rows.seq[r0 + i]) * a.H + c, in, left);
+          } else {
+            F2 h[kHalf];   // first what rows start from, then h
+            start_half(a.h0, s, q, h);
+#pragma unroll
+            for (int i = 0; i < kHalf; ++i) h[i] = in = step<kForm>(pick(s, i, h[i], in), kept[q][i], v[i].f());
+#pragma unroll
+            for (int i = 0; i < kHalf; ++i)
+              if (is >> i & 1u)
+                out_row(y, 0, q * kHalf + i, h[i]);
+              else if (a.fill && row + q * kHalf + i < a.T)
+                out_row(y, 0, q * kHalf + i, zero2());
+            if (e != 0 && a.final_state) {
+#pragma unroll
+              for (int i = 0; i < kHalf; ++i)
+                if (e >> i & 1u) store2<kFast>(a.final_state + int64_t(rows.seq[r0 + q * kHalf + i]) * a.H + c, h[i], left);
+            }
           }
         }
-      } else if constexpr (!kMapOnly) {
-        T* dg = static_cast<T*>(a.dgate) + row * a.H + c;
-        T* dv = static_cast<T*>(a.dvalue) + row * a.H + c;
+      } else {
+        T* const dg = static_cast<T*>(a.dgate);
+        T* const dv = static_cast<T*>(a.dvalue);
         const float2 before = *reinterpret_cast<const float2*>(&h_maps[warp][lane]);
-        F2 h = f2(before.x, before.y);
-        // dgate and dvalue of a row from D and E, h of the row before and its value
+        const F2 h_in = f2(before.x, before.y);
+        // dgate and dvalue of a row from D and E and h of the row before
         auto grads = [&](int i, F2 D, F2 E, F2 hp, F2& df, F2& dval) {
           if constexpr (kForm == kFormSigmoid) {
-            const F2 w = mul2(m[i], f2(-1.f));
-            df = mul2(mul2(E, w), sub2(hp, get(kV, i)));
+            const F2 w = mul2(kept[0][i], f2(-1.f));
+            df = mul2(mul2(E, w), sub2(hp, v[i].f()));
             dval = mul2(D, w);
           } else {
             df = mul2(E, hp);
             dval = D;
           }
         };
-        F2 hp[kRows], df, dval;   // hp: h of the row before
-        if (simple) {
-          boxed = kFast;
-#pragma unroll
-          for (int i = 0; i < kRows; ++i) {
-            hp[i] = h;
-            h = step<kForm>(h, m[i], get(kV, i));
+#pragma unroll 1
+        for (int q = kParts - 1; q >= 0; --q) {
+          const uint32_t s = starts >> (q * kHalf) & kAll, e = ends >> (q * kHalf) & kAll, is = valid >> (q * kHalf) & kAll;
+          if (q < kParts - 1) {   // the last one's rows are still there
+            load_gates(kept[0], q);
+            load_values(q);
           }
+          const F2(&m)[kHalf] = kept[0];
+          F2 h = q > 0 ? apply(first_h, h_in) : h_in, hp[kHalf], df, dval;   // hp: h of the row before
+          if (boxed && (s | e) == 0) {
 #pragma unroll
-          for (int i = kRows - 1; i >= 0; --i) {
-            const F2 D = add2(get(kD, i), in);
-            in = fma2(m[i], D, D);   // E
-            grads(i, D, in, hp[i], df, dval);
-            if constexpr (kFast) {
-              store2<true>(stage + i * kStrip, df, 2);
-              store2<true>(stage + kD * (kTile * kStrip) + i * kStrip, dval, 2);
-            } else {
-              store2<false>(dg + int64_t(i) * a.H, df, left);
-              store2<false>(dv + int64_t(i) * a.H, dval, left);
+            for (int i = 0; i < kHalf; ++i) {
+              hp[i] = h;
+              h = step<kForm>(h, m[i], v[i].f());
             }
-          }
-        } else {
 #pragma unroll
-          for (int i = 0; i < kRows; ++i) {
-            if (!inside(i)) continue;
-            if (starts >> i & 1u) h = of_seq(a.h0, rows.seq[r0 + i]);
-            hp[i] = h;
-            h = step<kForm>(h, m[i], get(kV, i));
-          }
+            for (int i = kHalf - 1; i >= 0; --i) {
+              const F2 D = add2(d[i].f(), in);
+              in = fma2(m[i], D, D);   // E
+              grads(i, D, in, hp[i], df, dval);
+              T* const p = reinterpret_cast<T*>(stage + (q * kHalf + i) * kRowBytes) + 2 * lane;
+              store2<true>(p, df, 2);
+              store2<true>(p + kD * kTensorBytes / static_cast<int>(sizeof(T)), dval, 2);
+            }
+          } else {
+            F2 from[kHalf];
+            start_half(a.h0, s, q, from);
 #pragma unroll
-          for (int i = kRows - 1; i >= 0; --i) {
-            if (!inside(i)) {
-              if (row + i < a.T) {
-                store2<kFast>(dg + int64_t(i) * a.H, zero2(), left);
-                store2<kFast>(dv + int64_t(i) * a.H, zero2(), left);
+            for (int i = 0; i < kHalf; ++i) {
+              hp[i] = h = pick(s, i, from[i], h);
+              h = step<kForm>(h, m[i], v[i].f());
+            }
+            start_half(a.dfinal, e, q, from);
+#pragma unroll
+            for (int i = kHalf - 1; i >= 0; --i) {
+              const F2 D = add2(d[i].f(), pick(e, i, from[i], in));
+              in = fma2(m[i], D, D);
+              grads(i, D, in, hp[i], df, dval);
+              from[i] = in;
+              if (!(is >> i & 1u)) df = dval = zero2();
+              if (row + q * kHalf + i < a.T) {
+                out_row(dg, 0, q * kHalf + i, df);
+                out_row(dv, kD, q * kHalf + i, dval);
               }
-              continue;
             }
-            if (ends >> i & 1u) in = of_seq(a.dfinal, rows.seq[r0 + i]);
-            const F2 D = add2(get(kD, i), in);
-            in = fma2(m[i], D, D);
-            grads(i, D, in, hp[i], df, dval);
-            store2<kFast>(dg + int64_t(i) * a.H, df, left);
-            store2<kFast>(dv + int64_t(i) * a.H, dval, left);
-            if ((starts >> i & 1u) && a.dinit) store2<kFast>(a.dinit + int64_t(rows.seq[r0 + i]) * a.H + c, in, left);
+            if (s != 0 && a.dinit) {
+#pragma unroll
+              for (int i = 0; i < kHalf; ++i)
+                if (s >> i & 1u) store2<kFast>(a.dinit + int64_t(rows.seq[r0 + q * kHalf + i]) * a.H + c, from[i], left);
+            }
           }
         }
       }
@@ -684,9 +805,9 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) scan_kernel(
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
-          const uint32_t box = smem_u32(smem_raw) + st * kStageBytes + r0 * kStrip * static_cast<int>(sizeof(T));
+          const uint32_t box = smem_u32(stage);
           tma_store_2d(&maps.out0, box, c0, static_cast<int>(row));
-          if constexpr (kBwd && !kMapOnly) tma_store_2d(&maps.out1, box + kD * kTensorBytes, c0, static_cast<int>(row));
+          if constexpr (kGrads) tma_store_2d(&maps.out1, box + kD * kTensorBytes, c0, static_cast<int>(row));
           bulk_commit_group();
         }
         held = st;
@@ -698,7 +819,6 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) scan_kernel(
     give_back();
     if (lane == 0) bulk_wait_group<0>();
     if constexpr (!kFast) cp_async_wait<0>();
-    if (kMapOnly && warp == 0 && rank == 0) a.seg_maps[(int64_t(seg) * strips + strip) * 32 + lane] = total;
   }
   __syncthreads();
   cluster_sync_all();   // no block leaves while a peer may still write to it
@@ -733,7 +853,7 @@ molt_status check_desc(const molt_scan_desc* d, bool packed) {
   if (d->dtype != MOLT_BF16 && d->dtype != MOLT_FP16 && d->dtype != MOLT_FP32)
     return fail(MOLT_ERR_INVALID_ARG, "unknown element type");
   if (d->form != MOLT_SCAN_SIGMOID && d->form != MOLT_SCAN_LOG) return fail(MOLT_ERR_INVALID_ARG, "unknown form of the recurrence");
-  if (d->T > 2147483647 - 2 * kTile || d->H > 65536 || d->B > 2147483647 - 64)
+  if (d->T > 2147483647 - 2 * kStateRows || d->H > 65536 || d->B > 2147483647 - 64)
     return fail(MOLT_ERR_UNSUPPORTED_SHAPE, "T and B must be below 2^31 - 256 and H at most 65536");
   if (!packed && (d->B == 0 ? d->T != 0 : d->T % d->B != 0))
     return fail(MOLT_ERR_INVALID_ARG, "without cu_seqlens T must be a multiple of B");
@@ -783,52 +903,95 @@ constexpr int kMaxSegments = 32;
 int64_t strips_of(const molt_scan_desc* d) { return (d->H + kStrip - 1) / kStrip; }
 size_t seg_bytes(const molt_scan_desc* d) { return static_cast<size_t>(kMaxSegments) * strips_of(d) * 32 * sizeof(float4) + 256; }
 
+constexpr int kDevices = 16;
+
+// One instance of the kernel.
+struct ScanKernel {
+  void (*fn)(const ScanMaps, const ScanArgs);
+  int smem;
+  // by device and a cluster's blocks: how many clusters run at once (0: not yet asked)
+  std::atomic<int> clusters[kDevices][kMaxCluster + 1];
+};
+template <class T, int kForm, bool kBwd, bool kMapOnly, bool kFast>
+ScanKernel* kernel_of() {
+  constexpr int kTensors = kBwd && !kMapOnly ? 3 : 2;
+  static ScanKernel k{&scan_kernel<T, kForm, kBwd, kMapOnly, kFast>,
+                      kStagesOf<kBwd, kMapOnly> * kTile<T, kBwd> * kRowsBytesOf<T, kTensors, kFast>, {}};
+  return &k;
+}
+template <class T, int kForm>
+ScanKernel* kernel_of(bool bwd, bool map_only, bool fast) {
+  if (fast)
+    return bwd ? (map_only ? kernel_of<T, kForm, true, true, true>() : kernel_of<T, kForm, true, false, true>())
+               : (map_only ? kernel_of<T, kForm, false, true, true>() : kernel_of<T, kForm, false, false, true>());
+  return bwd ? (map_only ? kernel_of<T, kForm, true, true, false>() : kernel_of<T, kForm, true, false, false>())
+             : (map_only ? kernel_of<T, kForm, false, true, false>() : kernel_of<T, kForm, false, false, false>());
+}
+template <class T>
+ScanKernel* kernel_of(int form, bool bwd, bool map_only, bool fast) {
+  return form == kFormSigmoid ? kernel_of<T, kFormSigmoid>(bwd, map_only, fast) : kernel_of<T, kFormLog>(bwd, map_only, fast);
+}
+ScanKernel* kernel_of(int dtype, int form, bool bwd, bool map_only, bool fast) {
+  return dtype == MOLT_FP32   ? kernel_of<float>(form, bwd, map_only, fast)
+         : dtype == MOLT_FP16 ? kernel_of<__half>(form, bwd, map_only, fast)
+                              : kernel_of<__nv_bfloat16>(form, bwd, map_only, fast);
+}
+
+struct ScanLaunch {
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr{};
+  ScanLaunch(const ScanKernel* k, int strips, int cluster, int segments, cudaStream_t s) {
+    cfg.gridDim = dim3(strips * cluster, segments);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = static_cast<size_t>(k->smem);
+    cfg.stream = s;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = cluster;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+  }
+};
+
+// Clusters of so many blocks that run at once.  Blocks that the SMs hold are not all of use: a
+// cluster's are in one GPC (clusters of 7 in three rounds of blocks to an SM: 448 of 456 blocks
+// asked for, and two waves).
+cudaError_t clusters_at_once(ScanKernel* k, int cluster, int& n) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  std::atomic<int>* const known = dev < kDevices ? &k->clusters[dev][cluster] : nullptr;
+  n = known ? known->load(std::memory_order_relaxed) : 0;
+  if (n > 0) return cudaSuccess;
+  e = cudaFuncSetAttribute(k->fn, cudaFuncAttributeMaxDynamicSharedMemorySize, k->smem);
+  if (e != cudaSuccess) return e;
+  ScanLaunch l(k, 1, cluster, 1, nullptr);
+  l.cfg.attrs = &l.attr;
+  e = cudaOccupancyMaxActiveClusters(&n, k->fn, &l.cfg);
+  if (e != cudaSuccess) return e;
+  n = std::max(n, 1);
+  if (known) known->store(n, std::memory_order_relaxed);
+  if (getenv("SCAN_DEBUG")) fprintf(stderr, "cluster %d: %d\n", cluster, n);
+  return cudaSuccess;
+}
+
 struct ScanPlan {
   int cluster, segments;
 };
-ScanPlan plan_of(const molt_scan_desc* d, int tiles, int n_sm, bool fast) {
-  const int64_t strips = strips_of(d), slots = int64_t(n_sm) * (d->dtype == MOLT_FP32 ? 1 : 2);
-  ScanPlan p;
-  p.cluster = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({fast ? kMaxCluster : kMaxCluster / 2, slots / strips, tiles})));
-  const int64_t room = slots / (strips * p.cluster), steps = (tiles + p.cluster - 1) / p.cluster;
-  p.segments = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({kMaxSegments, room, steps / 8})));
-  return p;
-}
-
-template <class T, int kForm, bool kBwd, bool kMapOnly, bool kFast>
-cudaError_t launch_kernel(const ScanMaps& m, const ScanArgs& a, int strips, int cluster, int segments, cudaStream_t s) {
-  constexpr int kTensors = kBwd && !kMapOnly ? 3 : 2;
-  constexpr int smem = kStagesOf<kTensors> * kStageBytesOf<T, kTensors, kFast>;
-  const auto k = &scan_kernel<T, kForm, kBwd, kMapOnly, kFast>;
-  if (const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem); e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(strips * cluster, segments);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = cluster;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, k, m, a);
-}
-template <class T, int kForm, bool kFast>
-cudaError_t launch_form(const ScanMaps& m, const ScanArgs& a, bool bwd, bool map_only, int strips, int cluster, int segments,
-                        cudaStream_t s) {
-  if (bwd)
-    return map_only ? launch_kernel<T, kForm, true, true, kFast>(m, a, strips, cluster, segments, s)
-                    : launch_kernel<T, kForm, true, false, kFast>(m, a, strips, cluster, segments, s);
-  return map_only ? launch_kernel<T, kForm, false, true, kFast>(m, a, strips, cluster, segments, s)
-                  : launch_kernel<T, kForm, false, false, kFast>(m, a, strips, cluster, segments, s);
-}
-template <class T>
-cudaError_t launch_type(const ScanMaps& m, const ScanArgs& a, int form, bool fast, bool bwd, bool map_only, int strips, int cluster,
-                        int segments, cudaStream_t s) {
-  const auto k = form == kFormSigmoid ? (fast ? launch_form<T, kFormSigmoid, true> : launch_form<T, kFormSigmoid, false>)
-                                      : (fast ? launch_form<T, kFormLog, true> : launch_form<T, kFormLog, false>);
-  return k(m, a, bwd, map_only, strips, cluster, segments, s);
+// The largest clusters with which all strips run at once; the rows in segments where there is
+// room for several times the strips, and each has eight steps or more.
+cudaError_t plan_of(ScanKernel* k, int64_t strips, int tiles, bool fast, ScanPlan& p) {
+  p.cluster = p.segments = 1;
+  int n = 0;
+  for (int s = fast ? kMaxCluster : kMaxCluster / 2; s >= 1; --s) {
+    if (s > tiles && s > 1) continue;
+    if (const cudaError_t e = clusters_at_once(k, s, n); e != cudaSuccess) return e;
+    p.cluster = s;
+    if (n >= strips) break;
+  }
+  const int64_t steps = (tiles + p.cluster - 1) / p.cluster;
+  p.segments = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({kMaxSegments, n / strips, steps / 8})));
+  return cudaSuccess;
 }
 
 molt_status launch(const molt_scan_desc* d, ScanArgs& a, bool bwd, void* workspace, size_t workspace_bytes, cudaStream_t s) {
@@ -836,9 +999,13 @@ molt_status launch(const molt_scan_desc* d, ScanArgs& a, bool bwd, void* workspa
   a.err = device_status_word(&st);
   if (!a.err) return st;
   const int strips = static_cast<int>(strips_of(d));
-  a.tiles = static_cast<int>((a.T + kTile - 1) / kTile);
+  const int tile = d->dtype == MOLT_FP32 ? (bwd ? kTile<float, true> : kTile<float, false>)
+                                         : (bwd ? kTile<__half, true> : kTile<__half, false>);
+  a.tiles = static_cast<int>((a.T + tile - 1) / tile);
   const bool fast = a.tiles > 0 && fast_of(a, d->dtype);
-  const ScanPlan plan = plan_of(d, a.tiles, device_sm_count(), fast);
+  ScanPlan plan;
+  if (const cudaError_t e = plan_of(kernel_of(d->dtype, d->form, bwd, false, fast), strips, a.tiles, fast, plan); e != cudaSuccess)
+    return cuda_fail(e, "gated scan");
   a.seg_tiles = (a.tiles + plan.segments - 1) / plan.segments;
   const int segments = a.tiles > 0 ? (a.tiles + a.seg_tiles - 1) / a.seg_tiles : 1;
   Scratch sc;
@@ -849,24 +1016,27 @@ molt_status launch(const molt_scan_desc* d, ScanArgs& a, bool bwd, void* workspa
   ScanMaps m{};
   if (fast) {
     const int e = dtype_bytes(d->dtype);
-    const auto encode = [&](CUtensorMap* t, const void* p, int64_t ld, int rows = kTile) {
+    const auto encode = [&](CUtensorMap* t, const void* p, int64_t ld, int rows) {
       return encode_tmap_plain(t, e == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, e, p, a.T, a.H, ld,
                                kStrip, rows);
     };
-    if (const molt_status q = encode(&m.gate, a.gate, a.gate_ld); q != MOLT_OK) return q;
-    if (const molt_status q = encode(&m.value, a.value, a.value_ld); q != MOLT_OK) return q;
+    if (const molt_status q = encode(&m.gate, a.gate, a.gate_ld, tile); q != MOLT_OK) return q;
+    if (const molt_status q = encode(&m.value, a.value, a.value_ld, tile); q != MOLT_OK) return q;
     if (bwd)
-      if (const molt_status q = encode(&m.dy, a.dy, a.dy_ld); q != MOLT_OK) return q;
-    if (const molt_status q = encode(&m.out0, bwd ? a.dgate : a.y, a.H, kRows); q != MOLT_OK) return q;
+      if (const molt_status q = encode(&m.dy, a.dy, a.dy_ld, tile); q != MOLT_OK) return q;
+    if (const molt_status q = encode(&m.out0, bwd ? a.dgate : a.y, a.H, tile / kWarps); q != MOLT_OK) return q;
     if (bwd)
-      if (const molt_status q = encode(&m.out1, a.dvalue, a.H, kRows); q != MOLT_OK) return q;
+      if (const molt_status q = encode(&m.out1, a.dvalue, a.H, tile / kWarps); q != MOLT_OK) return q;
   }
   for (int pass = segments > 1 ? 0 : 1; pass < 2; ++pass) {
-    const bool map_only = pass == 0;
-    const cudaError_t e =
-        d->dtype == MOLT_FP32   ? launch_type<float>(m, a, d->form, fast, bwd, map_only, strips, plan.cluster, segments, s)
-        : d->dtype == MOLT_FP16 ? launch_type<__half>(m, a, d->form, fast, bwd, map_only, strips, plan.cluster, segments, s)
-                                : launch_type<__nv_bfloat16>(m, a, d->form, fast, bwd, map_only, strips, plan.cluster, segments, s);
+    ScanKernel* const k = kernel_of(d->dtype, d->form, bwd, pass == 0, fast);
+    int n;   // (asked once: sets the kernel's shared memory)
+    cudaError_t e = clusters_at_once(k, plan.cluster, n);
+    if (e == cudaSuccess) {
+      ScanLaunch l(k, strips, plan.cluster, segments, s);
+      l.cfg.attrs = &l.attr;
+      e = cudaLaunchKernelEx(&l.cfg, k->fn, m, a);
+    }
     if (e != cudaSuccess) return cuda_fail(e, "gated scan");
     note_launches(1);
   }
