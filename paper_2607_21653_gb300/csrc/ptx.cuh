@@ -379,6 +379,13 @@ __device__ __forceinline__ void st_async_v4(uint32_t cluster_addr, uint32_t bar_
       "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w), "r"(bar_cluster)
       : "memory");
 }
+// bytes (a multiple of 16) from this CTA's shared memory to a CTA of the cluster, counted on a
+// barrier there
+__device__ __forceinline__ void bulk_copy_cluster(uint32_t dst_cluster, uint32_t src, uint32_t bytes, uint32_t bar_cluster) {
+  asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst_cluster),
+               "r"(src), "r"(bytes), "r"(bar_cluster)
+               : "memory");
+}
 __device__ __forceinline__ void fence_proxy_async_cluster() {
   asm volatile("fence.proxy.async.shared::cluster;" ::: "memory");
 }

@@ -265,12 +265,12 @@ __device__ __forceinline__ float4 compose(const float4& m, const float4& n) {
 }
 
 // What the warps of a block and the blocks of a cluster tell one another in a step.  warps:
-// the map of each warp's rows, then in x and y what enters them.  Two slots for the peers, so
-// that one a step ahead does not write what is still read.
+// the map of each warp's rows, then in x and y what enters them.  tiles: the maps of all
+// blocks' tiles, two slots, so that a peer a step ahead does not write what is still read.
 template <int kCluster>
 struct Exchange {
   float4 warps[kWarps][32];
-  float4 peers[2][kCluster - 1][32];
+  float4 tiles[2][kCluster][32];
 };
 
 // the eight warps with rows, and the one that folds
@@ -354,7 +354,7 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
   constexpr int kTensorBytes = kN * kRowBytes, kStageBytes = kTensors * kTensorBytes;
   extern __shared__ __align__(128) uint8_t smem_raw[];
   __shared__ __align__(16) Exchange<kFast ? kMaxCluster : kMaxCluster / 2> ex;
-  __shared__ float4 h_maps[kGrads ? kWarps : 1][32];   // then, in x and y, h before each warp's rows
+  __shared__ float2 h_maps[kGrads ? kWarps : 1][32];   // b of the maps of h, then h before each warp's rows
   __shared__ TileRows<kN> rows_sh[kStages];
   __shared__ __align__(8) uint64_t full_bar[kStages], empty_bar[kStages], peer_bar[2], in_bar[2];
   __shared__ int abort_sh;
@@ -432,44 +432,56 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
       float4(*const warps)[32] = ex.warps;
 #pragma unroll
       for (int j = 0; j < kWarps; ++j) m[j] = warps[kBwd ? kWarps - 1 - j : j][lane];
+      float4 of_h[kGrads ? kWarps : 1];
+      if constexpr (kGrads) {
+#pragma unroll
+        for (int j = 0; j < kWarps; ++j) {
+          const float2 b = h_maps[kWarps - 1 - j][lane];
+          const bool cut = __float_as_int(m[j].x) < 0, cut_h = __float_as_int(m[j].y) < 0;
+          const float x = fabsf(m[j].x), y = fabsf(m[j].y);
+          of_h[j] = make_float4(cut_h ? -1.f : x, cut_h ? -1.f : y, b.x, b.y);
+          m[j].x = cut ? -1.f : x;
+          m[j].y = cut ? -1.f : y;
+        }
+      }
 #pragma unroll
       for (int j = 0; j < 4; ++j) pair[j] = compose(m[2 * j], m[2 * j + 1]);
 #pragma unroll
       for (int j = 0; j < 2; ++j) quad[j] = compose(pair[2 * j], pair[2 * j + 1]);
       const float4 own = compose(quad[0], quad[1]);
-      const int4 bits = make_int4(__float_as_int(own.x), __float_as_int(own.y), __float_as_int(own.z), __float_as_int(own.w));
-      for (int p = 0; p < S; ++p)
-        if (p != rank)
-          st_async_v4(mapa_shared(smem_u32(&ex.peers[slot][rank < p ? rank : rank - 1][lane]), p), mapa_shared(bar, p), bits);
+      // one copy to each peer, all at once (a lane's 16 bytes to each in turn took 190 clocks a peer)
+      ex.tiles[slot][rank][lane] = own;
+      if (S > 1) {
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane < S && lane != rank) {
+          const uint32_t at = smem_u32(&ex.tiles[slot][rank][0]);
+          bulk_copy_cluster(mapa_shared(at, lane), at, 512, mapa_shared(bar, lane));
+        }
+      }
       if constexpr (kGrads) {   // while the peers' are on their way
-        float4 w[kWarps];
 #pragma unroll
-        for (int j = 0; j < kWarps; ++j) w[j] = h_maps[j][lane];
-#pragma unroll
-        for (int j = 0; j < kWarps; ++j) {
-          *reinterpret_cast<float2*>(&h_maps[j][lane]) = make_float2(h.x(), h.y());
-          h = apply(w[j], h);
+        for (int j = kWarps - 1; j >= 0; --j) {
+          h_maps[kWarps - 1 - j][lane] = make_float2(h.x(), h.y());
+          h = apply(of_h[j], h);
         }
       }
       // (a wait that runs out raises the block's flag; what follows is then of no use, but ends)
       if (S > 1) mbar_wait(bar, (k >> 1) & 1u, abort_flag, a.err);
-      constexpr int kPeers = (kFast ? kMaxCluster : kMaxCluster / 2) - 1;
-      float4 peer[kPeers];
+      constexpr int kTiles = kFast ? kMaxCluster : kMaxCluster / 2;
+      float4 t[kTiles];
 #pragma unroll
-      for (int p = 0; p < kPeers; ++p)
-        if (p < S - 1) peer[p] = ex.peers[slot][p][lane];
+      for (int p = 0; p < kTiles; ++p) t[p] = ex.tiles[slot][p][lane];   // (of no use from S on)
       F2 here = carry;
       float4 upto = identity;
 #pragma unroll
-      for (int p = 0; p <= kPeers; ++p) {
-        if (p == rank) {
-          here = carry;
-          if constexpr (kMapOnly) upto = compose(upto, own);
-          carry = apply(own, carry);
-        }
-        if (p < kPeers && p < S - 1) {
-          if constexpr (kMapOnly) upto = compose(upto, peer[p]);
-          carry = apply(peer[p], carry);
+      for (int p = 0; p < kTiles; ++p) {
+        if constexpr (kMapOnly) {
+          if (p < S) upto = compose(upto, t[p]);
+        } else {
+          here.v = p == rank ? carry.v : here.v;
+          const F2 next = apply(t[p], carry);
+          carry.v = p < S ? next.v : carry.v;
         }
       }
       if constexpr (kMapOnly) {
@@ -677,8 +689,14 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
           if constexpr (kGrads) mine_h = compose(mine_h, h);
         }
       }
-      ex.warps[warp][lane] = mine;
-      if constexpr (kGrads) h_maps[warp][lane] = mine_h;
+      if constexpr (!kGrads) ex.warps[warp][lane] = mine;
+      if constexpr (kGrads) {
+        // the maps of E and of h have one A but for their cuts, which go in its signs
+        const bool cut = mine.x < 0.f, cut_h = mine_h.x < 0.f;
+        const float2 A = cut ? make_float2(mine_h.x, mine_h.y) : make_float2(mine.x, mine.y);   // (of no use if both are cut)
+        ex.warps[warp][lane] = make_float4(copysignf(A.x, cut ? -1.f : 1.f), copysignf(A.y, cut_h ? -1.f : 1.f), mine.z, mine.w);
+        h_maps[warp][lane] = make_float2(mine_h.z, mine_h.w);
+      }
       give_back();
       maps_sync();
       if constexpr (kMapOnly) {
@@ -735,7 +753,7 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
       } else {
         T* const dg = static_cast<T*>(a.dgate);
         T* const dv = static_cast<T*>(a.dvalue);
-        const float2 before = *reinterpret_cast<const float2*>(&h_maps[warp][lane]);
+        const float2 before = h_maps[warp][lane];
         const F2 h_in = f2(before.x, before.y);
         // dgate and dvalue of a row from D and E and h of the row before
         auto grads = [&](int i, F2 D, F2 E, F2 hp, F2& df, F2& dval) {
