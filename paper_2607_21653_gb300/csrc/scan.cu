@@ -275,6 +275,10 @@ struct Exchange {
 
 // the eight warps with rows, and the one that folds
 __device__ __forceinline__ void maps_sync() { asm volatile("bar.sync 1, %0;" ::"n"((kWarps + 1) * 32) : "memory"); }
+// the latter's answer: the warps that wait for it at a barrier issue nothing meanwhile (polling an
+// mbarrier they took a third of the SM's instructions)
+__device__ __forceinline__ void folded() { asm volatile("bar.arrive 2, %0;" ::"n"((kWarps + 1) * 32) : "memory"); }
+__device__ __forceinline__ void wait_folded() { asm volatile("bar.sync 2, %0;" ::"n"((kWarps + 1) * 32) : "memory"); }
 
 // A stage is the tile's rows of each tensor.  As many as leave room for two blocks to an SM (fp32
 // backward: one).  Rows that do not come by TMA begin inside a word and may need one more.
@@ -356,7 +360,7 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
   __shared__ __align__(16) Exchange<kFast ? kMaxCluster : kMaxCluster / 2> ex;
   __shared__ float2 h_maps[kGrads ? kWarps : 1][32];   // b of the maps of h, then h before each warp's rows
   __shared__ TileRows<kN> rows_sh[kStages];
-  __shared__ __align__(8) uint64_t full_bar[kStages], empty_bar[kStages], peer_bar[2], in_bar[2];
+  __shared__ __align__(8) uint64_t full_bar[kStages], empty_bar[kStages], peer_bar[2];
   __shared__ int abort_sh;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   volatile int* abort_flag = &abort_sh;
@@ -378,10 +382,7 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
       mbar_init(smem_u32(&full_bar[s]), kFast ? 2 : 1);
       mbar_init(smem_u32(&empty_bar[s]), kWarps);
     }
-    for (int s = 0; s < 2; ++s) {
-      mbar_init(smem_u32(&peer_bar[s]), 1);
-      mbar_init(smem_u32(&in_bar[s]), 1);
-    }
+    for (int s = 0; s < 2; ++s) mbar_init(smem_u32(&peer_bar[s]), 1);
     abort_sh = 0;
     fence_mbar_init();
   }
@@ -486,8 +487,7 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
       }
       if constexpr (kMapOnly) {
         total = compose(total, upto);
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&in_bar[slot]));
+        folded();
         continue;
       }
       auto put = [&](int j, F2 x) {
@@ -502,8 +502,7 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
       put(5, apply(m[4], four));
       put(6, six);
       put(7, apply(m[6], six));
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&in_bar[slot]));
+      folded();
       if (!kBwd && a.states && tile >= 0 && tile % (kStateRows / kN) == 0)
         store2<kFast>(a.states + int64_t(tile / (kStateRows / kN)) * a.H + c, here, left);
     }
@@ -703,10 +702,7 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
         if (tile >= 0 && lane == 0) mbar_arrive(smem_u32(&empty_bar[st]));   // (behind the sync)
       }
       // what enters the warp's rows (or: the maps have been read)
-      if (!mbar_wait(smem_u32(&in_bar[k & 1]), (k >> 1) & 1u, abort_flag, a.err)) {
-        alive = false;
-        tile = -1;
-      }
+      wait_folded();
       if (kMapOnly || tile < 0) continue;
       const float2 entering = *reinterpret_cast<const float2*>(&ex.warps[warp][lane]);
       F2 in = f2(entering.x, entering.y);
