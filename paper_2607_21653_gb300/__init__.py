@@ -34,7 +34,7 @@ _BUILD = os.path.join(_ROOT, "_build")
 _LIB = os.path.join(_PKG, "libmolt.so")
 _SOURCES = ["rows.cu", "lmhead_fwd.cu", "lmhead_bwd.cu", "lmhead_bwd4.cu", "lmhead_bwd_chunk.cu", "api.cu", "noalloc.cu",
             "ce.cu", "embed.cu", "norm.cu", "norm_bf16.cu", "norm_fp16.cu", "norm_fp32.cu", "ffn.cu", "ffn_gemm.cu",
-            "scan.cu", "dropout.cu"]
+            "ffn_rows.cu", "scan.cu", "dropout.cu"]
 ARCH_FLAGS = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 STATUS = {

@@ -271,6 +271,20 @@ molt_status molt_gated_ffn_fwd(const molt_ffn_desc* desc, const void* x, const v
   if (!err) return st;
   const bool fp16 = desc->dtype == MOLT_FP16;
   char* h = static_cast<char*>(sc.aligned());
+  if (desc->T <= kFfnFewRows) {
+    FfnRows r{x, w_gate, w_up, ld_or(desc->x_stride, desc->H), ld_or(desc->w_gate_stride, desc->H),
+              ld_or(desc->w_up_stride, desc->H), {h, gate_out, up_out}, static_cast<int>(desc->T), static_cast<int>(desc->F),
+              static_cast<int>(desc->H), desc->activation};
+    cudaError_t e = launch_ffn_rows(r, true, fp16, stream);
+    if (e != cudaSuccess) return cuda_fail(e, "feed-forward rows");
+    note_launches(1);
+    r = FfnRows{h, w_down, nullptr, desc->F, ld_or(desc->w_down_stride, desc->F), 0, {y, nullptr, nullptr},
+                static_cast<int>(desc->T), static_cast<int>(desc->H), static_cast<int>(desc->F), desc->activation};
+    e = launch_ffn_rows(r, false, fp16, stream);
+    if (e != cudaSuccess) return cuda_fail(e, "feed-forward rows");
+    note_launches(1);
+    return MOLT_OK;
+  }
   void* parts = h + hidden_bytes(desc);
   const size_t parts_bytes = parts_fwd(desc, ffn_pairs(device_sm_count()));
   Product q;

@@ -61,6 +61,18 @@ struct FfnReduce {
   void* out[3];
 };
 
+// A product for a few rows: out[t, n] = x[t, k] w[n, k]^T; the first one of the block has w0 =
+// Wg and w1 = Wu and gives h (out[0]) and, unless nullptr, g and u.
+constexpr int kFfnFewRows = 16;
+struct FfnRows {
+  const void *x, *w0, *w1;
+  int64_t x_ld, w0_ld, w1_ld;
+  void* out[3];
+  int t, n, k;
+  int act;
+};
+cudaError_t launch_ffn_rows(const FfnRows& r, bool glu, bool fp16, cudaStream_t s);
+
 int ffn_pairs(int n_sm);   // CTA pairs of a launch
 cudaError_t launch_ffn_gemm(const FfnBatch& b, bool fp16, int n_sm, cudaStream_t s);
 cudaError_t launch_ffn_reduce(const FfnReduce& r, bool fp16, int n_sm, cudaStream_t s);

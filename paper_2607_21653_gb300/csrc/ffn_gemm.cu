@@ -30,6 +30,7 @@
 #include <type_traits>
 
 #include "ffn.cuh"
+#include "ffn_act.cuh"
 #include "molt_internal.cuh"
 #include "ptx.cuh"
 #include "vec.cuh"
@@ -48,33 +49,6 @@ constexpr int kWarpB = 2 + kEpiWarps;
 constexpr int kThreads = 32 * (kWarpB + 1);
 constexpr int kSmemBytes = 1024 + kOffBox + kEpiWarps * kBoxes * kBoxBytes;
 constexpr int kRaster = 8;                        // row tiles that a column tile is taken with
-constexpr float kLog2e = 1.4426950408889634f;
-
-// act(g), and with it act'(g)
-__device__ __forceinline__ float rcp_approx(float x) {
-  float y;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-// 2 sqrt(2 / pi) log2 e, and 0.044715 of it
-constexpr float kGeluA = 2.f * 0.7978845608028654f, kGeluB = 0.044715f;
-template <bool kGrad>
-__device__ __forceinline__ float activate(int act, float g, float& d) {
-  if (act == kActRelu) {
-    d = g > 0.f ? 1.f : 0.f;
-    return g <= 0.f ? 0.f : g;
-  }
-  if (act == kActSilu) {
-    const float p = rcp_approx(1.f + ex2_approx(-kLog2e * g));
-    if (kGrad) d = fmaf(g * (1.f - p), p, p);
-    return g * p;
-  }
-  // (1 + tanh z) / 2 = 1 / (1 + e^(-2 z)), z = sqrt(2 / pi) (g + 0.044715 g^3)
-  const float q = g * g;
-  const float p = rcp_approx(1.f + ex2_approx(-kLog2e * kGeluA * g * fmaf(kGeluB, q, 1.f)));
-  if (kGrad) d = fmaf(g * p * (1.f - p), kGeluA * fmaf(3.f * kGeluB, q, 1.f), p);
-  return g * p;
-}
 
 struct Unit {
   const FfnProblem* p;
@@ -343,7 +317,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             tmem_ld32(acc + c0 + h * 32, g);
             tmem_ld32(acc + half + c0 + h * 32, up);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) up[j] *= activate<false>(b.act, g[j], unused);
+            for (int j = 0; j < 32; ++j) up[j] *= ffn_activate<false>(b.act, g[j], unused);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
               put(box0, h * 4 + j, pack2(up[8 * j], up[8 * j + 1], tag), pack2(up[8 * j + 2], up[8 * j + 3], tag),
@@ -405,7 +379,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
               for (int e = 0; e < 8; e += 2) {
                 float d0, d1;
-                const float a0 = activate<true>(b.act, g[e], d0), a1 = activate<true>(b.act, g[e + 1], d1);
+                const float a0 = ffn_activate<true>(b.act, g[e], d0), a1 = ffn_activate<true>(b.act, g[e + 1], d1);
                 const float x0 = dh[j * 8 + e], x1 = dh[j * 8 + e + 1];
                 dg[e / 2] = pack2(x0 * up[e] * d0, x1 * up[e + 1] * d1, tag);
                 du[e / 2] = pack2(x0 * a0, x1 * a1, tag);
@@ -487,7 +461,7 @@ __global__ void __launch_bounds__(256) ffn_reduce_kernel(const FfnReduce r) {
         continue;
       }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) h[e] = activate<false>(r.act, v[e], unused) * up[e];
+      for (int e = 0; e < 4; ++e) h[e] = ffn_activate<false>(r.act, v[e], unused) * up[e];
       put(0, h);
       if (r.keep) {
         put(1, v);
@@ -505,7 +479,7 @@ __global__ void __launch_bounds__(256) ffn_reduce_kernel(const FfnReduce r) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         float d;
-        const float a = activate<true>(r.act, g[e], d);
+        const float a = ffn_activate<true>(r.act, g[e], d);
         dg[e] = v[e] * up[e] * d;
         du[e] = v[e] * a;
         h[e] = a * up[e];
