@@ -78,68 +78,95 @@ size_t part_bytes(std::initializer_list<Shape> shapes, int pairs) {
   return static_cast<size_t>(std::min(n, max_units(pairs)) * kUnitBytes);
 }
 
-// Cuts K so that the pairs finish together: of a few unit lengths the one whose longest
-// series of units, dealt in order, is shortest, parts counted with their way through memory.
-// In K blocks, of which one takes about 0.28 us: a unit's begin and end 6, a part's bytes
-// (written and read at 6.8 TB/s by all pairs together), a further launch 10.
-void plan_units(FfnBatch& b, int pairs) {
-  int64_t work = 0, whole = 0;
-  for (int i = 0; i < b.n; ++i) {
-    const int64_t t = int64_t(b.p[i].n_m) * b.p[i].n_n;
-    work += t * b.p[i].nk;
-    whole += t;
-  }
-  const int64_t limit = max_units(pairs);
-  auto cut = [&](int i, int64_t len, int& splits, int& unit) {
-    const int nk = b.p[i].nk;
-    const int64_t s = std::max<int64_t>(1, std::min<int64_t>((nk + len - 1) / len, nk / kMinUnit));
-    unit = static_cast<int>((nk + s - 1) / s);
-    splits = (nk + unit - 1) / unit;
-  };
-  double best = 0;
-  int64_t best_len = 1 << 30;
-  const int64_t share = std::max<int64_t>(1, (work + pairs - 1) / pairs);
-  for (int div = 0; whole <= limit && div <= 8; ++div) {
-    const int64_t len = div == 0 ? int64_t(1) << 30 : std::max<int64_t>(kMinUnit, share / div);
-    int64_t units = 0;
-    double load[kFfnProblems] = {}, extra = 0, longest = 0;
-    // the pairs' loads, dealt in order
-    static thread_local double sum[1024];
-    const int np = std::min(pairs, 1024);
-    std::fill(sum, sum + np, 0.0);
-    bool fits = true;
-    for (int i = 0; i < b.n && fits; ++i) {
-      int splits, unit;
-      cut(i, len, splits, unit);
-      const int64_t t = int64_t(b.p[i].n_m) * b.p[i].n_n, n = t * splits;
-      if (units + n > limit && div > 0) {
-        fits = false;
-        break;
-      }
-      load[i] = unit + 6.0;
-      if (splits > 1) extra += 10.0 + 2.0 * static_cast<double>(n) * kUnitBytes / 6.8e12 / 0.28e-6;
-      for (int64_t k = 0; k < n; ++k) {
-        const bool last = splits > 1 && k % splits == splits - 1;
-        double& x = sum[(units + k) % np];
-        x += last ? b.p[i].nk - unit * (splits - 1) + 6.0 : load[i];
-        longest = std::max(longest, x);
-      }
-      units += n;
+// Times in K blocks of a tile, of which one takes about 0.28 us: a unit's begin and end, what
+// a further launch takes, and a megabyte of parts, written and read.
+constexpr double kPerUnit = 1.5, kPerLaunch = 10.0, kPerMb = 2.0 / 6.8 / 0.28;
+
+// Units of at least kMinUnit K blocks; `splits` wanted, and got.
+void cut(int nk, int wanted, int& splits, int& unit) {
+  const int s = std::max(1, std::min(wanted, nk / kMinUnit));
+  unit = (nk + s - 1) / s;
+  splits = (nk + unit - 1) / unit;
+}
+double parts_cost(const FfnProblem& p, int64_t units) {
+  // (rows past the last one are not stored)
+  const double rows = std::min(256.0, static_cast<double>(p.m) / p.n_m);
+  return kPerLaunch + kPerMb * static_cast<double>(units) * rows * 256 * 4 / 1e6;
+}
+
+// One product: as many tiles as fill the pairs whole times, and the others with their K cut so
+// that they take less than a round (T = 64, H = 4096, F = 10944: 86 tiles on 76 pairs took 54 us
+// in two rounds).
+int plan_one(FfnProblem* p, int pairs) {
+  const int tiles = p->n_m * p->n_n, head = tiles / pairs * pairs, tail = tiles - head, nk = p->nk;
+  int splits = 1, unit = nk;
+  double best = nk + kPerUnit;
+  for (int s = 2; s <= 32 && tail > 0; ++s) {
+    int got, k;
+    cut(nk, s, got, k);
+    const int64_t units = int64_t(tail) * got;
+    if (got < s || units > max_units(pairs)) continue;
+    const double cost = static_cast<double>((units + pairs - 1) / pairs) * (k + kPerUnit) + parts_cost(*p, units);
+    if (cost < best) {
+      best = cost;
+      splits = got;
+      unit = k;
     }
-    if (!fits) continue;
-    if (div == 0 || longest + extra < best) {
-      best = longest + extra;
+  }
+  p->tile0 = 0;
+  p->splits = 1;
+  p->unit_k = nk;
+  p->n_tiles = tiles;
+  if (splits == 1) return 1;
+  FfnProblem* t = p;
+  if (head > 0) {
+    p->n_tiles = head;
+    t = p + 1;
+    *t = *p;
+  }
+  t->tile0 = head;
+  t->n_tiles = tail;
+  t->splits = splits;
+  t->unit_k = unit;
+  return head > 0 ? 2 : 1;
+}
+
+// Several products: units of one length at most, of a few lengths the one for which the pairs'
+// share and the longest unit that may come last take least.
+void plan_several(FfnProblem* p, int n, int pairs) {
+  int64_t work = 0;
+  for (int i = 0; i < n; ++i) work += int64_t(p[i].n_m) * p[i].n_n * p[i].nk;
+  const int64_t share = std::max<int64_t>(1, (work + pairs - 1) / pairs);
+  double best = -1;
+  int64_t best_len = 0;
+  for (int div = 0; div <= 8; ++div) {
+    const int64_t len = div == 0 ? int64_t(1) << 30 : std::max<int64_t>(kMinUnit, share / div);
+    double sum = 0, extra = 0;
+    int longest = 0;
+    int64_t split_units = 0;
+    for (int i = 0; i < n; ++i) {
+      int splits, unit;
+      cut(p[i].nk, static_cast<int>((p[i].nk + len - 1) / len), splits, unit);
+      const int64_t units = int64_t(p[i].n_m) * p[i].n_n * splits;
+      sum += static_cast<double>(units) * (unit + kPerUnit);
+      longest = std::max(longest, unit);
+      if (splits > 1) {
+        split_units += units;
+        extra += parts_cost(p[i], units);
+      }
+    }
+    if (split_units > max_units(pairs)) continue;
+    const double cost = std::max(sum / pairs + longest * (pairs - 1.0) / pairs / 2, longest + kPerUnit) + extra;
+    if (best < 0 || cost < best) {
+      best = cost;
       best_len = len;
     }
   }
-  int first = 0;
-  for (int i = 0; i < b.n; ++i) {
-    FfnProblem& p = b.p[i];
-    cut(i, best_len, p.splits, p.unit_k);
-    p.first = first;
-    first += p.n_m * p.n_n * p.splits;
+  for (int i = 0; i < n; ++i) {
+    cut(p[i].nk, static_cast<int>((p[i].nk + best_len - 1) / best_len), p[i].splits, p[i].unit_k);
+    p[i].tile0 = 0;
+    p[i].n_tiles = p[i].n_m * p[i].n_n;
   }
-  b.total = first;
 }
 
 constexpr CUtensorMapDataType k16 = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;   // bits are copied: both 16-bit types
@@ -173,51 +200,67 @@ struct Product {
 molt_status run(Product* q, int n, int act, bool fp16, void* parts, size_t parts_bytes, unsigned* err, cudaStream_t s) {
   const int n_sm = device_sm_count(), pairs = ffn_pairs(n_sm);
   FfnBatch b{};
-  b.n = n;
   b.act = act;
   b.err = err;
-  for (int i = 0; i < n; ++i) b.p[i] = q[i].p;
-  plan_units(b, pairs);
+  const Product* of[kFfnProblems];
+  if (n == 1) {
+    b.p[0] = q[0].p;
+    b.n = plan_one(b.p, pairs);
+    of[0] = of[1] = q;
+  } else {
+    for (int i = 0; i < n; ++i) {
+      b.p[i] = q[i].p;
+      of[i] = &q[i];
+    }
+    b.n = n;
+    plan_several(b.p, n, pairs);
+  }
   size_t at = 0;
-  for (int i = 0; i < n; ++i) {
+  int first = 0;
+  for (int i = 0; i < b.n; ++i) {
     FfnProblem& p = b.p[i];
+    p.first = first;
+    first += p.n_tiles * p.splits;
     if (p.splits > 1) {
-      const int64_t rows = int64_t(p.splits) * p.n_m * 256, cols = int64_t(p.n_n) * 256;
-      if (at + rows * cols * sizeof(float) > parts_bytes) return fail(MOLT_ERR_WORKSPACE, "parts of a split product do not fit");
+      const int64_t rows = int64_t(p.splits) * p.n_tiles * 256;
+      if (at + rows * 1024 > parts_bytes) return fail(MOLT_ERR_WORKSPACE, "parts of a split product do not fit");
       p.epi = kEpiPart;
-      FFN_TRY(out32(&p.out[0], static_cast<char*>(parts) + at, rows, cols));
-      at += rows * cols * sizeof(float);
+      FFN_TRY(out32(&p.out[0], static_cast<char*>(parts) + at, rows, 256));
+      at += rows * 1024;
       continue;
     }
     const int outs = p.epi == kEpiDglu || (p.epi == kEpiGlu && p.keep) ? 3 : p.epi == kEpiGlu32 ? 2 : 1;
     for (int k = 0; k < outs; ++k)
-      FFN_TRY(p.epi == kEpiStore32 || p.epi == kEpiGlu32 ? out32(&p.out[k], q[i].out[k], p.m, p.n)
-                                                         : out16(&p.out[k], q[i].out[k], p.m, p.n));
+      FFN_TRY(p.epi == kEpiStore32 || p.epi == kEpiGlu32 ? out32(&p.out[k], of[i]->out[k], p.m, p.n)
+                                                         : out16(&p.out[k], of[i]->out[k], p.m, p.n));
   }
+  b.total = first;
   if (const cudaError_t e = launch_ffn_gemm(b, fp16, n_sm, s); e != cudaSuccess) return cuda_fail(e, "feed-forward products");
   note_launches(1);
   at = 0;
-  for (int i = 0; i < n; ++i) {
+  for (int i = 0; i < b.n; ++i) {
     const FfnProblem& p = b.p[i];
     if (p.splits == 1) continue;
     FfnReduce r{};
     r.part = reinterpret_cast<const float*>(static_cast<char*>(parts) + at);
-    r.ld = p.n_n * 256;
-    r.split_stride = int64_t(p.n_m) * 256 * r.ld;
     r.splits = p.splits;
+    r.tile0 = p.tile0;
+    r.n_tiles = p.n_tiles;
+    r.n_m = p.n_m;
+    r.n_n = p.n_n;
     r.m = p.m;
     r.n = p.n;
-    r.epi = q[i].p.epi;
+    r.epi = of[i]->p.epi;
     r.act = act;
     r.add = p.add;
     r.keep = p.keep;
     r.wide = p.wide;
     r.gate = p.gate;
     r.up = p.up;
-    for (int k = 0; k < 3; ++k) r.out[k] = q[i].out[k];
-    if (const cudaError_t e = launch_ffn_reduce(r, fp16, n_sm, s); e != cudaSuccess) return cuda_fail(e, "feed-forward parts");
+    for (int k = 0; k < 3; ++k) r.out[k] = of[i]->out[k];
+    if (const cudaError_t e = launch_ffn_reduce(r, fp16, s); e != cudaSuccess) return cuda_fail(e, "feed-forward parts");
     note_launches(1);
-    at += static_cast<size_t>(p.splits) * r.split_stride * sizeof(float);
+    at += static_cast<size_t>(p.splits) * p.n_tiles * kUnitBytes;
   }
   return MOLT_OK;
 }

@@ -22,13 +22,17 @@ enum FfnEpilogue : int {
 
 // One product C[m,n] = sum_k A[m,k] B[n,k] in tiles of 256 x 256 (kEpiGlu*: 256 rows by 128
 // columns of g and the same of u).  K is a series of blocks of 64, the first nk0 from a[0]
-// and b[0], the others from a[1] and b[1]; it is cut into `splits` units of unit_k blocks.
+// and b[0], the others from a[1] and b[1]; it is cut into `splits` units of unit_k blocks.  The
+// tiles are numbered along columns, kFfnRaster rows of tiles at a time; a problem has n_tiles
+// of them from tile0 on.
+constexpr int kFfnRaster = 8;
 struct FfnProblem {
   CUtensorMap a[2], b[2], out[3];
   const void* gate;     // kEpiDglu: [m, n], of the operands' type or fp32 (wide)
   const void* up;
   int m, n;
-  int n_m, n_n;         // tiles
+  int n_m, n_n;         // the product's tiles
+  int tile0, n_tiles;
   int nk0, nk;
   int splits, unit_k;
   int first;            // the first of its units in the launch
@@ -39,7 +43,7 @@ struct FfnProblem {
   int keep;             // kEpiGlu
   int wide;             // kEpiDglu: gate and up are fp32
 };
-constexpr int kFfnProblems = 4;
+constexpr int kFfnProblems = 5;   // four products, one of them in two parts
 struct FfnBatch {
   FfnProblem p[kFfnProblems];
   int n;                // problems
@@ -50,9 +54,8 @@ struct FfnBatch {
 
 // Sums of a split K: out = sum_s part[s], as the problem's epilogue.
 struct FfnReduce {
-  const float* part;    // [splits][rows][ld]
-  int64_t split_stride;
-  int splits, ld;
+  const float* part;    // [splits][n_tiles][256][256]
+  int splits, tile0, n_tiles, n_m, n_n;
   int m, n;
   int epi;              // the unsplit problem's
   int act, add, keep, wide;
@@ -75,6 +78,6 @@ cudaError_t launch_ffn_rows(const FfnRows& r, bool glu, bool fp16, cudaStream_t 
 
 int ffn_pairs(int n_sm);   // CTA pairs of a launch
 cudaError_t launch_ffn_gemm(const FfnBatch& b, bool fp16, int n_sm, cudaStream_t s);
-cudaError_t launch_ffn_reduce(const FfnReduce& r, bool fp16, int n_sm, cudaStream_t s);
+cudaError_t launch_ffn_reduce(const FfnReduce& r, bool fp16, cudaStream_t s);
 
 }  // namespace molt

@@ -48,11 +48,19 @@ constexpr int kEpiWarps = 8;
 constexpr int kWarpB = 2 + kEpiWarps;
 constexpr int kThreads = 32 * (kWarpB + 1);
 constexpr int kSmemBytes = 1024 + kOffBox + kEpiWarps * kBoxes * kBoxBytes;
-constexpr int kRaster = 8;                        // row tiles that a column tile is taken with
+
+// row and column of a tile
+__device__ __forceinline__ void tile_at(int tile, int n_m, int n_n, int& tm, int& tn) {
+  const int per = kFfnRaster * n_n, group = tile / per, in = tile - group * per;
+  const int rows = min(kFfnRaster, n_m - group * kFfnRaster);
+  tn = in / rows;
+  tm = group * kFfnRaster + in - tn * rows;
+}
 
 struct Unit {
   const FfnProblem* p;
-  int tm, tn, split;
+  int tm, tn;
+  int part;        // of a split K: its place among the parts
   int k0, nk;      // first K block, K blocks
   int mma_n;       // columns of the products: 256, or 128 where the last tile has no more
 };
@@ -64,13 +72,10 @@ __device__ __forceinline__ Unit unit_at(const FfnBatch& b, int i) {
   Unit u;
   u.p = &p;
   i -= p.first;
-  const int tile = i / p.splits;
-  u.split = i - tile * p.splits;
-  const int per = kRaster * p.n_n, group = tile / per, in = tile - group * per;
-  const int rows = min(kRaster, p.n_m - group * kRaster);
-  u.tn = in / rows;
-  u.tm = group * kRaster + in - u.tn * rows;
-  u.k0 = u.split * p.unit_k;
+  const int tile = i / p.splits, split = i - tile * p.splits;
+  tile_at(p.tile0 + tile, p.n_m, p.n_n, u.tm, u.tn);
+  u.part = split * p.n_tiles + tile;
+  u.k0 = split * p.unit_k;
   u.nk = min(p.unit_k, p.nk - u.k0);
   const int left = p.glu ? 2 * (p.n - u.tn * 128) : p.n - u.tn * 256;
   u.mma_n = left > 128 ? 256 : 128;
@@ -259,7 +264,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         __syncwarp();
       };
       if (p.epi == kEpiStore32 || p.epi == kEpiPart || p.epi == kEpiGlu32) {
-        // 32 fp32 columns to a box.  Parts: the whole tile, rows of all splits below one another
+        // 32 fp32 columns to a box.  Parts: whole tiles, one below the other
         const bool part = p.epi == kEpiPart;
         const int wide = part ? 256 : p.glu ? u.mma_n : min(256, p.n - u.tn * 256);
 #pragma unroll 1
@@ -276,7 +281,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 __float_as_uint(v[4 * j + 3]));
           stored();
           if (part) {
-            store_box(&p.out[0], box, u.tn * 256 + col, u.split * p.n_m * 256 + r0, false);
+            store_box(&p.out[0], box, col, u.part * 256 + static_cast<int>(rank) * 128 + q * 32, false);
           } else if (p.glu) {
             const int half = u.mma_n / 2, c = col < half ? col : col - half;
             if (u.tn * 128 + c < p.n) store_box(&p.out[col < half ? 0 : 1], box, u.tn * 128 + c, r0, false);
@@ -417,23 +422,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   }
 }
 
-// Sums of the parts of a split K, in order, four columns to a thread.
+// Sums of the parts of a split K, in order: kReduceRows rows of a tile to a block, four columns
+// to a thread.
+constexpr int kReduceRows = 16;
 template <class T>
 __global__ void __launch_bounds__(256) ffn_reduce_kernel(const FfnReduce r) {
-  const int per_row = (r.n + 3) / 4;
-  const int64_t total = static_cast<int64_t>(r.m) * per_row;
-  for (int64_t i = blockIdx.x * int64_t(blockDim.x) + threadIdx.x; i < total; i += int64_t(gridDim.x) * blockDim.x) {
-    const int row = static_cast<int>(i / per_row), c = static_cast<int>(i - int64_t(row) * per_row) * 4;
+  constexpr int kBlocks = 256 / kReduceRows;
+  const int tile = blockIdx.x / kBlocks;
+  int tm, tn;
+  tile_at(r.tile0 + tile, r.n_m, r.n_n, tm, tn);
+  const bool glu = r.epi == kEpiGlu || r.epi == kEpiGlu32;
+  // the columns of g and u in a tile of parts: 128 each, 64 in a last tile of no more
+  const int wide = glu ? 128 : 256, quads = wide / 4;
+  const int half = glu && r.n - tn * 128 <= 64 ? 64 : 128;
+  const int64_t split_stride = static_cast<int64_t>(r.n_tiles) * 65536;
+  for (int i = threadIdx.x; i < kReduceRows * quads; i += 256) {
+    const int y = (blockIdx.x % kBlocks) * kReduceRows + i / quads, x = i % quads * 4;
+    const int row = tm * 256 + y, c = tn * wide + x;
+    if (row >= r.m || c >= r.n) continue;
     const int64_t at = static_cast<int64_t>(row) * r.n + c;
-    const bool glu = r.epi == kEpiGlu || r.epi == kEpiGlu32;
-    // the columns of g and u in a tile of parts: c in 128 (64 in a last tile of no more)
-    const int tile = c >> 7, half = glu && r.n - tile * 128 <= 64 ? 64 : 128;
-    const float* p = r.part + static_cast<int64_t>(row) * r.ld + (glu ? tile * 256 + (c & 127) : c);
+    const float* p = r.part + (static_cast<int64_t>(tile) * 256 + y) * 256 + x;
     auto sum = [&](int off, float (&v)[4]) {
       load_vec<4>(p + off, v);
       for (int s = 1; s < r.splits; ++s) {
         float w[4];
-        load_vec<4>(p + off + s * r.split_stride, w);
+        load_vec<4>(p + off + s * split_stride, w);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] += w[e];
       }
@@ -504,9 +517,8 @@ cudaError_t launch_ffn_gemm(const FfnBatch& b, bool fp16, int n_sm, cudaStream_t
   return cudaGetLastError();
 }
 
-cudaError_t launch_ffn_reduce(const FfnReduce& r, bool fp16, int n_sm, cudaStream_t s) {
-  const int64_t work = (static_cast<int64_t>(r.m) * ((r.n + 3) / 4) + 255) / 256;
-  const int grid = static_cast<int>(work < 8 * int64_t(n_sm) ? work : 8 * int64_t(n_sm));
+cudaError_t launch_ffn_reduce(const FfnReduce& r, bool fp16, cudaStream_t s) {
+  const int grid = r.n_tiles * (256 / kReduceRows);
   if (fp16)
     ffn_reduce_kernel<__half><<<grid, 256, 0, s>>>(r);
   else
