@@ -238,6 +238,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       const Unit u = unit_at(b, i);
       const FfnProblem& p = *u.p;
       const uint32_t buf = ai & 1u;
+      const int r0 = u.tm * 256 + static_cast<int>(rank) * 128 + q * 32;   // this warp's first row of C
+      const bool rows_in = r0 < p.m;
+      // kEpiDglu: g and u of 32 columns of the lane's row, as they are in memory; the first ones
+      // come while the products run
+      const int row = r0 + lane, col0 = u.tn * 256 + hf * 128;
+      uint4 gq[8], uq[8];
+      auto load_gu = [&](int c) {
+        const int per = p.wide ? 4 : 8, n = 32 / per;   // elements of a vector, vectors
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int f = col0 + c * 32 + j * per;
+          if (j < n && row < p.m && f < p.n) {
+            const int64_t at = (static_cast<int64_t>(row) * p.n + f) * (p.wide ? 4 : 2);
+            gq[j] = __ldg(reinterpret_cast<const uint4*>(static_cast<const char*>(p.gate) + at));
+            uq[j] = __ldg(reinterpret_cast<const uint4*>(static_cast<const char*>(p.up) + at));
+          } else {
+            gq[j] = uq[j] = make_uint4(0, 0, 0, 0);
+          }
+        }
+      };
+      if (p.epi == kEpiDglu && col0 < p.n) load_gu(0);
       if (!mbar_wait(smem_u32(&accf_bar[buf]), (ai >> 1) & 1u, abort_flag, b.err)) break;
       tc_fence_after();
       const uint32_t acc = tmem_base + lane_off + buf * 256;
@@ -247,8 +268,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster_relaxed(acce_lead0 + buf * 8);
       };
-      const int r0 = u.tm * 256 + static_cast<int>(rank) * 128 + q * 32;   // this warp's first row of C
-      const bool rows_in = r0 < p.m;
       // a box of 32 rows stored (or added) at column col
       auto store_box = [&](const CUtensorMap* m, uint32_t box, int col, int row, bool add) {
         if (lane == 0 && rows_in) {
@@ -351,8 +370,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
         release_acc();
       } else {   // kEpiDglu
-        const int row = r0 + lane;
-        const bool in = row < p.m;
 #pragma unroll 1
         for (int s = 0; s < 2; ++s) {
           const int col = hf * 128 + s * 64, f0 = u.tn * 256 + col;
@@ -363,35 +380,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           for (int h = 0; h < 2; ++h) {
             float dh[32];
             tmem_ld32(acc + col + h * 32, dh);
+            uint32_t dg[16], du[16];
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) {
+              float g0, g1, u0, u1;
+              if (p.wide) {
+                const uint4 a = gq[e / 4], c = uq[e / 4];
+                g0 = __uint_as_float(e & 2 ? a.z : a.x), g1 = __uint_as_float(e & 2 ? a.w : a.y);
+                u0 = __uint_as_float(e & 2 ? c.z : c.x), u1 = __uint_as_float(e & 2 ? c.w : c.y);
+              } else {
+                const uint4 a = gq[e / 8], c = uq[e / 8];
+                const int k = e / 2 % 4;
+                unpack2(k == 0 ? a.x : k == 1 ? a.y : k == 2 ? a.z : a.w, tag, g0, g1);
+                unpack2(k == 0 ? c.x : k == 1 ? c.y : k == 2 ? c.z : c.w, tag, u0, u1);
+              }
+              float d0, d1;
+              const float a0 = ffn_activate<true>(b.act, g0, d0), a1 = ffn_activate<true>(b.act, g1, d1);
+              dg[e / 2] = pack2(dh[e] * u0 * d0, dh[e + 1] * u1 * d1, tag);
+              du[e / 2] = pack2(dh[e] * a0, dh[e + 1] * a1, tag);
+              hw[h * 16 + e / 2] = pack2(a0 * u0, a1 * u1, tag);
+            }
+            if (s * 2 + h < 3) load_gu(s * 2 + h + 1);   // under the boxes' way out
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const int f = f0 + h * 32 + j * 8;
-              float g[8], up[8];
-              if (in && f < p.n) {
-                const int64_t at = static_cast<int64_t>(row) * p.n + f;
-                if (p.wide) {
-                  load_vec<8>(static_cast<const float*>(p.gate) + at, g);
-                  load_vec<8>(static_cast<const float*>(p.up) + at, up);
-                } else {
-                  load_vec<8>(static_cast<const T*>(p.gate) + at, g);
-                  load_vec<8>(static_cast<const T*>(p.up) + at, up);
-                }
-              } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) g[e] = up[e] = 0.f;
-              }
-              uint32_t dg[4], du[4];
-#pragma unroll
-              for (int e = 0; e < 8; e += 2) {
-                float d0, d1;
-                const float a0 = ffn_activate<true>(b.act, g[e], d0), a1 = ffn_activate<true>(b.act, g[e + 1], d1);
-                const float x0 = dh[j * 8 + e], x1 = dh[j * 8 + e + 1];
-                dg[e / 2] = pack2(x0 * up[e] * d0, x1 * up[e + 1] * d1, tag);
-                du[e / 2] = pack2(x0 * a0, x1 * a1, tag);
-                hw[h * 16 + j * 4 + e / 2] = pack2(a0 * up[e], a1 * up[e + 1], tag);
-              }
-              put(box0, h * 4 + j, dg[0], dg[1], dg[2], dg[3]);
-              put(box1, h * 4 + j, du[0], du[1], du[2], du[3]);
+              put(box0, h * 4 + j, dg[4 * j], dg[4 * j + 1], dg[4 * j + 2], dg[4 * j + 3]);
+              put(box1, h * 4 + j, du[4 * j], du[4 * j + 1], du[4 * j + 2], du[4 * j + 3]);
             }
           }
           if (s == 1 || f0 + 64 >= p.n) release_acc();
@@ -423,8 +436,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 }
 
 // Sums of the parts of a split K, in order: kReduceRows rows of a tile to a block, four columns
-// to a thread.
-constexpr int kReduceRows = 16;
+// to a thread, eight parts' loads at a time.
+constexpr int kReduceRows = 4;
 template <class T>
 __global__ void __launch_bounds__(256) ffn_reduce_kernel(const FfnReduce r) {
   constexpr int kBlocks = 256 / kReduceRows;
@@ -444,11 +457,18 @@ __global__ void __launch_bounds__(256) ffn_reduce_kernel(const FfnReduce r) {
     const float* p = r.part + (static_cast<int64_t>(tile) * 256 + y) * 256 + x;
     auto sum = [&](int off, float (&v)[4]) {
       load_vec<4>(p + off, v);
-      for (int s = 1; s < r.splits; ++s) {
-        float w[4];
-        load_vec<4>(p + off + s * split_stride, w);
+      for (int s0 = 1; s0 < r.splits; s0 += 8) {
+        float w[8][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] += w[e];
+        for (int i = 0; i < 8; ++i)
+          if (s0 + i < r.splits) load_vec<4>(p + off + (s0 + i) * split_stride, w[i]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (s0 + i < r.splits) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += w[i][e];
+          }
+        }
       }
     };
     float v[4];

@@ -11,7 +11,7 @@
 // are idle nine tenths of the time either way.  In the first product the 16 rows are eight of
 // Wg and the same eight of Wu, so that a lane ends with g and u of the same elements.
 //
-// A block's eight warps share its 16 rows and divide K; their sums are added in order.
+// A block's warps share its 16 rows and divide K; their sums are added in order.
 // T = 1, H = 4096, F = 10944, bf16: see ffn.cu for the times on both sides of the line.
 #include <cstdint>
 #include <cuda_bf16.h>
@@ -28,7 +28,6 @@
 namespace molt {
 namespace {
 
-constexpr int kWarps = 8;
 constexpr int kUnroll = 4;     // steps of 32 in flight: 4 KB of weights to a warp
 
 __device__ __forceinline__ uint4 load_stream(const void* p) {
@@ -52,7 +51,7 @@ __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1
 }
 
 // kTiles: eight tokens each.  kGlu: the first product, w0 and w1 are Wg and Wu; else w0 is Wd.
-template <class T, int kTiles, bool kGlu>
+template <class T, int kTiles, bool kGlu, int kWarps>
 __global__ void __launch_bounds__(32 * kWarps) ffn_rows_kernel(const FfnRows a) {
   __shared__ float4 part[kWarps - 1][kTiles][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
@@ -130,21 +129,29 @@ __global__ void __launch_bounds__(32 * kWarps) ffn_rows_kernel(const FfnRows a) 
   }
 }
 
-template <class T, int kTiles>
-void launch(const FfnRows& r, bool glu, cudaStream_t s) {
-  if (glu)
-    ffn_rows_kernel<T, kTiles, true><<<r.n / 8, 32 * kWarps, 0, s>>>(r);
+// Eight warps to a block, or sixteen where the SMs would otherwise hold fewer than sixteen
+// each (the second product at H = 4096, F = 10944: 256 blocks, 27 us with eight).
+template <class T, int kTiles, bool kGlu>
+void launch(const FfnRows& r, int n_sm, cudaStream_t s) {
+  const int blocks = kGlu ? r.n / 8 : (r.n + 15) / 16;
+  if (blocks < 2 * n_sm)
+    ffn_rows_kernel<T, kTiles, kGlu, 16><<<blocks, 512, 0, s>>>(r);
   else
-    ffn_rows_kernel<T, kTiles, false><<<(r.n + 15) / 16, 32 * kWarps, 0, s>>>(r);
+    ffn_rows_kernel<T, kTiles, kGlu, 8><<<blocks, 256, 0, s>>>(r);
+}
+template <class T, int kTiles>
+void launch(const FfnRows& r, bool glu, int n_sm, cudaStream_t s) {
+  glu ? launch<T, kTiles, true>(r, n_sm, s) : launch<T, kTiles, false>(r, n_sm, s);
 }
 
 }  // namespace
 
 cudaError_t launch_ffn_rows(const FfnRows& r, bool glu, bool fp16, cudaStream_t s) {
+  const int n_sm = device_sm_count();
   if (r.t <= 8)
-    fp16 ? launch<__half, 1>(r, glu, s) : launch<__nv_bfloat16, 1>(r, glu, s);
+    fp16 ? launch<__half, 1>(r, glu, n_sm, s) : launch<__nv_bfloat16, 1>(r, glu, n_sm, s);
   else
-    fp16 ? launch<__half, 2>(r, glu, s) : launch<__nv_bfloat16, 2>(r, glu, s);
+    fp16 ? launch<__half, 2>(r, glu, n_sm, s) : launch<__nv_bfloat16, 2>(r, glu, n_sm, s);
   return cudaGetLastError();
 }
 
