@@ -340,8 +340,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             float g[32], up[32], unused;
             tmem_ld32(acc + c0 + h * 32, g);
             tmem_ld32(acc + half + c0 + h * 32, up);
+            with_activation(b.act, [&](auto act) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) up[j] *= ffn_activate<false>(b.act, g[j], unused);
+              for (int j = 0; j < 32; ++j) up[j] *= ffn_activate<decltype(act)::value, false>(g[j], unused);
+            });
 #pragma unroll
             for (int j = 0; j < 4; ++j)
               put(box0, h * 4 + j, pack2(up[8 * j], up[8 * j + 1], tag), pack2(up[8 * j + 2], up[8 * j + 3], tag),
@@ -381,25 +383,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             float dh[32];
             tmem_ld32(acc + col + h * 32, dh);
             uint32_t dg[16], du[16];
+            with_activation(b.act, [&](auto act) {
 #pragma unroll
-            for (int e = 0; e < 32; e += 2) {
-              float g0, g1, u0, u1;
-              if (p.wide) {
-                const uint4 a = gq[e / 4], c = uq[e / 4];
-                g0 = __uint_as_float(e & 2 ? a.z : a.x), g1 = __uint_as_float(e & 2 ? a.w : a.y);
-                u0 = __uint_as_float(e & 2 ? c.z : c.x), u1 = __uint_as_float(e & 2 ? c.w : c.y);
-              } else {
-                const uint4 a = gq[e / 8], c = uq[e / 8];
-                const int k = e / 2 % 4;
-                unpack2(k == 0 ? a.x : k == 1 ? a.y : k == 2 ? a.z : a.w, tag, g0, g1);
-                unpack2(k == 0 ? c.x : k == 1 ? c.y : k == 2 ? c.z : c.w, tag, u0, u1);
+              for (int e = 0; e < 32; e += 2) {
+                float g0, g1, u0, u1;
+                if (p.wide) {
+                  const uint4 a = gq[e / 4], c = uq[e / 4];
+                  g0 = __uint_as_float(e & 2 ? a.z : a.x), g1 = __uint_as_float(e & 2 ? a.w : a.y);
+                  u0 = __uint_as_float(e & 2 ? c.z : c.x), u1 = __uint_as_float(e & 2 ? c.w : c.y);
+                } else {
+                  const uint4 a = gq[e / 8], c = uq[e / 8];
+                  const int k = e / 2 % 4;
+                  unpack2(k == 0 ? a.x : k == 1 ? a.y : k == 2 ? a.z : a.w, tag, g0, g1);
+                  unpack2(k == 0 ? c.x : k == 1 ? c.y : k == 2 ? c.z : c.w, tag, u0, u1);
+                }
+                float d0, d1;
+                const float a0 = ffn_activate<decltype(act)::value, true>(g0, d0), a1 = ffn_activate<decltype(act)::value, true>(g1, d1);
+                dg[e / 2] = pack2(dh[e] * u0 * d0, dh[e + 1] * u1 * d1, tag);
+                du[e / 2] = pack2(dh[e] * a0, dh[e + 1] * a1, tag);
+                hw[h * 16 + e / 2] = pack2(a0 * u0, a1 * u1, tag);
               }
-              float d0, d1;
-              const float a0 = ffn_activate<true>(b.act, g0, d0), a1 = ffn_activate<true>(b.act, g1, d1);
-              dg[e / 2] = pack2(dh[e] * u0 * d0, dh[e + 1] * u1 * d1, tag);
-              du[e / 2] = pack2(dh[e] * a0, dh[e + 1] * a1, tag);
-              hw[h * 16 + e / 2] = pack2(a0 * u0, a1 * u1, tag);
-            }
+            });
             if (s * 2 + h < 3) load_gu(s * 2 + h + 1);   // under the boxes' way out
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -493,8 +497,10 @@ __global__ void __launch_bounds__(256) ffn_reduce_kernel(const FfnReduce r) {
         store_vec<4>(static_cast<float*>(r.out[1]) + at, up);
         continue;
       }
+      with_activation(r.act, [&](auto act) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) h[e] = ffn_activate<false>(r.act, v[e], unused) * up[e];
+        for (int e = 0; e < 4; ++e) h[e] = ffn_activate<decltype(act)::value, false>(v[e], unused) * up[e];
+      });
       put(0, h);
       if (r.keep) {
         put(1, v);
@@ -509,14 +515,16 @@ __global__ void __launch_bounds__(256) ffn_reduce_kernel(const FfnReduce r) {
         load_vec<4>(static_cast<const T*>(r.gate) + at, g);
         load_vec<4>(static_cast<const T*>(r.up) + at, up);
       }
+      with_activation(r.act, [&](auto act) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float d;
-        const float a = ffn_activate<true>(r.act, g[e], d);
-        dg[e] = v[e] * up[e] * d;
-        du[e] = v[e] * a;
-        h[e] = a * up[e];
-      }
+        for (int e = 0; e < 4; ++e) {
+          float d;
+          const float a = ffn_activate<decltype(act)::value, true>(g[e], d);
+          dg[e] = v[e] * up[e] * d;
+          du[e] = v[e] * a;
+          h[e] = a * up[e];
+        }
+      });
       put(0, dg);
       put(1, du);
       put(2, h);

@@ -115,8 +115,10 @@ __global__ void __launch_bounds__(32 * kWarps) ffn_rows_kernel(const FfnRows a) 
       if (token >= a.t) continue;
       const int64_t at = static_cast<int64_t>(token) * a.n + r0 + g;
       if constexpr (kGlu) {
-        float unused;
-        from_float(ffn_activate<false>(a.act, acc[t][j], unused) * acc[t][2 + j], static_cast<T*>(a.out[0])[at]);
+        with_activation(a.act, [&](auto act) {
+          float unused;
+          from_float(ffn_activate<decltype(act)::value, false>(acc[t][j], unused) * acc[t][2 + j], static_cast<T*>(a.out[0])[at]);
+        });
         if (a.out[1] != nullptr) {
           from_float(acc[t][j], static_cast<T*>(a.out[1])[at]);
           from_float(acc[t][2 + j], static_cast<T*>(a.out[2])[at]);
