@@ -240,16 +240,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       const uint32_t buf = ai & 1u;
       const int r0 = u.tm * 256 + static_cast<int>(rank) * 128 + q * 32;   // this warp's first row of C
       const bool rows_in = r0 < p.m;
-      // kEpiDglu: g and u of 32 columns of the lane's row, as they are in memory; the first ones
-      // come while the products run
+      // kEpiDglu: g and u of 64 columns (fp32: 32) of the lane's row, as they are in memory.  The
+      // first ones come while the products run, the others while boxes go out, but not ahead
+      // of a fence, which would wait for them
       const int row = r0 + lane, col0 = u.tn * 256 + hf * 128;
       uint4 gq[8], uq[8];
-      auto load_gu = [&](int c) {
-        const int per = p.wide ? 4 : 8, n = 32 / per;   // elements of a vector, vectors
+      auto load_gu = [&](int c) {   // c: in 32 columns
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const int f = col0 + c * 32 + j * per;
-          if (j < n && row < p.m && f < p.n) {
+          const int f = col0 + c * 32 + j * (p.wide ? 4 : 8);
+          if (row < p.m && f < p.n) {
             const int64_t at = (static_cast<int64_t>(row) * p.n + f) * (p.wide ? 4 : 2);
             gq[j] = __ldg(reinterpret_cast<const uint4*>(static_cast<const char*>(p.gate) + at));
             uq[j] = __ldg(reinterpret_cast<const uint4*>(static_cast<const char*>(p.up) + at));
@@ -383,28 +383,35 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             float dh[32];
             tmem_ld32(acc + col + h * 32, dh);
             uint32_t dg[16], du[16];
-            with_activation(b.act, [&](auto act) {
+            auto gradients = [&](auto act, auto wide) {
 #pragma unroll
               for (int e = 0; e < 32; e += 2) {
                 float g0, g1, u0, u1;
-                if (p.wide) {
+                if constexpr (decltype(wide)::value) {
                   const uint4 a = gq[e / 4], c = uq[e / 4];
                   g0 = __uint_as_float(e & 2 ? a.z : a.x), g1 = __uint_as_float(e & 2 ? a.w : a.y);
                   u0 = __uint_as_float(e & 2 ? c.z : c.x), u1 = __uint_as_float(e & 2 ? c.w : c.y);
                 } else {
-                  const uint4 a = gq[e / 8], c = uq[e / 8];
+                  const uint4 a = gq[h * 4 + e / 8], c = uq[h * 4 + e / 8];
                   const int k = e / 2 % 4;
                   unpack2(k == 0 ? a.x : k == 1 ? a.y : k == 2 ? a.z : a.w, tag, g0, g1);
                   unpack2(k == 0 ? c.x : k == 1 ? c.y : k == 2 ? c.z : c.w, tag, u0, u1);
                 }
                 float d0, d1;
-                const float a0 = ffn_activate<decltype(act)::value, true>(g0, d0), a1 = ffn_activate<decltype(act)::value, true>(g1, d1);
+                const float a0 = ffn_activate<decltype(act)::value, true>(g0, d0);
+                const float a1 = ffn_activate<decltype(act)::value, true>(g1, d1);
                 dg[e / 2] = pack2(dh[e] * u0 * d0, dh[e + 1] * u1 * d1, tag);
                 du[e / 2] = pack2(dh[e] * a0, dh[e + 1] * a1, tag);
                 hw[h * 16 + e / 2] = pack2(a0 * u0, a1 * u1, tag);
               }
+            };
+            with_activation(b.act, [&](auto act) {
+              if (p.wide)
+                gradients(act, std::true_type{});
+              else
+                gradients(act, std::false_type{});
             });
-            if (s * 2 + h < 3) load_gu(s * 2 + h + 1);   // under the boxes' way out
+            if (p.wide && h == 0) load_gu(s * 2 + 1);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               put(box0, h * 4 + j, dg[4 * j], dg[4 * j + 1], dg[4 * j + 2], dg[4 * j + 3]);
@@ -415,6 +422,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           stored();
           store_box(&p.out[0], box0, f0, r0, false);
           store_box(&p.out[1], box1, f0, r0, false);
+          if (s == 0 && f0 + 64 < p.n) load_gu(2);
           boxes_free();
 #pragma unroll
           for (int j = 0; j < 8; ++j) put(box0, j, hw[4 * j], hw[4 * j + 1], hw[4 * j + 2], hw[4 * j + 3]);
