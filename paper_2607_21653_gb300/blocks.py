@@ -39,17 +39,37 @@ def _call(fn, dev, *args):
     """A call of the C ABI with the tensors' device as the current one."""
     torch = _torch()
     if torch._C._cuda_getDevice() == dev.index:
-        _check(fn(*args))
+        status = fn(*args)
+        if status:
+            _check(status)
         return
     with torch.cuda.device(dev):
         _check(fn(*args))
+
+
+# The checks of _at and _rows (.stream) in the order in which a good argument passes soonest: the
+# marshalling of a small call takes longer than its kernels.
+def _vec(t, dtype, dev, name):
+    """Pointer of a contiguous tensor of this type on this device (None -> NULL)."""
+    if t is None:
+        return None
+    if t.dtype is dtype and t.is_contiguous() and t.get_device() == dev.index:
+        return t.data_ptr()
+    return _at(t, dtype, dev, name)
+
+
+def _mat(t, dtype, dev, name):
+    """(pointer, row stride, 0 for rows side by side) of a matrix whose rows are contiguous."""
+    if t is not None and t.dtype is dtype and t.is_contiguous() and t.get_device() == dev.index:
+        return t.data_ptr(), 0
+    return _rows(t, dtype, dev, name)
 
 
 def _scratch(nbytes, dev, key, stream):
     """Workspace of a call: the binding's buffer of this stream, or inside a capture memory of
     the graph's own pool (a buffer that other calls share could be replaced under the graph)."""
     torch = _torch()
-    if not torch.cuda.is_current_stream_capturing():
+    if not torch._C._cuda_isCurrentStreamCapturing():
         return _workspace(nbytes, dev, key, stream)
     with torch.cuda.stream(torch.cuda.current_stream(dev) if stream is None else stream):
         return torch.empty(nbytes, dtype=torch.uint8, device=dev)
@@ -100,10 +120,10 @@ def gated_ffn_fwd(x, w_gate, w_up, w_down, activation="silu", keep=False, stream
     torch = _torch()
     T, H, F = _ffn_shapes(x, w_gate, w_up, w_down)
     dev, dtype = _cuda(x, "x"), x.dtype
-    xp, xs = _rows(x, dtype, dev, "x")
-    gp, gs = _rows(w_gate, dtype, dev, "w_gate")
-    up, us = _rows(w_up, dtype, dev, "w_up")
-    dp, ds = _rows(w_down, dtype, dev, "w_down")
+    xp, xs = _mat(x, dtype, dev, "x")
+    gp, gs = _mat(w_gate, dtype, dev, "w_gate")
+    up, us = _mat(w_up, dtype, dev, "w_up")
+    dp, ds = _mat(w_down, dtype, dev, "w_down")
     y = torch.empty(T, H, dtype=dtype, device=dev)
     gate = torch.empty(T, F, dtype=dtype, device=dev) if keep else None
     upo = torch.empty(T, F, dtype=dtype, device=dev) if keep else None
@@ -145,17 +165,17 @@ def gated_ffn_bwd(dy, x, w_gate, w_up, w_down, gate=None, up=None, activation="s
             _shaped(t, (T, F), name)
     if (gate is None) != (up is None):
         raise ValueError("gate and up come together")
-    dyp, dys = _rows(dy, dtype, dev, "dy")
-    xp, xs = _rows(x, dtype, dev, "x")
-    gp, gs = _rows(w_gate, dtype, dev, "w_gate")
-    upp, us = _rows(w_up, dtype, dev, "w_up")
-    dp, ds = _rows(w_down, dtype, dev, "w_down")
+    dyp, dys = _mat(dy, dtype, dev, "dy")
+    xp, xs = _mat(x, dtype, dev, "x")
+    gp, gs = _mat(w_gate, dtype, dev, "w_gate")
+    upp, us = _mat(w_up, dtype, dev, "w_up")
+    dp, ds = _mat(w_down, dtype, dev, "w_down")
     dx = torch.empty(T, H, dtype=dtype, device=dev)
     ref, nbytes = _desc(FfnDesc, (T, H, F, xs, gs, us, ds, dys, _dtype_code(dtype, "x"), _activation(activation)),
                         "molt_gated_ffn_bwd_workspace_bytes", 0 if gate is None else 1)
     ws = workspace if workspace is not None else _scratch(nbytes, dev, "gated_ffn", stream)
-    _call(load().molt_gated_ffn_bwd, dev, ref, dyp, xp, gp, upp, dp, _at(gate, dtype, dev, "gate"), _at(up, dtype, dev, "up"),
-          dx.data_ptr(), *[_at(t, dw_dtype, dev, name) for t, (name, _) in zip(given, shapes)],
+    _call(load().molt_gated_ffn_bwd, dev, ref, dyp, xp, gp, upp, dp, _vec(gate, dtype, dev, "gate"), _vec(up, dtype, dev, "up"),
+          dx.data_ptr(), *[_vec(t, dw_dtype, dev, name) for t, (name, _) in zip(given, shapes)],
           _dtype_code(dw_dtype, "dw_dtype"), 1 if accumulate else 0, ws.data_ptr(), ws.numel(), _stream(stream, dev.index))
     return {"dx": dx, "dw_gate": given[0], "dw_up": given[1], "dw_down": given[2]}
 
@@ -181,7 +201,7 @@ def _scan_shapes(gate, cu_seqlens, dev):
     n, = cu_seqlens.shape
     if n < 1:
         raise ValueError("cu_seqlens has one entry more than there are sequences")
-    return T, H, n - 1, _at(cu_seqlens, _torch().int32, dev, "cu_seqlens")
+    return T, H, n - 1, _vec(cu_seqlens, _torch().int32, dev, "cu_seqlens")
 
 
 def _packed(t, like, name):
@@ -203,8 +223,8 @@ def gated_scan_fwd(gate, value, initial_state=None, cu_seqlens=None, kind="sigmo
     torch = _torch()
     dev, dtype = _cuda(gate, "gate"), gate.dtype
     T, H, B, cu = _scan_shapes(gate, cu_seqlens, dev)
-    gp, gs = _rows(_packed(gate, gate, "gate"), dtype, dev, "gate")
-    vp, vs = _rows(_packed(value, gate, "value"), dtype, dev, "value")
+    gp, gs = _mat(_packed(gate, gate, "gate"), dtype, dev, "gate")
+    vp, vs = _mat(_packed(value, gate, "value"), dtype, dev, "value")
     f32 = torch.float32
     if initial_state is not None:
         _shaped(initial_state, (B, H), "initial_state")
@@ -216,8 +236,8 @@ def gated_scan_fwd(gate, value, initial_state=None, cu_seqlens=None, kind="sigmo
     ref, nbytes = _desc(ScanDesc, (T, H, B, gs, vs, 0, _dtype_code(dtype, "gate"), _form(kind), fill),
                         "molt_gated_scan_workspace_bytes")
     ws = workspace if workspace is not None else _scratch(nbytes, dev, "gated_scan", stream)
-    _call(load().molt_gated_scan_fwd, dev, ref, gp, vp, _at(initial_state, f32, dev, "initial_state"), cu,
-          _at(_shaped(out, gate.shape, "out"), dtype, dev, "out"), final if final is None else final.data_ptr(),
+    _call(load().molt_gated_scan_fwd, dev, ref, gp, vp, _vec(initial_state, f32, dev, "initial_state"), cu,
+          _vec(_shaped(out, gate.shape, "out"), dtype, dev, "out"), final if final is None else final.data_ptr(),
           states if states is None else states.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream, dev.index))
     return {"y": out, "final_state": final, "states": states}
 
@@ -231,9 +251,9 @@ def gated_scan_bwd(dy, gate, value, states, initial_state=None, cu_seqlens=None,
     torch = _torch()
     dev, dtype = _cuda(gate, "gate"), gate.dtype
     T, H, B, cu = _scan_shapes(gate, cu_seqlens, dev)
-    gp, gs = _rows(_packed(gate, gate, "gate"), dtype, dev, "gate")
-    vp, vs = _rows(_packed(value, gate, "value"), dtype, dev, "value")
-    dp, ds = _rows(_packed(dy, gate, "dy"), dtype, dev, "dy")
+    gp, gs = _mat(_packed(gate, gate, "gate"), dtype, dev, "gate")
+    vp, vs = _mat(_packed(value, gate, "value"), dtype, dev, "value")
+    dp, ds = _mat(_packed(dy, gate, "dy"), dtype, dev, "dy")
     f32 = torch.float32
     _shaped(states, ((T + STATE_ROWS - 1) // STATE_ROWS, H), "states")
     for name, t in (("initial_state", initial_state), ("dfinal_state", dfinal_state)):
@@ -244,8 +264,8 @@ def gated_scan_bwd(dy, gate, value, states, initial_state=None, cu_seqlens=None,
     ref, nbytes = _desc(ScanDesc, (T, H, B, gs, vs, ds, _dtype_code(dtype, "gate"), _form(kind), 0),
                         "molt_gated_scan_workspace_bytes")
     ws = workspace if workspace is not None else _scratch(nbytes, dev, "gated_scan", stream)
-    _call(load().molt_gated_scan_bwd, dev, ref, dp, gp, vp, _at(states, f32, dev, "states"),
-          _at(initial_state, f32, dev, "initial_state"), cu, _at(dfinal_state, f32, dev, "dfinal_state"),
+    _call(load().molt_gated_scan_bwd, dev, ref, dp, gp, vp, _vec(states, f32, dev, "states"),
+          _vec(initial_state, f32, dev, "initial_state"), cu, _vec(dfinal_state, f32, dev, "dfinal_state"),
           dgate.data_ptr(), dvalue.data_ptr(), dinit if dinit is None else dinit.data_ptr(), ws.data_ptr(), ws.numel(),
           _stream(stream, dev.index))
     return {"dgate": dgate, "dvalue": dvalue, "dinitial_state": dinit}
@@ -258,14 +278,14 @@ def gated_scan_step(gate, value, state, kind="sigmoid", out_state=None, stream=N
     torch = _torch()
     B, H = gate.shape
     dev, dtype = _cuda(gate, "gate"), gate.dtype
-    gp, gs = _rows(gate, dtype, dev, "gate")
-    vp, vs = _rows(_shaped(value, (B, H), "value"), dtype, dev, "value")
+    gp, gs = _mat(gate, dtype, dev, "gate")
+    vp, vs = _mat(_shaped(value, (B, H), "value"), dtype, dev, "value")
     f32 = torch.float32
     y = torch.empty(B, H, dtype=dtype, device=dev)
     new = torch.empty(B, H, dtype=f32, device=dev) if out_state is None else _shaped(out_state, (B, H), "out_state")
     ref, _ = _desc(ScanDesc, (B, H, B, gs, vs, 0, _dtype_code(dtype, "gate"), _form(kind), 0))
-    _call(load().molt_gated_scan_step, dev, ref, gp, vp, _at(_shaped(state, (B, H), "state"), f32, dev, "state"), y.data_ptr(),
-          _at(new, f32, dev, "out_state"), _stream(stream, dev.index))
+    _call(load().molt_gated_scan_step, dev, ref, gp, vp, _vec(_shaped(state, (B, H), "state"), f32, dev, "state"), y.data_ptr(),
+          _vec(new, f32, dev, "out_state"), _stream(stream, dev.index))
     return {"y": y, "state": new}
 
 
@@ -278,18 +298,18 @@ def _dropout(x, p, seed, offset, residual, res_scale, first_row, out, out_dtype,
     if isinstance(seed, torch.Tensor):
         if offset != 0:
             raise ValueError("a seed on the device brings its offset with it")
-        words, seed = _at(_shaped(seed, (2,), "seed"), torch.int64, dev, "seed"), 0
+        words, seed = _vec(_shaped(seed, (2,), "seed"), torch.int64, dev, "seed"), 0
     elif not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
         raise ValueError("seed and offset must be in [0, 2^64)")
-    xp, xs = _rows(x, dtype, dev, "x")
+    xp, xs = _mat(x, dtype, dev, "x")
     rp = rs = None
     if residual is not None:
-        rp, rs = _rows(_shaped(residual, (T, H), "residual"), out_dtype, dev, "residual")
+        rp, rs = _mat(_shaped(residual, (T, H), "residual"), out_dtype, dev, "residual")
     if out is None:
         out = torch.empty(T, H, dtype=out_dtype, device=dev)
     d = DropoutDesc(T, H, xs, rs or 0, first_row, seed, offset, p, res_scale, _dtype_code(dtype, "x"),
                     _dtype_code(out_dtype, "out"))
-    _call(load().molt_dropout, dev, ctypes.byref(d), xp, rp, words, _at(_shaped(out, (T, H), "out"), out_dtype, dev, "out"),
+    _call(load().molt_dropout, dev, ctypes.byref(d), xp, rp, words, _vec(_shaped(out, (T, H), "out"), out_dtype, dev, "out"),
           _stream(stream, dev.index))
     return out
 
