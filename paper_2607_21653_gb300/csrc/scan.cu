@@ -54,7 +54,11 @@ constexpr int kTile = kWarps * kHalves<T, kBwd> * kHalf;
 static_assert(kTile<float, true> == kStateRows && kStateRows % kTile<float, false> == 0);
 constexpr int kThreads = 32 * (kWarps + 2);
 constexpr int kStrip = 64;               // channels of a block
-constexpr int kMaxCluster = 8;           // 4 where tiles do not come by TMA (shared memory for two blocks to an SM)
+constexpr int kMaxCluster = 8;
+// Blocks of a cluster, at most: fewer where the tiles' rows have a word more (shared memory for two
+// blocks to an SM).
+template <class T, bool kBwd, bool kFast>
+constexpr int kClusterOf = kBwd && !kFast && sizeof(T) == 2 ? 6 : kMaxCluster;
 constexpr int kFormSigmoid = 0, kFormLog = 1;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -138,6 +142,32 @@ __device__ __forceinline__ void store2(T* p, F2 x, int left) {
   } else {
     if (left > 0) from_float(x.x(), p[0]);
     if (left > 1) from_float(x.y(), p[1]);
+  }
+}
+
+// A row's results, two to a lane, as words where the row begins on one, else as words of neighbours'
+// (n channels of the strip; p: the strip's first)
+template <class T>
+__device__ __forceinline__ void store_row(T* p, F2 x, int n, int lane) {
+  if constexpr (sizeof(T) == 4) {
+    store2<false>(p + 2 * lane, x, n - 2 * lane);
+  } else {
+    const int c = 2 * lane, left = n - c;
+    if (reinterpret_cast<uintptr_t>(p) % 4 == 0) {
+      const float v[2] = {x.x(), x.y()};
+      if (left > 1)
+        store_vec<2>(p + c, v);
+      else if (left > 0)
+        from_float(x.x(), p[c]);
+    } else {
+      const float next = __shfl_down_sync(0xffffffffu, x.x(), 1);
+      const float v[2] = {x.y(), next};
+      if (lane == 0 && n > 0) from_float(x.x(), p[0]);
+      if (left > 2 && lane < 31)
+        store_vec<2>(p + c + 1, v);
+      else if (left > 1)
+        from_float(x.y(), p[c + 1]);
+    }
   }
 }
 
@@ -298,30 +328,32 @@ __device__ __forceinline__ void cp_async_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-// A row's channels c0 .. c0 + n - 1 to shared memory, by words, from any address; first, last:
-// no element lies before or behind them that may be read along.
-template <class T>
-__device__ __forceinline__ void copy_row(uint32_t dst, const T* row, int n, bool first, bool last, int lane) {
+// `rows` rows' channels, n of them from `row` on, to shared memory by words, from any address; first,
+// last: no element lies before the first row's, behind the last row's, that may be read
+// along with it.
+template <class T, int kPitchBytes>
+__device__ __forceinline__ void copy_rows(uint32_t dst, const T* row, int64_t ld, int rows, int n, bool first, bool last, int lane) {
   if constexpr (sizeof(T) == 4) {
-    if (lane < n) cp_async4(dst + 4 * lane, row + lane);
-    if (lane + 32 < n) cp_async4(dst + 4 * (lane + 32), row + lane + 32);
+    const bool in0 = lane < n, in1 = lane + 32 < n;
+    const T* p = row + lane;
+#pragma unroll 4
+    for (int i = 0; i < rows; ++i, p += ld, dst += kPitchBytes) {
+      if (in0) cp_async4(dst + 4 * lane, p);
+      if (in1) cp_async4(dst + 4 * lane + 128, p + 32);
+    }
   } else {
-    const int off = static_cast<int>(reinterpret_cast<uintptr_t>(row) >> 1 & 1);
-    auto word = [&](int l) {
-      const int e = 2 * l - off;   // its first element
-      if (e >= n) return;
-      if ((e < 0 && first) || (e + 1 >= n && last)) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-          if (e + j >= 0 && e + j < n)
-            asm volatile("st.shared.u16 [%0], %1;" ::"r"(dst + 4 * l + 2 * j), "h"(reinterpret_cast<const uint16_t*>(row)[e + j])
-                         : "memory");
-        return;
+#pragma unroll 4
+    for (int i = 0; i < rows; ++i, row += ld, dst += kPitchBytes) {
+      const int off = static_cast<int>(reinterpret_cast<uintptr_t>(row) >> 1 & 1), e = 2 * lane - off;   // the lane's first element
+      if ((first && i == 0) || (last && i == rows - 1)) {
+        for (int k = lane; k < n; k += 32)
+          asm volatile("st.shared.u16 [%0], %1;" ::"r"(dst + 2 * (k + off)), "h"(reinterpret_cast<const uint16_t*>(row)[k])
+                       : "memory");
+        continue;
       }
-      cp_async4(dst + 4 * l, row + e);
-    };
-    word(lane);
-    if (off && lane == 0) word(32);
+      if (e < n) cp_async4(dst + 4 * lane, row + e);
+      if (off && lane == 0 && n == kStrip) cp_async4(dst + 128, row + 63);
+    }
   }
 }
 
@@ -357,7 +389,7 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
   constexpr int kRowBytes = kPitch<T, kFast>;
   constexpr int kTensorBytes = kN * kRowBytes, kStageBytes = kTensors * kTensorBytes;
   extern __shared__ __align__(128) uint8_t smem_raw[];
-  __shared__ __align__(16) Exchange<kFast ? kMaxCluster : kMaxCluster / 2> ex;
+  __shared__ __align__(16) Exchange<kClusterOf<T, kBwd, kFast>> ex;
   __shared__ float2 h_maps[kGrads ? kWarps : 1][32];   // b of the maps of h, then h before each warp's rows
   __shared__ TileRows<kN> rows_sh[kStages];
   __shared__ __align__(8) uint64_t full_bar[kStages], empty_bar[kStages], peer_bar[2];
@@ -469,7 +501,7 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
       }
       // (a wait that runs out raises the block's flag; what follows is then of no use, but ends)
       if (S > 1) mbar_wait(bar, (k >> 1) & 1u, abort_flag, a.err);
-      constexpr int kTiles = kFast ? kMaxCluster : kMaxCluster / 2;
+      constexpr int kTiles = kClusterOf<T, kBwd, kFast>;
       float4 t[kTiles];
 #pragma unroll
       for (int p = 0; p < kTiles; ++p) t[p] = ex.tiles[slot][p][lane];   // (of no use from S on)
@@ -523,13 +555,11 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
 #pragma unroll
         for (int j = 0; j < kTensors; ++j) {
           const uint32_t dst = smem_u32(smem_raw) + (k % kStages) * kStageBytes + j * kTensorBytes + r0 * kRowBytes;
-#pragma unroll 4
-          for (int i = 0; i < kRows; ++i) {
-            const int64_t r = int64_t(t) * kN + r0 + i;
-            if (r >= a.T) break;
-            copy_row(dst + i * kRowBytes, static_cast<const T*>(tensor_of[j]) + r * ld_of[j] + c0, min(kStrip, a.H - c0),
-                     r == 0 && c0 == 0, r == a.T - 1 && c0 + kStrip >= a.H, lane);
-          }
+          const int64_t r = int64_t(t) * kN + r0;
+          const int rows = static_cast<int>(min(int64_t(kRows), a.T - r));
+          if (rows > 0)
+            copy_rows<T, kRowBytes>(dst, static_cast<const T*>(tensor_of[j]) + r * ld_of[j] + c0, ld_of[j], rows,
+                                    min(kStrip, a.H - c0), r == 0 && c0 == 0, r + rows == a.T && c0 + kStrip >= a.H, lane);
         }
       }
       cp_async_commit();
@@ -710,11 +740,17 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
       // ---- the rows again.  Where all of the warp's are in sequences their results go out as a box,
       // from where the gates (and dy) have been
       const bool boxed = kFast && valid == (1u << kRows) - 1u;
+      auto store_out = [&](T* p, F2 x) {
+        if constexpr (kFast)
+          store2<true>(p + 2 * lane, x, left);
+        else
+          store_row(p, x, min(kStrip, a.H - c0), lane);
+      };
       auto out_row = [&](T* base, int tensor, int i, F2 x) {
         if (boxed)
           store2<true>(reinterpret_cast<T*>(stage + tensor * kTensorBytes + i * kRowBytes) + 2 * lane, x, 2);
         else
-          store2<kFast>(base + (row + i) * a.H + c, x, left);
+          store_out(base + (row + i) * a.H + c0, x);
       };
       if constexpr (!kBwd) {
         T* const y = static_cast<T*>(a.y);
@@ -722,11 +758,11 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
         for (int q = 0; q < kParts; ++q) {
           const uint32_t s = starts >> (q * kHalf) & kAll, e = ends >> (q * kHalf) & kAll, is = valid >> (q * kHalf) & kAll;
           if (kParts > 1) load_values(q);
-          if (boxed && (s | e) == 0) {
+          if (is == kAll && (s | e) == 0) {
 #pragma unroll
             for (int i = 0; i < kHalf; ++i) {
               in = step<kForm>(in, kept[q][i], v[i].f());
-              store2<true>(reinterpret_cast<T*>(stage + (q * kHalf + i) * kRowBytes) + 2 * lane, in, 2);
+              out_row(y, 0, q * kHalf + i, in);
             }
           } else {
             F2 h[kHalf];   // first what rows start from, then h
@@ -771,7 +807,7 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
           }
           const F2(&m)[kHalf] = kept[0];
           F2 h = q > 0 ? apply(first_h, h_in) : h_in, hp[kHalf], df, dval;   // hp: h of the row before
-          if (boxed && (s | e) == 0) {
+          if (is == kAll && (s | e) == 0) {
 #pragma unroll
             for (int i = 0; i < kHalf; ++i) {
               hp[i] = h;
@@ -782,9 +818,8 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
               const F2 D = add2(d[i].f(), in);
               in = fma2(m[i], D, D);   // E
               grads(i, D, in, hp[i], df, dval);
-              T* const p = reinterpret_cast<T*>(stage + (q * kHalf + i) * kRowBytes) + 2 * lane;
-              store2<true>(p, df, 2);
-              store2<true>(p + kD * kTensorBytes / static_cast<int>(sizeof(T)), dval, 2);
+              out_row(dg, 0, q * kHalf + i, df);
+              out_row(dv, kD, q * kHalf + i, dval);
             }
           } else {
             F2 from[kHalf];
@@ -922,7 +957,7 @@ constexpr int kDevices = 16;
 // One instance of the kernel.
 struct ScanKernel {
   void (*fn)(const ScanMaps, const ScanArgs);
-  int smem;
+  int smem, max_cluster;
   // by device and a cluster's blocks: how many clusters run at once (0: not yet asked)
   std::atomic<int> clusters[kDevices][kMaxCluster + 1];
 };
@@ -930,7 +965,8 @@ template <class T, int kForm, bool kBwd, bool kMapOnly, bool kFast>
 ScanKernel* kernel_of() {
   constexpr int kTensors = kBwd && !kMapOnly ? 3 : 2;
   static ScanKernel k{&scan_kernel<T, kForm, kBwd, kMapOnly, kFast>,
-                      kStagesOf<kBwd, kMapOnly> * kTile<T, kBwd> * kRowsBytesOf<T, kTensors, kFast>, {}};
+                      kStagesOf<kBwd, kMapOnly> * kTile<T, kBwd> * kRowsBytesOf<T, kTensors, kFast>, kClusterOf<T, kBwd, kFast>,
+                      {}};
   return &k;
 }
 template <class T, int kForm>
@@ -994,10 +1030,10 @@ struct ScanPlan {
 };
 // The largest clusters with which all strips run at once; the rows in segments where there is
 // room for several times the strips, and each has eight steps or more.
-cudaError_t plan_of(ScanKernel* k, int64_t strips, int tiles, bool fast, ScanPlan& p) {
+cudaError_t plan_of(ScanKernel* k, int64_t strips, int tiles, ScanPlan& p) {
   p.cluster = p.segments = 1;
   int n = 0;
-  for (int s = fast ? kMaxCluster : kMaxCluster / 2; s >= 1; --s) {
+  for (int s = k->max_cluster; s >= 1; --s) {
     if (s > tiles && s > 1) continue;
     if (const cudaError_t e = clusters_at_once(k, s, n); e != cudaSuccess) return e;
     p.cluster = s;
@@ -1018,7 +1054,7 @@ molt_status launch(const molt_scan_desc* d, ScanArgs& a, bool bwd, void* workspa
   a.tiles = static_cast<int>((a.T + tile - 1) / tile);
   const bool fast = a.tiles > 0 && fast_of(a, d->dtype);
   ScanPlan plan;
-  if (const cudaError_t e = plan_of(kernel_of(d->dtype, d->form, bwd, false, fast), strips, a.tiles, fast, plan); e != cudaSuccess)
+  if (const cudaError_t e = plan_of(kernel_of(d->dtype, d->form, bwd, false, fast), strips, a.tiles, plan); e != cudaSuccess)
     return cuda_fail(e, "gated scan");
   a.seg_tiles = (a.tiles + plan.segments - 1) / plan.segments;
   const int segments = a.tiles > 0 ? (a.tiles + a.seg_tiles - 1) / a.seg_tiles : 1;
