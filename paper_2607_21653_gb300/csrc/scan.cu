@@ -53,12 +53,11 @@ template <class T, bool kBwd>
 constexpr int kTile = kWarps * kHalves<T, kBwd> * kHalf;
 static_assert(kTile<float, true> == kStateRows && kStateRows % kTile<float, false> == 0);
 constexpr int kThreads = 32 * (kWarps + 2);
-constexpr int kStrip = 64;               // channels of a block
+// Channels of a block: 64, or as many as fill a row of the same bytes from any place in a 16-byte
+// word.
+template <class T, bool kFast>
+constexpr int kStrip = kFast ? 64 : sizeof(T) == 2 ? 56 : 60;
 constexpr int kMaxCluster = 8;
-// Blocks of a cluster, at most: fewer where the tiles' rows have a word more (shared memory for two
-// blocks to an SM).
-template <class T, bool kBwd, bool kFast>
-constexpr int kClusterOf = kBwd && !kFast && sizeof(T) == 2 ? 6 : kMaxCluster;
 constexpr int kFormSigmoid = 0, kFormLog = 1;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -145,29 +144,31 @@ __device__ __forceinline__ void store2(T* p, F2 x, int left) {
   }
 }
 
-// A row's results, two to a lane, as words where the row begins on one, else as words of neighbours'
-// (n channels of the strip; p: the strip's first)
+__device__ __forceinline__ void store32_if(bool on, void* p, uint32_t v) {
+  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q st.global.b32 [%0], %1;\n}" ::"l"(p), "r"(v), "r"(int(on)) : "memory");
+}
+__device__ __forceinline__ void store16_if(bool on, void* p, uint32_t v) {
+  asm volatile("{\n\t.reg .pred q;\n\t.reg .b16 h, g;\n\tsetp.ne.b32 q, %2, 0;\n\tmov.b32 {h, g}, %1;\n\t@q st.global.b16 [%0], h;\n}" ::"l"(p),
+               "r"(v), "r"(int(on))
+               : "memory");
+}
+// A row's results, two to a lane, n channels from p on: as words, of neighbours' halves where the row
+// begins inside one.  Predicates and no branches: those took longer than the rest of a row.
 template <class T>
 __device__ __forceinline__ void store_row(T* p, F2 x, int n, int lane) {
+  const int left = n - 2 * lane;
   if constexpr (sizeof(T) == 4) {
-    store2<false>(p + 2 * lane, x, n - 2 * lane);
+    store32_if(left > 0, p + 2 * lane, __float_as_uint(x.x()));
+    store32_if(left > 1, p + 2 * lane + 1, __float_as_uint(x.y()));
   } else {
-    const int c = 2 * lane, left = n - c;
-    if (reinterpret_cast<uintptr_t>(p) % 4 == 0) {
-      const float v[2] = {x.x(), x.y()};
-      if (left > 1)
-        store_vec<2>(p + c, v);
-      else if (left > 0)
-        from_float(x.x(), p[c]);
-    } else {
-      const float next = __shfl_down_sync(0xffffffffu, x.x(), 1);
-      const float v[2] = {x.y(), next};
-      if (lane == 0 && n > 0) from_float(x.x(), p[0]);
-      if (left > 2 && lane < 31)
-        store_vec<2>(p + c + 1, v);
-      else if (left > 1)
-        from_float(x.y(), p[c + 1]);
-    }
+    const bool off = reinterpret_cast<uintptr_t>(p) & 2;
+    const uint32_t own = pack2(x.x(), x.y(), p), next = __shfl_down_sync(0xffffffffu, own, 1);
+    T* const q = p + 2 * lane + (off ? 1 : 0);
+    const int rest = left - (off ? 1 : 0);   // channels from q on
+    const uint32_t w = off ? __byte_perm(own, next, 0x5432) : own;
+    store16_if(off && lane == 0 && n > 0, p, own);
+    store32_if(rest > 1, q, w);
+    store16_if(rest == 1, q, w);
   }
 }
 
@@ -258,12 +259,12 @@ __device__ __forceinline__ int64_t mark_rows(const ScanArgs& a, int64_t row0, Ti
 }
 
 // Sequences without rows keep their state: out = in (0 where there is none).
-__device__ __forceinline__ void pass_empty(const ScanArgs& a, const float* in, float* out, int c0, int block, int blocks) {
+__device__ __forceinline__ void pass_empty(const ScanArgs& a, const float* in, float* out, int c0, int wide, int block, int blocks) {
   if (out == nullptr || (a.cu == nullptr && a.L > 0)) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   for (int64_t b = int64_t(block) * kWarps + warp; b < a.B; b += int64_t(blocks) * kWarps) {
     if (a.cu != nullptr && a.cu[b + 1] > a.cu[b]) continue;
-    for (int c = c0 + lane; c < min(c0 + kStrip, a.H); c += 32) out[b * a.H + c] = in ? in[b * a.H + c] : 0.f;
+    for (int c = c0 + lane; c < min(c0 + wide, a.H); c += 32) out[b * a.H + c] = in ? in[b * a.H + c] : 0.f;
   }
 }
 // cu_seqlens that descend or leave the rows are reported.
@@ -297,10 +298,9 @@ __device__ __forceinline__ float4 compose(const float4& m, const float4& n) {
 // What the warps of a block and the blocks of a cluster tell one another in a step.  warps:
 // the map of each warp's rows, then in x and y what enters them.  tiles: the maps of all
 // blocks' tiles, two slots, so that a peer a step ahead does not write what is still read.
-template <int kCluster>
 struct Exchange {
   float4 warps[kWarps][32];
-  float4 tiles[2][kCluster][32];
+  float4 tiles[2][kMaxCluster][32];
 };
 
 // the eight warps with rows, and the one that folds
@@ -310,17 +310,15 @@ __device__ __forceinline__ void maps_sync() { asm volatile("bar.sync 1, %0;" ::"
 __device__ __forceinline__ void folded() { asm volatile("bar.arrive 2, %0;" ::"n"((kWarps + 1) * 32) : "memory"); }
 __device__ __forceinline__ void wait_folded() { asm volatile("bar.sync 2, %0;" ::"n"((kWarps + 1) * 32) : "memory"); }
 
-// A stage is the tile's rows of each tensor.  As many as leave room for two blocks to an SM (fp32
-// backward: one).  Rows that do not come by TMA begin inside a word and may need one more.
-template <class T, bool kFast>
-constexpr int kPitch = kStrip * static_cast<int>(sizeof(T)) + (kFast || sizeof(T) == 4 ? 0 : 4);
-template <class T, int kTensors, bool kFast>
-constexpr int kRowsBytesOf = kTensors * kPitch<T, kFast>;   // of one row of all tensors
+// A stage is the tile's rows of each tensor, 64 channels' bytes each.  As many as leave room for
+// two blocks to an SM (fp32 backward: one).
+template <class T>
+constexpr int kPitch = 64 * static_cast<int>(sizeof(T));
 template <bool kBwd, bool kMapOnly>
 constexpr int kStagesOf = kBwd && !kMapOnly ? 2 : 3;
 
-__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -328,32 +326,29 @@ __device__ __forceinline__ void cp_async_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-// `rows` rows' channels, n of them from `row` on, to shared memory by words, from any address; first,
-// last: no element lies before the first row's, behind the last row's, that may be read
-// along with it.
-template <class T, int kPitchBytes>
-__device__ __forceinline__ void copy_rows(uint32_t dst, const T* row, int64_t ld, int rows, int n, bool first, bool last, int lane) {
-  if constexpr (sizeof(T) == 4) {
-    const bool in0 = lane < n, in1 = lane + 32 < n;
-    const T* p = row + lane;
-#pragma unroll 4
-    for (int i = 0; i < rows; ++i, p += ld, dst += kPitchBytes) {
-      if (in0) cp_async4(dst + 4 * lane, p);
-      if (in1) cp_async4(dst + 4 * lane + 128, p + 32);
-    }
-  } else {
-#pragma unroll 4
-    for (int i = 0; i < rows; ++i, row += ld, dst += kPitchBytes) {
-      const int off = static_cast<int>(reinterpret_cast<uintptr_t>(row) >> 1 & 1), e = 2 * lane - off;   // the lane's first element
-      if ((first && i == 0) || (last && i == rows - 1)) {
-        for (int k = lane; k < n; k += 32)
-          asm volatile("st.shared.u16 [%0], %1;" ::"r"(dst + 2 * (k + off)), "h"(reinterpret_cast<const uint16_t*>(row)[k])
-                       : "memory");
-        continue;
-      }
-      if (e < n) cp_async4(dst + 4 * lane, row + e);
-      if (off && lane == 0 && n == kStrip) cp_async4(dst + 128, row + 63);
-    }
+// kRows rows' channels, n of them from `row` on, to shared memory in the 16-byte words that hold them,
+// several rows at a time.  (Words of four bytes took four times as long: 20000 x 1031 forward 150 us.)
+template <class T, int kRows>
+__device__ __forceinline__ void copy_rows(uint32_t dst, const T* row, int64_t ld, int n, int lane) {
+  constexpr int kWords = kPitch<T> / 16, kAtOnce = 32 / kWords;
+  const int word = lane % kWords, sub = lane / kWords;
+  uintptr_t p = reinterpret_cast<uintptr_t>(row + sub * ld);
+  dst += sub * kPitch<T> + word * 16;
+#pragma unroll
+  for (int i = 0; i < kRows / kAtOnce; ++i) {
+    const int off = static_cast<int>(p & 15);
+    if (word * 16 < off + n * static_cast<int>(sizeof(T)))
+      cp_async16(dst + i * kAtOnce * kPitch<T>, reinterpret_cast<const void*>(p - off + word * 16));
+    p += static_cast<uintptr_t>(kAtOnce * ld * static_cast<int64_t>(sizeof(T)));
+  }
+}
+// The same for the first or last rows of the tensor, a number of them that need not be kRows, element by
+// element: nothing beside them is read.
+template <class T>
+__device__ __forceinline__ void copy_edge_rows(uint8_t* dst, const T* row, int64_t ld, int rows, int n, int lane) {
+  for (int i = 0; i < rows; ++i, row += ld, dst += kPitch<T>) {
+    T* const at = reinterpret_cast<T*>(dst + (reinterpret_cast<uintptr_t>(row) & 15));
+    for (int k = lane; k < n; k += 32) at[k] = row[k];
   }
 }
 
@@ -386,10 +381,10 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
   constexpr int kTensors = kGrads ? 3 : 2, kV = 1, kD = kValue ? 2 : 1;
   constexpr int kStages = kStagesOf<kBwd, kMapOnly>, kN = kTile<T, kBwd>, kParts = kHalves<T, kBwd>, kRows = kParts * kHalf;
   constexpr uint32_t kAll = (1u << kHalf) - 1u;
-  constexpr int kRowBytes = kPitch<T, kFast>;
+  constexpr int kRowBytes = kPitch<T>, kS = kStrip<T, kFast>;
   constexpr int kTensorBytes = kN * kRowBytes, kStageBytes = kTensors * kTensorBytes;
   extern __shared__ __align__(128) uint8_t smem_raw[];
-  __shared__ __align__(16) Exchange<kClusterOf<T, kBwd, kFast>> ex;
+  __shared__ __align__(16) Exchange ex;
   __shared__ float2 h_maps[kGrads ? kWarps : 1][32];   // b of the maps of h, then h before each warp's rows
   __shared__ TileRows<kN> rows_sh[kStages];
   __shared__ __align__(8) uint64_t full_bar[kStages], empty_bar[kStages], peer_bar[2];
@@ -400,7 +395,7 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
   asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(size));
   const int S = static_cast<int>(size), rank = static_cast<int>(cluster_ctarank());
   const int strip = blockIdx.x / S, strips = gridDim.x / S;
-  const int c0 = strip * kStrip, c = c0 + 2 * lane, left = a.H - c;
+  const int c0 = strip * kS, c = c0 + 2 * lane, wide = min(kS, a.H - c0), left = wide - 2 * lane;
   const int seg = blockIdx.y, seg0 = seg * a.seg_tiles, seg_n = min(a.seg_tiles, a.tiles - seg0);
   const int n_steps = (seg_n + S - 1) / S;
   // the tile of step k, or -1
@@ -501,7 +496,7 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
       }
       // (a wait that runs out raises the block's flag; what follows is then of no use, but ends)
       if (S > 1) mbar_wait(bar, (k >> 1) & 1u, abort_flag, a.err);
-      constexpr int kTiles = kClusterOf<T, kBwd, kFast>;
+      constexpr int kTiles = kMaxCluster;
       float4 t[kTiles];
 #pragma unroll
       for (int p = 0; p < kTiles; ++p) t[p] = ex.tiles[slot][p][lane];   // (of no use from S on)
@@ -541,35 +536,30 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
     if (kMapOnly && rank == 0) a.seg_maps[(int64_t(seg) * strips + strip) * 32 + lane] = total;
   } else {
     if (!kMapOnly && seg == 0) {
-      pass_empty(a, kBwd ? a.dfinal : a.h0, kBwd ? a.dinit : a.final_state, c0, rank, S);
+      pass_empty(a, kBwd ? a.dfinal : a.h0, kBwd ? a.dinit : a.final_state, c0, kS, rank, S);
       if (strip == 0) check_bounds(a, rank, S);
     }
     const int r0 = warp * kRows;
     // rows that do not come by TMA: every warp copies its own, all stages but one ahead
     const void* const tensor_of[3] = {a.gate, kValue ? a.value : a.dy, a.dy};
     const int64_t ld_of[3] = {a.gate_ld, kValue ? a.value_ld : a.dy_ld, a.dy_ld};
-    uint32_t odd_base = 0, odd_ld = 0;   // whether a tensor's rows begin inside a word: at row 0, and for odd rows besides
     auto load_rows = [&](int k) {
       const int t = k < n_steps ? tile_of(k) : -1;
       if (t >= 0) {
 #pragma unroll
         for (int j = 0; j < kTensors; ++j) {
-          const uint32_t dst = smem_u32(smem_raw) + (k % kStages) * kStageBytes + j * kTensorBytes + r0 * kRowBytes;
+          uint8_t* const dst = smem_raw + (k % kStages) * kStageBytes + j * kTensorBytes + r0 * kRowBytes;
           const int64_t r = int64_t(t) * kN + r0;
-          const int rows = static_cast<int>(min(int64_t(kRows), a.T - r));
-          if (rows > 0)
-            copy_rows<T, kRowBytes>(dst, static_cast<const T*>(tensor_of[j]) + r * ld_of[j] + c0, ld_of[j], rows,
-                                    min(kStrip, a.H - c0), r == 0 && c0 == 0, r + rows == a.T && c0 + kStrip >= a.H, lane);
+          const T* const src = static_cast<const T*>(tensor_of[j]) + r * ld_of[j] + c0;
+          if (r > 0 && r + kRows < a.T)
+            copy_rows<T, kRows>(smem_u32(dst), src, ld_of[j], wide, lane);
+          else if (r < a.T)
+            copy_edge_rows<T>(dst, src, ld_of[j], static_cast<int>(min(int64_t(kRows), a.T - r)), wide, lane);
         }
       }
       cp_async_commit();
     };
     if constexpr (!kFast) {
-#pragma unroll
-      for (int j = 0; j < kTensors; ++j) {
-        odd_base |= static_cast<uint32_t>(reinterpret_cast<uintptr_t>(tensor_of[j]) >> 1 & 1) << j;   // (c0 is even)
-        odd_ld |= static_cast<uint32_t>(ld_of[j] & 1) << j;
-      }
 #pragma unroll
       for (int k = 0; k < kStages - 1; ++k) load_rows(k);
     }
@@ -615,16 +605,32 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
         }
       }
       uint8_t* const stage = smem_raw + st * kStageBytes + r0 * kRowBytes;
+      // where a tensor's rows begin in their first 16-byte words: of the warp's first row, and from row to row
+      uint32_t off[kTensors], off_step[kTensors];
+      if constexpr (!kFast) {
+#pragma unroll
+        for (int j = 0; j < kTensors; ++j) {
+          off_step[j] = static_cast<uint32_t>(ld_of[j]) * static_cast<uint32_t>(sizeof(T));
+          off[j] = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(tensor_of[j])) + static_cast<uint32_t>(row) * off_step[j] +
+                   static_cast<uint32_t>(c0) * static_cast<uint32_t>(sizeof(T));
+        }
+      }
       auto get = [&](int tensor, int i) -> Raw<T> {
         const uint8_t* const p = stage + tensor * kTensorBytes + i * kRowBytes;
         Raw<T> r;
-        if constexpr (sizeof(T) == 4) {
-          r.w.v = *reinterpret_cast<const unsigned long long*>(p + 8 * lane);
+        if constexpr (kFast) {
+          if constexpr (sizeof(T) == 4)
+            r.w.v = *reinterpret_cast<const unsigned long long*>(p + 8 * lane);
+          else
+            r.w = *reinterpret_cast<const uint32_t*>(p + 4 * lane);
         } else {
-          r.w = *reinterpret_cast<const uint32_t*>(p + 4 * lane);
-          if constexpr (!kFast) {
-            const uint32_t next = *reinterpret_cast<const uint32_t*>(p + 4 * lane + 4);
-            if ((odd_base >> tensor ^ (odd_ld >> tensor & static_cast<uint32_t>(row + i))) & 1u) r.w = __byte_perm(r.w, next, 0x5432);
+          const uint32_t o = (off[tensor] + i * off_step[tensor]) & 15u;
+          if constexpr (sizeof(T) == 4) {
+            const float* const q = reinterpret_cast<const float*>(p + o) + 2 * lane;
+            r.w = f2(q[0], q[1]);
+          } else {
+            const uint32_t* const q = reinterpret_cast<const uint32_t*>(p + (o & 12u)) + lane;
+            r.w = __byte_perm(q[0], q[1], o & 2u ? 0x5432 : 0x3210);
           }
         }
         return r;
@@ -744,7 +750,7 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
         if constexpr (kFast)
           store2<true>(p + 2 * lane, x, left);
         else
-          store_row(p, x, min(kStrip, a.H - c0), lane);
+          store_row(p, x, wide, lane);
       };
       auto out_row = [&](T* base, int tensor, int i, F2 x) {
         if (boxed)
@@ -949,15 +955,21 @@ bool fast_of(const ScanArgs& a, int dtype) {
 }
 
 constexpr int kMaxSegments = 32;
-int64_t strips_of(const molt_scan_desc* d) { return (d->H + kStrip - 1) / kStrip; }
-size_t seg_bytes(const molt_scan_desc* d) { return static_cast<size_t>(kMaxSegments) * strips_of(d) * 32 * sizeof(float4) + 256; }
+int64_t strips_of(const molt_scan_desc* d, bool fast) {
+  const int wide = d->dtype == MOLT_FP32 ? (fast ? kStrip<float, true> : kStrip<float, false>)
+                                         : (fast ? kStrip<__half, true> : kStrip<__half, false>);
+  return (d->H + wide - 1) / wide;
+}
+size_t seg_bytes(const molt_scan_desc* d) {
+  return static_cast<size_t>(kMaxSegments) * strips_of(d, false) * 32 * sizeof(float4) + 256;
+}
 
 constexpr int kDevices = 16;
 
 // One instance of the kernel.
 struct ScanKernel {
   void (*fn)(const ScanMaps, const ScanArgs);
-  int smem, max_cluster;
+  int smem;
   // by device and a cluster's blocks: how many clusters run at once (0: not yet asked)
   std::atomic<int> clusters[kDevices][kMaxCluster + 1];
 };
@@ -965,8 +977,7 @@ template <class T, int kForm, bool kBwd, bool kMapOnly, bool kFast>
 ScanKernel* kernel_of() {
   constexpr int kTensors = kBwd && !kMapOnly ? 3 : 2;
   static ScanKernel k{&scan_kernel<T, kForm, kBwd, kMapOnly, kFast>,
-                      kStagesOf<kBwd, kMapOnly> * kTile<T, kBwd> * kRowsBytesOf<T, kTensors, kFast>, kClusterOf<T, kBwd, kFast>,
-                      {}};
+                      kStagesOf<kBwd, kMapOnly> * kTile<T, kBwd> * kTensors * kPitch<T> + (kFast ? 0 : 128), {}};
   return &k;
 }
 template <class T, int kForm>
@@ -1033,7 +1044,7 @@ struct ScanPlan {
 cudaError_t plan_of(ScanKernel* k, int64_t strips, int tiles, ScanPlan& p) {
   p.cluster = p.segments = 1;
   int n = 0;
-  for (int s = k->max_cluster; s >= 1; --s) {
+  for (int s = kMaxCluster; s >= 1; --s) {
     if (s > tiles && s > 1) continue;
     if (const cudaError_t e = clusters_at_once(k, s, n); e != cudaSuccess) return e;
     p.cluster = s;
@@ -1048,11 +1059,11 @@ molt_status launch(const molt_scan_desc* d, ScanArgs& a, bool bwd, void* workspa
   molt_status st;
   a.err = device_status_word(&st);
   if (!a.err) return st;
-  const int strips = static_cast<int>(strips_of(d));
   const int tile = d->dtype == MOLT_FP32 ? (bwd ? kTile<float, true> : kTile<float, false>)
                                          : (bwd ? kTile<__half, true> : kTile<__half, false>);
   a.tiles = static_cast<int>((a.T + tile - 1) / tile);
   const bool fast = a.tiles > 0 && fast_of(a, d->dtype);
+  const int strips = static_cast<int>(strips_of(d, fast));
   ScanPlan plan;
   if (const cudaError_t e = plan_of(kernel_of(d->dtype, d->form, bwd, false, fast), strips, a.tiles, plan); e != cudaSuccess)
     return cuda_fail(e, "gated scan");
@@ -1068,7 +1079,7 @@ molt_status launch(const molt_scan_desc* d, ScanArgs& a, bool bwd, void* workspa
     const int e = dtype_bytes(d->dtype);
     const auto encode = [&](CUtensorMap* t, const void* p, int64_t ld, int rows) {
       return encode_tmap_plain(t, e == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, e, p, a.T, a.H, ld,
-                               kStrip, rows);
+                               kStrip<float, true>, rows);
     };
     if (const molt_status q = encode(&m.gate, a.gate, a.gate_ld, tile); q != MOLT_OK) return q;
     if (const molt_status q = encode(&m.value, a.value, a.value_ld, tile); q != MOLT_OK) return q;
