@@ -7,6 +7,7 @@
 // counter's words are (column / 8, row, offset low, offset high), the key is the seed; one
 // call of the generator serves eight columns, column 8 g + j taking half j % 2 (low first)
 // of word j / 2.  The backward is the same map on the gradient.
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <cuda_runtime.h>
@@ -27,66 +28,139 @@ struct DropArgs {
   int H, groups;            // groups of eight columns of a row
   int rows;                 // rows of a tile
   uint32_t magic;           // i / groups = (i magic) >> 32 inside a tile
-  uint32_t threshold, row0;
+  uint32_t bound;           // keep: 16 bits, in a word's upper half, are not below it
+  uint32_t row0;
   float scale, res_scale;
-  uint64_t seed, offset;
+  uint64_t offset;
+  uint2 keys[10];           // the rounds' keys of a seed on the host
   const uint64_t* words;    // seed and offset on the device, or nullptr
 };
 
-// 128 bits of the generator
-__device__ __forceinline__ uint4 philox(uint4 c, uint2 k) {
+__host__ __device__ inline void round_keys(uint64_t seed, uint2 (&keys)[10]) {
+  uint32_t x = static_cast<uint32_t>(seed), y = static_cast<uint32_t>(seed >> 32);
+#pragma unroll
+  for (int i = 0; i < 10; ++i) {
+    keys[i].x = x;
+    keys[i].y = y;
+    x += 0x9E3779B9u;
+    y += 0xBB67AE85u;
+  }
+}
+// 128 bits of the generator.  The rounds' keys stand in the launch's parameters (or, of a seed on
+// the device, in registers), where an instruction takes them as they are.
+__device__ __forceinline__ uint4 philox(uint4 c, const uint2 (&k)[10]) {
 #pragma unroll
   for (int i = 0; i < 10; ++i) {
     const uint64_t p0 = uint64_t(0xD2511F53u) * c.x, p1 = uint64_t(0xCD9E8D57u) * c.z;
-    c = make_uint4(static_cast<uint32_t>(p1 >> 32) ^ c.y ^ k.x, static_cast<uint32_t>(p1),
-                   static_cast<uint32_t>(p0 >> 32) ^ c.w ^ k.y, static_cast<uint32_t>(p0));
-    k.x += 0x9E3779B9u;
-    k.y += 0xBB67AE85u;
+    c = make_uint4(static_cast<uint32_t>(p1 >> 32) ^ c.y ^ k[i].x, static_cast<uint32_t>(p1),
+                   static_cast<uint32_t>(p0 >> 32) ^ c.w ^ k[i].y, static_cast<uint32_t>(p0));
   }
   return c;
 }
 
-template <class Tin, class Tout, bool kVec>
-__global__ void __launch_bounds__(kThreads) dropout_kernel(const DropArgs a) {
+// 16 bytes, asked for where the statement stands; kApart: of a tensor that the call does not write
+// (16001 x 5120 bf16: 62 us as read-only data, else 69).
+template <bool kApart>
+__device__ __forceinline__ uint4 load_now(const void* p) {
+  uint4 v;
+  if constexpr (kApart)
+    asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  else
+    asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+
+// Eight elements as they are in memory.
+template <class T, bool kApart>
+struct Raw8 {
+  uint4 q[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) q[i] = load_now<kApart>(reinterpret_cast<const uint4*>(p) + i);
+  }
+  __device__ __forceinline__ void get(float (&v)[8]) const { load_vec<8>(reinterpret_cast<const T*>(q), v); }
+};
+
+// A thread's next group is on its way while it works on one (32768 x 4096 into an fp32 stream 240 us
+// without, 212 with two groups at once, 205 so; 16001 x 5120 bf16 64, 73 and 62).
+template <class Tin, class Tout, bool kVec, bool kRes, bool kWords, bool kApart>
+__global__ void __launch_bounds__(kThreads) dropout_kernel(const __grid_constant__ DropArgs a) {
   const Tin* x = static_cast<const Tin*>(a.x);
   const Tout* res = static_cast<const Tout*>(a.residual);
   Tout* out = static_cast<Tout*>(a.out);
-  const uint64_t seed = a.words ? a.words[0] : a.seed, offset = a.words ? a.words[1] : a.offset;
-  const uint2 key = make_uint2(static_cast<uint32_t>(seed), static_cast<uint32_t>(seed >> 32));
+  uint2 own_keys[10];
+  uint64_t offset = a.offset;
+  if constexpr (kWords) {
+    round_keys(a.words[0], own_keys);
+    offset = a.words[1];
+  }
+  struct Group {
+    int64_t t;
+    int c;
+  };
   for (int64_t t0 = int64_t(blockIdx.x) * a.rows; t0 < a.T; t0 += int64_t(gridDim.x) * a.rows) {
     const int n = static_cast<int>(min(int64_t(a.rows), a.T - t0)) * a.groups;
-    for (int i = threadIdx.x; i < n; i += kThreads) {
+    auto group = [&](int i) -> Group {
       const int r = a.groups == 1 ? i : static_cast<int>(__umulhi(static_cast<uint32_t>(i), a.magic));
-      const int g = i - r * a.groups, c = g * 8;
-      const int64_t t = t0 + r;
-      float v[8], o[8];
-      const int left = min(8, a.H - c);
-      if constexpr (kVec) {
-        load_vec<8>(x + t * a.x_ld + c, v);
-        if (res) load_vec<8>(res + t * a.r_ld + c, o);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          v[j] = j < left ? to_float(x[t * a.x_ld + c + j]) : 0.f;
-          o[j] = res && j < left ? to_float(res[t * a.r_ld + c + j]) : 0.f;
-        }
-      }
-      const uint4 w = philox(make_uint4(static_cast<uint32_t>(g), a.row0 + static_cast<uint32_t>(t),
-                                        static_cast<uint32_t>(offset), static_cast<uint32_t>(offset >> 32)), key);
+      return {t0 + r, (i - r * a.groups) * 8};
+    };
+    auto work = [&](const Group& g, float (&v)[8], float (&o)[8]) {
+      const uint4 c = make_uint4(static_cast<uint32_t>(g.c) / 8u, a.row0 + static_cast<uint32_t>(g.t), static_cast<uint32_t>(offset),
+                                 static_cast<uint32_t>(offset >> 32));
+      uint4 w;
+      if constexpr (kWords)
+        w = philox(c, own_keys);
+      else
+        w = philox(c, a.keys);
       const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const uint32_t bits = j & 1 ? ws[j / 2] >> 16 : ws[j / 2] & 0xffffu;
+        const uint32_t bits = j & 1 ? ws[j / 2] & 0xffff0000u : ws[j / 2] << 16;
         // a dropped value is left out, not multiplied by zero
-        const float d = bits >= a.threshold ? v[j] * a.scale : 0.f;
-        o[j] = res ? fmaf(a.res_scale, o[j], d) : d;
+        const float d = bits >= a.bound ? v[j] * a.scale : 0.f;
+        o[j] = kRes ? fmaf(a.res_scale, o[j], d) : d;
       }
-      if constexpr (kVec) {
-        store_vec<8>(out + t * a.H + c, o);
-      } else {
+    };
+    if constexpr (kVec) {
+      Raw8<Tin, kApart> xr, x_next;
+      Raw8<Tout, kApart> rr, r_next;
+      int i = threadIdx.x;
+      Group g = group(i);
+      if (i < n) {
+        xr.load(x + g.t * a.x_ld + g.c);
+        if constexpr (kRes) rr.load(res + g.t * a.r_ld + g.c);
+      }
+      while (i < n) {
+        const int next = i + kThreads;
+        const Group h = group(next);
+        if (next < n) {
+          x_next.load(x + h.t * a.x_ld + h.c);
+          if constexpr (kRes) r_next.load(res + h.t * a.r_ld + h.c);
+        }
+        float v[8], o[8];
+        xr.get(v);
+        if constexpr (kRes) rr.get(o);
+        work(g, v, o);
+        store_vec<8>(out + g.t * a.H + g.c, o);
+        i = next;
+        g = h;
+        xr = x_next;
+        rr = r_next;
+      }
+    } else {
+      for (int i = threadIdx.x; i < n; i += kThreads) {
+        const Group g = group(i);
+        const int left = min(8, a.H - g.c);
+        float v[8], o[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          v[j] = j < left ? to_float(x[g.t * a.x_ld + g.c + j]) : 0.f;
+          o[j] = kRes && j < left ? to_float(res[g.t * a.r_ld + g.c + j]) : 0.f;
+        }
+        work(g, v, o);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (j < left) from_float(o[j], out[t * a.H + c + j]);
+          if (j < left) from_float(o[j], out[g.t * a.H + g.c + j]);
       }
     }
   }
@@ -97,12 +171,19 @@ molt_status fail(molt_status s, const char* msg) {
   return s;
 }
 
+template <class Tin, class Tout, bool kVec, bool kRes>
+void launch(const DropArgs& a, int grid, cudaStream_t s) {
+  const bool apart = kVec && a.out != a.x && a.out != a.residual;
+  const auto k = a.words ? (apart ? dropout_kernel<Tin, Tout, kVec, kRes, true, kVec> : dropout_kernel<Tin, Tout, kVec, kRes, true, false>)
+                         : (apart ? dropout_kernel<Tin, Tout, kVec, kRes, false, kVec> : dropout_kernel<Tin, Tout, kVec, kRes, false, false>);
+  k<<<grid, kThreads, 0, s>>>(a);
+}
 template <class Tin, class Tout>
 void launch(const DropArgs& a, bool vec, int grid, cudaStream_t s) {
   if (vec)
-    dropout_kernel<Tin, Tout, true><<<grid, kThreads, 0, s>>>(a);
+    a.residual ? launch<Tin, Tout, true, true>(a, grid, s) : launch<Tin, Tout, true, false>(a, grid, s);
   else
-    dropout_kernel<Tin, Tout, false><<<grid, kThreads, 0, s>>>(a);
+    a.residual ? launch<Tin, Tout, false, true>(a, grid, s) : launch<Tin, Tout, false, false>(a, grid, s);
 }
 
 bool known_type(int dt) { return dt == MOLT_BF16 || dt == MOLT_FP16 || dt == MOLT_FP32; }
@@ -144,20 +225,23 @@ extern "C" molt_status molt_dropout(const molt_dropout_desc* d, const void* x, c
   a.x_ld = x_ld;
   a.r_ld = r_ld;
   a.groups = (a.H + 7) / 8;
-  // about eight groups to a thread; i < 2^14 and groups <= 2^13, so that the magic
-  // division is exact (i groups < 2^32)
-  a.rows = 8 * kThreads / a.groups > 1 ? 8 * kThreads / a.groups : 1;
+  // up to 16 groups to a thread, fewer where there would be too few blocks; i < 2^13 and groups
+  // <= 2^13, so that the magic division is exact (i groups < 2^32)
+  const int64_t most = 8 * int64_t(device_sm_count());
+  a.rows = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(16 * kThreads / a.groups, (d->T + most - 1) / most)));
+  a.rows = std::max(a.rows, std::min(1024, kThreads / a.groups));
   a.magic = a.groups == 1 ? 0 : static_cast<uint32_t>(((uint64_t(1) << 32) + a.groups - 1) / a.groups);
-  a.threshold = static_cast<uint32_t>(std::floor(d->p * 65536.0 + 0.5));
-  a.scale = a.threshold < 65536 ? static_cast<float>(65536.0 / (65536.0 - a.threshold)) : 0.f;
+  const uint32_t threshold = static_cast<uint32_t>(std::floor(d->p * 65536.0 + 0.5));
+  a.bound = threshold < 65536 ? threshold << 16 : 0xffffffffu;   // (no 16 bits in an upper half reach that)
+  a.scale = threshold < 65536 ? static_cast<float>(65536.0 / (65536.0 - threshold)) : 0.f;
   a.res_scale = d->res_scale;
   a.row0 = static_cast<uint32_t>(d->first_row);
-  a.seed = d->seed;
+  round_keys(d->seed, a.keys);
   a.offset = d->offset;
   a.words = seed_offset;
   const bool vec = a.H % 8 == 0 && aligned(x, 16) && aligned(out, 16) && aligned(residual, 16) && x_ld * ib % 16 == 0 &&
                    r_ld * ob % 16 == 0;
-  const int64_t tiles = (d->T + a.rows - 1) / a.rows, most = 8 * int64_t(device_sm_count());
+  const int64_t tiles = (d->T + a.rows - 1) / a.rows;
   const int grid = static_cast<int>(tiles < most ? tiles : most);
   using Launch = void (*)(const DropArgs&, bool, int, cudaStream_t);
   const bool i32 = d->dtype == MOLT_FP32, o32 = d->out_dtype == MOLT_FP32;

@@ -879,17 +879,22 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
   cluster_sync_all();   // no block leaves while a peer may still write to it
 }
 
-template <class T, int kForm>
+// One row of each sequence: kVec channels to a thread, `chunks` blocks to a row.
+template <class T, int kForm, int kVec>
 __global__ void __launch_bounds__(256) scan_step_kernel(const T* gate, const T* value, const float* state, int64_t B, int H,
-                                                        int64_t gate_ld, int64_t value_ld, T* y, float* state_out) {
-  const int64_t n = B * H;
-  for (int64_t i = blockIdx.x * int64_t(256) + threadIdx.x; i < n; i += gridDim.x * int64_t(256)) {
-    const int64_t b = i / H;
-    const int c = static_cast<int>(i - b * H);
-    const F2 h = step<kForm>(f2(state[i]), decay<kForm>(f2(to_float(gate[b * gate_ld + c]))),
-                             f2(to_float(value[b * value_ld + c])));
-    state_out[i] = h.x();
-    from_float(h.x(), y[i]);
+                                                        int64_t gate_ld, int64_t value_ld, int chunks, T* y, float* state_out) {
+  for (int64_t i = blockIdx.x; i < B * chunks; i += gridDim.x) {
+    const int64_t b = i / chunks;
+    const int c = (static_cast<int>(i - b * chunks) * 256 + static_cast<int>(threadIdx.x)) * kVec;
+    if (c >= H) continue;
+    float f[kVec], v[kVec], h[kVec];
+    load_vec<kVec>(gate + b * gate_ld + c, f);
+    load_vec<kVec>(value + b * value_ld + c, v);
+    load_vec<kVec>(state + b * H + c, h);
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) h[j] = step<kForm>(f2(h[j]), decay<kForm>(f2(f[j])), f2(v[j])).x();
+    store_vec<kVec>(state_out + b * H + c, h);
+    store_vec<kVec>(y + b * H + c, h);
   }
 }
 
@@ -1106,10 +1111,17 @@ molt_status launch(const molt_scan_desc* d, ScanArgs& a, bool bwd, void* workspa
 
 template <class T, int kForm>
 void launch_step(const molt_scan_desc* d, const void* gate, const void* value, const float* state, void* y, float* out,
-                 int grid, cudaStream_t s) {
-  scan_step_kernel<T, kForm><<<grid, 256, 0, s>>>(
-      static_cast<const T*>(gate), static_cast<const T*>(value), state, d->B, static_cast<int>(d->H),
-      d->gate_stride ? d->gate_stride : d->H, d->value_stride ? d->value_stride : d->H, static_cast<T*>(y), out);
+                 cudaStream_t s) {
+  const int H = static_cast<int>(d->H);
+  const int64_t g_ld = d->gate_stride ? d->gate_stride : H, v_ld = d->value_stride ? d->value_stride : H;
+  const auto at = [](const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; };
+  const bool vec = H % 4 == 0 && g_ld % 4 == 0 && v_ld % 4 == 0 && at(gate, 4 * sizeof(T)) && at(value, 4 * sizeof(T)) &&
+                   at(y, 4 * sizeof(T)) && at(state, 16) && at(out, 16);
+  const int chunks = (H + 256 * (vec ? 4 : 1) - 1) / (256 * (vec ? 4 : 1));
+  const int grid = static_cast<int>(std::min<int64_t>(d->B * chunks, 16 * int64_t(device_sm_count())));
+  const auto k = vec ? scan_step_kernel<T, kForm, 4> : scan_step_kernel<T, kForm, 1>;
+  k<<<grid, 256, 0, s>>>(static_cast<const T*>(gate), static_cast<const T*>(value), state, d->B, H, g_ld, v_ld, chunks,
+                         static_cast<T*>(y), out);
 }
 
 }  // namespace
@@ -1196,13 +1208,11 @@ molt_status molt_gated_scan_step(const molt_scan_desc* desc, const void* gate, c
                                              {state_out, MOLT_FP32}});
       st != MOLT_OK)
     return st;
-  const int64_t blocks = (desc->B * desc->H + 255) / 256;
-  const int grid = static_cast<int>(std::min<int64_t>(blocks, 16 * int64_t(device_sm_count())));
   const bool sig = desc->form == MOLT_SCAN_SIGMOID;
   const auto k = desc->dtype == MOLT_FP32   ? (sig ? launch_step<float, kFormSigmoid> : launch_step<float, kFormLog>)
                  : desc->dtype == MOLT_FP16 ? (sig ? launch_step<__half, kFormSigmoid> : launch_step<__half, kFormLog>)
                                             : (sig ? launch_step<__nv_bfloat16, kFormSigmoid> : launch_step<__nv_bfloat16, kFormLog>);
-  k(desc, gate, value, state, y, state_out, grid, stream);
+  k(desc, gate, value, state, y, state_out, stream);
   if (const cudaError_t e = cudaGetLastError(); e != cudaSuccess) return cuda_fail(e, "gated scan step");
   note_launches(1);
   return MOLT_OK;
