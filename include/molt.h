@@ -608,9 +608,10 @@ molt_status molt_gated_ffn_bwd(const molt_ffn_desc* desc, const void* dy, const 
  * projection are); states fp32.  Sequence b is rows cu_seqlens[b] .. cu_seqlens[b+1] - 1 (device
  * int32 [B+1], ascending, within [0, T]; sequences may be empty), or with cu_seqlens NULL the b-th
  * T / B rows.  It begins with initial_state[b] ([B,H], NULL: 0).  Rows of y outside of every
- * sequence are left as they were, or with fill_outside 0; their gradients are 0.  cu_seqlens that descend or leave [0, T] set
- * MOLT_DEV_UNSORTED_GROUPS; what is then written is unspecified, but lies inside the outputs.
- * Nothing of a sequence, not even an infinity or a NaN, reaches another.
+ * sequence are left as they were, or with fill_outside 0; their gradients are 0.  cu_seqlens that
+ * descend or leave [0, T] set MOLT_DEV_UNSORTED_GROUPS; what is then written is unspecified, but
+ * lies inside the outputs.  Nothing of a sequence, not even an infinity or a NaN, reaches
+ * another.  Outputs overlap neither one another nor the inputs.
  */
 #define MOLT_SCAN_SIGMOID 0
 #define MOLT_SCAN_LOG 1
@@ -655,7 +656,8 @@ molt_status molt_gated_scan_step(const molt_scan_desc* desc, const void* gate, c
  * (first_row), and the backward is the same call on the gradient: dx = dropout of dout (its
  * residual's gradient is res_scale dout).  Dropped values are left out, whatever they are.
  * x [T,H] of dtype, residual (NULL: none) and out of out_dtype: dtype, or one of the two is
- * MOLT_FP32.  out may be x or the residual where rows lie side by side and the type is the same.
+ * MOLT_FP32.  out may be x or the residual where rows lie side by side and the type is the same,
+ * and overlaps them in no other way.
  * seed_offset: device uint64 [2], read when the call runs, in the place of seed and offset (a
  * captured graph draws a new mask at every replay when the program changes them), or NULL.
  */

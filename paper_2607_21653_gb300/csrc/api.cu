@@ -1137,6 +1137,22 @@ int ordered_splits(int64_t Tcap, int64_t V, int n_sm) {
   return static_cast<int>(std::max<int64_t>(1, std::min((int64_t(16) * n_sm + n_mt - 1) / n_mt, n_vt)));
 }
 
+bool spans_apart(std::initializer_list<Span> written, std::initializer_list<Span> read) {
+  const auto apart = [](const Span& a, const Span& b) {
+    if (!a.p || !b.p || a.rows < 1 || b.rows < 1) return true;
+    const auto end = [](const Span& s) {
+      return reinterpret_cast<uintptr_t>(s.p) + static_cast<uintptr_t>(((s.rows - 1) * (s.ld ? s.ld : s.cols) + s.cols) * s.bytes);
+    };
+    return end(a) <= reinterpret_cast<uintptr_t>(b.p) || end(b) <= reinterpret_cast<uintptr_t>(a.p);
+  };
+  for (const Span* w = written.begin(); w != written.end(); ++w) {
+    for (const Span* v = w + 1; v != written.end(); ++v)
+      if (!apart(*w, *v)) return false;
+    for (const Span& r : read)
+      if (!apart(*w, r)) return false;
+  }
+  return true;
+}
 molt_status encode_tmap_2d(CUtensorMap* m, CUtensorMapDataType dt, int elem_bytes, const void* base, uint64_t rows,
                            uint64_t cols, uint32_t box_cols, uint32_t box_rows) {
   return make_tmap(m, dt, elem_bytes, base, rows, cols, box_cols, box_rows);

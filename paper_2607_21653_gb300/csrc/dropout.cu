@@ -216,6 +216,10 @@ extern "C" molt_status molt_dropout(const molt_dropout_desc* d, const void* x, c
   // written where it is read, element by element, by the thread that has read it
   if ((x == out && (ib != ob || (x_ld != d->H && d->T > 1))) || (residual == out && r_ld != d->H && d->T > 1))
     return fail(MOLT_ERR_INVALID_ARG, "a tensor is updated in place where its rows lie side by side and its type stays");
+  if (const int eb = static_cast<int>(ib); !spans_apart({{out, d->T, d->H, static_cast<int>(ob)}},
+                                                        {{x == out ? nullptr : x, d->T, d->H, eb, x_ld},
+                                                         {residual == out ? nullptr : residual, d->T, d->H, static_cast<int>(ob), r_ld}}))
+    return fail(MOLT_ERR_INVALID_ARG, "out is x, the residual or memory of its own");
   DropArgs a{};
   a.x = x;
   a.residual = residual;

@@ -307,6 +307,11 @@ molt_status molt_gated_ffn_fwd(const molt_ffn_desc* desc, const void* x, const v
   if (desc->T == 0) return MOLT_OK;
   if (!x || !w_gate || !w_up || !w_down || !y) return fail(MOLT_ERR_INVALID_ARG, "null pointer");
   FFN_TRY(check16({x, w_gate, w_up, w_down, y, gate_out, up_out}));
+  if (const int64_t T = desc->T, H = desc->H, F = desc->F;
+      !spans_apart({{y, T, H, 2}, {gate_out, T, F, 2}, {up_out, T, F, 2}},
+                   {{x, T, H, 2, desc->x_stride}, {w_gate, F, H, 2, desc->w_gate_stride}, {w_up, F, H, 2, desc->w_up_stride},
+                    {w_down, H, F, 2, desc->w_down_stride}}))
+    return fail(MOLT_ERR_INVALID_ARG, "outputs may not share memory with one another or with inputs");
   Scratch sc;
   FFN_TRY(get_scratch(sc, workspace, workspace_bytes, molt_gated_ffn_fwd_workspace_bytes(desc), stream));
   molt_status st;
@@ -362,10 +367,13 @@ molt_status molt_gated_ffn_bwd(const molt_ffn_desc* desc, const void* dy, const 
     return fail(MOLT_ERR_INVALID_ARG, "the weights' gradients are of the block's type or fp32");
   if (accumulate && dw_dtype != MOLT_FP32) return fail(MOLT_ERR_INVALID_ARG, "gradients are added in fp32 only");
   if (!dw_gate || !dw_up || !dw_down) return fail(MOLT_ERR_INVALID_ARG, "null pointer");
-  if (dw_gate == dw_up || dw_gate == dw_down || dw_up == dw_down)
-    return fail(MOLT_ERR_INVALID_ARG, "every weight needs a gradient buffer of its own");
   FFN_TRY(check16({dw_gate, dw_up, dw_down}));
   const int64_t T = desc->T, H = desc->H, F = desc->F;
+  const int db = dtype_bytes(dw_dtype);
+  if (!spans_apart({{dx, T, H, 2}, {dw_gate, F, H, db}, {dw_up, F, H, db}, {dw_down, H, F, db}},
+                   {{dy, T, H, 2, desc->dy_stride}, {x, T, H, 2, desc->x_stride}, {w_gate, F, H, 2, desc->w_gate_stride},
+                    {w_up, F, H, 2, desc->w_up_stride}, {w_down, H, F, 2, desc->w_down_stride}, {gate, T, F, 2}, {up, T, F, 2}}))
+    return fail(MOLT_ERR_INVALID_ARG, "outputs may not share memory with one another or with inputs");
   if (T == 0) {
     const size_t n = static_cast<size_t>(H) * F * dtype_bytes(dw_dtype);
     for (void* p : {dw_gate, dw_up, dw_down})

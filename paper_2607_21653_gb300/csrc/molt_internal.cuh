@@ -4,6 +4,7 @@
 #include <cstdint>
 #include <cuda.h>
 #include <cuda_runtime.h>
+#include <initializer_list>
 #include <string>
 
 #include "../../include/molt.h"
@@ -180,6 +181,15 @@ int device_sm_count();                           // current device's SM count
 // vocab splits of the forward pass over Tcap packed rows
 int forward_splits(int64_t Tcap, int64_t H, int64_t V, int n_sm);
 int ordered_splits(int64_t Tcap, int64_t V, int n_sm);   // the reproducible loss call's
+// Memory of a matrix of `rows` rows, ld elements apart; nullptr or no rows: none.
+struct Span {
+  const void* p;
+  int64_t rows, cols;
+  int64_t bytes;    // of an element
+  int64_t ld = 0;   // 0: cols
+};
+// Whether none of the written ones shares memory with another or with what is read.
+bool spans_apart(std::initializer_list<Span> written, std::initializer_list<Span> read);
 molt_status encode_tmap_2d(CUtensorMap* m, CUtensorMapDataType dt, int elem_bytes, const void* base, uint64_t rows,
                            uint64_t cols, uint32_t box_cols, uint32_t box_rows);
 // the same for rows that lie ld elements apart

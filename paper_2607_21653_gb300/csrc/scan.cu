@@ -29,8 +29,6 @@
 #include <algorithm>
 #include <atomic>
 #include <cstdint>
-#include <cstdio>
-#include <cstdlib>
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <initializer_list>
@@ -1037,7 +1035,6 @@ cudaError_t clusters_at_once(ScanKernel* k, int cluster, int& n) {
   if (e != cudaSuccess) return e;
   n = std::max(n, 1);
   if (known) known->store(n, std::memory_order_relaxed);
-  if (getenv("SCAN_DEBUG")) fprintf(stderr, "cluster %d: %d\n", cluster, n);
   return cudaSuccess;
 }
 
@@ -1149,6 +1146,11 @@ molt_status molt_gated_scan_fwd(const molt_scan_desc* desc, const void* gate, co
                                              {states, MOLT_FP32}});
       st != MOLT_OK)
     return st;
+  if (const int64_t T = desc->T, H = desc->H, B = desc->B, e = dtype_bytes(desc->dtype);
+      !spans_apart({{y, T, H, e}, {final_state, B, H, 4}, {states, (T + kStateRows - 1) / kStateRows, H, 4}},
+                   {{gate, T, H, e, desc->gate_stride}, {value, T, H, e, desc->value_stride}, {initial_state, B, H, 4},
+                    {cu_seqlens, B + 1, 1, 4}}))
+    return fail(MOLT_ERR_INVALID_ARG, "outputs may not share memory with one another or with inputs");
   if (desc->T == 0 && (desc->B == 0 || !final_state)) return MOLT_OK;
   if (workspace && workspace_bytes < seg_bytes(desc)) return fail(MOLT_ERR_WORKSPACE, "workspace too small");
   ScanArgs a = base_args(desc, cu_seqlens);
@@ -1180,6 +1182,12 @@ molt_status molt_gated_scan_bwd(const molt_scan_desc* desc, const void* dy, cons
                                              {dinitial_state, MOLT_FP32}});
       st != MOLT_OK)
     return st;
+  if (const int64_t T = desc->T, H = desc->H, B = desc->B, e = dtype_bytes(desc->dtype);
+      !spans_apart({{dgate, T, H, e}, {dvalue, T, H, e}, {dinitial_state, B, H, 4}},
+                   {{dy, T, H, e, desc->dy_stride}, {gate, T, H, e, desc->gate_stride}, {value, T, H, e, desc->value_stride},
+                    {states, (T + kStateRows - 1) / kStateRows, H, 4}, {initial_state, B, H, 4}, {dfinal_state, B, H, 4},
+                    {cu_seqlens, B + 1, 1, 4}}))
+    return fail(MOLT_ERR_INVALID_ARG, "outputs may not share memory with one another or with inputs");
   if (desc->T == 0 && (desc->B == 0 || !dinitial_state)) return MOLT_OK;
   if (workspace && workspace_bytes < seg_bytes(desc)) return fail(MOLT_ERR_WORKSPACE, "workspace too small");
   ScanArgs a = base_args(desc, cu_seqlens);
@@ -1208,12 +1216,18 @@ molt_status molt_gated_scan_step(const molt_scan_desc* desc, const void* gate, c
                                              {state_out, MOLT_FP32}});
       st != MOLT_OK)
     return st;
+  const int64_t H = desc->H, B = desc->B;
+  const int e = dtype_bytes(desc->dtype);
+  // the state may be updated in place: each element by the thread that has read it
+  if (!spans_apart({{y, B, H, e}, {state_out, B, H, 4}}, {{gate, B, H, e, desc->gate_stride}, {value, B, H, e, desc->value_stride}}) ||
+      !spans_apart({{y, B, H, e}, {state_out == state ? nullptr : state_out, B, H, 4}}, {{state, B, H, 4}}))
+    return fail(MOLT_ERR_INVALID_ARG, "outputs may not share memory with one another or with inputs (but state_out may be state)");
   const bool sig = desc->form == MOLT_SCAN_SIGMOID;
   const auto k = desc->dtype == MOLT_FP32   ? (sig ? launch_step<float, kFormSigmoid> : launch_step<float, kFormLog>)
                  : desc->dtype == MOLT_FP16 ? (sig ? launch_step<__half, kFormSigmoid> : launch_step<__half, kFormLog>)
                                             : (sig ? launch_step<__nv_bfloat16, kFormSigmoid> : launch_step<__nv_bfloat16, kFormLog>);
   k(desc, gate, value, state, y, state_out, stream);
-  if (const cudaError_t e = cudaGetLastError(); e != cudaSuccess) return cuda_fail(e, "gated scan step");
+  if (const cudaError_t status = cudaGetLastError(); status != cudaSuccess) return cuda_fail(status, "gated scan step");
   note_launches(1);
   return MOLT_OK;
 }

@@ -8,7 +8,7 @@ import torch
 import paper_2607_21653_gb300 as molt
 from paper_2607_21653_gb300 import blocks as B
 
-FAKE = 0x1000   # never dereferenced: every call below fails validation first
+FAKE = 1 << 20   # never dereferenced: every call below fails validation first
 BAD, SHAPE = "MOLT_ERR_INVALID_ARG", "MOLT_ERR_UNSUPPORTED_SHAPE"
 
 
@@ -44,13 +44,13 @@ def status(code):
 
 def ffn_fwd(lib, d, **kw):
     names = ("x", "w_gate", "w_up", "w_down", "y", "gate_out", "up_out", "ws")
-    ptr = {**{n: FAKE for n in names}, "gate_out": None, "up_out": None, **kw}
+    ptr = {**{n: FAKE * (i + 1) for i, n in enumerate(names)}, "gate_out": None, "up_out": None, **kw}
     return status(lib.molt_gated_ffn_fwd(ctypes.byref(d), *[ptr[n] for n in names], 16, None))
 
 
 def ffn_bwd(lib, d, dw_dtype=2, accumulate=0, **kw):
     names = ("dy", "x", "w_gate", "w_up", "w_down", "gate", "up", "dx", "dw_gate", "dw_up", "dw_down")
-    ptr = {**{n: FAKE + 16 * i for i, n in enumerate(names)}, **kw}
+    ptr = {**{n: FAKE * (i + 1) for i, n in enumerate(names)}, **kw}
     return status(lib.molt_gated_ffn_bwd(ctypes.byref(d), *[ptr[n] for n in names], dw_dtype, accumulate, FAKE, 16, None))
 
 
@@ -83,7 +83,6 @@ def test_ffn_refuses_pointers(lib):
         assert ffn_bwd(lib, ffn(), **{n: FAKE + 4}) == BAD, n
     assert ffn_bwd(lib, ffn(), dw_dtype=1) == BAD
     assert ffn_bwd(lib, ffn(), dw_dtype=0, accumulate=1) == BAD
-    assert ffn_bwd(lib, ffn(), dw_up=FAKE, dw_gate=FAKE) == BAD
     assert ffn_bwd(lib, ffn()) == "MOLT_ERR_WORKSPACE"
     assert status(lib.molt_gated_ffn_fwd(None, *[FAKE] * 8, 16, None)) == BAD
 
@@ -100,19 +99,19 @@ def test_ffn_workspaces_never_shrink_as_tokens_grow(lib):
 
 def scan_fwd(lib, d, **kw):
     names = ("gate", "value", "h0", "cu", "y", "final", "states")
-    ptr = {**{n: FAKE for n in names}, **kw}
+    ptr = {**{n: FAKE * (i + 1) for i, n in enumerate(names)}, **kw}
     return status(lib.molt_gated_scan_fwd(ctypes.byref(d), *[ptr[n] for n in names], FAKE, 16, None))
 
 
 def scan_bwd(lib, d, **kw):
     names = ("dy", "gate", "value", "states", "h0", "cu", "dfinal", "dgate", "dvalue", "dinit")
-    ptr = {**{n: FAKE for n in names}, **kw}
+    ptr = {**{n: FAKE * (i + 1) for i, n in enumerate(names)}, **kw}
     return status(lib.molt_gated_scan_bwd(ctypes.byref(d), *[ptr[n] for n in names], FAKE, 16, None))
 
 
 def scan_step(lib, d, **kw):
     names = ("gate", "value", "state", "y", "out")
-    ptr = {**{n: FAKE for n in names}, **kw}
+    ptr = {**{n: FAKE * (i + 1) for i, n in enumerate(names)}, **kw}
     return status(lib.molt_gated_scan_step(ctypes.byref(d), *[ptr[n] for n in names], None))
 
 
@@ -183,6 +182,21 @@ def test_dropout_refuses_pointers(lib):
     assert dropout(lib, drop(residual_stride=72), r=2 * FAKE) == BAD
     assert dropout(lib, drop(T=0), x=None, out=None) == "MOLT_OK"
     assert status(lib.molt_dropout(None, FAKE, None, None, FAKE, None)) == BAD
+
+
+def test_outputs_that_share_memory_are_refused(lib):
+    """... with another output, with the last byte of an input, or a strided input's."""
+    n = 4 * 64 * 2   # bytes of four rows
+    assert ffn_fwd(lib, ffn(), y=FAKE) == ffn_fwd(lib, ffn(), y=FAKE + n - 16) == ffn_fwd(lib, ffn(x_stride=128), y=FAKE + n) == BAD
+    assert ffn_fwd(lib, ffn(), y=FAKE + n) == ffn_fwd(lib, ffn(x_stride=128), y=FAKE + 2 * n - 128) == "MOLT_ERR_WORKSPACE"
+    assert ffn_fwd(lib, ffn(), gate_out=20 * FAKE, up_out=20 * FAKE + 1008) == BAD
+    assert ffn_bwd(lib, ffn(), dx=FAKE) == ffn_bwd(lib, ffn(), dw_up=20 * FAKE, dw_gate=20 * FAKE) == BAD
+    assert ffn_bwd(lib, ffn(), dw_up=20 * FAKE, dw_gate=20 * FAKE + 128 * 64 * 4) == "MOLT_ERR_WORKSPACE"
+    assert scan_fwd(lib, scan(), y=FAKE) == scan_fwd(lib, scan(), final=3 * FAKE) == scan_fwd(lib, scan(gate_stride=128), y=FAKE + 800) == BAD
+    assert scan_fwd(lib, scan(), final=3 * FAKE + 2 * 64 * 4) == "MOLT_ERR_WORKSPACE"
+    assert scan_bwd(lib, scan(), dgate=FAKE) == scan_bwd(lib, scan(), dinit=5 * FAKE) == BAD
+    assert scan_step(lib, scan(T=2), y=FAKE) == scan_step(lib, scan(T=2), out=3 * FAKE + 4) == scan_step(lib, scan(T=2), out=4 * FAKE) == BAD
+    assert dropout(lib, drop(), out=FAKE + 16) == dropout(lib, drop(), r=3 * FAKE, out=3 * FAKE - 16) == BAD
 
 
 def test_layouts_match_the_header(tmp_path):
