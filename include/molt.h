@@ -604,6 +604,8 @@ molt_status molt_gated_ffn_bwd(const molt_ffn_desc* desc, const void* dy, const 
  * Gated linear recurrence over packed sequences, channel by channel:
  *   MOLT_SCAN_SIGMOID  h_t = a_t h_{t-1} + (1 - a_t) value_t,  a_t = 1 / (1 + e^-gate_t)
  *   MOLT_SCAN_LOG      h_t = a_t h_{t-1} + value_t,            a_t = e^gate_t
+ * (Gates of the log form are not above 0 in use; above it the product of a sequence's a_t has to
+ * stay in fp32's range, as h must: rows are taken together by such products.)
  * gate, value, y [T,H] of one type (rows of gate and value may be strided, as the halves of one
  * projection are); states fp32.  Sequence b is rows cu_seqlens[b] .. cu_seqlens[b+1] - 1 (device
  * int32 [B+1], ascending, within [0, T]; sequences may be empty), or with cu_seqlens NULL the b-th

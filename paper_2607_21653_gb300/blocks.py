@@ -215,7 +215,8 @@ def gated_scan_fwd(gate, value, initial_state=None, cu_seqlens=None, kind="sigmo
     """Gated linear recurrence over sequences, channel by channel (molt_gated_scan_fwd):
         "sigmoid":  h_t = a_t h_{t-1} + (1 - a_t) value_t,  a_t = sigmoid(gate_t)
         "log":      h_t = a_t h_{t-1} + value_t,            a_t = exp(gate_t)
-    gate, value: packed rows [T, H] of the sequences cu_seqlens [B + 1] (int32, on the device;
+    (gates of the log form are at most 0, or the product of a sequence's a_t stays in float32's
+    range).  gate, value: packed rows [T, H] of the sequences cu_seqlens [B + 1] (int32, on the device;
     None: one sequence), or [B, L, H]; bfloat16, float16 or float32, rows may be strided.
     initial_state [B, H] float32 or None.  Returns dict(y = h, final_state [B, H] float32, states):
     with want_states=True what the backward reads, else None.  Rows of a given `out` outside of

@@ -10,28 +10,40 @@
 //
 // What a row does to h is an affine map (a, b), and maps compose, so rows can be taken
 // together: a tile is 128 rows (64 of the forward in fp32) by 64 channels, a warp has 16 (8)
-// rows of it, a lane two channels.  Every warp composes its rows' maps; the maps of a tile's warps, and of the tiles of a
-// cluster, are folded in order; and then every warp goes through its rows again from the
-// state that it now knows.  The backward's E is the same from the other end; h it forms
+// rows of it, a lane two channels.  Every warp composes its rows' maps; the maps of a tile's
+// warps, and of the tiles of a cluster, are folded in order; and then every warp goes through
+// its rows again from the state that it now knows.  The backward's E is the same from the other end; h it forms
 // again from the states that the forward kept at every 128th row.  A row that begins a
 // sequence cuts: what comes before is not multiplied by zero but left out, so that an
 // infinite or NaN state stays in its sequence.
 //
 // Everything is held as m = a - 1: with a as a float near 1 the memory 1 / (1 - a) of a
-// channel would be off by 2^-24 / (1 - a); h + m (h - v) and h + m h + v need no a at all.
+// channel would be off by 2^-24 / (1 - a); h + m (h - v) and h + m h + v need no a at all.  Of
+// a near 0 it is dgate, a multiple of a, that 1 + m would leave with few digits: there a is
+// formed from the gate again, in fp32 always, in 16 bits for eight rows of which one has an a
+// below 2^-7 (of others 2^-17 is lost, a fraction of the rounding to 16 bits).
 //
 // Layout: a strip of channels belongs to a cluster of up to eight blocks, which take a
 // tile each, exchange their maps through one another's shared memory (512 bytes to each
 // peer) and go on together, so that the inputs are read once and a super step of 1024 rows
 // costs one exchange.  Of two further warps one brings the tiles ahead (TMA, and from
-// cu_seqlens which rows begin and end a sequence), the other folds the maps.  Few strips and many rows are cut into segments besides: a first
-// launch folds each segment's map, the second starts from what precedes its own.
+// cu_seqlens which rows begin and end a sequence), the other folds the maps.  Few strips and
+// many rows are cut into segments besides: a first launch folds each segment's map, the second
+// starts from what precedes its own.  Rows that TMA cannot take (an odd number of bytes, any
+// address) are copied in the 16-byte words that hold them, in strips of 56 (fp32: 60) channels.
+//
+// Bound by memory and, close behind, by what the SM issues: bf16, 65536 x 4096 in four sequences
+// 310 us forward (238 for its bytes at 6.8 TB/s), 32768 x 2048 in one 137 us backward (99).  Also
+// tried: tiles of 64 rows with three blocks to an SM (482 us for the first), the same a step ahead
+// of the exchange (384), 128 rows a step ahead with m formed twice (362: the exponentials), one
+// block of 16 warps a step ahead (399; narrow ones gain, 32768 x 1024 72 us for 89, but not so much).
 #include <algorithm>
 #include <atomic>
 #include <cstdint>
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <initializer_list>
+#include <type_traits>
 
 #include "molt_internal.cuh"
 #include "ptx.cuh"
@@ -110,6 +122,19 @@ __device__ __forceinline__ F2 decay(F2 f) {
     p = mul2(p, f);
     const F2 x = mul2(f, f2(kLog2e));
     return f2(fabsf(f.x()) < 0.35f ? p.x() : ex2_approx(x.x()) - 1.f, fabsf(f.y()) < 0.35f ? p.y() : ex2_approx(x.y()) - 1.f);
+  }
+}
+// What D_t is multiplied by in dgate besides h_{t-1} - v_t or h_{t-1}: a (1 - a), or a; from the gate
+// where 1 + m loses digits.
+template <int kForm>
+__device__ __forceinline__ F2 gate_slope(F2 f, F2 m) {
+  const F2 x = mul2(f, f2(kLog2e));
+  const F2 e = f2(ex2_approx(x.x()), ex2_approx(x.y()));
+  if constexpr (kForm == kFormSigmoid) {
+    const F2 w = mul2(m, f2(-1.f)), near0 = mul2(mul2(e, w), w), near1 = fma2(m, w, w);
+    return f2(f.x() < 0.f ? near0.x() : near1.x(), f.y() < 0.f ? near0.y() : near1.y());
+  } else {
+    return f2(f.x() < -0.5f ? e.x() : 1.f + m.x(), f.y() < -0.5f ? e.y() : 1.f + m.y());
   }
 }
 // h_t from h_{t-1}
@@ -274,8 +299,9 @@ __device__ __forceinline__ void check_bounds(const ScanArgs& a, int block, int b
   if (bad) atomicOr(a.err, kDevErrUnsortedGroups);
 }
 
-// An affine map of two channels' states, h -> A h + b, with a cut in A's sign (A of a map
-// that has none is not negative).
+// An affine map of two channels' states, h -> A h + b, with a cut in the signs of both A.  (A
+// reciprocal's last bit may leave a channel's A below 0 by 2^-23 of what it was, where it should
+// be 0: a cut of that channel is then as good, and is none of the other's.)
 struct Map {
   F2 A, b;
 };
@@ -289,7 +315,7 @@ __device__ __forceinline__ F2 apply(const float4& m, F2 h) {
 // first m, then n
 __device__ __forceinline__ float4 compose(const float4& m, const float4& n) {
   const F2 b = apply(n, f2(m.z, m.w));
-  const bool cut = n.x < 0.f || m.x < 0.f || n.y < 0.f || m.y < 0.f;   // in both channels at once
+  const bool cut = (n.x < 0.f && n.y < 0.f) || (m.x < 0.f && m.y < 0.f);
   return make_float4(cut ? -1.f : m.x * n.x, cut ? -1.f : m.y * n.y, b.x(), b.y());
 }
 
@@ -725,7 +751,7 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
       if constexpr (!kGrads) ex.warps[warp][lane] = mine;
       if constexpr (kGrads) {
         // the maps of E and of h have one A but for their cuts, which go in its signs
-        const bool cut = mine.x < 0.f, cut_h = mine_h.x < 0.f;
+        const bool cut = mine.x < 0.f && mine.y < 0.f, cut_h = mine_h.x < 0.f && mine_h.y < 0.f;
         const float2 A = cut ? make_float2(mine_h.x, mine_h.y) : make_float2(mine.x, mine.y);   // (of no use if both are cut)
         ex.warps[warp][lane] = make_float4(copysignf(A.x, cut ? -1.f : 1.f), copysignf(A.y, cut_h ? -1.f : 1.f), mine.z, mine.w);
         h_maps[warp][lane] = make_float2(mine_h.z, mine_h.w);
@@ -792,15 +818,14 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
         const float2 before = h_maps[warp][lane];
         const F2 h_in = f2(before.x, before.y);
         // dgate and dvalue of a row from D and E and h of the row before
-        auto grads = [&](int i, F2 D, F2 E, F2 hp, F2& df, F2& dval) {
-          if constexpr (kForm == kFormSigmoid) {
-            const F2 w = mul2(kept[0][i], f2(-1.f));
-            df = mul2(mul2(E, w), sub2(hp, v[i].f()));
-            dval = mul2(D, w);
-          } else {
-            df = mul2(E, hp);
-            dval = D;
-          }
+        auto grads = [&](int q, int i, auto small, F2 D, F2 E, F2 hp, F2& df, F2& dval) {
+          const F2 w = mul2(kept[0][i], f2(-1.f));
+          const F2 x = kForm == kFormSigmoid ? sub2(hp, v[i].f()) : hp;
+          dval = kForm == kFormSigmoid ? mul2(D, w) : D;
+          if constexpr (decltype(small)::value)
+            df = mul2(mul2(D, gate_slope<kForm>(get(0, q * kHalf + i).f(), kept[0][i])), x);
+          else
+            df = mul2(kForm == kFormSigmoid ? mul2(E, w) : E, x);
         };
 #pragma unroll 1
         for (int q = kParts - 1; q >= 0; --q) {
@@ -811,7 +836,15 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
           }
           const F2(&m)[kHalf] = kept[0];
           F2 h = q > 0 ? apply(first_h, h_in) : h_in, hp[kHalf], df, dval;   // hp: h of the row before
-          if (is == kAll && (s | e) == 0) {
+          // (the branch for bounds forms a from the gates again)
+          bool small = false;
+          if constexpr (sizeof(T) == 2) {
+            float least = 0.f;
+#pragma unroll
+            for (int i = 0; i < kHalf; ++i) least = fminf(least, fminf(m[i].x(), m[i].y()));
+            small = __any_sync(0xffffffffu, least < 0.0078125f - 1.f);
+          }
+          if (is == kAll && (s | e) == 0 && !small) {
 #pragma unroll
             for (int i = 0; i < kHalf; ++i) {
               hp[i] = h;
@@ -821,7 +854,7 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
             for (int i = kHalf - 1; i >= 0; --i) {
               const F2 D = add2(d[i].f(), in);
               in = fma2(m[i], D, D);   // E
-              grads(i, D, in, hp[i], df, dval);
+              grads(q, i, std::bool_constant<sizeof(T) == 4>{}, D, in, hp[i], df, dval);
               out_row(dg, 0, q * kHalf + i, df);
               out_row(dv, kD, q * kHalf + i, dval);
             }
@@ -838,7 +871,7 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
             for (int i = kHalf - 1; i >= 0; --i) {
               const F2 D = add2(d[i].f(), pick(e, i, from[i], in));
               in = fma2(m[i], D, D);
-              grads(i, D, in, hp[i], df, dval);
+              grads(q, i, std::true_type{}, D, in, hp[i], df, dval);
               from[i] = in;
               if (!(is >> i & 1u)) df = dval = zero2();
               if (row + q * kHalf + i < a.T) {

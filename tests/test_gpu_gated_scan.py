@@ -230,6 +230,25 @@ def test_log_gates_of_any_sign():
         check(out[k], fin(ref[k]), torch.float32, k)
 
 
+@pytest.mark.parametrize("kind", ["sigmoid", "log"])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_channels_without_memory_beside_long_ones(dtype, kind):
+    """Gates at which a is next to 0, in every other channel; their neighbours remember many rows.
+    dgate in 16 bits: an a above 2^-7 may be off by 2^-24 twice over, 2^-16 of it."""
+    T, H = 1000, 64
+    s = make(T, H, 1, torch.float32, kind, 5)
+    g = torch.Generator(device=dev()).manual_seed(6)
+    s["gate"][:, ::2] = -3 - 30 * torch.rand(T, H // 2, device=dev(), generator=g)
+    s["gate"][:, 1::2] = 9 + torch.rand(T, H // 2, device=dev(), generator=g) if kind == "sigmoid" else -1e-3
+    for k in ("gate", "value", "dy"):
+        s[k] = s[k].to(dtype)
+    ref, out = reference(s, [0, T], kind), run(s, [0, T], kind)
+    for k in ("y", "dvalue", "final_state", "dinitial_state"):
+        check(out[k], ref[k], out[k].dtype, k)
+    r, e = ref["dgate"]
+    check(out["dgate"], (r, e + (r.abs() * 2.0 ** -16 if dtype != torch.float32 else 0)), dtype, "dgate")
+
+
 @pytest.mark.parametrize("H,extra", [(64, 64), (65, 3), (128, 1), (320, 320)])
 def test_strided_and_odd_rows(H, extra):
     """The halves of one projection, and rows that begin anywhere."""
