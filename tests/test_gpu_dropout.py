@@ -162,6 +162,18 @@ def test_strides_alignment_and_in_place():
         molt.dropout_fwd(base, 0.2, torch.zeros(2, dtype=torch.int32, device=dev()))
 
 
+@pytest.mark.parametrize("H", [5, 8])
+def test_rows_far_apart(H):
+    """160 rows, 2^25 elements from one to the next: offsets past 32 bits within a tile."""
+    T, ld = 160, 1 << 25
+    x = torch.empty(T * ld, dtype=BF, device=dev()).as_strided((T, H), (ld, 1))
+    x.copy_(torch.arange(1, T * H + 1, device=dev()).view(T, H))
+    for r in (None, x):
+        got = molt.dropout_fwd(x, 0.3, 11, residual=r)
+        assert torch.equal(got, molt.dropout_fwd(x.contiguous(), 0.3, 11, residual=None if r is None else r.contiguous()))
+    assert float(got.float().abs().sum()) > 0
+
+
 def test_no_rows():
     assert molt.dropout_fwd(torch.empty(0, 64, device=dev()), 0.1, 1).shape == (0, 64)
 
