@@ -779,14 +779,7 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
       auto to_box = [&](int tensor, int i, F2 x) {
         store2<true>(reinterpret_cast<T*>(stage + tensor * kTensorBytes + i * kRowBytes) + 2 * lane, x, 2);
       };
-      auto out_row = [&](T* base, int tensor, int i, F2 x) {
-        if (boxed)
-          to_box(tensor, i, x);
-        else
-          store_out(base + (row + i) * a.H + c0, x);
-      };
-      // the same in a half whose rows are all in sequences: no branch at every row (65536 x 4096 forward 310 us
-      // for 359)
+      // a half whose rows are all in sequences: no branch at every row (65536 x 4096 forward 310 us for 359)
       auto out_whole = [&](T* base, int tensor, int i, F2 x) {
         if constexpr (kFast)
           to_box(tensor, i, x);
@@ -810,12 +803,17 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
             start_half(a.h0, s, q, h);
 #pragma unroll
             for (int i = 0; i < kHalf; ++i) h[i] = in = step<kForm>(pick(s, i, h[i], in), kept[q][i], v[i].f());
+            if (boxed) {
 #pragma unroll
-            for (int i = 0; i < kHalf; ++i)
-              if (is >> i & 1u)
-                out_row(y, 0, q * kHalf + i, h[i]);
-              else if (a.fill && row + q * kHalf + i < a.T)
-                out_row(y, 0, q * kHalf + i, zero2());
+              for (int i = 0; i < kHalf; ++i) to_box(0, q * kHalf + i, h[i]);
+            } else {
+#pragma unroll
+              for (int i = 0; i < kHalf; ++i)
+                if (is >> i & 1u)
+                  store_out(y + (row + q * kHalf + i) * a.H + c0, h[i]);
+                else if (a.fill && row + q * kHalf + i < a.T)
+                  store_out(y + (row + q * kHalf + i) * a.H + c0, zero2());
+            }
             if (e != 0 && a.final_state) {
 #pragma unroll
               for (int i = 0; i < kHalf; ++i)
@@ -878,18 +876,27 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
               h = step<kForm>(h, m[i], v[i].f());
             }
             start_half(a.dfinal, e, q, from);
+            auto walk = [&](auto box) {
 #pragma unroll
-            for (int i = kHalf - 1; i >= 0; --i) {
-              const F2 D = add2(d[i].f(), pick(e, i, from[i], in));
-              in = fma2(m[i], D, D);
-              grads(q, i, std::true_type{}, D, in, hp[i], df, dval);
-              from[i] = in;
-              if (!(is >> i & 1u)) df = dval = zero2();
-              if (row + q * kHalf + i < a.T) {
-                out_row(dg, 0, q * kHalf + i, df);
-                out_row(dv, kD, q * kHalf + i, dval);
+              for (int i = kHalf - 1; i >= 0; --i) {
+                const F2 D = add2(d[i].f(), pick(e, i, from[i], in));
+                in = fma2(m[i], D, D);
+                grads(q, i, std::true_type{}, D, in, hp[i], df, dval);
+                from[i] = in;
+                if constexpr (decltype(box)::value) {
+                  to_box(0, q * kHalf + i, df);
+                  to_box(kD, q * kHalf + i, dval);
+                } else if (row + q * kHalf + i < a.T) {
+                  const bool in_one = is >> i & 1u;
+                  store_out(dg + (row + q * kHalf + i) * a.H + c0, in_one ? df : zero2());
+                  store_out(dv + (row + q * kHalf + i) * a.H + c0, in_one ? dval : zero2());
+                }
               }
-            }
+            };
+            if (kFast && boxed)
+              walk(std::true_type{});
+            else
+              walk(std::false_type{});
             if (s != 0 && a.dinit) {
 #pragma unroll
               for (int i = 0; i < kHalf; ++i)
