@@ -32,8 +32,9 @@
 // starts from what precedes its own.  Rows that TMA cannot take (an odd number of bytes, any
 // address) are copied in the 16-byte words that hold them, in strips of 56 (fp32: 60) channels.
 //
-// Bound by memory and, close behind, by what the SM issues: bf16, 65536 x 4096 in four sequences
-// 310 us forward (238 for its bytes at 6.8 TB/s), 32768 x 2048 in one 137 us backward (99).  Also
+// Bound by a step's chain (maps, exchange, results), with memory and what the SM issues close
+// behind: bf16, 65536 x 4096 in four sequences 315 us forward (238 for its bytes at 6.8 TB/s),
+// 32768 x 2048 in one 141 us backward (99).  Also
 // tried: tiles of 64 rows with three blocks to an SM (482 us for the first), the same a step ahead
 // of the exchange (384), 128 rows a step ahead with m formed twice (362: the exponentials), one
 // block of 16 warps a step ahead (399; narrow ones gain, 32768 x 1024 72 us for 89, but not so much).
@@ -204,11 +205,20 @@ struct TileRows {
   int lo, hi;
 };
 
+// The states of sequence b in the strip of channels from c0 on, which will be wanted soon (32768 x 2048
+// in 1024 sequences with initial states 183 -> 168 us).
+__device__ __forceinline__ void fetch_states(const float* p, const ScanArgs& a, int64_t b, int c0) {
+  if (p == nullptr) return;
+  p += b * a.H + c0;
+  asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
+  if (c0 + 63 < a.H) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + 32));
+}
+
 // Fills `t` for the rows from row0 on; by one warp.  Returns the first bound that is not below
 // row0; `at` is what it returned for the tile before in the walk (at first 0, backwards
 // B + 1).
 template <int kN, bool kBwd>
-__device__ __forceinline__ int64_t mark_rows(const ScanArgs& a, int64_t row0, TileRows<kN>& t, int64_t at, int lane) {
+__device__ __forceinline__ int64_t mark_rows(const ScanArgs& a, int64_t row0, TileRows<kN>& t, int64_t at, int c0, int lane) {
   const int n = static_cast<int>(a.T - row0 < kN ? a.T - row0 : kN);
   if (lane < kN / 32) t.starts[lane] = t.ends[lane] = 0u;
   __syncwarp();
@@ -223,11 +233,13 @@ __device__ __forceinline__ int64_t mark_rows(const ScanArgs& a, int64_t row0, Ti
       if (v >= 0) {
         t.seq[v] = static_cast<int>(b);
         atomicOr(&t.starts[v >> 5], 1u << (v & 31));
+        fetch_states(a.h0, a, b, c0);
       }
       const int64_t e = v + a.L - 1;
       if (e < n) {
         t.seq[e] = static_cast<int>(b);
         atomicOr(&t.ends[e >> 5], 1u << (e & 31));
+        if (kBwd) fetch_states(a.dfinal, a, b, c0);
       }
     }
     __syncwarp();
@@ -270,10 +282,12 @@ __device__ __forceinline__ int64_t mark_rows(const ScanArgs& a, int64_t row0, Ti
     if (in && v < n && b < a.B && a.cu[b + 1] - row0 > v) {
       t.seq[v] = static_cast<int>(b);
       atomicOr(&t.starts[v >> 5], 1u << (v & 31));
+      fetch_states(a.h0, a, b, c0);
     }
     if (in && v > 0 && b > 0 && a.cu[b - 1] - row0 < v) {
       t.seq[v - 1] = static_cast<int>(b - 1);
       atomicOr(&t.ends[(v - 1) >> 5], 1u << ((v - 1) & 31));
+      if (kBwd) fetch_states(a.dfinal, a, b - 1, c0);
     }
     if (!__all_sync(0xffffffffu, in)) break;
   }
@@ -351,7 +365,8 @@ __device__ __forceinline__ void cp_async_wait() {
 }
 
 // kRows rows' channels, n of them from `row` on, to shared memory in the 16-byte words that hold them,
-// several rows at a time.  (Words of four bytes took four times as long: 20000 x 1031 forward 150 us.)
+// several rows at a time.  (20000 x 1031 forward 124 us; in words of four bytes, as many copies again
+// three times, 150.)
 template <class T, int kRows>
 __device__ __forceinline__ void copy_rows(uint32_t dst, const T* row, int64_t ld, int n, int lane) {
   constexpr int kWords = kPitch<T> / 16, kAtOnce = 32 / kWords;
@@ -457,7 +472,7 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
         if constexpr (kBwd) tma_load_2d(dst + kD * kTensorBytes, &maps.dy, bar, c0, tile * kN);
       }
       ++issued;
-      at = mark_rows<kN, kBwd>(a, int64_t(tile) * kN, rows_sh[st], at, lane);
+      at = mark_rows<kN, kBwd>(a, int64_t(tile) * kN, rows_sh[st], at, c0, lane);
       if (lane == 0) mbar_arrive(smem_u32(&full_bar[st]));
     }
     // copies land in this block's memory: wait for the last ones before it may exit
