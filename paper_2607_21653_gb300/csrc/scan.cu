@@ -157,6 +157,21 @@ __device__ __forceinline__ F2 load2(const T* p, int left) {
   }
   return f2(v[0], v[1]);
 }
+// The same of fp32 if `on`, else zeros, by predicate: several loads go out together.
+template <bool kPair>
+__device__ __forceinline__ F2 load2_if(bool on, const float* p, int left) {
+  float x = 0.f, y = 0.f;
+  if constexpr (kPair) {
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %3, 0;\n\t@q ld.global.v2.f32 {%0, %1}, [%2];\n}"
+                 : "+f"(x), "+f"(y)
+                 : "l"(p), "r"(int(on && left > 1)));
+  } else {
+    asm volatile("{\n\t.reg .pred q, r;\n\tsetp.ne.b32 q, %3, 0;\n\tsetp.ne.b32 r, %4, 0;\n\t@q ld.global.f32 %0, [%2];\n\t@r ld.global.f32 %1, [%2+4];\n}"
+                 : "+f"(x), "+f"(y)
+                 : "l"(p), "r"(int(on && left > 0)), "r"(int(on && left > 1)));
+  }
+  return f2(x, y);
+}
 template <bool kPair, class T>
 __device__ __forceinline__ void store2(T* p, F2 x, int left) {
   if constexpr (kPair) {
@@ -206,7 +221,7 @@ struct TileRows {
 };
 
 // The states of sequence b in the strip of channels from c0 on, which will be wanted soon (32768 x 2048
-// in 1024 sequences with initial states 183 -> 168 us).
+// in 1024 sequences with initial states 183 -> 168 us; 136 with the loads by predicate).
 __device__ __forceinline__ void fetch_states(const float* p, const ScanArgs& a, int64_t b, int c0) {
   if (p == nullptr) return;
   p += b * a.H + c0;
@@ -701,12 +716,16 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
       };
       // what the rows of these bits start from
       auto start_half = [&](const float* p, uint32_t bits, int q, F2 (&x)[kHalf]) {
+        if (p == nullptr || bits == 0) {
 #pragma unroll
-        for (int i = 0; i < kHalf; ++i) x[i] = zero2();
-        if (p == nullptr || bits == 0) return;
+          for (int i = 0; i < kHalf; ++i) x[i] = zero2();
+          return;
+        }
+        int seq[kHalf];   // (of rows without a bit: whatever stands there, and not read by)
 #pragma unroll
-        for (int i = 0; i < kHalf; ++i)
-          if (bits >> i & 1u) x[i] = load2<kFast>(p + int64_t(rows.seq[r0 + q * kHalf + i]) * a.H + c, left);
+        for (int i = 0; i < kHalf; ++i) seq[i] = rows.seq[r0 + q * kHalf + i];
+#pragma unroll
+        for (int i = 0; i < kHalf; ++i) x[i] = load2_if<kFast>(bits >> i & 1u, p + (int64_t(seq[i]) * a.H + c), left);
       };
       auto pick = [](uint32_t bits, int i, F2 x, F2 y) -> F2 { return F2{bits >> i & 1u ? x.v : y.v}; };
       // the half's map of h (A, x), and in a backward walk of E (A, x) and of h (A, z)
