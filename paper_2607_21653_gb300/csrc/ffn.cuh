@@ -66,8 +66,8 @@ struct FfnReduce {
 
 // A product for a few rows: out[t, n] = x[t, k] w[n, k]^T; the first one of the block has w0 =
 // Wg and w1 = Wu and gives h (out[0]) and, unless nullptr, g and u.  Up to 16 rows: the whole block at
-// H = 4096, F = 10944 takes 45 us of one row, 47 of 8 and 60 of 16, where the tiles' kernel has 77 at
-// 17 and 32 (from 16 on the rows' loads fill the registers that the weights' should have).
+// H = 4096, F = 10944 takes 45 us of one row, 47 of 8 and 60 of 16, where the tiles' kernel has 68 of
+// 32 (from 16 on the rows' loads fill the registers that the weights' should have).
 constexpr int kFfnFewRows = 16;
 struct FfnRows {
   const void *x, *w0, *w1;
