@@ -268,6 +268,31 @@ def test_two_streams_at_once():
             assert torch.equal(a[k], b[k])
 
 
+def test_calls_one_after_another_without_a_wait():
+    """Launches begin while the ones before them end: calls of many sizes on one workspace, each
+    input the output of the call before, have the bits that they have one by one."""
+    H, F, sizes = 256, 704, (1, 16, 17, 300, 5, 1031, 2, 600, 1)
+    s = inputs(1031, H, F, BF, 3)
+    w = (s["w_gate"], s["w_up"], s["w_down"])
+
+    def calls(wait):
+        x, out = s["x"], []
+        for T in sizes * 4:
+            f = molt.gated_ffn_fwd(x[:T], *w, keep=True)
+            g = molt.gated_ffn_bwd(x[:T], f["y"], *w, *((f["gate"], f["up"]) if T % 2 else ()))
+            x = x.clone()
+            x[:T] = 0.5 * f["y"] + g["dx"] / (1 + g["dx"].abs().max())
+            out += [f["y"], f["gate"], g["dx"], g["dw_gate"], g["dw_down"]]
+            if wait:
+                torch.cuda.synchronize()
+        return out
+
+    want = calls(True)
+    for _ in range(3):
+        for a, b in zip(want, calls(False)):
+            assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("T", [1, 40, 600])
 def test_in_two_captured_graphs(T):
     """Replayed in turn on new inputs, with the bits of the calls outside of them."""
