@@ -884,7 +884,11 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
           if constexpr (sizeof(T) == 2) {
             float least = 0.f;
 #pragma unroll
-            for (int i = 0; i < kHalf; ++i) least = fminf(least, fminf(m[i].x(), m[i].y()));
+            for (int i = 0; i < kHalf; ++i) {
+              // (a channel that there is not may be what an earlier kernel has left in shared memory)
+              if (kFast || left > 0) least = fminf(least, m[i].x());
+              if (kFast || left > 1) least = fminf(least, m[i].y());
+            }
             small = __any_sync(0xffffffffu, least < 0.0078125f - 1.f);
           }
           if ((kFast ? boxed : is == kAll) && (s | e) == 0 && !small) {
