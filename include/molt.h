@@ -613,7 +613,10 @@ molt_status molt_gated_ffn_bwd(const molt_ffn_desc* desc, const void* dy, const 
  * sequence are left as they were, or with fill_outside 0; their gradients are 0.  cu_seqlens that
  * descend or leave [0, T] set MOLT_DEV_UNSORTED_GROUPS; what is then written is unspecified, but
  * lies inside the outputs.  Nothing of a sequence, not even an infinity or a NaN, reaches
- * another.  Outputs overlap neither one another nor the inputs.
+ * another; behind an infinite state its own sequence is infinite or NaN.  A row's a and 1 - a are
+ * right to |gate| 2^-23 + 2^-21 of themselves (of 16-bit inputs a above 2^-7 to 2^-22 of 1), so that what
+ * a gate far below 0 leaves of a large state or gradient keeps its digits.  Outputs overlap neither one
+ * another nor the inputs.
  */
 #define MOLT_SCAN_SIGMOID 0
 #define MOLT_SCAN_LOG 1

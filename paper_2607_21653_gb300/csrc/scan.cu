@@ -17,11 +17,12 @@
 // sequence cuts: what comes before is not multiplied by zero but left out, so that an
 // infinite or NaN state stays in its sequence.
 //
-// Everything is held as m = a - 1: with a as a float near 1 the memory 1 / (1 - a) of a
-// channel would be off by 2^-24 / (1 - a); h + m (h - v) and h + m h + v need no a at all.  Of
-// a near 0 it is dgate, a multiple of a, that 1 + m would leave with few digits: there a is
-// formed from the gate again, in fp32 always, in 16 bits for eight rows of which one has an a
-// below 2^-7 (of others 2^-17 is lost, a fraction of the rounding to 16 bits).
+// A row is held as m = a - 1: with a as a float near 1 the memory 1 / (1 - a) of a
+// channel would be off by 2^-24 / (1 - a); h + m (h - v) and h + m h + v need no a at all.  But of
+// a near 0, which 1 + m has to 2^-24 of 1, h_t, E_t and dgate are multiples: such a row is held as a
+// itself, h_t = v + a (h - v) and a h + v, with a bit that says so: in fp32 where a is below 1/2 (log: 0.7), in
+// 16 bits where it is below 2^-7.  Above that 1 + m is off by 2^-15 of a at most, a sixteenth of an fp16
+// result's rounding, and a warp's rows of which none is below take no selects.
 //
 // Layout: a strip of channels belongs to a cluster of up to eight blocks, which take a
 // tile each, exchange their maps through one another's shared memory (512 bytes to each
@@ -33,8 +34,8 @@
 // address) are copied in the 16-byte words that hold them, in strips of 56 (fp32: 60) channels.
 //
 // Bound by a step's chain (maps, exchange, results), with memory and what the SM issues close
-// behind: bf16, 65536 x 4096 in four sequences 315 us forward (238 for its bytes at 6.8 TB/s),
-// 32768 x 2048 in one 141 us backward (99).  Also
+// behind: bf16, 65536 x 4096 in four sequences 305 us forward (238 for its bytes at 6.8 TB/s),
+// 32768 x 2048 in one 147 us backward (99).  Also
 // tried: tiles of 64 rows with three blocks to an SM (482 us for the first), the same a step ahead
 // of the exchange (384), 128 rows a step ahead with m formed twice (362: the exponentials), one
 // block of 16 warps a step ahead (399; narrow ones gain, 32768 x 1024 72 us for 89, but not so much).
@@ -71,6 +72,9 @@ constexpr int kStrip = kFast ? 64 : sizeof(T) == 2 ? 56 : 60;
 constexpr int kMaxCluster = 8;
 constexpr int kFormSigmoid = 0, kFormLog = 1;
 constexpr float kLog2e = 1.4426950408889634f;
+// Gates below it are held as a and not as a - 1.
+template <class T, int kForm>
+constexpr float kLowGate = sizeof(T) == 2 ? -4.875f : kForm == kFormSigmoid ? 0.f : -0.35f;
 
 struct ScanArgs {
   const void *gate, *value, *dy;
@@ -104,15 +108,18 @@ __device__ __forceinline__ float rcp_approx(float x) {
 __device__ __forceinline__ F2 zero2() { return f2(0.f, 0.f); }
 __device__ __forceinline__ F2 sub2(F2 a, F2 b) { return fma2(b, f2(-1.f), a); }
 
-// m = a - 1 of two gates.  sigmoid: -1 / (1 + e^f), no digits lost on either side.  log: e^f - 1,
+// m = a - 1 of two gates, and a.  sigmoid: -1 / (1 + e^f), no digits lost on either side.  log: e^f - 1,
 // by its series where the difference would lose digits (the first term left out is
 // 0.35^7 / 8! of the first, 1.6e-8)
 template <int kForm>
-__device__ __forceinline__ F2 decay(F2 f) {
+__device__ __forceinline__ F2 decay(F2 f, F2& a) {
+  const F2 x = mul2(f, f2(kLog2e)), e = f2(ex2_approx(x.x()), ex2_approx(x.y()));
   if constexpr (kForm == kFormSigmoid) {
-    const F2 x = mul2(f, f2(kLog2e));
-    return f2(rcp_approx(-1.f - ex2_approx(x.x())), rcp_approx(-1.f - ex2_approx(x.y())));
+    const F2 m = f2(rcp_approx(-1.f - e.x()), rcp_approx(-1.f - e.y()));
+    a = mul2(e, mul2(m, f2(-1.f)));
+    return m;
   } else {
+    a = e;
     F2 p = f2(1.f / 5040.f);
     p = fma2(p, f, f2(1.f / 720.f));
     p = fma2(p, f, f2(1.f / 120.f));
@@ -121,28 +128,31 @@ __device__ __forceinline__ F2 decay(F2 f) {
     p = fma2(p, f, f2(0.5f));
     p = fma2(p, f, f2(1.f));
     p = mul2(p, f);
-    const F2 x = mul2(f, f2(kLog2e));
-    return f2(fabsf(f.x()) < 0.35f ? p.x() : ex2_approx(x.x()) - 1.f, fabsf(f.y()) < 0.35f ? p.y() : ex2_approx(x.y()) - 1.f);
+    return f2(fabsf(f.x()) < 0.35f ? p.x() : e.x() - 1.f, fabsf(f.y()) < 0.35f ? p.y() : e.y() - 1.f);
   }
 }
-// What D_t is multiplied by in dgate besides h_{t-1} - v_t or h_{t-1}: a (1 - a), or a; from the gate
-// where 1 + m loses digits.
-template <int kForm>
-__device__ __forceinline__ F2 gate_slope(F2 f, F2 m) {
-  const F2 x = mul2(f, f2(kLog2e));
-  const F2 e = f2(ex2_approx(x.x()), ex2_approx(x.y()));
-  if constexpr (kForm == kFormSigmoid) {
-    const F2 w = mul2(m, f2(-1.f)), near0 = mul2(mul2(e, w), w), near1 = fma2(m, w, w);
-    return f2(f.x() < 0.f ? near0.x() : near1.x(), f.y() < 0.f ? near0.y() : near1.y());
-  } else {
-    return f2(f.x() < -0.5f ? e.x() : 1.f + m.x(), f.y() < -0.5f ? e.y() : 1.f + m.y());
-  }
+// Channels with a bit (of two) have x, the others y.
+__device__ __forceinline__ F2 pick2(uint32_t bits, F2 x, F2 y) {
+  return f2(bits & 1u ? x.x() : y.x(), bits & 2u ? x.y() : y.y());
 }
-// h_t from h_{t-1}
+// m of two gates, but a itself of those that are below `from`, which have their bit in `low`
 template <int kForm>
-__device__ __forceinline__ F2 step(F2 h, F2 m, F2 v) {
-  if constexpr (kForm == kFormSigmoid) return fma2(m, sub2(h, v), h);
-  return add2(fma2(m, h, h), v);
+__device__ __forceinline__ F2 coefficient(F2 f, float from, uint32_t& low) {
+  F2 a;
+  const F2 m = decay<kForm>(f, a);
+  low = (f.x() < from ? 1u : 0u) | (f.y() < from ? 2u : 0u);
+  return pick2(low, a, m);
+}
+// c A, c = m (bit 0 of a channel) or a (bit 1): a A
+template <bool kSelect>
+__device__ __forceinline__ F2 decayed(F2 A, F2 c, uint32_t low) {
+  return fma2(c, A, kSelect ? pick2(low, zero2(), A) : A);
+}
+// h_t from h_{t-1}: h + m (h - v) = v + a (h - v);  (h + m h) + v = a h + v
+template <int kForm, bool kSelect>
+__device__ __forceinline__ F2 step(F2 h, F2 c, F2 v, uint32_t low) {
+  if constexpr (kForm == kFormSigmoid) return fma2(c, sub2(h, v), kSelect ? pick2(low, v, h) : h);
+  return add2(decayed<kSelect>(h, c, low), v);
 }
 
 // two neighbouring channels of a row, of which `left` exist; kPair: both or none, aligned
@@ -328,9 +338,8 @@ __device__ __forceinline__ void check_bounds(const ScanArgs& a, int block, int b
   if (bad) atomicOr(a.err, kDevErrUnsortedGroups);
 }
 
-// An affine map of two channels' states, h -> A h + b, with a cut in the signs of both A.  (A
-// reciprocal's last bit may leave a channel's A below 0 by 2^-23 of what it was, where it should
-// be 0: a cut of that channel is then as good, and is none of the other's.)
+// An affine map of two channels' states, h -> A h + b, with a cut in the signs of both A (which are
+// otherwise not below 0).
 struct Map {
   F2 A, b;
 };
@@ -422,6 +431,11 @@ struct Raw<float> {
   __device__ __forceinline__ F2 f() const { return w; }
 };
 
+// Bits of kLowGate in 16 bits.  Two numbers of one sign compare as their bits do, and one below 0 has more
+// than any above: a maximum finds the gates furthest below 0.
+template <class T>
+constexpr uint32_t kLowBits = std::is_same<T, __half>::value ? 0xc4e0u : 0xc09cu;
+
 template <class T, bool kBwd>
 constexpr int kBlocksPerSM = kBwd && sizeof(T) == 4 ? 1 : 2;
 
@@ -435,6 +449,7 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
   constexpr int kTensors = kGrads ? 3 : 2, kV = 1, kD = kValue ? 2 : 1;
   constexpr int kStages = kStagesOf<kBwd, kMapOnly>, kN = kTile<T, kBwd>, kParts = kHalves<T, kBwd>, kRows = kParts * kHalf;
   constexpr uint32_t kAll = (1u << kHalf) - 1u;
+  constexpr bool kSelect = sizeof(T) == 4;   // rows held as a are as common as others
   constexpr int kRowBytes = kPitch<T>, kS = kStrip<T, kFast>;
   constexpr int kTensorBytes = kN * kRowBytes, kStageBytes = kTensors * kTensorBytes;
   extern __shared__ __align__(128) uint8_t smem_raw[];
@@ -633,6 +648,9 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
     // backward that of the last.
     constexpr int kKept = kBwd ? 1 : kParts;
     F2 kept[kKept][kHalf];
+    uint32_t low[kKept];   // two bits to a row: channels held as a
+    uint32_t most = 0;     // of a warp's rows: see load_gates
+    bool some = false;     // any held as a among the warp's channels (fp32: not asked)
     Raw<T> v[kHalf], d[kHalf];
     for (int k = 0; k < n_steps; ++k) {
       const int st = k % kStages;
@@ -669,49 +687,78 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
                    static_cast<uint32_t>(c0) * static_cast<uint32_t>(sizeof(T));
         }
       }
-      auto get = [&](int tensor, int i) -> Raw<T> {
+      // `anew`: from memory whatever has been read before, so that nothing is kept in registers for it
+      auto read = [&](int tensor, int i, auto anew) -> Raw<T> {
+        using Word = std::conditional_t<decltype(anew)::value, const volatile uint32_t, const uint32_t>;
         const uint8_t* const p = stage + tensor * kTensorBytes + i * kRowBytes;
         Raw<T> r;
         if constexpr (kFast) {
           if constexpr (sizeof(T) == 4)
             r.w.v = *reinterpret_cast<const unsigned long long*>(p + 8 * lane);
           else
-            r.w = *reinterpret_cast<const uint32_t*>(p + 4 * lane);
+            r.w = *reinterpret_cast<Word*>(p + 4 * lane);
         } else {
           const uint32_t o = (off[tensor] + i * off_step[tensor]) & 15u;
           if constexpr (sizeof(T) == 4) {
             const float* const q = reinterpret_cast<const float*>(p + o) + 2 * lane;
             r.w = f2(q[0], q[1]);
           } else {
-            const uint32_t* const q = reinterpret_cast<const uint32_t*>(p + (o & 12u)) + lane;
+            Word* const q = reinterpret_cast<Word*>(p + (o & 12u)) + lane;
             r.w = __byte_perm(q[0], q[1], o & 2u ? 0x5432 : 0x3210);
           }
         }
         return r;
       };
+      auto get = [&](int tensor, int i) -> Raw<T> { return read(tensor, i, std::false_type{}); };
 
-      auto load_gates = [&](F2 (&m)[kHalf], int q) {
-#pragma unroll
-        for (int i = 0; i < kHalf; ++i) m[i] = decay<kForm>(get(0, q * kHalf + i).f());
-        const uint32_t in = valid >> (q * kHalf) & kAll;
-        if (in != kAll) {
-          // rows outside of every sequence change nothing (no h behind the last one is used)
-#pragma unroll
-          for (int i = 0; i < kHalf; ++i)
-            if (!(in >> i & 1u)) m[i] = zero2();
-        }
-      };
-      auto load_values = [&](int q) {
+      constexpr std::true_type kYes{};
+      constexpr std::false_type kNo{};
+      // a half's bits of `starts` and so on; plain: all of its rows are in one sequence and go on after it
+      auto half_of = [&](uint32_t rows_bits, int q) -> uint32_t { return rows_bits >> (q * kHalf) & kAll; };
+      auto plain = [&](int q) -> bool { return half_of(valid, q) == kAll && (half_of(starts, q) | half_of(ends, q)) == 0; };
+      auto load_values = [&](int q, auto anew) {
 #pragma unroll
         for (int i = 0; i < kHalf; ++i) {
-          if constexpr (kValue) v[i] = get(kV, q * kHalf + i);
-          if constexpr (kBwd) d[i] = get(kD, q * kHalf + i);
+          if constexpr (kValue) v[i] = read(kV, q * kHalf + i, anew);
+          if constexpr (kBwd) d[i] = read(kD, q * kHalf + i, anew);
         }
-        const uint32_t in = valid >> (q * kHalf) & kAll;
-        if (in != kAll) {
+      };
+      // m of the half's rows; `most` becomes at least the bits of each channel's gate that is furthest below 0
+      auto load_gates = [&](F2 (&m)[kHalf], int q, auto asked, uint32_t& most) {
+        uint32_t w[kHalf] = {};
+        F2 unused;
 #pragma unroll
-          for (int i = 0; i < kHalf; ++i)
-            if (!(in >> i & 1u)) v[i] = d[i] = Raw<T>{};
+        for (int i = 0; i < kHalf; ++i) {
+          const Raw<T> f = get(0, q * kHalf + i);
+          if constexpr (!kSelect) w[i] = f.w;
+          m[i] = decay<kForm>(f.f(), unused);
+        }
+        if constexpr (!kSelect && decltype(asked)::value) {
+          most = __vimax3_u16x2(most, w[0], w[1]);
+#pragma unroll
+          for (int i = 2; i < kHalf; i += 2) most = __vimax3_u16x2(most, w[i], w[i + 1]);
+        }
+      };
+      // the same with a for the gates below, which have their bits in `low`
+      auto load_coefficients = [&](F2 (&m)[kHalf], uint32_t& low, int q) {
+        low = 0;
+#pragma unroll
+        for (int i = 0; i < kHalf; ++i) {
+          uint32_t bits;
+          m[i] = coefficient<kForm>(read(0, q * kHalf + i, std::bool_constant<!kSelect>{}).f(), kLowGate<T, kForm>, bits);
+          low |= bits << (2 * i);
+        }
+      };
+      // rows outside of every sequence change nothing (no h behind the last one is used)
+      auto leave_out = [&](F2 (&m)[kHalf], uint32_t& low, int q) {
+        const uint32_t in = half_of(valid, q);
+        if (in == kAll) return;
+#pragma unroll
+        for (int i = 0; i < kHalf; ++i) {
+          if (in >> i & 1u) continue;
+          m[i] = zero2();
+          v[i] = d[i] = Raw<T>{};
+          low &= ~(3u << (2 * i));
         }
       };
       // what the rows of these bits start from
@@ -728,58 +775,67 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
         for (int i = 0; i < kHalf; ++i) x[i] = load2_if<kFast>(bits >> i & 1u, p + (int64_t(seq[i]) * a.H + c), left);
       };
       auto pick = [](uint32_t bits, int i, F2 x, F2 y) -> F2 { return F2{bits >> i & 1u ? x.v : y.v}; };
-      // the half's map of h (A, x), and in a backward walk of E (A, x) and of h (A, z)
-      auto map_half = [&](const F2 (&m)[kHalf], int q, float4& of_walk, float4& of_h) {
-        const uint32_t s = starts >> (q * kHalf) & kAll, e = ends >> (q * kHalf) & kAll;
-        F2 A = f2(1.f), x = zero2(), z = zero2();
-        if ((s | e) == 0) {
+      // the half's map of h (A, x), and in a backward walk of E (A, x) and of h (A, z); kCut: rows that begin or
+      // end sequences may be among them, kSel: rows held as a
+      auto map_half = [&](auto cuts, auto select, const F2 (&m)[kHalf], uint32_t low, int q, float4& of_walk, float4& of_h) {
+        constexpr bool kCut = decltype(cuts)::value, kSel = decltype(select)::value;
+        const uint32_t s = kCut ? half_of(starts, q) : 0u, e = kCut ? half_of(ends, q) : 0u;
+        F2 A = f2(1.f), x = zero2(), z = zero2(), from[kHalf];
+        if constexpr (kCut && kValue) start_half(a.h0, s, q, from);
 #pragma unroll
-          for (int i = 0; i < kHalf; ++i) {
-            A = fma2(m[i], A, A);
-            if constexpr (kValue) z = step<kForm>(z, m[i], v[i].f());
-          }
-          if constexpr (kBwd) {
+        for (int i = 0; i < kHalf; ++i) {
+          A = decayed<kSel>(A, m[i], low >> (2 * i));
+          if constexpr (kValue) z = step<kForm, kSel>(kCut ? pick(s, i, from[i], z) : z, m[i], v[i].f(), low >> (2 * i));
+        }
+        if constexpr (kBwd) {
+          if constexpr (kCut) start_half(a.dfinal, e, q, from);
 #pragma unroll
-            for (int i = kHalf - 1; i >= 0; --i) {
-              x = add2(x, d[i].f());
-              x = fma2(m[i], x, x);
-            }
-          }
-        } else {
-          F2 from[kHalf];
-          if constexpr (kValue) start_half(a.h0, s, q, from);
-#pragma unroll
-          for (int i = 0; i < kHalf; ++i) {
-            A = fma2(m[i], A, A);
-            if constexpr (kValue) z = step<kForm>(pick(s, i, from[i], z), m[i], v[i].f());
-          }
-          if constexpr (kBwd) {
-            start_half(a.dfinal, e, q, from);
-#pragma unroll
-            for (int i = kHalf - 1; i >= 0; --i) {
-              x = add2(pick(e, i, from[i], x), d[i].f());
-              x = fma2(m[i], x, x);
-            }
-          }
+          for (int i = kHalf - 1; i >= 0; --i)
+            x = decayed<kSel>(add2(kCut ? pick(e, i, from[i], x) : x, d[i].f()), m[i], low >> (2 * i));
         }
         of_h = pack(Map{A, z}, s != 0);
         of_walk = kBwd ? pack(Map{A, x}, e != 0) : of_h;
+      };
+      auto take_half = [&](auto select, F2 (&m)[kHalf], uint32_t& low, int q, float4& of_walk, float4& of_h) {
+        if constexpr (decltype(select)::value) {
+          load_coefficients(m, low, q);
+        } else {
+          load_gates(m, q, kYes, most);
+          low = 0;
+        }
+        load_values(q, std::bool_constant<!kSelect && decltype(select)::value>{});
+        if (plain(q) && decltype(select)::value == kSelect) {
+          map_half(kNo, select, m, low, q, of_walk, of_h);
+        } else {
+          leave_out(m, low, q);
+          map_half(kYes, select, m, low, q, of_walk, of_h);
+        }
       };
 
       // ---- the maps of the warp's rows
       float4 mine = identity, mine_h = identity, first_h = identity;   // first_h: the first half's
       if (tile >= 0) {
-        float4 w, h;
-        load_gates(kept[0], 0);
-        load_values(0);
-        map_half(kept[0], 0, mine, mine_h);
-        if constexpr (kParts == 2) {
-          first_h = mine_h;
-          load_gates(kept[kKept - 1], 1);
-          load_values(1);
-          map_half(kept[kKept - 1], 1, w, h);
-          mine = kBwd ? compose(w, mine) : compose(mine, w);
-          if constexpr (kGrads) mine_h = compose(mine_h, h);
+        auto take = [&](auto select) {
+          [[maybe_unused]] float4 w, h;
+          take_half(select, kept[0], low[0], 0, mine, mine_h);
+          if constexpr (kParts == 2) {
+            first_h = mine_h;
+            take_half(select, kept[kKept - 1], low[kKept - 1], 1, w, h);
+            mine = kBwd ? compose(w, mine) : compose(mine, w);
+            if constexpr (kGrads) mine_h = compose(mine_h, h);
+          }
+        };
+        most = 0;
+        take(std::bool_constant<kSelect>{});
+        // Gates below kLowGate, which are seldom in 16 bits, are found beside the rest, and all is done again
+        // (65536 x 4096 forward 305 us; 359 with a branch behind the gates of every half, 400 with the
+        // selects always.  Of inputs that have one in every tile 649, backward 1440 for 535; to look for them
+        // first where the tile before had some, 559 and 1310, took 4 % of all others)
+        if constexpr (!kSelect) {
+          // (a channel that there is not may be what an earlier kernel has left in shared memory)
+          some = __any_sync(0xffffffffu, ((kFast || left > 0) && (most << 16) > (kLowBits<T> << 16)) ||
+                                             ((kFast || left > 1) && most > (kLowBits<T> << 16 | 0xffffu)));
+          if (some) take(kYes);
         }
       }
       if constexpr (!kGrads) ex.warps[warp][lane] = mine;
@@ -803,7 +859,7 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
 
       // ---- the rows again.  Where all of the warp's are in sequences their results go out as a box,
       // from where the gates (and dy) have been
-      const bool boxed = kFast && valid == (1u << kRows) - 1u;
+      const bool boxed = kFast && valid == (1u << kRows) - 1u && !(kBwd && some);
       auto store_out = [&](T* p, F2 x) {
         if constexpr (kFast)
           store2<true>(p + 2 * lane, x, left);
@@ -813,7 +869,7 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
       auto to_box = [&](int tensor, int i, F2 x) {
         store2<true>(reinterpret_cast<T*>(stage + tensor * kTensorBytes + i * kRowBytes) + 2 * lane, x, 2);
       };
-      // a half whose rows are all in sequences: no branch at every row (65536 x 4096 forward 310 us for 359)
+      // a half whose rows are all in sequences: no branch at every row (65536 x 4096 forward 359 us with one, where it took 310)
       auto out_whole = [&](T* base, int tensor, int i, F2 x) {
         if constexpr (kFast)
           to_box(tensor, i, x);
@@ -824,35 +880,43 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
         T* const y = static_cast<T*>(a.y);
 #pragma unroll
         for (int q = 0; q < kParts; ++q) {
-          const uint32_t s = starts >> (q * kHalf) & kAll, e = ends >> (q * kHalf) & kAll, is = valid >> (q * kHalf) & kAll;
-          if (kParts > 1) load_values(q);
-          if ((kFast ? boxed : is == kAll) && (s | e) == 0) {
+          if (kParts > 1) load_values(q, kNo);
+          if (plain(q) && (!kFast || boxed) && !some) {
 #pragma unroll
             for (int i = 0; i < kHalf; ++i) {
-              in = step<kForm>(in, kept[q][i], v[i].f());
+              in = step<kForm, kSelect>(in, kept[q][i], v[i].f(), low[q] >> (2 * i));
               out_whole(y, 0, q * kHalf + i, in);
             }
+            continue;
+          }
+          const uint32_t s = half_of(starts, q), e = half_of(ends, q), is = half_of(valid, q);
+          if (kParts > 1) leave_out(kept[q], low[q], q);
+          F2 h[kHalf];   // first what rows start from, then h
+          start_half(a.h0, s, q, h);
+          auto walk = [&](auto select) {
+#pragma unroll
+            for (int i = 0; i < kHalf; ++i)
+              h[i] = in = step<kForm, decltype(select)::value>(pick(s, i, h[i], in), kept[q][i], v[i].f(), low[q] >> (2 * i));
+          };
+          if (some)
+            walk(kYes);
+          else
+            walk(std::bool_constant<kSelect>{});
+          if (boxed) {
+#pragma unroll
+            for (int i = 0; i < kHalf; ++i) to_box(0, q * kHalf + i, h[i]);
           } else {
-            F2 h[kHalf];   // first what rows start from, then h
-            start_half(a.h0, s, q, h);
 #pragma unroll
-            for (int i = 0; i < kHalf; ++i) h[i] = in = step<kForm>(pick(s, i, h[i], in), kept[q][i], v[i].f());
-            if (boxed) {
+            for (int i = 0; i < kHalf; ++i)
+              if (is >> i & 1u)
+                store_out(y + (row + q * kHalf + i) * a.H + c0, h[i]);
+              else if (a.fill && row + q * kHalf + i < a.T)
+                store_out(y + (row + q * kHalf + i) * a.H + c0, zero2());
+          }
+          if (e != 0 && a.final_state) {
 #pragma unroll
-              for (int i = 0; i < kHalf; ++i) to_box(0, q * kHalf + i, h[i]);
-            } else {
-#pragma unroll
-              for (int i = 0; i < kHalf; ++i)
-                if (is >> i & 1u)
-                  store_out(y + (row + q * kHalf + i) * a.H + c0, h[i]);
-                else if (a.fill && row + q * kHalf + i < a.T)
-                  store_out(y + (row + q * kHalf + i) * a.H + c0, zero2());
-            }
-            if (e != 0 && a.final_state) {
-#pragma unroll
-              for (int i = 0; i < kHalf; ++i)
-                if (e >> i & 1u) store2<kFast>(a.final_state + int64_t(rows.seq[r0 + q * kHalf + i]) * a.H + c, h[i], left);
-            }
+            for (int i = 0; i < kHalf; ++i)
+              if (e >> i & 1u) store2<kFast>(a.final_state + int64_t(rows.seq[r0 + q * kHalf + i]) * a.H + c, h[i], left);
           }
         }
       } else {
@@ -861,85 +925,87 @@ __global__ void __launch_bounds__(kThreads, (kBlocksPerSM<T, kBwd>)) scan_kernel
         const float2 before = h_maps[warp][lane];
         const F2 h_in = f2(before.x, before.y);
         // dgate and dvalue of a row from D and E and h of the row before
-        auto grads = [&](int q, int i, auto small, F2 D, F2 E, F2 hp, F2& df, F2& dval) {
-          const F2 w = mul2(kept[0][i], f2(-1.f));
-          const F2 x = kForm == kFormSigmoid ? sub2(hp, v[i].f()) : hp;
-          dval = kForm == kFormSigmoid ? mul2(D, w) : D;
-          if constexpr (decltype(small)::value)
-            df = mul2(mul2(D, gate_slope<kForm>(get(0, q * kHalf + i).f(), kept[0][i])), x);
-          else
-            df = mul2(kForm == kFormSigmoid ? mul2(E, w) : E, x);
+        auto grads = [&](auto select, int i, F2 D, F2 E, F2 hp, F2& df, F2& dval) {
+          if constexpr (kForm == kFormSigmoid) {
+            const F2 c = kept[0][i], w = decltype(select)::value ? sub2(pick2(low[0] >> (2 * i), f2(1.f), zero2()), c) : mul2(c, f2(-1.f));
+            dval = mul2(D, w);
+            df = mul2(mul2(E, w), sub2(hp, v[i].f()));
+          } else {
+            dval = D;
+            df = mul2(E, hp);
+          }
         };
 #pragma unroll 1
         for (int q = kParts - 1; q >= 0; --q) {
-          const uint32_t s = starts >> (q * kHalf) & kAll, e = ends >> (q * kHalf) & kAll, is = valid >> (q * kHalf) & kAll;
-          if (q < kParts - 1) {   // the last one's rows are still there
-            load_gates(kept[0], q);
-            load_values(q);
-          }
           const F2(&m)[kHalf] = kept[0];
           F2 h = q > 0 ? apply(first_h, h_in) : h_in, hp[kHalf], df, dval;   // hp: h of the row before
-          // (the branch for bounds forms a from the gates again)
-          bool small = false;
-          if constexpr (sizeof(T) == 2) {
-            float least = 0.f;
-#pragma unroll
-            for (int i = 0; i < kHalf; ++i) {
-              // (a channel that there is not may be what an earlier kernel has left in shared memory)
-              if (kFast || left > 0) least = fminf(least, m[i].x());
-              if (kFast || left > 1) least = fminf(least, m[i].y());
+          const bool again = q < kParts - 1;   // the last one's rows are still there
+          if (plain(q) && (!kFast || boxed) && !some) {
+            if (again) {
+              if constexpr (kSelect)
+                load_coefficients(kept[0], low[0], q);
+              else
+                load_gates(kept[0], q, kNo, most);
+              load_values(q, kNo);
             }
-            small = __any_sync(0xffffffffu, least < 0.0078125f - 1.f);
-          }
-          if ((kFast ? boxed : is == kAll) && (s | e) == 0 && !small) {
 #pragma unroll
             for (int i = 0; i < kHalf; ++i) {
               hp[i] = h;
-              h = step<kForm>(h, m[i], v[i].f());
+              h = step<kForm, kSelect>(h, m[i], v[i].f(), low[0] >> (2 * i));
             }
 #pragma unroll
             for (int i = kHalf - 1; i >= 0; --i) {
               const F2 D = add2(d[i].f(), in);
-              in = fma2(m[i], D, D);   // E
-              grads(q, i, std::bool_constant<sizeof(T) == 4>{}, D, in, hp[i], df, dval);
+              in = decayed<kSelect>(D, m[i], low[0] >> (2 * i));   // E
+              grads(std::bool_constant<kSelect>{}, i, D, in, hp[i], df, dval);
               out_whole(dg, 0, q * kHalf + i, df);
               out_whole(dv, kD, q * kHalf + i, dval);
             }
-          } else {
-            F2 from[kHalf];
+            continue;
+          }
+          const uint32_t s = half_of(starts, q), e = half_of(ends, q), is = half_of(valid, q);
+          F2 from[kHalf];
+          auto walk = [&](auto select, auto box) {
+            constexpr bool kSel = decltype(select)::value;
+            if (again) {
+              if constexpr (kSel)
+                load_coefficients(kept[0], low[0], q);
+              else
+                load_gates(kept[0], q, kNo, most);
+              load_values(q, kNo);
+              leave_out(kept[0], low[0], q);
+            }
             start_half(a.h0, s, q, from);
 #pragma unroll
             for (int i = 0; i < kHalf; ++i) {
               hp[i] = h = pick(s, i, from[i], h);
-              h = step<kForm>(h, m[i], v[i].f());
+              h = step<kForm, kSel>(h, m[i], v[i].f(), low[0] >> (2 * i));
             }
             start_half(a.dfinal, e, q, from);
-            auto walk = [&](auto box) {
 #pragma unroll
-              for (int i = kHalf - 1; i >= 0; --i) {
-                const F2 D = add2(d[i].f(), pick(e, i, from[i], in));
-                in = fma2(m[i], D, D);
-                grads(q, i, std::true_type{}, D, in, hp[i], df, dval);
-                from[i] = in;
-                if constexpr (decltype(box)::value) {
-                  to_box(0, q * kHalf + i, df);
-                  to_box(kD, q * kHalf + i, dval);
-                } else if (row + q * kHalf + i < a.T) {
-                  const bool in_one = is >> i & 1u;
-                  store_out(dg + (row + q * kHalf + i) * a.H + c0, in_one ? df : zero2());
-                  store_out(dv + (row + q * kHalf + i) * a.H + c0, in_one ? dval : zero2());
-                }
+            for (int i = kHalf - 1; i >= 0; --i) {
+              const F2 D = add2(d[i].f(), pick(e, i, from[i], in));
+              in = decayed<kSel>(D, m[i], low[0] >> (2 * i));
+              grads(select, i, D, in, hp[i], df, dval);
+              from[i] = in;
+              if constexpr (decltype(box)::value) {
+                to_box(0, q * kHalf + i, df);
+                to_box(kD, q * kHalf + i, dval);
+              } else if (row + q * kHalf + i < a.T) {
+                const bool in_one = is >> i & 1u;
+                store_out(dg + (row + q * kHalf + i) * a.H + c0, in_one ? df : zero2());
+                store_out(dv + (row + q * kHalf + i) * a.H + c0, in_one ? dval : zero2());
               }
-            };
-            if (kFast && boxed)
-              walk(std::true_type{});
-            else
-              walk(std::false_type{});
-            if (s != 0 && a.dinit) {
-#pragma unroll
-              for (int i = 0; i < kHalf; ++i)
-                if (s >> i & 1u) store2<kFast>(a.dinit + int64_t(rows.seq[r0 + q * kHalf + i]) * a.H + c, from[i], left);
             }
+          };
+          if (kFast ? !boxed : some)
+            walk(kYes, kNo);   // (with no bit in low the same)
+          else
+            walk(std::bool_constant<kSelect>{}, std::bool_constant<kFast>{});
+          if (s != 0 && a.dinit) {
+#pragma unroll
+            for (int i = 0; i < kHalf; ++i)
+              if (s >> i & 1u) store2<kFast>(a.dinit + int64_t(rows.seq[r0 + q * kHalf + i]) * a.H + c, from[i], left);
           }
         }
       }
@@ -979,7 +1045,11 @@ __global__ void __launch_bounds__(256) scan_step_kernel(const T* gate, const T* 
     load_vec<kVec>(value + b * value_ld + c, v);
     load_vec<kVec>(state + b * H + c, h);
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) h[j] = step<kForm>(f2(h[j]), decay<kForm>(f2(f[j])), f2(v[j])).x();
+    for (int j = 0; j < kVec; ++j) {
+      uint32_t low;
+      const F2 k = coefficient<kForm>(f2(f[j]), kLowGate<float, kForm>, low);
+      h[j] = step<kForm, true>(f2(h[j]), k, f2(v[j]), low).x();
+    }
     store_vec<kVec>(state_out + b * H + c, h);
     store_vec<kVec>(y + b * H + c, h);
   }
