@@ -10,6 +10,8 @@ CUDA device, the call raises.
 from __future__ import annotations
 
 import ctypes
+import functools
+import inspect
 import os
 import re
 import subprocess
@@ -280,6 +282,24 @@ def _stream(stream=None, device_index=None):
         return stream.cuda_stream
     c = _torch()._C
     return c._cuda_getCurrentRawStream(c._cuda_getDevice() if device_index is None else device_index)
+
+
+def _on_stream(f):
+    """A function of the binding with its `stream` (None: the current one) as the current stream: what it
+    allocates and fills belongs to the stream that its kernels run on, as inside `with
+    torch.cuda.stream(stream)`.  Memory of another stream's pool may still be in use there, and a fill on
+    another stream could come after the kernels."""
+    at = list(inspect.signature(f).parameters).index("stream")
+
+    @functools.wraps(f)
+    def call(*args, **kw):
+        stream = args[at] if len(args) > at else kw.get("stream")
+        if stream is None:
+            return f(*args, **kw)
+        with _torch().cuda.stream(stream):
+            return f(*args, **kw)
+
+    return call
 
 
 _ws_cache: dict = {}

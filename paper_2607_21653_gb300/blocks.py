@@ -2,12 +2,12 @@
 feed-forward block, the gated linear recurrence over packed sequences and dropout from a
 counter, with their gradients.  As in the rest of the binding, every function marshals its
 arguments into the C ABI (include/molt.h) and runs on the current CUDA stream of its
-tensors' device."""
+tensors' device, or on `stream`; what it returns belongs to that stream."""
 from __future__ import annotations
 
 import ctypes
 
-from . import _check, _stream, _torch, _workspace, load
+from . import _check, _on_stream, _stream, _torch, _workspace, load
 from .stream import _at, _cuda, _dtype_code, _rows, _shaped
 
 ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
@@ -45,6 +45,13 @@ def _call(fn, dev, *args):
         return
     with torch.cuda.device(dev):
         _check(fn(*args))
+
+
+def _handle(stream, dev):
+    """cudaStream_t of a call on tensors of this device."""
+    if stream is not None and stream.device != dev:
+        raise ValueError(f"stream is on {stream.device}, the call's tensors on {dev}")
+    return _stream(stream, dev.index)
 
 
 # The checks of _at and _rows (.stream) in the order in which a good argument passes soonest: the
@@ -110,6 +117,7 @@ def _ffn_shapes(x, w_gate, w_up, w_down):
     return T, H, F
 
 
+@_on_stream
 def gated_ffn_fwd(x, w_gate, w_up, w_down, activation="silu", keep=False, stream=None, workspace=None):
     """Gated feed-forward block (molt_gated_ffn_fwd):
         y = (act(x w_gate^T) * (x w_up^T)) w_down^T
@@ -131,10 +139,11 @@ def gated_ffn_fwd(x, w_gate, w_up, w_down, activation="silu", keep=False, stream
                         "molt_gated_ffn_fwd_workspace_bytes")
     ws = workspace if workspace is not None else _scratch(nbytes, dev, "gated_ffn", stream)
     _call(load().molt_gated_ffn_fwd, dev, ref, xp, gp, up, dp, y.data_ptr(), gate if gate is None else gate.data_ptr(),
-          upo if upo is None else upo.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream, dev.index))
+          upo if upo is None else upo.data_ptr(), ws.data_ptr(), ws.numel(), _handle(stream, dev))
     return {"y": y, "gate": gate, "up": upo}
 
 
+@_on_stream
 def gated_ffn_bwd(dy, x, w_gate, w_up, w_down, gate=None, up=None, activation="silu", dw_dtype=None, dw_gate=None,
                   dw_up=None, dw_down=None, accumulate=False, stream=None, workspace=None):
     """Gradients of gated_ffn_fwd (molt_gated_ffn_bwd) from dy [T, H].  gate, up: what the
@@ -176,7 +185,7 @@ def gated_ffn_bwd(dy, x, w_gate, w_up, w_down, gate=None, up=None, activation="s
     ws = workspace if workspace is not None else _scratch(nbytes, dev, "gated_ffn", stream)
     _call(load().molt_gated_ffn_bwd, dev, ref, dyp, xp, gp, upp, dp, _vec(gate, dtype, dev, "gate"), _vec(up, dtype, dev, "up"),
           dx.data_ptr(), *[_vec(t, dw_dtype, dev, name) for t, (name, _) in zip(given, shapes)],
-          _dtype_code(dw_dtype, "dw_dtype"), 1 if accumulate else 0, ws.data_ptr(), ws.numel(), _stream(stream, dev.index))
+          _dtype_code(dw_dtype, "dw_dtype"), 1 if accumulate else 0, ws.data_ptr(), ws.numel(), _handle(stream, dev))
     return {"dx": dx, "dw_gate": given[0], "dw_up": given[1], "dw_down": given[2]}
 
 
@@ -210,6 +219,7 @@ def _packed(t, like, name):
     return t if t.dim() == 2 else t.view(-1, t.shape[2])
 
 
+@_on_stream
 def gated_scan_fwd(gate, value, initial_state=None, cu_seqlens=None, kind="sigmoid", want_states=False,
                    want_final_state=True, out=None, stream=None, workspace=None):
     """Gated linear recurrence over sequences, channel by channel (molt_gated_scan_fwd):
@@ -239,10 +249,11 @@ def gated_scan_fwd(gate, value, initial_state=None, cu_seqlens=None, kind="sigmo
     ws = workspace if workspace is not None else _scratch(nbytes, dev, "gated_scan", stream)
     _call(load().molt_gated_scan_fwd, dev, ref, gp, vp, _vec(initial_state, f32, dev, "initial_state"), cu,
           _vec(_shaped(out, gate.shape, "out"), dtype, dev, "out"), final if final is None else final.data_ptr(),
-          states if states is None else states.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream, dev.index))
+          states if states is None else states.data_ptr(), ws.data_ptr(), ws.numel(), _handle(stream, dev))
     return {"y": out, "final_state": final, "states": states}
 
 
+@_on_stream
 def gated_scan_bwd(dy, gate, value, states, initial_state=None, cu_seqlens=None, dfinal_state=None, kind="sigmoid",
                    stream=None, workspace=None):
     """Gradients of gated_scan_fwd (molt_gated_scan_bwd) from dy and dfinal_state [B, H]
@@ -268,10 +279,11 @@ def gated_scan_bwd(dy, gate, value, states, initial_state=None, cu_seqlens=None,
     _call(load().molt_gated_scan_bwd, dev, ref, dp, gp, vp, _vec(states, f32, dev, "states"),
           _vec(initial_state, f32, dev, "initial_state"), cu, _vec(dfinal_state, f32, dev, "dfinal_state"),
           dgate.data_ptr(), dvalue.data_ptr(), dinit if dinit is None else dinit.data_ptr(), ws.data_ptr(), ws.numel(),
-          _stream(stream, dev.index))
+          _handle(stream, dev))
     return {"dgate": dgate, "dvalue": dvalue, "dinitial_state": dinit}
 
 
+@_on_stream
 def gated_scan_step(gate, value, state, kind="sigmoid", out_state=None, stream=None):
     """One row of each of B sequences (molt_gated_scan_step), as decoding takes them: gate,
     value [B, H], state [B, H] float32.  Returns dict(y, state): the new state, in `out_state`
@@ -286,7 +298,7 @@ def gated_scan_step(gate, value, state, kind="sigmoid", out_state=None, stream=N
     new = torch.empty(B, H, dtype=f32, device=dev) if out_state is None else _shaped(out_state, (B, H), "out_state")
     ref, _ = _desc(ScanDesc, (B, H, B, gs, vs, 0, _dtype_code(dtype, "gate"), _form(kind), 0))
     _call(load().molt_gated_scan_step, dev, ref, gp, vp, _vec(_shaped(state, (B, H), "state"), f32, dev, "state"), y.data_ptr(),
-          _vec(new, f32, dev, "out_state"), _stream(stream, dev.index))
+          _vec(new, f32, dev, "out_state"), _handle(stream, dev))
     return {"y": y, "state": new}
 
 
@@ -311,10 +323,11 @@ def _dropout(x, p, seed, offset, residual, res_scale, first_row, out, out_dtype,
     d = DropoutDesc(T, H, xs, rs or 0, first_row, seed, offset, p, res_scale, _dtype_code(dtype, "x"),
                     _dtype_code(out_dtype, "out"))
     _call(load().molt_dropout, dev, ctypes.byref(d), xp, rp, words, _vec(_shaped(out, (T, H), "out"), out_dtype, dev, "out"),
-          _stream(stream, dev.index))
+          _handle(stream, dev))
     return out
 
 
+@_on_stream
 def dropout_fwd(x, p, seed, offset=0, residual=None, res_scale=1.0, first_row=0, out=None, stream=None):
     """res_scale * residual + x with a share p of its elements left out and the others divided
     by 1 - p (molt_dropout); p counts in steps of 2^-16.  The mask is a function of (seed, offset,
@@ -327,6 +340,7 @@ def dropout_fwd(x, p, seed, offset=0, residual=None, res_scale=1.0, first_row=0,
                     x.dtype if residual is None else residual.dtype, stream)
 
 
+@_on_stream
 def dropout_bwd(dout, p, seed, offset=0, first_row=0, dtype=None, out=None, stream=None):
     """Gradient of dropout_fwd for x, of dout's type or `dtype` (molt_dropout); the residual's
     is res_scale * dout."""
