@@ -356,6 +356,7 @@ def backward_plan(T, H, V, deterministic=False) -> dict:
     return out
 
 
+@_on_stream
 def group_advantages(rewards, group_ids, eps: float = 1e-6, out=None, stream=None):
     torch = _torch()
     n = rewards.shape[0]
@@ -368,6 +369,7 @@ def group_advantages(rewards, group_ids, eps: float = 1e-6, out=None, stream=Non
 ESTIMATORS = {"grpo": 0, "group_mean": 1, "dr_grpo": 2, "rloo": 3, "reinforce_pp": 4}
 
 
+@_on_stream
 def advantages(rewards, group_ids, estimator="grpo", eps: float = 1e-6, out=None, stream=None):
     """Per-rollout advantages with one of the estimators of Sec. 4.5."""
     torch = _torch()
@@ -379,6 +381,7 @@ def advantages(rewards, group_ids, estimator="grpo", eps: float = 1e-6, out=None
     return out
 
 
+@_on_stream
 def broadcast_advantages(adv_resp, resp_of_token, out=None, stream=None):
     torch = _torch()
     T = resp_of_token.shape[0]
@@ -389,6 +392,7 @@ def broadcast_advantages(adv_resp, resp_of_token, out=None, stream=None):
     return out
 
 
+@_on_stream
 def mask_count(mask, out=None, stream=None):
     torch = _torch()
     out = torch.empty(1, dtype=torch.int64, device=mask.device) if out is None else out
@@ -414,6 +418,7 @@ def _bf16_bits(t, name):
     raise TypeError(f"{name} must be bfloat16 (or its 16-bit pattern)")
 
 
+@_on_stream
 def token_logprobs(hidden, weight, tokens, mask=None, want_entropy=True, stream=None, workspace=None):
     """logp[T] and entropy[T] (fp32) of the generated tokens; rows with mask 0 give 0."""
     torch = _torch()
@@ -442,6 +447,7 @@ def _header_define(name: str) -> int:
 NOALLOC_MAX_TOKENS = _header_define("MOLT_NOALLOC_MAX_TOKENS")
 
 
+@_on_stream
 def token_logprobs_noalloc(hidden, weight, tokens, mask=None, want_entropy=True, stream=None):
     """Like token_logprobs, through molt_token_logprobs_fwd_noalloc: the library
     allocates nothing (its scratch is a fixed device array); T is at most
@@ -458,6 +464,7 @@ def token_logprobs_noalloc(hidden, weight, tokens, mask=None, want_entropy=True,
     return logp, ent
 
 
+@_on_stream
 def policy_loss_fwd_bwd(hidden, weight, tokens, behavior_logp, adv, mask=None, clip_lo=0.2, clip_hi=0.2,
                         denom=0.0, dW=None, accumulate_dW=False, want_token_outputs=True, stream=None,
                         workspace=None):
@@ -517,6 +524,7 @@ class LossOptions(ctypes.Structure):
                 ("deterministic", ctypes.c_int), ("det_clusters", ctypes.c_int)]
 
 
+@_on_stream
 def policy_loss_fwd_bwd_ex(hidden, weight, tokens, behavior_logp, adv, mask=None, clip_lo=0.2, clip_hi=0.2,
                            denom=0.0, kl_coef=0.0, ref_logp=None, entropy_coef=0.0, seq_of_token=None,
                            gate_lo=0.0, gate_hi=float("inf"), deterministic=False, det_clusters=0, dW=None,
@@ -567,6 +575,7 @@ def vocab_shard_bounds(V: int, n_shards: int) -> list:
     return [(r * V // n_shards, (r + 1) * V // n_shards) for r in range(n_shards)]
 
 
+@_on_stream
 def vp_partials(hidden, weight_shard, tokens, v_begin, mask=None, stream=None, workspace=None):
     """Per-token statistics (M, S, Q, z_x) of one vocabulary shard
     (molt_vp_partials): fp32 [T, 4]."""
@@ -582,6 +591,7 @@ def vp_partials(hidden, weight_shard, tokens, v_begin, mask=None, stream=None, w
     return out
 
 
+@_on_stream
 def vp_loss(partials, behavior_logp, adv, mask=None, clip_lo=0.2, clip_hi=0.2, denom=0.0, stream=None):
     """Merge of the shards' statistics ([n_shards, T, 4], shard order) with
     the clipped surrogate and Eq. 2 (molt_vp_loss).  Returns dict(loss, lse,
@@ -606,6 +616,7 @@ def vp_loss(partials, behavior_logp, adv, mask=None, clip_lo=0.2, clip_hi=0.2, d
     return out
 
 
+@_on_stream
 def vp_backward(hidden, weight_shard, tokens, lse, coef, v_begin, dW=None, accumulate_dW=False, stream=None):
     """One shard's backward (molt_vp_backward): returns (dhidden contribution
     fp32 [T, H], dW shard fp32 [V_shard, H])."""
@@ -646,6 +657,7 @@ def sum_dhidden(partial, group=None):
     return partial
 
 
+@_on_stream
 def policy_loss_vocab_parallel(hidden, weight_shard, v_begin, tokens, behavior_logp, adv, mask=None, clip_lo=0.2,
                                clip_hi=0.2, denom=0.0, group=None, stream=None):
     """One rank's policy-loss step with W split by vocabulary over the ranks

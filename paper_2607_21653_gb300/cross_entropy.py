@@ -4,7 +4,7 @@ from __future__ import annotations
 
 import ctypes
 
-from . import _check, _stream, _torch, _workspace, load
+from . import _check, _on_stream, _stream, _torch, _workspace, load
 from .stream import _at, _cuda, _dtype_code, _shaped
 
 
@@ -42,6 +42,7 @@ def _prepare(hidden, weight, targets, token_weight):
     return T, H, V
 
 
+@_on_stream
 def cross_entropy_fwd(hidden, weight, targets, token_weight=None, denom=0.0, ignore_index=-100, label_smoothing=0.0,
                       z_loss=0.0, want_token_outputs=True, stream=None, workspace=None):
     """Cross entropy of the next token over the LM head, without its gradient
@@ -69,6 +70,7 @@ def cross_entropy_fwd(hidden, weight, targets, token_weight=None, denom=0.0, ign
     return {"loss": loss, "logp": logp, "lse": lse, "stats": stats}
 
 
+@_on_stream
 def cross_entropy_fwd_bwd(hidden, weight, targets, token_weight=None, denom=0.0, ignore_index=-100,
                           label_smoothing=0.0, z_loss=0.0, dW=None, accumulate_dW=False, dW_dtype=None,
                           want_token_outputs=True, stream=None, workspace=None, max_kept_bytes=None):

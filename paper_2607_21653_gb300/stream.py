@@ -6,7 +6,7 @@ from __future__ import annotations
 
 import ctypes
 
-from . import _check, _ptr, _stream, _torch, _workspace, load
+from . import _check, _on_stream, _ptr, _stream, _torch, _workspace, load
 
 _DTYPES = None
 
@@ -68,6 +68,7 @@ def _rows(t, dtype, dev, name):
 
 
 # ----------------------------------------------------------------- embedding
+@_on_stream
 def token_embedding(weight, tokens, scale=1.0, out_dtype=None, out=None, stream=None):
     """scale * weight[tokens] as [T, H] of weight's type, or of `out_dtype` =
     float32 (molt_token_embedding).  A token outside [0, V) gives a row of zeros
@@ -87,6 +88,7 @@ def token_embedding(weight, tokens, scale=1.0, out_dtype=None, out=None, stream=
     return out
 
 
+@_on_stream
 def token_embedding_bwd(dout, tokens, V, scale=1.0, padding_idx=None, dtype=None, dW=None, accumulate_dW=False,
                         stream=None, workspace=None):
     """The embedding's gradient, scale * the sum of dout's rows by token
@@ -186,6 +188,7 @@ def _param_type(dtype, H, w_post, w_pre, gate):
     return dtype if found is None else found
 
 
+@_on_stream
 def residual_norm_fwd(x, residual=None, w_post=None, gate=None, w_pre=None, res_scale=1.0, eps=1e-6, weight_offset=0.0,
                       residual_dtype=None, want_stats=True, stream=None, gate_kind=None):
     """A block's output x into the residual stream, and out of it again
@@ -232,6 +235,7 @@ def residual_norm_fwd(x, residual=None, w_post=None, gate=None, w_pre=None, res_
     return out
 
 
+@_on_stream
 def residual_norm_bwd(dy, dresidual, x, residual, rstd_pre, rstd_post=None, w_post=None, gate=None, w_pre=None,
                       res_scale=1.0, weight_offset=0.0, want_dresidual=True, dw_post=None, dgate=None, dw_pre=None,
                       accumulate=False, stream=None, workspace=None, gate_kind=None):

@@ -1,4 +1,4 @@
-"""`stream` of the operators inside a block: their whole body runs with it as the current stream."""
+"""`stream` of the calls: their whole body runs with it as the current stream."""
 import contextlib
 import inspect
 
@@ -62,3 +62,10 @@ def test_refusals_come_from_inside_it(current, name):
     finally:
         torch.cuda.stream = real
     assert entered == ["s"]
+
+
+def test_every_call_with_a_stream():
+    for name in molt.__all__:
+        f = getattr(molt, name)
+        if callable(f) and not inspect.isclass(f) and "stream" in inspect.signature(f).parameters:
+            assert hasattr(f, "__wrapped__") != (name in ("device_status", "selftest_wait_timeout")), name
