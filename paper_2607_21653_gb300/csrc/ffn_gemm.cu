@@ -256,7 +256,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       const bool rows_in = r0 < p.m;
       // kEpiDglu: g and u of 64 columns (fp32: 32) of the lane's row, as they are in memory.  The
       // first ones come while the products run, the others while boxes go out, but not ahead
-      // of a fence, which would wait for them
+      // of a fence, which would wait for them.  Not as read-only data: the launch before, which may
+      // have written them, can end after this one has begun
       const int row = r0 + lane, col0 = u.tn * 256 + hf * 128;
       uint4 gq[8], uq[8];
       auto load_gu = [&](int c) {   // c: in 32 columns
@@ -265,8 +266,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           const int f = col0 + c * 32 + j * (p.wide ? 4 : 8);
           if (row < p.m && f < p.n) {
             const int64_t at = (static_cast<int64_t>(row) * p.n + f) * (p.wide ? 4 : 2);
-            gq[j] = __ldg(reinterpret_cast<const uint4*>(static_cast<const char*>(p.gate) + at));
-            uq[j] = __ldg(reinterpret_cast<const uint4*>(static_cast<const char*>(p.up) + at));
+            gq[j] = __ldcg(reinterpret_cast<const uint4*>(static_cast<const char*>(p.gate) + at));
+            uq[j] = __ldcg(reinterpret_cast<const uint4*>(static_cast<const char*>(p.up) + at));
           } else {
             gq[j] = uq[j] = make_uint4(0, 0, 0, 0);
           }
