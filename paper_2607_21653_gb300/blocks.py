@@ -82,19 +82,22 @@ def _scratch(nbytes, dev, key, stream):
         return torch.empty(nbytes, dtype=torch.uint8, device=dev)
 
 
-# Descriptors by their values, with the workspace bytes of the call: read only.
+# Descriptors by their values, with the workspace bytes of the call, by device: read only.
 _desc_cache: dict = {}
 _DESC_CACHE_MAX = 256
 
 
-def _desc(cls, values, query=None, *more):
-    key = (cls, values, query, more)
+def _desc(dev, cls, values, query=None, *more):
+    key = (dev.index, cls, values, query, more)
     entry = _desc_cache.get(key)
     if entry is None:
         if len(_desc_cache) >= _DESC_CACHE_MAX:
             _desc_cache.clear()
-        ref = ctypes.byref(cls(*values))
-        entry = _desc_cache[key] = ref, getattr(load(), query)(ref, *more) if query else 0
+        ref, nbytes = ctypes.byref(cls(*values)), 0
+        if query:
+            with _torch().cuda.device(dev):   # a size can go by the device's SMs
+                nbytes = getattr(load(), query)(ref, *more)
+        entry = _desc_cache[key] = ref, nbytes
     return entry
 
 
@@ -135,7 +138,7 @@ def gated_ffn_fwd(x, w_gate, w_up, w_down, activation="silu", keep=False, stream
     y = torch.empty(T, H, dtype=dtype, device=dev)
     gate = torch.empty(T, F, dtype=dtype, device=dev) if keep else None
     upo = torch.empty(T, F, dtype=dtype, device=dev) if keep else None
-    ref, nbytes = _desc(FfnDesc, (T, H, F, xs, gs, us, ds, 0, _dtype_code(dtype, "x"), _activation(activation)),
+    ref, nbytes = _desc(dev, FfnDesc, (T, H, F, xs, gs, us, ds, 0, _dtype_code(dtype, "x"), _activation(activation)),
                         "molt_gated_ffn_fwd_workspace_bytes")
     ws = workspace if workspace is not None else _scratch(nbytes, dev, "gated_ffn", stream)
     _call(load().molt_gated_ffn_fwd, dev, ref, xp, gp, up, dp, y.data_ptr(), gate if gate is None else gate.data_ptr(),
@@ -180,7 +183,7 @@ def gated_ffn_bwd(dy, x, w_gate, w_up, w_down, gate=None, up=None, activation="s
     upp, us = _mat(w_up, dtype, dev, "w_up")
     dp, ds = _mat(w_down, dtype, dev, "w_down")
     dx = torch.empty(T, H, dtype=dtype, device=dev)
-    ref, nbytes = _desc(FfnDesc, (T, H, F, xs, gs, us, ds, dys, _dtype_code(dtype, "x"), _activation(activation)),
+    ref, nbytes = _desc(dev, FfnDesc, (T, H, F, xs, gs, us, ds, dys, _dtype_code(dtype, "x"), _activation(activation)),
                         "molt_gated_ffn_bwd_workspace_bytes", 0 if gate is None else 1)
     ws = workspace if workspace is not None else _scratch(nbytes, dev, "gated_ffn", stream)
     _call(load().molt_gated_ffn_bwd, dev, ref, dyp, xp, gp, upp, dp, _vec(gate, dtype, dev, "gate"), _vec(up, dtype, dev, "up"),
@@ -244,7 +247,7 @@ def gated_scan_fwd(gate, value, initial_state=None, cu_seqlens=None, kind="sigmo
         out = torch.empty(gate.shape, dtype=dtype, device=dev)
     final = torch.empty(B, H, dtype=f32, device=dev) if want_final_state else None
     states = torch.empty((T + STATE_ROWS - 1) // STATE_ROWS, H, dtype=f32, device=dev) if want_states else None
-    ref, nbytes = _desc(ScanDesc, (T, H, B, gs, vs, 0, _dtype_code(dtype, "gate"), _form(kind), fill),
+    ref, nbytes = _desc(dev, ScanDesc, (T, H, B, gs, vs, 0, _dtype_code(dtype, "gate"), _form(kind), fill),
                         "molt_gated_scan_workspace_bytes")
     ws = workspace if workspace is not None else _scratch(nbytes, dev, "gated_scan", stream)
     _call(load().molt_gated_scan_fwd, dev, ref, gp, vp, _vec(initial_state, f32, dev, "initial_state"), cu,
@@ -273,7 +276,7 @@ def gated_scan_bwd(dy, gate, value, states, initial_state=None, cu_seqlens=None,
             _shaped(t, (B, H), name)
     dgate, dvalue = (torch.empty(gate.shape, dtype=dtype, device=dev) for _ in range(2))
     dinit = None if initial_state is None else torch.empty(B, H, dtype=f32, device=dev)
-    ref, nbytes = _desc(ScanDesc, (T, H, B, gs, vs, ds, _dtype_code(dtype, "gate"), _form(kind), 0),
+    ref, nbytes = _desc(dev, ScanDesc, (T, H, B, gs, vs, ds, _dtype_code(dtype, "gate"), _form(kind), 0),
                         "molt_gated_scan_workspace_bytes")
     ws = workspace if workspace is not None else _scratch(nbytes, dev, "gated_scan", stream)
     _call(load().molt_gated_scan_bwd, dev, ref, dp, gp, vp, _vec(states, f32, dev, "states"),
@@ -296,7 +299,7 @@ def gated_scan_step(gate, value, state, kind="sigmoid", out_state=None, stream=N
     f32 = torch.float32
     y = torch.empty(B, H, dtype=dtype, device=dev)
     new = torch.empty(B, H, dtype=f32, device=dev) if out_state is None else _shaped(out_state, (B, H), "out_state")
-    ref, _ = _desc(ScanDesc, (B, H, B, gs, vs, 0, _dtype_code(dtype, "gate"), _form(kind), 0))
+    ref, _ = _desc(dev, ScanDesc, (B, H, B, gs, vs, 0, _dtype_code(dtype, "gate"), _form(kind), 0))
     _call(load().molt_gated_scan_step, dev, ref, gp, vp, _vec(_shaped(state, (B, H), "state"), f32, dev, "state"), y.data_ptr(),
           _vec(new, f32, dev, "out_state"), _handle(stream, dev))
     return {"y": y, "state": new}
