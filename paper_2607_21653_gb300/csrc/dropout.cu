@@ -225,7 +225,7 @@ extern "C" molt_status molt_dropout(const molt_dropout_desc* d, const void* x, c
                                     const uint64_t* seed_offset, void* out, cudaStream_t stream) {
   if (!d) return fail(MOLT_ERR_INVALID_ARG, "desc is NULL");
   if (d->T < 0 || d->H < 1) return fail(MOLT_ERR_INVALID_ARG, "sizes must satisfy T >= 0, H >= 1");
-  if (d->H > 65536 || d->T > (int64_t(1) << 32) || d->first_row < 0 || d->first_row + d->T > (int64_t(1) << 32))
+  if (d->H > 65536 || d->T > (int64_t(1) << 32) || d->first_row < 0 || d->first_row > (int64_t(1) << 32) - d->T)
     return fail(MOLT_ERR_UNSUPPORTED_SHAPE, "H must be at most 65536 and the rows lie in [0, 2^32)");
   if (!known_type(d->dtype) || !known_type(d->out_dtype)) return fail(MOLT_ERR_INVALID_ARG, "unknown element type");
   if (d->dtype != d->out_dtype && d->dtype != MOLT_FP32 && d->out_dtype != MOLT_FP32)
