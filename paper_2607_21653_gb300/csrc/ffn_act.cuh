@@ -31,7 +31,8 @@ __device__ __forceinline__ float ffn_activate(float g, float& d) {
   }
   // (1 + tanh z) / 2 = 1 / (1 + e^(-2 z)), z = sqrt(2 / pi) (g + 0.044715 g^3)
   static_assert(kAct == kActRelu || kAct == kActSilu || kAct == kActGelu);
-  const float q = g * g;
+  // (p is 0 or 1 from |g| = 100 on; the derivative's g^2, infinite from 2^64 on, would make 0 times it NaN)
+  const float q = fminf(g * g, 1e4f);
   const float p = ffn_rcp(1.f + ex2_approx(-kFfnLog2e * kGeluA * g * fmaf(kGeluB, q, 1.f)));
   if (kGrad) d = fmaf(g * p * (1.f - p), kGeluA * fmaf(3.f * kGeluB, q, 1.f), p);
   return g * p;
