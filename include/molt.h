@@ -565,7 +565,8 @@ molt_status molt_cross_entropy_fwd_bwd(const uint16_t* hidden, const uint16_t* W
  *   g = x w_gate^T, u = x w_up^T  [T,F];   h = act(g) u;   y = h w_down^T  [T,H]
  * x [T,H], w_gate, w_up [F,H], w_down [H,F] (nn.Linear layouts) and y of one 16-bit type;
  * sums in fp32, h rounded once to the type for the second product, g and u kept (or not)
- * rounded once.  Rows of the operands may be strided; the outputs' rows lie side by side.  All
+ * rounded once.  (Of MOLT_FP16 an h past 65504 is infinite, one below 2^-25 is 0; so are dg and du
+ * in the backward.)  Rows of the operands may be strided; the outputs' rows lie side by side.  All
  * pointers 16-byte aligned; outputs overlap neither one another nor the inputs.
  */
 #define MOLT_ACT_SILU 0       /* g / (1 + e^-g) */

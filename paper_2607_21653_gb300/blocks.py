@@ -125,7 +125,8 @@ def gated_ffn_fwd(x, w_gate, w_up, w_down, activation="silu", keep=False, stream
     """Gated feed-forward block (molt_gated_ffn_fwd):
         y = (act(x w_gate^T) * (x w_up^T)) w_down^T
     x [T, H], w_gate and w_up [F, H], w_down [H, F], bfloat16 or float16, H and F multiples of
-    8, rows may be strided by multiples of 8.  activation: "silu", "gelu" (its tanh form),
+    8, rows may be strided by multiples of 8; act(..) * (..) is rounded to x's type before the second
+    product (in float16 it is infinite past 65504).  activation: "silu", "gelu" (its tanh form),
     "relu".  Returns dict(y [T, H], gate, up): with keep=True the two products [T, F] for
     the backward, else None."""
     torch = _torch()

@@ -66,8 +66,9 @@ struct FfnReduce {
 
 // A product for a few rows: out[t, n] = x[t, k] w[n, k]^T; the first one of the block has w0 =
 // Wg and w1 = Wu and gives h (out[0]) and, unless nullptr, g and u.  Up to 16 rows: the whole block at
-// H = 4096, F = 10944 takes 45 us of one row, 47 of 8 and 60 of 16, where the tiles' kernel has 68 of
-// 32 (from 16 on the rows' loads fill the registers that the weights' should have).
+// H = 4096, F = 10944 takes 46 us of one row, 48 of 8, 58 of 9 and 61 of 16, where the tiles' kernel has 68 of
+// 17 and of 32; at H = 896, F = 2392 17 of 16 rows and 22 of 17 (past 16 the rows' loads fill the registers
+// that the weights' should have).
 constexpr int kFfnFewRows = 16;
 struct FfnRows {
   const void *x, *w0, *w1;

@@ -14,10 +14,15 @@
 // where it leaves TMEM.  g, u and dh are never in memory unless the caller keeps g and u.
 //
 // A launch takes up to four problems (dx and the three weight gradients are one), whose
-// units are dealt to the pairs in order; long ones come first, so that the end is
-// ragged by a short unit.  Where there are fewer tiles than pairs K is cut into
+// units are dealt to the pairs in order: dx, which has 2 F of K, then the gradients, which have T
+// (up to T = 2 F the end is ragged by a short unit).  Where there are fewer tiles than pairs K is cut into
 // units whose fp32 parts launch_ffn_reduce adds in order (no atomics: the same bits in
 // every run).
+//
+// Between the products h, dg and du are rounded to the operands' type, which the tensor cores take two of: a
+// second rounding of the size of the result's (errors against 64 bits 1.4 times those of one; h
+// as two 16-bit parts would be a third more operations forward and twice as many backward).  In fp16 what
+// passes 65504 there is infinite, as in a model whose layers are all in fp16.
 //
 // Bound by the tensor cores, in long calls at the power cap: bf16, H = 4096, F = 10944, 16384 rows
 // forward with g and u kept 2.46 to 2.8 ms over boxes (1.72 PFLOP/s are 2.56); 4096 rows, the product of g and
